@@ -338,6 +338,106 @@ const char* dash_last_error(void);
    next call reallocates on its device). */
 void dash_release_workspace(void);
 
+/* ======================================================================
+ * Sequences of different lengths: packed prompts, a paged key-value cache
+ * and attention of one new token.
+ *
+ * Conventions of these entry points, beside the shared ones above:
+ *  - Query head h reads K/V head h / (heads_q / heads_kv); heads_kv divides heads_q.
+ *  - Tensors are [rows][heads][d] with strides in elements; the d elements
+ *    of a head are contiguous.  Row and head strides are multiples of 8, pointers
+ *    16-byte aligned (e4m3 caches: strides multiples of 16), row strides at least d
+ *    and at most 2^22.  Elements that a call writes may not overlap.
+ *  - Lengths, offsets and tables are read on the device when the call runs, so
+ *    a captured call follows their later contents.  Values outside their range are
+ *    clamped before use: no entry point reads or writes outside the tensors
+ *    that its arguments describe.
+ *  - A row whose keys are all masked, or all score -infinity, has O = 0, L = -infinity
+ *    and no gradient.
+ *  - Results are bitwise reproducible for the same call.
+ * ====================================================================== */
+
+typedef enum {
+  DASH_CACHE_BF16 = 0,
+  DASH_CACHE_E4M3 = 1 /* OCP 8-bit e4m3 */
+} dash_cache_type_t;
+
+/* A paged key-value cache: `pages` pages of page_size rows for each of heads_kv
+   heads, and for each of `batch` sequences the pages that hold its rows in order.
+   page_size is a multiple of 16.  Key j of sequence s is row j % page_size
+   of page block_table[s * table_stride + j / page_size]. */
+typedef struct {
+  int batch, heads_q, heads_kv, d;
+  int pages, page_size;
+  int table_width; /* entries of a sequence in block_table */
+  int cache_type;  /* DASH_CACHE_* */
+  void* k_cache;
+  void* v_cache;
+  /* strides in elements from page to page, head to head and row to row */
+  int64_t k_page_stride, k_head_stride, k_row_stride;
+  int64_t v_page_stride, v_head_stride, v_row_stride;
+  const int32_t* block_table;
+  int64_t table_stride;
+  const int32_t* lens; /* [batch] */
+  /* [heads_kv] or NULL (1): a cached value stands for itself times its head's
+     scale.  E4M3 only. */
+  const float* k_scale;
+  const float* v_scale;
+} dash_paged_cache_t;
+
+/* New tokens of dash_kv_append. */
+typedef struct {
+  int tokens;
+  /* [batch + 1]: the tokens of sequence s are rows cu[s] .. cu[s+1]-1.  Rows from
+     cu[batch] on are left alone, in q_out and k_out too.  NULL: one token per
+     sequence (tokens == batch). */
+  const int32_t* cu;
+  const void* k; /* bf16 [tokens][heads_kv][d] */
+  const void* v;
+  const void* q; /* bf16 [tokens][heads_q][d], or NULL: no queries */
+  void* q_out;   /* receives the rotated queries (may be q) */
+  void* k_out;   /* or NULL; receives the rotated keys (may be k) */
+  int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  int64_t q_row_stride, q_head_stride, q_out_row_stride, q_out_head_stride;
+  int64_t k_out_row_stride, k_out_head_stride;
+  /* [rotary_dim / 2] or NULL (no rotation): pair i of a token at place p turns by
+     the angle p * inv_freq[i] */
+  const float* inv_freq;
+  int rotary_dim;  /* a multiple of 16, at most d; the components behind it stay */
+  int interleaved; /* 0: pairs (i, i + rotary_dim/2); else (2i, 2i + 1) */
+} dash_append_t;
+
+/*
+ * Stores new keys and values at the end of their sequences in a paged cache:
+ * token t of sequence s goes to place lens[s] + t - cu[s], with its key (and its
+ * query, into q_out) rotated by that place.  cache->lens holds the lengths before
+ * the call and is not changed.  The angle is computed in 64 bits, the rest in 32 with
+ * one rounding at the store; E4M3 stores value / scale rounded to nearest even and
+ * saturated at 448.  status: NULL or a device int that the call sets to 1
+ * when a token's place lies outside its row of block_table or in a page
+ * outside 0 .. pages-1 (that token is not stored; its q_out and k_out are still
+ * written).  The call never sets it to 0.
+ */
+int dash_kv_append(const dash_paged_cache_t* cache, const dash_append_t* x, int* status, void* stream);
+
+/* Bytes of workspace for dash_attn_decode (0 if the arguments are invalid). */
+size_t dash_decode_workspace_size(int batch, int heads_q, int heads_kv, int d, int page_size, int table_width);
+
+/*
+ * Attention of one query token per sequence over its lens[s] cached keys: q, o bf16
+ * [batch][heads_q][d]; lse NULL or fp32 [batch][heads_q].  scale as in
+ * dash_attn_fwd_ex (0: 1/sqrt(d)), on top of k_scale.  A sequence of length 0
+ * has O = 0, L = -infinity.  What the cache holds behind a sequence's last key does not
+ * reach its result.  Asynchronous on `stream`; the workspace (256-byte
+ * aligned, any contents) must not be used by another call until this one has
+ * finished.  status: NULL or a device int that the call sets to 1 when a length is
+ * negative or more than table_width * page_size (clamped), or a page that it needs lies
+ * outside 0 .. pages-1 (that sequence's output is then undefined); never to 0.
+ */
+int dash_attn_decode(const dash_paged_cache_t* cache, const void* q, int64_t q_row_stride, int64_t q_head_stride,
+                     void* o, int64_t o_row_stride, int64_t o_head_stride, float* lse, float scale, void* workspace,
+                     size_t ws_bytes, int* status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

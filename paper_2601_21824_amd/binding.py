@@ -29,7 +29,9 @@ DASH_PLACEMENT_AUTO, DASH_PLACEMENT_GLOBAL, DASH_PLACEMENT_XCD = 0, 1, 2
 EXPORTS = ("dash_attn_fwd", "dash_attn_fwd_ex", "dash_attn_bwd", "dash_bwd_workspace_size",
            "dash_attn_bwd_ex", "dash_attn_bwd_noalloc", "dash_bwd_check", "dash_resolve_schedule", "dash_schedule_table",
            "dash_bwd_placement", "dash_mfma_peak", "dash_last_error", "dash_release_workspace",
-           "dash_auto_schedule", "dash_model_makespan")
+           "dash_auto_schedule", "dash_model_makespan", "dash_kv_append", "dash_attn_decode",
+           "dash_decode_workspace_size")
+DASH_CACHE_BF16, DASH_CACHE_E4M3 = 0, 1
 
 
 class DashError(RuntimeError):
@@ -45,6 +47,25 @@ class dash_bwd_options_t(ctypes.Structure):
                 ("event_main_end", ctypes.c_void_p), ("max_workgroups", ctypes.c_int),
                 ("ticket_order", ctypes.c_int), ("placement", ctypes.c_int),
                 ("wait_stats", ctypes.c_void_p)]
+
+
+_VP, _CI, _I64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
+
+
+class dash_paged_cache_t(ctypes.Structure):
+    _fields_ = [("batch", _CI), ("heads_q", _CI), ("heads_kv", _CI), ("d", _CI), ("pages", _CI), ("page_size", _CI),
+                ("table_width", _CI), ("cache_type", _CI), ("k_cache", _VP), ("v_cache", _VP),
+                ("k_page_stride", _I64), ("k_head_stride", _I64), ("k_row_stride", _I64),
+                ("v_page_stride", _I64), ("v_head_stride", _I64), ("v_row_stride", _I64),
+                ("block_table", _VP), ("table_stride", _I64), ("lens", _VP), ("k_scale", _VP), ("v_scale", _VP)]
+
+
+class dash_append_t(ctypes.Structure):
+    _fields_ = [("tokens", _CI), ("cu", _VP), ("k", _VP), ("v", _VP), ("q", _VP), ("q_out", _VP), ("k_out", _VP),
+                ("k_row_stride", _I64), ("k_head_stride", _I64), ("v_row_stride", _I64), ("v_head_stride", _I64),
+                ("q_row_stride", _I64), ("q_head_stride", _I64), ("q_out_row_stride", _I64),
+                ("q_out_head_stride", _I64), ("k_out_row_stride", _I64), ("k_out_head_stride", _I64),
+                ("inv_freq", _VP), ("rotary_dim", _CI), ("interleaved", _CI)]
 
 
 _lib = None
@@ -75,11 +96,16 @@ def load():
         dp = ctypes.POINTER(ctypes.c_double)
         lib.dash_auto_schedule.argtypes = [ci] * 6 + [ip, dp]
         lib.dash_model_makespan.argtypes = [ci] * 9 + [ctypes.c_double, ctypes.c_double, dp]
+        lib.dash_kv_append.argtypes = [ctypes.POINTER(dash_paged_cache_t), ctypes.POINTER(dash_append_t), vp, vp]
+        lib.dash_attn_decode.argtypes = [ctypes.POINTER(dash_paged_cache_t), vp, _I64, _I64, vp, _I64, _I64, vp, cf, vp,
+                                         sz, vp, vp]
+        lib.dash_decode_workspace_size.argtypes = [ci] * 6
+        lib.dash_decode_workspace_size.restype = sz
         lib.dash_last_error.restype = ctypes.c_char_p
         lib.dash_release_workspace.restype = None
         for f in ("dash_attn_fwd", "dash_attn_fwd_ex", "dash_attn_bwd", "dash_attn_bwd_ex", "dash_attn_bwd_noalloc",
                   "dash_bwd_check", "dash_resolve_schedule", "dash_schedule_table", "dash_bwd_placement",
-                  "dash_mfma_peak", "dash_auto_schedule", "dash_model_makespan"):
+                  "dash_mfma_peak", "dash_auto_schedule", "dash_model_makespan", "dash_kv_append", "dash_attn_decode"):
             getattr(lib, f).restype = ci
         _lib = lib
     return _lib
@@ -243,6 +269,163 @@ def dash_schedule_table(schedule, N: int, d: int, causal: bool, placement=DASH_P
     return dict(t_r=t_r, t_c=t_c, br=br, chains=chains, bc=bc, group=grp, chain_len=chain_len,
                 task_kv=task_kv.reshape(chains, cap), task_q=task_q.reshape(chains, cap),
                 rank=rank.reshape(t_r, t_c))
+
+
+# ----------------------------------------------------------------- sequences of different lengths
+def _bad(msg: str):
+    raise DashError(DASH_ERR_INVALID_ARG, msg)
+
+
+def _rows(name, t, dtype, device, rows, heads, d):
+    """A [rows, heads, d] tensor whose heads are contiguous: its pointer and strides."""
+    if t.dtype is not dtype or t.device != device or t.shape != (rows, heads, d):
+        _bad(f"{name} must be a {dtype} [{rows}, {heads}, {d}] tensor on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    row, head, one = t.stride()
+    if one != 1:
+        _bad(f"{name}: the last dimension must be contiguous")
+    return t.data_ptr(), row, head
+
+
+def _flat(name, t, dtype, device, n):
+    """A contiguous tensor of n values, or None: its pointer."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.device != device or t.numel() != n or not t.is_contiguous():
+        _bad(f"{name} must be a contiguous {dtype} tensor of {n} values on {device}")
+    return t.data_ptr()
+
+
+def _device(t):
+    """The device of a call's tensors: a GPU."""
+    if not t.is_cuda:
+        _bad("expected device tensors")
+    return t.device
+
+
+class _On:
+    """The call's device made current, as the library launches on the current one."""
+
+    def __init__(self, device):
+        import torch
+        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _stream_of(stream, device):
+    if stream is None:
+        import torch
+        return torch.cuda.current_stream(device).cuda_stream
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q):
+    """dash_paged_cache_t of [pages, heads_kv, page_size, d] caches (any strides, contiguous rows)."""
+    import torch
+    dev = _device(k_cache)
+    dt = k_cache.dtype
+    if dt is not torch.bfloat16 and dt is not torch.float8_e4m3fn:
+        _bad("caches must be bfloat16 or float8_e4m3fn")
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or v_cache.dtype is not dt or v_cache.device != dev:
+        _bad("k_cache and v_cache must be [pages, heads_kv, page_size, d] tensors alike")
+    pages, heads_kv, page, d = k_cache.shape
+    (kp, kh, kr, k1), (vp, vh, vr, v1) = k_cache.stride(), v_cache.stride()
+    if k1 != 1 or v1 != 1:
+        _bad("the last dimension of the caches must be contiguous")
+    batch = lens.numel()
+    if (block_table.dtype is not torch.int32 or block_table.device != dev or block_table.dim() != 2
+            or block_table.shape[0] != batch or (block_table.shape[1] > 1 and block_table.stride(1) != 1)):
+        _bad("block_table must be an int32 [batch, width] tensor with contiguous rows")
+    e4m3 = dt is torch.float8_e4m3fn
+    return dash_paged_cache_t(
+        batch, heads_q, heads_kv, d, pages, page, block_table.shape[1], DASH_CACHE_E4M3 if e4m3 else DASH_CACHE_BF16,
+        k_cache.data_ptr(), v_cache.data_ptr(), kp, kh, kr, vp, vh, vr, block_table.data_ptr(),
+        block_table.stride(0) if batch > 1 else block_table.shape[1], _flat("lens", lens, torch.int32, dev, batch),
+        _flat("k_scale", k_scale, torch.float32, dev, heads_kv), _flat("v_scale", v_scale, torch.float32, dev, heads_kv))
+
+
+def dash_kv_append(k, v, k_cache, v_cache, block_table, lens, cu=None, q=None, q_out=None, k_out=None, inv_freq=None,
+                   interleaved: bool = False, k_scale=None, v_scale=None, status=None, stream=None):
+    """New keys and values (bf16 [tokens, heads_kv, d]) into a paged cache behind the
+    ``lens`` rows that each sequence has, keys and queries rotated by their place
+    (``inv_freq``: fp32, one per rotated pair).  ``cu``: int32 [batch + 1], where each
+    sequence's tokens begin; without it every sequence gets one token.  The rotated
+    queries go to ``q_out`` and, if given, the rotated keys to ``k_out``.
+    ``status``: optional int32 that a token without a page sets to 1."""
+    import torch
+    if k.dim() != 3:
+        _bad("k must be [tokens, heads_kv, d]")
+    if (q is None) != (q_out is None):
+        _bad("q and q_out come together")
+    if q is not None and q.dim() != 3:
+        _bad("q must be [tokens, heads_q, d]")
+    tokens, heads_kv, d = k.shape
+    heads_q = heads_kv if q is None else q.shape[1]
+    c = _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q)
+    dev = k_cache.device
+    bf = torch.bfloat16
+    if c.heads_kv != heads_kv or c.d != d:
+        _bad("k and k_cache must have the same heads and head dim")
+    none = (None, 0, 0)
+    kp, vp = _rows("k", k, bf, dev, tokens, heads_kv, d), _rows("v", v, bf, dev, tokens, heads_kv, d)
+    qp = none if q is None else _rows("q", q, bf, dev, tokens, heads_q, d)
+    qo = none if q is None else _rows("q_out", q_out, bf, dev, tokens, heads_q, d)
+    ko = none if k_out is None else _rows("k_out", k_out, bf, dev, tokens, heads_kv, d)
+    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+    x = dash_append_t(tokens, _flat("cu", cu, torch.int32, dev, c.batch + 1), kp[0], vp[0], qp[0], qo[0], ko[0], *kp[1:],
+                      *vp[1:], *qp[1:], *qo[1:], *ko[1:], _flat("inv_freq", inv_freq, torch.float32, dev, rot // 2), rot,
+                      int(interleaved))
+    with _On(dev):
+        _check(load().dash_kv_append(ctypes.byref(c), ctypes.byref(x), _flat("status", status, torch.int32, dev, 1),
+                                     _stream_of(stream, dev)))
+
+
+def dash_decode_workspace_size(batch: int, heads_q: int, heads_kv: int, d: int, page_size: int, table_width: int) -> int:
+    return int(load().dash_decode_workspace_size(batch, heads_q, heads_kv, d, page_size, table_width))
+
+
+def dash_attn_decode(q, k_cache, v_cache, block_table, lens, o, lse=None, scale=None, k_scale=None, v_scale=None,
+                     workspace=None, status=None, stream=None):
+    """Attention of one query token per sequence (q: bf16 [batch, heads_q, d]) over its
+    ``lens`` cached keys into o and, if given, lse (fp32 [batch, heads_q]).
+    ``workspace``: a uint8 device tensor of dash_decode_workspace_size bytes (without
+    it one is allocated).  ``status``: optional int32 that a length or a
+    page out of range sets to 1."""
+    import torch
+    if q.dim() != 3:
+        _bad("q must be [batch, heads_q, d]")
+    batch, heads_q, d = q.shape
+    c = _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q)
+    dev = k_cache.device
+    if c.batch != batch or c.d != d:
+        _bad("q, lens and the caches must have the same batch and head dim")
+    qp, op = _rows("q", q, torch.bfloat16, dev, batch, heads_q, d), _rows("o", o, torch.bfloat16, dev, batch, heads_q, d)
+    lib = load()
+    if workspace is None:
+        if stream is not None:
+            _bad("a call on an explicit stream needs an explicit workspace")
+        n = lib.dash_decode_workspace_size(batch, heads_q, c.heads_kv, d, c.page_size, c.table_width)
+        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=dev)
+    ws = _flat("workspace", workspace, torch.uint8, dev, workspace.numel())
+    with _On(dev):
+        _check(lib.dash_attn_decode(ctypes.byref(c), qp[0], qp[1], qp[2], op[0], op[1], op[2],
+                                    _flat("lse", lse, torch.float32, dev, batch * heads_q),
+                                    0.0 if scale is None else float(scale), ws, workspace.numel(),
+                                    _flat("status", status, torch.int32, dev, 1), _stream_of(stream, dev)))
+
+
+def attn_decode(q, k_cache, v_cache, block_table, lens, scale=None, k_scale=None, v_scale=None, workspace=None,
+                status=None):
+    import torch
+    o = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    dash_attn_decode(q, k_cache, v_cache, block_table, lens, o, None, scale, k_scale, v_scale, workspace, status)
+    return o
 
 
 # ----------------------------------------------------------------- helpers

@@ -12,6 +12,7 @@
 #include <string>
 #include <tuple>
 
+#include "api.h"
 #include "dag_model.h"
 #include "dash.h"
 #include "kernels.h"
@@ -19,17 +20,25 @@
 #include "schedule.h"
 
 namespace {
-
 thread_local std::string g_err;
+}  // namespace
 
-int fail(int code, const std::string& msg) {
+int dash::api::fail(int code, const std::string& msg) {
   g_err = msg;
   return code;
 }
 
-int hip_fail(hipError_t e, const char* what) {
+int dash::api::hip_fail(hipError_t e, const char* what) {
   return fail(DASH_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
+
+namespace {
+
+using dash::api::clear_flags;
+using dash::api::device_info;
+using dash::api::DeviceInfo;
+using dash::api::fail;
+using dash::api::hip_fail;
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -89,14 +98,6 @@ Layout layout(int B, int H, int N, int d, int sched) {
   return L;
 }
 
-struct DeviceInfo {
-  int device = -1;
-  int cus = 0;
-  int occ64 = 0, occ128 = 0, occ256 = 0;
-  bool probed = false;  // nxcd is known (the probe allocates, so it runs only when XCD placement is asked for)
-  int nxcd = 0;  // XCDs, when workgroup i runs on XCD i % nxcd (0: not usable for XCD-local placement)
-};
-
 // A call with no rows still reports "no timeout": one lane stores 0 into the
 // workspace's error flag and / or the caller's status word (a kernel, not a
 // memset, so that the call stays capturable into a HIP graph).
@@ -106,8 +107,6 @@ __global__ void clear_flags_kernel(int* flag, int* status) {
     if (status) *status = 0;
   }
 }
-
-int clear_flags(int* flag, int* status, void* stream);
 
 // Each workgroup records the XCD it runs on.
 __global__ void xcc_probe_kernel(int* out) {
@@ -149,12 +148,7 @@ constexpr size_t kScratchBytes = (size_t)256 << 20;
 // module load until the process ends.
 static __device__ __align__(256) unsigned char dash_scratch[kScratchBytes];
 
-namespace {
-
-// The current device's properties (queried once per device).  With xcd, also
-// whether XCD-local placement is usable: that probe runs a kernel on a small
-// buffer it allocates, so only calls that ask for XCD placement run it.
-int device_info(DeviceInfo* out, bool xcd = false) {
+int dash::api::device_info(DeviceInfo* out, bool xcd) {
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return fail(DASH_ERR_NO_DEVICE, std::string("hipGetDevice: ") + hipGetErrorString(e));
@@ -181,6 +175,8 @@ int device_info(DeviceInfo* out, bool xcd = false) {
   *out = di;
   return DASH_OK;
 }
+
+namespace {
 
 int check_shape(int B, int H, int N, int d) {
   if (B < 0 || H < 0 || N < 0) return fail(DASH_ERR_INVALID_ARG, "B, H and N must be >= 0");
@@ -485,14 +481,14 @@ int dash_attn_fwd(const void* q, const void* k, const void* v, void* o, float* l
 
 }  // extern "C"
 
-namespace {
-
-int clear_flags(int* flag, int* status, void* stream) {
+int dash::api::clear_flags(int* flag, int* status, void* stream) {
   if (!flag && !status) return DASH_OK;
   hipLaunchKernelGGL(clear_flags_kernel, dim3(1), dim3(64), 0, (hipStream_t)stream, flag, status);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? DASH_OK : hip_fail(e, "flag reset launch");
 }
+
+namespace {
 
 // The backward on `workspace` (dash_attn_bwd_ex's contract); `status`, if
 // non-null, is a device int that bwd_pre zeroes and a wait timeout sets.

@@ -1,0 +1,185 @@
+// kv_append.hip -- new keys and values into a paged cache, keys (and queries)
+// rotated by their position on the way.
+//
+// Token t of sequence s stands at place p = lens[s] + (t - cu[s]).  Pair i of a
+// head's first `rotary` components turns by the angle p f_i:
+//   (x, y) -> (x cos - y sin, x sin + y cos),
+// pairs being (i, i + rotary / 2), or (2i, 2i + 1) when interleaved.  The angle is
+// reduced in 64 bits: at p = 10^5 a product in 32 bits is off by 2^-24 10^5 = 0.006
+// radians, more than a bf16 rounding.  The rest is 32 bits with one rounding at the
+// store (bf16, or value / scale[head] in e4m3).
+//
+// Bound by memory for prompts (q, k, v in, q and the cache rows out) and by the
+// launch for single tokens.  One wave per token: it takes sine and cosine of every
+// pair once (through LDS, for all heads), then 64 items of 16 components a round --
+// the 8 pairs 8j .. 8j+7 of a head, which in both pairings are two 16-byte chunks, so
+// that a lane never needs another lane's data and q_out may be q.  Calls with few
+// tokens give each wave one round only, and the waves of a token redo its sines.
+#include "common.h"
+#include "ops.h"
+#include "page_index.h"
+#include "paged.h"
+
+namespace dash {
+namespace {
+
+constexpr int kWaves = 4;
+
+__device__ inline float bf_lo(unsigned x) { return __builtin_bit_cast(float, x << 16); }
+__device__ inline float bf_hi(unsigned x) { return __builtin_bit_cast(float, x & 0xffff0000u); }
+
+// 4 values -> e4m3, saturated at 448 (a NaN stays one)
+__device__ inline unsigned pack_e4m3(const float* x) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = x[i] != x[i] ? x[i] : __builtin_amdgcn_fmed3f(x[i], -448.f, 448.f);
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], r, true);
+}
+
+template <int D>
+__global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, int rounds) {
+  constexpr int IPH = D / 16;    // items per head
+  constexpr int HPR = 64 / IPH;  // heads per round
+  __shared__ float2 turn[kWaves][D / 2];
+  const CacheArgs& c = a.c;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
+  const int hq = a.q ? c.heads_q : 0, heads = hq + 2 * c.heads_kv;
+  const int total_rounds = (heads + HPR - 1) / HPR;
+  const int per_token = (total_rounds + rounds - 1) / rounds;  // waves
+  const long wave = (long)blockIdx.x * kWaves + w;
+  const int t = (int)(wave / per_token);
+  if (t >= a.tokens) return;
+  const int first = (int)(wave % per_token) * rounds;
+
+  int s = t, place = 0;
+  if (a.cu) {
+    s = find_sequence(a.cu, c.batch, t, l);
+    if (s < 0) return;  // behind the last sequence
+    place = t - a.cu[s];
+  }
+  const int old = c.lens[s];
+  const int64_t at_place = (int64_t)place + old;
+
+  // sine and cosine of pair i = l, l + 64: whole turns are taken off in 64 bits
+  const int pairs = a.inv_freq ? a.rotary >> 1 : 0;
+  for (int i = l; i < pairs; i += 64) {
+    const double turns = (double)at_place * (double)a.inv_freq[i] * 0.15915494309189535;
+    const float part = (float)(2.0 * (turns - rint(turns)));  // half turns, -1 .. 1
+    float sn, cs;
+    sincospif(part, &sn, &cs);
+    turn[w][i] = make_float2(cs, sn);
+  }
+  // (a wave's own LDS writes and reads are in order)
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+
+  // the token's cache row
+  const PageRow to = page_row(c.table + s * c.table_stride, c.table_width, c.page_size, c.pages, old < 0 ? -1 : at_place);
+  if (!to.ok && l == 0 && c.status) *c.status = 1;
+
+  const int j = l % IPH;
+  const bool rot = 8 * j < pairs;
+  const bool split = rot && !a.interleaved;
+  // element offsets of the item's two chunks
+  const int e0 = split ? 8 * j : 16 * j, e1 = split ? e0 + pairs : e0 + 8;
+  float cs[8], sn[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float2 x = rot ? turn[w][8 * j + i] : make_float2(1.f, 0.f);
+    cs[i] = x.x;
+    sn[i] = x.y;
+  }
+  for (int r = first; r < first + rounds; ++r) {
+    const int h = r * HPR + l / IPH;
+    if (h >= heads) return;
+    const int kind = h < hq ? 0 : h < hq + c.heads_kv ? 1 : 2;  // q, k, v
+    const int hk = kind == 1 ? h - hq : h - hq - c.heads_kv;    // head of the cache
+    const __bf16* src = kind == 0   ? (const __bf16*)a.q + t * a.qs.row + h * a.qs.head
+                        : kind == 1 ? (const __bf16*)a.k + t * a.ks.row + hk * a.ks.head
+                                    : (const __bf16*)a.v + t * a.vs.row + hk * a.vs.head;
+    u32x4 x0 = *(const u32x4*)(src + e0), x1 = *(const u32x4*)(src + e1);
+    float y0[8], y1[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y0[2 * i] = bf_lo(x0[i]);
+      y0[2 * i + 1] = bf_hi(x0[i]);
+      y1[2 * i] = bf_lo(x1[i]);
+      y1[2 * i + 1] = bf_hi(x1[i]);
+    }
+    if (kind != 2 && rot) {
+      if (split) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float x = y0[i], y = y1[i];
+          y0[i] = x * cs[i] - y * sn[i];
+          y1[i] = x * sn[i] + y * cs[i];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x = y0[2 * i], y = y0[2 * i + 1];
+          y0[2 * i] = x * cs[i] - y * sn[i];
+          y0[2 * i + 1] = x * sn[i] + y * cs[i];
+          x = y1[2 * i], y = y1[2 * i + 1];
+          y1[2 * i] = x * cs[4 + i] - y * sn[4 + i];
+          y1[2 * i + 1] = x * sn[4 + i] + y * cs[4 + i];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x0[i] = pack_bf16(y0[2 * i], y0[2 * i + 1]);
+        x1[i] = pack_bf16(y1[2 * i], y1[2 * i + 1]);
+      }
+    }
+    __bf16* out = kind == 0                ? (__bf16*)a.q_out + t * a.qos.row + h * a.qos.head
+                  : kind == 1 && a.k_out   ? (__bf16*)a.k_out + t * a.kos.row + hk * a.kos.head
+                                           : nullptr;
+    if (out) {
+      *(u32x4*)(out + e0) = x0;
+      *(u32x4*)(out + e1) = x1;
+    }
+    if (kind == 0 || !to.ok) continue;
+    const int64_t at = kind == 1 ? to.page * c.k_page + hk * c.k_head + to.row * c.k_row : to.page * c.v_page + hk * c.v_head + to.row * c.v_row;
+    if (!c.e4m3) {
+      __bf16* dst = (__bf16*)(kind == 1 ? c.k : c.v) + at;
+      *(u32x4*)(dst + e0) = x0;
+      *(u32x4*)(dst + e1) = x1;
+    } else {
+      const float* sc = kind == 1 ? c.k_scale : c.v_scale;
+      if (sc) {
+        const float scale = sc[hk];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          y0[i] /= scale;
+          y1[i] /= scale;
+        }
+      }
+      uint8_t* dst = (uint8_t*)(kind == 1 ? c.k : c.v) + at;
+      *(u32x2*)(dst + e0) = u32x2{pack_e4m3(y0), pack_e4m3(y0 + 4)};
+      *(u32x2*)(dst + e1) = u32x2{pack_e4m3(y1), pack_e4m3(y1 + 4)};
+    }
+  }
+}
+
+template <int D>
+void launch(const AppendArgs& a, hipStream_t stream) {
+  constexpr int HPR = 64 / (D / 16);
+  const int heads = (a.q ? a.c.heads_q : 0) + 2 * a.c.heads_kv;
+  const int total = (heads + HPR - 1) / HPR;
+  // one round per wave until the waves fill the GPU (256 CUs of 16), then as many
+  // rounds as a token has
+  const int rounds = (long)a.tokens * total <= 4096 ? 1 : total;
+  const long waves = (long)a.tokens * ((total + rounds - 1) / rounds);
+  hipLaunchKernelGGL(kv_append_kernel<D>, dim3((unsigned)((waves + kWaves - 1) / kWaves)), dim3(64 * kWaves), 0, stream, a, rounds);
+}
+
+}  // namespace
+
+hipError_t launch_kv_append(const AppendArgs& a, hipStream_t stream) {
+  if (a.c.d == 64) launch<64>(a, stream);
+  else if (a.c.d == 128) launch<128>(a, stream);
+  else launch<256>(a, stream);
+  return hipGetLastError();
+}
+
+}  // namespace dash

@@ -1,0 +1,55 @@
+// paged.h -- device pieces shared by the variable-length operators: which
+// sequence a row belongs to, and reductions over the wave.
+#pragma once
+#include "common.h"
+
+namespace dash {
+
+// The sequence that row t lies in: the last s with cu[s] <= t, or -1 where t is at
+// or behind cu[batch].  A search with 64 samples a step (one load per lane): two
+// steps up to 4096 sequences.  Wave-uniform, all lanes active.  A table that
+// does not rise gives some s in 0 .. batch-1 or -1.
+__device__ inline int find_sequence(const int32_t* cu, int batch, int t, int l) {
+  if (t >= cu[batch]) return -1;
+  int lo = 0, n = batch;  // the answer is in [lo, lo + n)
+  while (n > 1) {
+    const int step = (n + 63) / 64;
+    const int at = l * step;
+    const bool below = at < n && cu[lo + at] <= t;
+    const int c = __builtin_popcountll(__ballot(below));  // samples at or below t: a prefix
+    const int k = c > 0 ? c - 1 : 0;
+    lo += k * step;
+    n = n - k * step < step ? n - k * step : step;
+  }
+  return lo;
+}
+
+// sum over the 64 lanes, all lanes receive it
+__device__ inline int wave_sum(int x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+  return x;
+}
+
+// Over the four lanes l % 16 + 16 i.  The swaps exchange the upper half (every odd
+// row of 16) of one register with the lower half (even row) of another, here two
+// copies of x: afterwards the two hold x of both partners.
+template <typename Op>
+__device__ inline float quad_reduce(float x, Op&& op) {
+  const unsigned u = __builtin_bit_cast(unsigned, x);
+  const auto p = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const unsigned p0 = p[0], p1 = p[1];  // (a bit cast of p[1] itself would take p[0])
+  const float y = op(__builtin_bit_cast(float, p0), __builtin_bit_cast(float, p1));
+  const unsigned v = __builtin_bit_cast(unsigned, y);
+  const auto q = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  const unsigned q0 = q[0], q1 = q[1];
+  return op(__builtin_bit_cast(float, q0), __builtin_bit_cast(float, q1));
+}
+__device__ inline float quad_max(float x) {
+  return quad_reduce(x, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ inline float quad_sum(float x) {
+  return quad_reduce(x, [](float a, float b) { return a + b; });
+}
+
+}  // namespace dash
