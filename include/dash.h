@@ -438,6 +438,31 @@ int dash_attn_decode(const dash_paged_cache_t* cache, const void* q, int64_t q_r
                      void* o, int64_t o_row_stride, int64_t o_head_stride, float* lse, float scale, void* workspace,
                      size_t ws_bytes, int* status, void* stream);
 
+/* Packed sequences: the queries of sequence s are rows cu_q[s] .. cu_q[s+1]-1 of q
+   (keys: cu_k, k and v); offsets rise from 0.  Rows from cu_q[batch] (cu_k[batch]) on
+   belong to nobody: what they hold is not read into any result, and outputs are left
+   alone there.  With m queries and n keys and causal != 0, query i of a sequence sees
+   key j iff j - i <= n - m (the last query sees every key); else all n.  A NaN or an
+   infinity in V reaches, under a causal mask, queries before it as well where they share a
+   tile with it (0 * NaN): up to 31 rows back in O, a KV tile in dQ; one in K the latter. */
+typedef struct {
+  int batch, heads_q, heads_kv, d, causal;
+  int total_q, total_k; /* rows of the tensors */
+  float scale;          /* as in dash_attn_fwd_ex */
+  const int32_t* cu_q;  /* [batch + 1] */
+  const int32_t* cu_k;  /* [batch + 1]; NULL: cu_q */
+  /* strides in elements; those of dO, dq, dk, dv are for the backward */
+  int64_t q_row_stride, q_head_stride, k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  int64_t o_row_stride, o_head_stride, do_row_stride, do_head_stride;
+  int64_t dq_row_stride, dq_head_stride, dk_row_stride, dk_head_stride, dv_row_stride, dv_head_stride;
+} dash_packed_t;
+
+/* Forward over packed sequences: q, o bf16 [total_q][heads_q][d], k, v bf16
+   [total_k][heads_kv][d], lse fp32 [heads_q][total_q] contiguous.  Asynchronous on
+   `stream`. */
+int dash_attn_packed_fwd(const dash_packed_t* p, const void* q, const void* k, const void* v, void* o, float* lse,
+                         void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -30,7 +30,7 @@ EXPORTS = ("dash_attn_fwd", "dash_attn_fwd_ex", "dash_attn_bwd", "dash_bwd_works
            "dash_attn_bwd_ex", "dash_attn_bwd_noalloc", "dash_bwd_check", "dash_resolve_schedule", "dash_schedule_table",
            "dash_bwd_placement", "dash_mfma_peak", "dash_last_error", "dash_release_workspace",
            "dash_auto_schedule", "dash_model_makespan", "dash_kv_append", "dash_attn_decode",
-           "dash_decode_workspace_size")
+           "dash_decode_workspace_size", "dash_attn_packed_fwd")
 DASH_CACHE_BF16, DASH_CACHE_E4M3 = 0, 1
 
 
@@ -68,6 +68,12 @@ class dash_append_t(ctypes.Structure):
                 ("inv_freq", _VP), ("rotary_dim", _CI), ("interleaved", _CI)]
 
 
+class dash_packed_t(ctypes.Structure):
+    _fields_ = [("batch", _CI), ("heads_q", _CI), ("heads_kv", _CI), ("d", _CI), ("causal", _CI), ("total_q", _CI),
+                ("total_k", _CI), ("scale", ctypes.c_float), ("cu_q", _VP), ("cu_k", _VP)]
+    _fields_ += [(f"{t}_{s}_stride", _I64) for t in ("q", "k", "v", "o", "do", "dq", "dk", "dv") for s in ("row", "head")]
+
+
 _lib = None
 
 
@@ -100,12 +106,14 @@ def load():
         lib.dash_attn_decode.argtypes = [ctypes.POINTER(dash_paged_cache_t), vp, _I64, _I64, vp, _I64, _I64, vp, cf, vp,
                                          sz, vp, vp]
         lib.dash_decode_workspace_size.argtypes = [ci] * 6
+        lib.dash_attn_packed_fwd.argtypes = [ctypes.POINTER(dash_packed_t)] + [vp] * 6
         lib.dash_decode_workspace_size.restype = sz
         lib.dash_last_error.restype = ctypes.c_char_p
         lib.dash_release_workspace.restype = None
         for f in ("dash_attn_fwd", "dash_attn_fwd_ex", "dash_attn_bwd", "dash_attn_bwd_ex", "dash_attn_bwd_noalloc",
                   "dash_bwd_check", "dash_resolve_schedule", "dash_schedule_table", "dash_bwd_placement",
-                  "dash_mfma_peak", "dash_auto_schedule", "dash_model_makespan", "dash_kv_append", "dash_attn_decode"):
+                  "dash_mfma_peak", "dash_auto_schedule", "dash_model_makespan", "dash_kv_append", "dash_attn_decode",
+                  "dash_attn_packed_fwd"):
             getattr(lib, f).restype = ci
         _lib = lib
     return _lib
@@ -426,6 +434,47 @@ def attn_decode(q, k_cache, v_cache, block_table, lens, scale=None, k_scale=None
     o = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
     dash_attn_decode(q, k_cache, v_cache, block_table, lens, o, None, scale, k_scale, v_scale, workspace, status)
     return o
+
+
+def _packed(q, k, cu_q, cu_k, causal, scale):
+    """dash_packed_t of a packed call, the strides still to be set."""
+    import torch
+    if q.dim() != 3 or k.dim() != 3:
+        _bad("q and k must be [tokens, heads, d]")
+    (tq, hq, d), (tk, hkv, _) = q.shape, k.shape
+    dev = _device(q)
+    if cu_q.dim() != 1 or cu_q.numel() < 1:
+        _bad("cu_q must be int32 [batch + 1]")
+    batch = cu_q.numel() - 1
+    if cu_k is None and tk != tq:
+        _bad("without cu_k, k must have as many rows as q")
+    return dash_packed_t(batch, hq, hkv, d, int(causal), tq, tk, 0.0 if scale is None else float(scale),
+                         _flat("cu_q", cu_q, torch.int32, dev, batch + 1), _flat("cu_k", cu_k, torch.int32, dev, batch + 1)), dev
+
+
+def dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k=None, causal: bool = True, scale=None, stream=None):
+    """O and L of attention over packed sequences into o (bf16 [total_q, heads_q, d]) and
+    lse (fp32 [heads_q, total_q]); q like o, k and v [total_k, heads_kv, d], any row and
+    head strides.  ``cu_q``, ``cu_k``: int32 [batch + 1], where each sequence's queries and
+    keys begin (the same without ``cu_k``); a causal mask is aligned to the last key."""
+    import torch
+    p, dev = _packed(q, k, cu_q, cu_k, causal, scale)
+    bf = torch.bfloat16
+    a, p.q_row_stride, p.q_head_stride = _rows("q", q, bf, dev, p.total_q, p.heads_q, p.d)
+    b, p.k_row_stride, p.k_head_stride = _rows("k", k, bf, dev, p.total_k, p.heads_kv, p.d)
+    c, p.v_row_stride, p.v_head_stride = _rows("v", v, bf, dev, p.total_k, p.heads_kv, p.d)
+    e, p.o_row_stride, p.o_head_stride = _rows("o", o, bf, dev, p.total_q, p.heads_q, p.d)
+    with _On(dev):
+        _check(load().dash_attn_packed_fwd(ctypes.byref(p), a, b, c, e, _flat("lse", lse, torch.float32, dev, p.heads_q * p.total_q),
+                                           _stream_of(stream, dev)))
+
+
+def attn_packed_fwd(q, k, v, cu_q, cu_k=None, causal: bool = True, scale=None):
+    import torch
+    o = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
+    dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k, causal, scale)
+    return o, lse
 
 
 # ----------------------------------------------------------------- helpers

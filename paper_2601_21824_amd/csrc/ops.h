@@ -59,4 +59,16 @@ int decode_workers(int heads_q, int heads_kv);
 int decode_slots(int batch, int heads_q, int heads_kv, int table_tokens);
 hipError_t launch_decode(const DecodeArgs& a, hipStream_t stream);
 
+// ---------------------------------------------------------------- packed sequences
+struct PackedArgs {
+  const void *q, *k, *v;
+  void* o;
+  float* lse;  // [heads_q][total_q]
+  const int32_t *cu_q, *cu_k;
+  int batch, heads_q, heads_kv, total_q, total_k, causal;
+  float scale;
+  Strides qs, ks, vs, os;
+};
+hipError_t launch_packed_fwd(const PackedArgs& a, int d, hipStream_t stream);
+
 }  // namespace dash

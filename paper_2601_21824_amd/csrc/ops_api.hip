@@ -20,7 +20,7 @@ using dash::api::hip_fail;
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 constexpr int64_t kMaxRowStride = 1 << 22;
-constexpr int kMaxBatch = 1 << 20, kMaxHeads = 1 << 12;
+constexpr int kMaxBatch = 1 << 20, kMaxHeads = 1 << 12, kMaxRows = 1 << 28;
 
 int check_heads(int batch, int heads_q, int heads_kv, int d) {
   if (batch < 0 || batch > kMaxBatch) return fail(DASH_ERR_INVALID_ARG, "batch must be in 0 .. 2^20");
@@ -182,6 +182,48 @@ int attn_decode(const dash_paged_cache_t* c, const void* q, int64_t q_row, int64
   return e == hipSuccess ? DASH_OK : hip_fail(e, "decode launch");
 }
 
+// what both directions of a packed call need; false in *work: nothing to compute
+int check_packed(const dash_packed_t* p, float* scale, const void* q, const void* k, const void* v, const void* o, bool o_written,
+                 const float* lse, bool* work) {
+  if (!p) return fail(DASH_ERR_INVALID_ARG, "null problem");
+  int rc = check_heads(p->batch, p->heads_q, p->heads_kv, p->d);
+  if (rc) return rc;
+  *scale = p->scale;
+  if ((rc = check_scale(scale, p->d))) return rc;
+  if (p->total_q < 0 || p->total_k < 0 || p->total_q > kMaxRows || p->total_k > kMaxRows)
+    return fail(DASH_ERR_INVALID_ARG, "total_q and total_k must be in 0 .. 2^28");
+  if ((int64_t)(p->total_q / 64 + p->batch) * p->heads_q >= (1 << 24))
+    return fail(DASH_ERR_UNSUPPORTED, "(total_q / 64 + batch) * heads_q must be below 2^24");
+  *work = p->batch > 0 && (p->total_q > 0 || p->total_k > 0);
+  if (!*work) return DASH_OK;
+  if (!p->cu_q) return fail(DASH_ERR_INVALID_ARG, "null cu_q");
+  if (!p->cu_k && p->total_k != p->total_q) return fail(DASH_ERR_INVALID_ARG, "without cu_k, total_k must be total_q");
+  const int64_t nq = p->total_q, nk = p->total_k;
+  if (nq && (rc = check_tensor("q", q, nq, p->heads_q, p->d, p->q_row_stride, p->q_head_stride, 8, false))) return rc;
+  if (nk && (rc = check_tensor("k", k, nk, p->heads_kv, p->d, p->k_row_stride, p->k_head_stride, 8, false))) return rc;
+  if (nk && (rc = check_tensor("v", v, nk, p->heads_kv, p->d, p->v_row_stride, p->v_head_stride, 8, false))) return rc;
+  if (nq && (rc = check_tensor("o", o, nq, p->heads_q, p->d, p->o_row_stride, p->o_head_stride, 8, o_written))) return rc;
+  if (nq && !lse) return fail(DASH_ERR_INVALID_ARG, "lse: null pointer");
+  return DASH_OK;
+}
+
+dash::PackedArgs packed_args(const dash_packed_t* p, float scale, const void* q, const void* k, const void* v, void* o, float* lse) {
+  return {q, k, v, o, lse, p->cu_q, p->cu_k ? p->cu_k : p->cu_q, p->batch, p->heads_q, p->heads_kv, p->total_q, p->total_k,
+          p->causal ? 1 : 0, scale, {p->q_row_stride, p->q_head_stride}, {p->k_row_stride, p->k_head_stride},
+          {p->v_row_stride, p->v_head_stride}, {p->o_row_stride, p->o_head_stride}};
+}
+
+int attn_packed_fwd(const dash_packed_t* p, const void* q, const void* k, const void* v, void* o, float* lse, void* stream) {
+  bool work = false;
+  float scale = 0.f;
+  int rc = check_packed(p, &scale, q, k, v, o, true, lse, &work);
+  if (rc || !work || p->total_q == 0) return rc;
+  DeviceInfo di;
+  if ((rc = device_info(&di))) return rc;
+  const hipError_t e = dash::launch_packed_fwd(packed_args(p, scale, q, k, v, o, lse), p->d, (hipStream_t)stream);
+  return e == hipSuccess ? DASH_OK : hip_fail(e, "packed forward launch");
+}
+
 // no C++ exception (an error message that finds no memory) crosses the interface
 template <typename F>
 int guarded(F&& f) {
@@ -218,6 +260,10 @@ int dash_attn_decode(const dash_paged_cache_t* cache, const void* q, int64_t q_r
     return attn_decode(cache, q, q_row_stride, q_head_stride, o, o_row_stride, o_head_stride, lse, scale, workspace, ws_bytes,
                        status, stream);
   });
+}
+
+int dash_attn_packed_fwd(const dash_packed_t* p, const void* q, const void* k, const void* v, void* o, float* lse, void* stream) {
+  return guarded([&] { return attn_packed_fwd(p, q, k, v, o, lse, stream); });
 }
 
 }  // extern "C"

@@ -5,17 +5,16 @@
 
 namespace dash {
 
-// The sequence that row t lies in: the last s with cu[s] <= t, or -1 where t is at
-// or behind cu[batch].  A search with 64 samples a step (one load per lane): two
-// steps up to 4096 sequences.  Wave-uniform, all lanes active.  A table that
-// does not rise gives some s in 0 .. batch-1 or -1.
-__device__ inline int find_sequence(const int32_t* cu, int batch, int t, int l) {
-  if (t >= cu[batch]) return -1;
-  int lo = 0, n = batch;  // the answer is in [lo, lo + n)
+// The last s in 0 .. n-1 with key(s) <= t (0 if there is none), for keys that rise.
+// A search with 64 samples a step (one key per lane): two steps up to 4096.
+// Wave-uniform, all lanes active.  Keys that do not rise give some s in 0 .. n-1.
+template <typename Key>
+__device__ inline int find_last(int n, int t, int l, Key&& key) {
+  int lo = 0;  // the answer is in [lo, lo + n)
   while (n > 1) {
     const int step = (n + 63) / 64;
     const int at = l * step;
-    const bool below = at < n && cu[lo + at] <= t;
+    const bool below = at < n && key(lo + at) <= t;
     const int c = __builtin_popcountll(__ballot(below));  // samples at or below t: a prefix
     const int k = c > 0 ? c - 1 : 0;
     lo += k * step;
@@ -23,6 +22,29 @@ __device__ inline int find_sequence(const int32_t* cu, int batch, int t, int l) 
   }
   return lo;
 }
+
+// The sequence that row t lies in, -1 where t is at or behind cu[batch].
+__device__ inline int find_sequence(const int32_t* cu, int batch, int t, int l) {
+  if (t >= cu[batch]) return -1;
+  return find_last(batch, t, l, [&](int s) { return cu[s]; });
+}
+
+// Rows of sequence s among `total`: offsets outside 0 .. total are clamped, and an
+// end before its start makes an empty sequence.
+struct Span {
+  int start, len;
+};
+__device__ inline int clamp_row(int x, int total) { return x < 0 ? 0 : x > total ? total : x; }
+__device__ inline Span span_of(const int32_t* cu, int s, int total) {
+  const int b = clamp_row(cu[s], total), e = clamp_row(cu[s + 1], total);
+  return {b, e > b ? e - b : 0};
+}
+
+// Blocks of `rows` rows, numbered so that no prefix sum is needed: those of
+// sequence s begin at start / rows + s.  (A sequence of n rows has at most
+// (start + n) / rows - start / rows + 1 of them.)  At most total / rows + batch slots;
+// those between two sequences' blocks are empty.
+__device__ inline int first_slot(const int32_t* cu, int s, int total, int rows) { return clamp_row(cu[s], total) / rows + s; }
 
 // sum over the 64 lanes, all lanes receive it
 __device__ inline int wave_sum(int x) {
