@@ -463,6 +463,26 @@ typedef struct {
 int dash_attn_packed_fwd(const dash_packed_t* p, const void* q, const void* k, const void* v, void* o, float* lse,
                          void* stream);
 
+/* Bytes of workspace for dash_attn_packed_bwd (0 if the arguments are invalid). */
+size_t dash_packed_workspace_size(int batch, int total_q, int total_k, int heads_q, int heads_kv, int d);
+
+/*
+ * Backward over packed sequences, from the forward's O and L: dq like q, dk and dv like k
+ * (each K/V head's gradient is the sum over its query heads).  Deterministic: dK and dV
+ * are summed by one workgroup, dQ over the KV tiles in ascending order by the ordered
+ * reduction of dash_attn_bwd_ex (Descending Q-Tile Iteration, Section 3.3, over the
+ * blocks of all query heads of a group).  The KV tile, and with it the order of the
+ * sums, depends on total_k and heads_kv at d = 128.  Asynchronous on `stream`, launched
+ * without cooperation: its waits only point to work that started earlier.
+ * Workspace of ws_bytes >= dash_packed_workspace_size(...) bytes, 256-byte aligned, any
+ * contents, not used by another call until this one has finished.  A wait timeout is
+ * recorded there (dash_bwd_check) and in status (NULL or a device int that the call sets
+ * to 0, or 1 after a timeout): it can only happen where cu_q or cu_k do not rise.
+ */
+int dash_attn_packed_bwd(const dash_packed_t* p, const void* q, const void* k, const void* v, const void* o,
+                         const void* dO, const float* lse, void* dq, void* dk, void* dv, void* workspace,
+                         size_t ws_bytes, int* status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

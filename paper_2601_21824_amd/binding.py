@@ -30,7 +30,8 @@ EXPORTS = ("dash_attn_fwd", "dash_attn_fwd_ex", "dash_attn_bwd", "dash_bwd_works
            "dash_attn_bwd_ex", "dash_attn_bwd_noalloc", "dash_bwd_check", "dash_resolve_schedule", "dash_schedule_table",
            "dash_bwd_placement", "dash_mfma_peak", "dash_last_error", "dash_release_workspace",
            "dash_auto_schedule", "dash_model_makespan", "dash_kv_append", "dash_attn_decode",
-           "dash_decode_workspace_size", "dash_attn_packed_fwd")
+           "dash_decode_workspace_size", "dash_attn_packed_fwd", "dash_attn_packed_bwd",
+           "dash_packed_workspace_size")
 DASH_CACHE_BF16, DASH_CACHE_E4M3 = 0, 1
 
 
@@ -106,6 +107,9 @@ def load():
         lib.dash_attn_decode.argtypes = [ctypes.POINTER(dash_paged_cache_t), vp, _I64, _I64, vp, _I64, _I64, vp, cf, vp,
                                          sz, vp, vp]
         lib.dash_decode_workspace_size.argtypes = [ci] * 6
+        lib.dash_attn_packed_bwd.argtypes = [ctypes.POINTER(dash_packed_t)] + [vp] * 10 + [sz, vp, vp]
+        lib.dash_packed_workspace_size.argtypes = [ci] * 6
+        lib.dash_packed_workspace_size.restype = sz
         lib.dash_attn_packed_fwd.argtypes = [ctypes.POINTER(dash_packed_t)] + [vp] * 6
         lib.dash_decode_workspace_size.restype = sz
         lib.dash_last_error.restype = ctypes.c_char_p
@@ -113,7 +117,8 @@ def load():
         for f in ("dash_attn_fwd", "dash_attn_fwd_ex", "dash_attn_bwd", "dash_attn_bwd_ex", "dash_attn_bwd_noalloc",
                   "dash_bwd_check", "dash_resolve_schedule", "dash_schedule_table", "dash_bwd_placement",
                   "dash_mfma_peak", "dash_auto_schedule", "dash_model_makespan", "dash_kv_append", "dash_attn_decode",
-                  "dash_attn_packed_fwd"):
+                  "dash_attn_packed_fwd", "dash_attn_packed_bwd",
+           "dash_packed_workspace_size"):
             getattr(lib, f).restype = ci
         _lib = lib
     return _lib
@@ -475,6 +480,48 @@ def attn_packed_fwd(q, k, v, cu_q, cu_k=None, causal: bool = True, scale=None):
     lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
     dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k, causal, scale)
     return o, lse
+
+
+def dash_packed_workspace_size(batch: int, total_q: int, total_k: int, heads_q: int, heads_kv: int, d: int) -> int:
+    return int(load().dash_packed_workspace_size(batch, total_q, total_k, heads_q, heads_kv, d))
+
+
+def dash_attn_packed_bwd(q, k, v, o, dO, lse, dq, dk, dv, cu_q, cu_k=None, causal: bool = True, scale=None,
+                         workspace=None, status=None, stream=None):
+    """Backward of dash_attn_packed_fwd into dq (like q), dk and dv (like k), from its o
+    and lse.  ``workspace``: a uint8 device tensor of dash_packed_workspace_size bytes
+    (without it one is allocated).  ``status``: optional int32 that receives 0, or 1
+    after a wait timeout (offsets that do not rise)."""
+    import torch
+    p, dev = _packed(q, k, cu_q, cu_k, causal, scale)
+    bf = torch.bfloat16
+    a, p.q_row_stride, p.q_head_stride = _rows("q", q, bf, dev, p.total_q, p.heads_q, p.d)
+    b, p.k_row_stride, p.k_head_stride = _rows("k", k, bf, dev, p.total_k, p.heads_kv, p.d)
+    c, p.v_row_stride, p.v_head_stride = _rows("v", v, bf, dev, p.total_k, p.heads_kv, p.d)
+    e, p.o_row_stride, p.o_head_stride = _rows("o", o, bf, dev, p.total_q, p.heads_q, p.d)
+    f, p.do_row_stride, p.do_head_stride = _rows("dO", dO, bf, dev, p.total_q, p.heads_q, p.d)
+    x, p.dq_row_stride, p.dq_head_stride = _rows("dq", dq, bf, dev, p.total_q, p.heads_q, p.d)
+    y, p.dk_row_stride, p.dk_head_stride = _rows("dk", dk, bf, dev, p.total_k, p.heads_kv, p.d)
+    z, p.dv_row_stride, p.dv_head_stride = _rows("dv", dv, bf, dev, p.total_k, p.heads_kv, p.d)
+    lib = load()
+    if workspace is None:
+        if stream is not None:
+            _bad("a call on an explicit stream needs an explicit workspace")
+        n = lib.dash_packed_workspace_size(p.batch, p.total_q, p.total_k, p.heads_q, p.heads_kv, p.d)
+        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=dev)
+    ws = _flat("workspace", workspace, torch.uint8, dev, workspace.numel())
+    with _On(dev):
+        _check(lib.dash_attn_packed_bwd(ctypes.byref(p), a, b, c, e, f,
+                                        _flat("lse", lse, torch.float32, dev, p.heads_q * p.total_q), x, y, z, ws,
+                                        workspace.numel(), _flat("status", status, torch.int32, dev, 1),
+                                        _stream_of(stream, dev)))
+
+
+def attn_packed_bwd(q, k, v, o, dO, lse, cu_q, cu_k=None, causal: bool = True, scale=None, workspace=None):
+    import torch
+    dq, dk, dv = (torch.empty(t.shape, dtype=torch.bfloat16, device=t.device) for t in (q, k, v))
+    dash_attn_packed_bwd(q, k, v, o, dO, lse, dq, dk, dv, cu_q, cu_k, causal, scale, workspace)
+    return dq, dk, dv
 
 
 # ----------------------------------------------------------------- helpers

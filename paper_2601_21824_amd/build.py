@@ -13,9 +13,9 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libdash.so")
 SOURCES = ["attn_fwd.hip", "attn_bwd.hip", "attn_bwd_d64.hip", "attn_bwd64w.hip", "attn_bwd256.hip", "attn_bwdw.hip", "attn_dq.hip", "mfma_peak.hip",
-           "kv_append.hip", "attn_decode.hip", "attn_packed_fwd.hip", "dash_api.hip", "ops_api.hip"]
+           "kv_append.hip", "attn_decode.hip", "attn_packed_fwd.hip", "attn_packed_bwd.hip", "dash_api.hip", "ops_api.hip"]
 HEADERS = ["common.h", "kernels.h", "schedule.h", "bwd_common.h", "bwd_main.h", "lds_layout.h", "dag_model.h", "model_calibration.h",
-           "fwd_main.h", "api.h", "ops.h", "paged.h", "page_index.h"]
+           "fwd_main.h", "api.h", "ops.h", "paged.h", "packed_order.h", "packed_chain.h", "page_index.h"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -210,6 +210,10 @@ hipError_t launch_all(const BwdArgs& a, int grid_main, hipStream_t stream) {
   return hipGetLastError();
 }
 
+hipError_t launch_packed_main128(const PackedBwdArgs& a, int grid, hipStream_t stream) {
+  return launch_packed_main<128>(a, grid, stream);
+}
+
 hipError_t launch_bwd(const BwdArgs& a, int d, int grid_main, hipStream_t stream) {
   if (d == 64) return launch_all<64>(a, grid_main, stream);
   if (d == 128) return launch_all<128>(a, grid_main, stream);

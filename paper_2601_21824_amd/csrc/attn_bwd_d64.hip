@@ -12,6 +12,10 @@ hipError_t launch_main64(const BwdArgs& a, int grid_main, hipStream_t stream) {
   return launch_main<64>(a, grid_main, stream);
 }
 
+hipError_t launch_packed_main64(const PackedBwdArgs& a, int grid, hipStream_t stream) {
+  return launch_packed_main<64>(a, grid, stream);
+}
+
 int main64_occupancy() { return main_occupancy<64>(); }
 
 }  // namespace dash

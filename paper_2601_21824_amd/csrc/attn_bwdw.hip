@@ -44,6 +44,7 @@
 #include "kernels.h"
 #include "bwd_common.h"
 #include "lds_layout.h"
+#include "packed_chain.h"
 
 namespace dash {
 namespace {
@@ -92,9 +93,13 @@ __device__ inline void vm_wait_few(int n) {
   else vm_wait<0>();
 }
 
-template <int D, bool CAUSAL, int MODE, bool STATS = false>
-__global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
+// Args: as in bwd_main.h
+template <int D, bool CAUSAL, int MODE, bool STATS = false, typename Args = BwdArgs>
+__global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
   using SM = SmemW<D>;
+  constexpr bool PACKED = std::is_same_v<Args, PackedBwdArgs>;
+  static_assert(!PACKED || MODE == kModeOrdered, "packed sequences: the ordered reduction");
+  using Blk = std::conditional_t<PACKED, PackedBlk, int>;  // a query block (dense: of the chain's head)
   constexpr int BC = SM::BC;
   constexpr int NKB = BC / 128;   // 32-key blocks per wave
   constexpr int KS = D / 16;      // k-steps over d
@@ -115,9 +120,11 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
   const float c2 = a.scale * kLog2e;
   const uint32_t hbytes = (uint32_t)((size_t)N * D * 2);
   constexpr bool ordered = MODE == kModeOrdered;
-  const bool xcd = a.nxcd > 0;
+  const bool xcd = !PACKED && a.nxcd > 0;
   const int xq = xcd ? xcc_id() : 0;
-  const int total = xcd ? (xq < a.nxcd ? xcd_heads(a.bh, a.nxcd, xq) * G.chains : 0) : a.bh * G.chains;
+  int total_items = 0;
+  if constexpr (PACKED) total_items = a.ctrl[kCtrlItems] * a.p.heads_kv;
+  const int total = PACKED ? total_items : xcd ? (xq < a.nxcd ? xcd_heads(a.bh, a.nxcd, xq) * G.chains : 0) : a.bh * G.chains;
   int* const ticket = &a.ctrl[xcd ? kCtrlXcdTicket + xq : kCtrlTicket];
   const int* const order = a.order + (xcd ? 2 * xq * a.xcd_cap : 0);
   const uint32_t sm_lds = lds_base(&sm);
@@ -125,7 +132,7 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
   // Shift-type orders: the next contributor to a block reaches it two or more
   // blocks later, so the counter release waits until the next sub-step, when
   // the stores have drained without a wait of their own
-  const bool deferred = G.sched == S_SHIFT || G.sched == S_SYMSHIFT;
+  const bool deferred = !PACKED && (G.sched == S_SHIFT || G.sched == S_SYMSHIFT);
   bool failed = false;
   WaitStats wst;
   if constexpr (STATS) stats_wave_begin(wst);
@@ -135,19 +142,31 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
     __syncthreads();
     const int item = __builtin_amdgcn_readfirstlane(sm.item);
     if (item >= total) break;
-    const int bh = __builtin_amdgcn_readfirstlane(order[2 * item]);
-    const int wch = __builtin_amdgcn_readfirstlane(order[2 * item + 1]);
+    std::conditional_t<PACKED, PackedChain<D, BC>, NoChain> ch(a);
+    if constexpr (PACKED) {
+      if (!ch.init(item)) {
+        __syncthreads();  // sm.item is rewritten by the next ticket
+        continue;
+      }
+    }
+    const int bh = PACKED ? 0 : __builtin_amdgcn_readfirstlane(order[2 * item]);
+    const int wch = PACKED ? 0 : __builtin_amdgcn_readfirstlane(order[2 * item + 1]);
     const size_t head = (size_t)bh * N * D;
     const auto rq = make_rsrc((const __bf16*)a.q + head, hbytes);
     const auto rk = make_rsrc((const __bf16*)a.k + head, hbytes);
     const auto rdo = make_rsrc((const __bf16*)a.dO + head, hbytes);
-    int* ctr_head = a.counters + (size_t)bh * a.nblk * kCtrStride;
+    int* ctr_head = PACKED ? a.counters : a.counters + (size_t)bh * a.nblk * kCtrStride;
     const auto rctr = make_rsrc(ctr_head, (uint32_t)a.nblk * kCtrStride * 4);
 
     const unsigned* tab = a.steps + (size_t)wch * a.step_cap;
-    const int nsteps = __builtin_amdgcn_readfirstlane((int)tab[0]);
-    for (int st = tid; st < nsteps; st += NT) sm.steps[st] = tab[1 + st];
-    __syncthreads();
+    int nsteps;
+    if constexpr (PACKED) {
+      nsteps = ch.steps();
+    } else {
+      nsteps = __builtin_amdgcn_readfirstlane((int)tab[0]);
+      for (int st = tid; st < nsteps; st += NT) sm.steps[st] = tab[1 + st];
+      __syncthreads();
+    }
 
     int cur_j = -1;
     bf16x8 vreg[NKB][KS];                       // V rows of the wave's keys (B of dP = dO V^T)
@@ -155,7 +174,7 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
     f32x16 dq[DQT];                             // dQ^T of the sub-step before
     f32x4 old[NACC];                            // its accumulator slice
     // the sub-step before: its block (half h ^ 1), whether there is one, its turn
-    int p_pb = 0;
+    Blk p_pb{};
     bool p_valid = false, p_last = false, p_turn = false, p_add = false;
     int rel_pb = -1;   // block whose stores are issued and whose counter this wave still has to advance
     int vm_st = 0;     // vector memory operations since the copies of the coming sub-step
@@ -163,45 +182,65 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
 
     auto step_at = [&](int st) -> unsigned { return __builtin_amdgcn_readfirstlane(sm.steps[st]); };
     auto next_valid = [&](int st) {
-      while (st < nsteps && step_at(st) == kNoStep) ++st;
+      if constexpr (!PACKED)
+        while (st < nsteps && step_at(st) == kNoStep) ++st;
       return st;
     };
+    // number of a block's counter (and, packed, of its accumulator)
+    auto ctr_at = [&](Blk b) {
+      if constexpr (PACKED) return ch.index(b);
+      else return b;
+    };
     // part k of the Q and dO rows of half h of block pb into buffer h
-    auto load_part = [&](int pb, int h, int k) {
+    auto load_part = [&](Blk pb, int h, int k) {
       const int t0 = 64 * w + fresh_lane();
       const int r = t0 / CPR + k * (NT / CPR), c = (t0 % CPR) ^ tile_swz<D>(r);
       const uint32_t at = lds_of(&sm.qs[h][0]) + 1024u * w + 4096u * k;
-      dma16_pair(rq, rdo, at, at + (uint32_t)sizeof(sm.qs), (uint32_t)((pb * BM + SQ * h + r) * D + 8 * c) * 2, 0);
+      if constexpr (PACKED) {
+        dma16(ch.q(pb), at, ch.at(a.p.qs, SQ * h + r, 8 * c));
+        dma16(ch.dO(pb), at + (uint32_t)sizeof(sm.qs), ch.at(a.dos, SQ * h + r, 8 * c));
+      } else {
+        dma16_pair(rq, rdo, at, at + (uint32_t)sizeof(sm.qs), (uint32_t)((pb * BM + SQ * h + r) * D + 8 * c) * 2, 0);
+      }
     };
-    auto load_ld = [&](int pb, int par) {  // L * log2(e) and D of a block's rows
+    auto load_ld = [&](Blk pb, int par) {  // L * log2(e) and D of a block's rows
+      if constexpr (PACKED) {
+        const uint32_t row = (uint32_t)fresh_lane();
+        if (w == 0) dma4(ch.vec(a.lse2, pb), lds_of(&sm.ls[par][0]), row * 4);
+        if (w == 1) dma4(ch.vec(a.dvec, pb), lds_of(&sm.ds[par][0]), row * 4);
+      } else {
       const uint32_t row = (uint32_t)(pb * BM + fresh_lane());
       // padded rows of a ragged last block read L = D = 0 (P = 1 there), and
       // their Q and dO rows read 0: they add nothing to dK and dV
       if (w == 0) dma4(make_rsrc(a.lse2 + (size_t)bh * N, (uint32_t)N * 4), lds_of(&sm.ls[par][0]), row * 4);
       if (w == 1) dma4(make_rsrc(a.dvec + (size_t)bh * N, (uint32_t)N * 4), lds_of(&sm.ds[par][0]), row * 4);
+      }
     };
-    auto poll_copy = [&](int pb) { dma4_coherent(rctr, lds_of(&sm.poll[w][0]), (uint32_t)pb * kCtrStride * 4); };
+    auto poll_copy = [&](Blk pb) { dma4_coherent(rctr, lds_of(&sm.poll[w][0]), (uint32_t)ctr_at(pb) * kCtrStride * 4); };
     // The accumulator in register order, as bwd_sum_partials reads it: block pb
     // is BM*D floats at pb*BM*D, 32 x 32 tile T = 2 (d block) + (query half) at
     // T*1024, chunk rb of lane l at rb*256 + 4l: row 32 half + l%32 of the block,
     // columns 32 (d block) + 8rb + 4(l/32) .. +3.  Wave w: d blocks w DQT ...
-    auto acc_off = [&](int pb, int h, int k) {  // wave-uniform part
-      return (uint32_t)(pb * BM * D + (2 * (w * DQT + (k >> 2)) + h) * 1024 + (k & 3) * 256) * 4;
+    auto acc_off = [&](Blk pb, int h, int k) {  // wave-uniform part (packed: within the block)
+      int at = (2 * (w * DQT + (k >> 2)) + h) * 1024 + (k & 3) * 256;
+      if constexpr (!PACKED) at += pb * BM * D;
+      return (uint32_t)at * 4;
     };
     // An accumulator slice is loaded and stored by straight-line code in every
     // sub-step: where there is nothing to load or store, the descriptor covers 0
     // bytes (loads read 0, stores are dropped).  Behind a branch the compiler
     // loses count of what is in flight and waits for everything, the stores of
     // the chunk before included, at every chunk.
-    auto acc_rsrc = [&](bool on) {
-      return make_rsrc(a.dqacc + (size_t)bh * a.nblk * BM * D, on ? (uint32_t)a.nblk * BM * D * 4 : 0u);
+    auto acc_rsrc = [&](Blk pb, bool on) {
+      if constexpr (PACKED) return ch.acc(pb, on);
+      else return make_rsrc(a.dqacc + (size_t)bh * a.nblk * BM * D, on ? (uint32_t)a.nblk * BM * D * 4 : 0u);
     };
-    auto load_old1 = [&](__amdgpu_buffer_rsrc_t r, int pb, int h, int k, int lane) {
+    auto load_old1 = [&](__amdgpu_buffer_rsrc_t r, Blk pb, int h, int k, int lane) {
       old[k] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, 16 * lane, acc_off(pb, h, k), kCoherent));
     };
-    auto load_old = [&](int pb, int h, bool add) {
+    auto load_old = [&](Blk pb, int h, bool add) {
       const int lf = fresh_lane();
-      const auto r = acc_rsrc(add);
+      const auto r = acc_rsrc(pb, add);
 #pragma unroll
       for (int k = 0; k < NACC; ++k) load_old1(r, pb, h, k, lf);
     };
@@ -212,7 +251,7 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
     };
     // chunk k of dQ^T of half h of block pb: added to the slice (the first
     // contributor: as it is) and stored; the last contributor also writes bf16 s*dQ
-    auto put = [&](__amdgpu_buffer_rsrc_t r, int pb, int h, bool add, bool last, int k, int lf) {
+    auto put = [&](__amdgpu_buffer_rsrc_t r, Blk pb, int h, bool add, bool last, int k, int lf) {
       const int t = k >> 2, rb = k & 3;
       f32x4 v = {dq[t][4 * rb], dq[t][4 * rb + 1], dq[t][4 * rb + 2], dq[t][4 * rb + 3]};
       if constexpr (MODE == kModePartials) {
@@ -224,7 +263,11 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
           v[x] = add ? sum : v[x];
         }
         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, 16 * lf, acc_off(pb, h, k), kCoherent);
-        if (last) {
+        if constexpr (PACKED) {
+          if (last)
+            st8(ch.dq(pb), ch.at(a.dqs, SQ * h + (lf & 31), 32 * (w * DQT + t) + 8 * rb + 4 * (lf >> 5)),
+                u32x2{pack_bf16(v[0] * a.scale, v[1] * a.scale), pack_bf16(v[2] * a.scale, v[3] * a.scale)});
+        } else if (last) {
           const uint32_t off = (uint32_t)((pb * BM + SQ * h + (lf & 31)) * D + 32 * (w * DQT + t) + 8 * rb + 4 * (lf >> 5));
           st8(make_rsrc((__bf16*)a.dq + head, hbytes), off * 2,
               u32x2{pack_bf16(v[0] * a.scale, v[1] * a.scale), pack_bf16(v[2] * a.scale, v[3] * a.scale)});
@@ -232,19 +275,21 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
         }
       }
     };
-    auto put_rsrc = [&](bool on, int j) {
+    auto put_rsrc = [&](Blk pb, bool on, int j) {
       if constexpr (MODE == kModePartials)
         return make_rsrc(a.dqacc + ((size_t)bh * a.tc + j) * a.nblk * BM * D, on ? (uint32_t)a.nblk * BM * D * 4 : 0u);
       else
-        return acc_rsrc(on);
+        return acc_rsrc(pb, on);
     };
-    auto put_all = [&](int pb, int h, bool add, bool last, int j) {
+    auto put_all = [&](Blk pb, int h, bool add, bool last, int j) {
       const int lf = fresh_lane();
-      const auto r = put_rsrc(true, j);
+      const auto r = put_rsrc(pb, true, j);
 #pragma unroll
       for (int k = 0; k < NACC; ++k) put(r, pb, h, add, last, k, lf);
     };
-    auto put_partial = [&](int pb, int h, int j) {  // the partials option (debugging)
+    auto put_partial = [&](Blk pb, int h, int j) {  // the partials option (debugging)
+      if constexpr (PACKED) return;
+      else {
       const auto rp = make_rsrc(a.partials + ((size_t)bh * a.tc + j) * N * D, hbytes * 2);
       const int lf = fresh_lane();
 #pragma unroll
@@ -253,15 +298,17 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
         st16(rp, (uint32_t)((pb * BM + SQ * h + (lf & 31)) * D + 32 * (w * DQT + t) + 8 * rb + 4 * (lf >> 5)) * 4,
              __builtin_bit_cast(u32x4, f32x4{dq[t][4 * rb], dq[t][4 * rb + 1], dq[t][4 * rb + 2], dq[t][4 * rb + 3]}));
       }
+      }
     };
-    auto note_witness = [&](int pb, int rank, int j) {
-      if (tid == 0 && a.witness && rank < a.tc) a.witness[((size_t)bh * a.nblk + pb) * a.tc + rank] = j;
+    auto note_witness = [&](Blk pb, int rank, int j) {
+      if constexpr (PACKED) return;
+      else if (tid == 0 && a.witness && rank < a.tc) a.witness[((size_t)bh * a.nblk + pb) * a.tc + rank] = j;
     };
     // wait for block pb's turn (rank), late: its early look had not seen it
-    auto take_turn = [&](int pb, int rank) {
+    auto take_turn = [&](Blk pb, int rank) {
       if constexpr (STATS) vm_wait<0>();  // time the wait only, not this wave's own loads
       const unsigned long long t0 = STATS ? clock_now() : 0ull;
-      const bool ok = wait_turn(ctr_head + (size_t)pb * kCtrStride, NW * rank, a.spin_limit);
+      const bool ok = wait_turn(ctr_head + (size_t)ctr_at(pb) * kCtrStride, NW * rank, a.spin_limit);
       if constexpr (STATS) stats_wait(wst, t0);
       if (!ok) {
         failed = true;
@@ -329,10 +376,10 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
 #pragma unroll
       for (int ks = 0; ks < DQR - 1; ++ks) dq_rd(ks);
       dq_run([](int) {});
-      if (a.partials) put_partial(p_pb, 1, cur_j);
+      if (!PACKED && a.partials) put_partial(p_pb, 1, cur_j);
       if (!ordered || p_turn) put_all(p_pb, 1, p_add, p_last, cur_j);  // (its slice was loaded by the last sub-step)
       if constexpr (ordered) {
-        rel_pb = p_pb;
+        rel_pb = ctr_at(p_pb);
         vm_wait<0>();
         release();
       }
@@ -343,8 +390,15 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
       // every wave is past its dQ^T (the K tile's last reads): its quarter of
       // the tile becomes a store pad, 32 rows at a time
       __syncthreads();
-      const auto rdk = make_rsrc((__bf16*)a.dk + head, hbytes);
-      const auto rdv = make_rsrc((__bf16*)a.dv + head, hbytes);
+      auto dkv_rsrc = [&](void* p, bool of_k) {
+        if constexpr (PACKED) return ch.tile(p, of_k ? a.dks : a.dvs);
+        else return make_rsrc((__bf16*)p + head, hbytes);
+      };
+      const auto rdk = dkv_rsrc(a.dk, true);
+      const auto rdv = dkv_rsrc(a.dv, false);
+      const int row0 = PACKED ? 0 : j * BC;  // row of the tile's first key in those
+      int64_t ldk = D, ldv = D;
+      if constexpr (PACKED) ldk = a.dks.row, ldv = a.dvs.row;
       char* pad = (char*)sm.kt + w * 16384;
       const int lf = fresh_lane();
 #pragma unroll
@@ -354,34 +408,75 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
           acc_settle(dvacc[kb][nb]);
           acc_settle(dkacc[kb][nb]);
         }
-        store_block32<D>(rdv, pad, dvacc[kb], 1.f, j * BC + 32 * (NKB * w + kb), lf);
-        store_block32<D>(rdk, pad, dkacc[kb], a.scale, j * BC + 32 * (NKB * w + kb), lf);
+        if constexpr (PACKED) {
+          store_block32_strided<D>(rdv, pad, dvacc[kb], 1.f, row0 + 32 * (NKB * w + kb), lf, (uint32_t)ldv);
+          store_block32_strided<D>(rdk, pad, dkacc[kb], a.scale, row0 + 32 * (NKB * w + kb), lf, (uint32_t)ldk);
+        } else {
+          store_block32<D>(rdv, pad, dvacc[kb], 1.f, row0 + 32 * (NKB * w + kb), lf);
+          store_block32<D>(rdk, pad, dkacc[kb], a.scale, row0 + 32 * (NKB * w + kb), lf);
+        }
       }
     };
 
     int st = next_valid(0);
+    Blk cur{};  // packed: the step's block
+    if constexpr (PACKED) {
+      cur = ch.first();
+      if (nsteps == 0) {  // no query sees the tile: dK = dV = 0
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dkacc[kb][nb][r] = dvacc[kb][nb][r] = 0.f;
+        store_dkdv(ch.j);
+      }
+    }
     if (st < nsteps) {
-      const int pb0 = step_at(st) & 0xfff;
+      Blk pb0;
+      if constexpr (PACKED) pb0 = cur;
+      else pb0 = step_at(st) & 0xfff;
 #pragma unroll
       for (int k = 0; k < QP; ++k) load_part(pb0, 0, k);
       load_ld(pb0, bpar);
       if (ordered) poll_copy(pb0);
     }
-    unsigned e = st < nsteps ? step_at(st) : 0u;
+    unsigned e = 0u;
+    if constexpr (!PACKED) e = st < nsteps ? step_at(st) : 0u;
 
     for (; st < nsteps;) {
-      const int pb = e & 0xfff, j = (e >> 12) & 0x1ff, rank = (e >> 21) & 0x3ff;
-      const bool last = (e >> 31) != 0;
+      Blk pb;
+      int j, rank, q0;  // q0: the block's first row, as the causal mask counts
+      bool last;
+      if constexpr (PACKED) {
+        pb = cur;
+        j = rank = ch.j;
+        last = ch.last(pb);
+        q0 = pb.pb * BM + ch.sg.off();
+      } else {
+        pb = e & 0xfff;
+        j = (e >> 12) & 0x1ff;
+        rank = (e >> 21) & 0x3ff;
+        last = (e >> 31) != 0;
+        q0 = pb * BM;
+      }
 
       if (j != cur_j) {  // new KV tile
         const int lf = fresh_lane();
-        const auto rv = make_rsrc((const __bf16*)a.v + head, hbytes);
+        auto kv_rsrc = [&](const void* p, bool of_k) {
+          if constexpr (PACKED) return ch.tile(p, of_k ? a.p.ks : a.p.vs);
+          else return make_rsrc((const __bf16*)p + head, hbytes);
+        };
+        auto kv_at = [&](bool of_k, int row, int col) {  // row of the tile
+          if constexpr (PACKED) return ch.at(of_k ? a.p.ks : a.p.vs, row, col);
+          else return (uint32_t)((j * BC + row) * D + col) * 2;
+        };
+        const auto rv = kv_rsrc(a.v, false);
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks)
-            vreg[kb][ks] = as_bf16x8(
-                ld16(rv, (uint32_t)((j * BC + 32 * (NKB * w + kb) + (lf & 31)) * D + 16 * ks + 8 * (lf >> 5)) * 2));
+            vreg[kb][ks] = as_bf16x8(ld16(rv, kv_at(false, 32 * (NKB * w + kb) + (lf & 31), 16 * ks + 8 * (lf >> 5))));
         if (cur_j >= 0) {  // (the V loads above are on their way meanwhile)
           flush();
           store_dkdv(cur_j);
@@ -394,7 +489,7 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
 #pragma unroll
           for (int k = 0; k < KP; ++k) {
             const int r = t0 / CPR + k * (NT / CPR), c = (t0 % CPR) ^ tile_swz<D>(r);
-            dma16(rk, at + 4096u * k, (uint32_t)((j * BC + r) * D + 8 * c) * 2);
+            dma16(kv_rsrc(a.k, true), at + 4096u * k, kv_at(true, r, 8 * c));
           }
         }
         vm_wait<0>();  // published by the barrier at the top of the sub-step
@@ -410,7 +505,9 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
             }
       }
 
-      int nst = st + 1, pb_next = -1;  // the next block (looked up in the first sub-step)
+      int nst = st + 1;  // the next block (looked up in the first sub-step)
+      Blk pb_next{};
+      bool has_next = false;
       unsigned e_next = 0;
       bool turn = !ordered;  // this block's turn
 
@@ -424,7 +521,7 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
         const int lf0 = fresh_lane();
         const int g = lf0 >> 5, lc = lf0 & 31;
         unsigned e_v = 0;
-        if constexpr (h == 0) e_v = sm.steps[st + 1 < nsteps ? st + 1 : st];
+        if constexpr (h == 0 && !PACKED) e_v = sm.steps[st + 1 < nsteps ? st + 1 : st];
 
         // ---- this block's turn: looked up a sub-step ahead of its first half's
         //      slice loads, once more a sub-step later, and waited for at the end
@@ -442,7 +539,7 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
         // slice for this one's is loaded behind it
         const bool do_put = h == 0 ? p_valid && p_turn : turn;
         const bool do_load = ordered && turn, add = rank > 0;
-        const int d_pb = h == 0 ? p_pb : pb;
+        const Blk d_pb = h == 0 ? p_pb : pb;
         const bool d_last = do_put && (h == 0 ? p_last : last), d_add = h == 0 ? p_add : add;
 
         // ---- phase 1: S = Q K^T, dP = dO V^T (A = Q / dO rows, B = K rows, all
@@ -481,7 +578,7 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
             if (h == 0) {
               if (ks == 0 && ordered && !turn) poll_copy(pb);
               if (ks % GAP == 1 && ks / GAP < QP) load_part(pb, 1, ks / GAP);
-            } else if (pb_next >= 0) {
+            } else if (has_next) {
               if (ks == 0 && ordered) poll_copy(pb_next);
               if (ks == 0) load_ld(pb_next, bpar ^ 1);
               if (ks % GAP == 1 && ks / GAP < QP) load_part(pb_next, 0, ks / GAP);
@@ -493,7 +590,12 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
             __builtin_amdgcn_sched_barrier(0);
           }
         }
-        if constexpr (h == 0) {
+        if constexpr (PACKED) {
+          if constexpr (h == 0) {
+            has_next = nst < nsteps;
+            pb_next = ch.next(pb);
+          }
+        } else if constexpr (h == 0) {
           nst = st + 1;
           if (nst < nsteps) {
             e_next = __builtin_amdgcn_readfirstlane(e_v);
@@ -502,11 +604,12 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
               if (nst < nsteps) e_next = step_at(nst);
             }
           }
-          pb_next = nst < nsteps ? (int)(e_next & 0xfff) : -1;
+          has_next = nst < nsteps;
+          pb_next = (int)(e_next & 0xfff);
         }
         // deferred release of the block whose second half was stored a sub-step ago
         if (ordered && h == 1 && rel_pb >= 0) {
-          vm_wait_few(pb_next >= 0 ? 2 * QP : 0);  // (the copies issued since)
+          vm_wait_few(has_next ? 2 * QP : 0);  // (the copies issued since)
           release();
         }
 
@@ -514,10 +617,10 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
         // 32 (NKB w + kb) + lc of the tile.  Keys past N need no mask: their
         // K, V rows read as zero, P is at most 1 there and their dK, dV rows are
         // not stored.
-        if (CAUSAL && j * BC + 32 * NKB * (w + 1) - 1 > pb * BM + SQ * h) {
+        if (CAUSAL && j * BC + 32 * NKB * (w + 1) - 1 > q0 + SQ * h) {
 #pragma unroll
           for (int kb = 0; kb < NKB; ++kb) {
-            const int thr = j * BC + 32 * (NKB * w + kb) + lc - pb * BM - SQ * h - 4 * g;  // masked iff query < thr
+            const int thr = j * BC + 32 * (NKB * w + kb) + lc - q0 - SQ * h - 4 * g;  // masked iff query < thr
 #pragma unroll
             for (int r = 0; r < 16; ++r)
               if (8 * (r >> 2) + (r & 3) < thr) s[kb][r] = -INFINITY;
@@ -584,15 +687,15 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
             }
           }
         });
-        if (a.partials && (h == 1 || p_valid)) put_partial(d_pb, h ^ 1, j);
+        if (!PACKED && a.partials && (h == 1 || p_valid)) put_partial(d_pb, h ^ 1, j);
 
         // ---- phase 3: dV += P^T dO beside dS = P (dP - D), the
         //      ordered add and the stores of dQ^T, then dK += dS^T Q beside the dS^T stores
         //      and the loads of the next slice.  A = P^T, dS^T from registers.
         asm volatile("s_nop 1" ::: "memory");  // two wait states between the packs and their first MFMA
         const int lfp = fresh_lane();
-        const auto r_put = put_rsrc(do_put, j);
-        const auto r_ld = acc_rsrc(do_load && add);
+        const auto r_put = put_rsrc(d_pb, do_put, j);
+        const auto r_ld = acc_rsrc(pb, do_load && add);
         constexpr int EV = 16 / NACC;  // slots per chunk
         dvdk_run(DV{}, pbf, dvacc, [&](int i) {  // slot i: element i of every key block
           if ((i & 3) == 0 && i < 12) dd[((i >> 2) + 1) & 1] = lds16f(ds_at + 32 * ((i >> 2) + 1));
@@ -621,7 +724,7 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
         vm_st = ordered ? 2 * NACC : NACC;  // this sub-step's stores, then loads
         if constexpr (h == 0) {
           if (ordered && p_valid) {
-            rel_pb = p_pb;
+            rel_pb = ctr_at(p_pb);
             if (!deferred) {
               vm_wait_few(NACC);  // the stores (the loads came after)
               release();
@@ -651,6 +754,7 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(BwdArgs a) {
       bpar ^= 1;
       st = nst;
       e = e_next;
+      if constexpr (PACKED) cur = pb_next;
     }
     if (cur_j >= 0) {
       flush();
@@ -684,7 +788,18 @@ bool resident_all(int* lo) {
   return ok;
 }
 
+template <int D>
+hipError_t launch_packed(const PackedBwdArgs& a, int grid, hipStream_t stream) {
+  if (a.p.causal) hipLaunchKernelGGL((bwd_mainw_kernel<D, true, kModeOrdered, false, PackedBwdArgs>), dim3(grid), dim3(NT), 0, stream, a);
+  else hipLaunchKernelGGL((bwd_mainw_kernel<D, false, kModeOrdered, false, PackedBwdArgs>), dim3(grid), dim3(NT), 0, stream, a);
+  return hipGetLastError();
+}
+
 }  // namespace
+
+hipError_t launch_packed_mainw(const PackedBwdArgs& a, int d, int grid, hipStream_t stream) {
+  return d == 128 ? launch_packed<128>(a, grid, stream) : launch_packed<256>(a, grid, stream);
+}
 
 hipError_t launch_mainw(const BwdArgs& a, int d, int grid_main, hipStream_t stream) {
   if (d == 128) return a.G.causal ? launch_mask<128, true>(a, grid_main, stream) : launch_mask<128, false>(a, grid_main, stream);

@@ -1,0 +1,144 @@
+// attn_packed_bwd.hip -- the deterministic backward over packed sequences: the kernel
+// before the main kernel, and the launch sequence of a call.  The main kernels are
+// bwd_main.h (128-row KV tiles at d = 64 and 128) and attn_bwdw.hip (256 rows at d =
+// 128, 128 at d = 256) on the chains of packed_chain.h, with the ordered dQ reduction
+// of the dense calls in Descending order.
+//
+// packed_pre: per 64-row query block and head, D = rowsum(dO o O) and L log2(e) (+inf for
+// a row that sees nothing, so that its P is 0); the block's ordering counter; dQ = 0
+// where no KV tile sees the block.  Further waves put the KV tiles' chains in the order
+// in which they start (packed_order.h): longest first over all sequences, each
+// sequence's own in ascending order.  Memory-bound, as bwd_pre: O and dO once.
+#include "common.h"
+#include "ops.h"
+#include "packed_order.h"
+#include "paged.h"
+
+namespace dash {
+namespace {
+
+constexpr int BM = kBlockRows;
+
+template <int D>
+__global__ __launch_bounds__(256) void packed_pre_kernel(PackedBwdArgs a) {
+  constexpr int TPR = D / 8;        // threads per row, 8 elements each
+  constexpr int RPP = 256 / TPR;    // rows per pass
+  constexpr int U = BM / RPP;       // passes
+  const PackedArgs& p = a.p;
+  const int tid = threadIdx.x, l = tid & 63;
+  const bool causal = p.causal != 0;
+  const int blocks = a.slots_q * p.heads_q;
+  if ((int)blockIdx.x < blocks) {
+    const int slot = (int)blockIdx.x / p.heads_q, h = (int)blockIdx.x % p.heads_q;
+    if (blockIdx.x == 0 && tid == 0) {
+      a.ctrl[kCtrlTicket] = 0;
+      a.ctrl[kCtrlError] = 0;
+      if (a.status) *a.status = 0;
+    }
+    const int s = __builtin_amdgcn_readfirstlane(
+        find_last(p.batch, slot, l, [&](int x) { return first_slot(p.cu_q, x, p.total_q, BM); }));
+    const Span q = span_of(p.cu_q, s, p.total_q), k = span_of(p.cu_k, s, p.total_k);
+    const int pb = slot - first_slot(p.cu_q, s, p.total_q, BM);
+    if (pb < 0 || pb * BM >= q.len) return;
+    const int rows = q.len - pb * BM < BM ? q.len - pb * BM : BM;
+    const int64_t row0 = (int64_t)q.start + pb * BM;
+    const int c = tid % TPR, r0 = tid / TPR;
+    u32x4 x[U], y[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      int r = r0 + u * RPP;
+      r = r < rows ? r : rows - 1;  // (read, not written)
+      x[u] = *(const u32x4*)((const __bf16*)a.dO + (row0 + r) * a.dos.row + h * a.dos.head + 8 * c);
+      y[u] = *(const u32x4*)((const __bf16*)a.o + (row0 + r) * p.os.row + h * p.os.head + 8 * c);
+    }
+    const int64_t vec = (int64_t)h * p.total_q + row0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float acc = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float xf = bf16_to_f32((unsigned short)(x[u][e >> 1] >> (16 * (e & 1))));
+        const float yf = bf16_to_f32((unsigned short)(y[u][e >> 1] >> (16 * (e & 1))));
+        acc = __builtin_fmaf(xf, yf, acc);
+      }
+      // butterfly over the TPR lanes of a row, as in bwd_pre
+#pragma unroll
+      for (int o = 1; o < TPR; o <<= 1) acc += __shfl_xor(acc, o);
+      const int r = r0 + u * RPP;
+      if (c == 0 && r < rows) {
+        a.dvec[vec + r] = acc;
+        const float L = p.lse[vec + r];
+        a.lse2[vec + r] = L == -INFINITY ? INFINITY : L * kLog2e;
+      }
+    }
+    if (tid == 0) a.counters[((size_t)slot * p.heads_q + h) * kCtrStride] = a.poison ? kPoison : 0;
+    const SeqGeom g{q.len, k.len, causal, a.bc};
+    if (g.last_tile(pb) < 0) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int r = r0 + u * RPP;
+        if (r < rows) *(u32x4*)((__bf16*)a.dq + (row0 + r) * a.dqs.row + h * a.dqs.head + 8 * c) = u32x4{0, 0, 0, 0};
+      }
+    }
+    return;
+  }
+  // ---- one wave per KV-tile slot
+  const int slot = __builtin_amdgcn_readfirstlane(((int)blockIdx.x - blocks) * 4 + (tid >> 6));
+  if (slot >= a.slots_k) return;
+  const int s = __builtin_amdgcn_readfirstlane(
+      find_last(p.batch, slot, l, [&](int x) { return first_slot(p.cu_k, x, p.total_k, a.bc); }));
+  auto geom = [&](int x) {
+    return SeqGeom{span_of(p.cu_q, x, p.total_q).len, span_of(p.cu_k, x, p.total_k).len, causal, a.bc};
+  };
+  const SeqGeom g = geom(s);
+  const int j = slot - first_slot(p.cu_k, s, p.total_k, a.bc);
+  const int length = g.chain(j);
+  int place = 0, total = 0;
+  for (int b = 0; b < p.batch; b += 64) {
+    const int o = b + l;
+    if (o < p.batch) {
+      const SeqGeom og = geom(o);
+      place += order_part(og, o, s, j, length);
+      total += og.tiles();
+    }
+  }
+  place = wave_sum(place);
+  total = wave_sum(total);
+  if (l != 0) return;
+  if (slot == 0) a.ctrl[kCtrlItems] = total < a.slots_k ? total : a.slots_k;
+  if (j >= 0 && j < g.tiles() && place < a.slots_k) {
+    a.order[2 * (size_t)place] = s;
+    a.order[2 * (size_t)place + 1] = j;
+  }
+}
+
+template <int D>
+hipError_t launch(const PackedBwdArgs& a, int cus, hipStream_t stream) {
+  const unsigned grid = (unsigned)(a.slots_q * a.p.heads_q + (a.slots_k + 3) / 4);
+  hipLaunchKernelGGL(packed_pre_kernel<D>, dim3(grid), dim3(256), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  // persistent workgroups: as many as stay resident (two per CU at d = 64, else one).
+  // A chain waits only on chains that took an earlier ticket, so any count is safe.
+  const long items = (long)a.slots_k * a.p.heads_kv, cap = (long)cus * (D == 64 ? 2 : 1);
+  const int g = (int)(items < cap ? items : cap);
+  if constexpr (D == 64) return launch_packed_main64(a, g, stream);
+  else if constexpr (D == 256) return launch_packed_mainw(a, D, g, stream);
+  else return a.bc == 256 ? launch_packed_mainw(a, D, g, stream) : launch_packed_main128(a, g, stream);
+}
+
+}  // namespace
+
+int packed_tile_rows(int d, int total_q, int total_k, int batch, int heads_kv) {
+  (void)total_q;
+  (void)batch;
+  return d == 128 && (long)(total_k / 256) * heads_kv >= 256 ? 256 : 128;
+}
+
+hipError_t launch_packed_bwd(const PackedBwdArgs& a, int d, int cus, hipStream_t stream) {
+  if (d == 64) return launch<64>(a, cus, stream);
+  if (d == 128) return launch<128>(a, cus, stream);
+  return launch<256>(a, cus, stream);
+}
+
+}  // namespace dash

@@ -193,6 +193,23 @@ __device__ inline void store_block32(__amdgpu_buffer_rsrc_t r, void* pad, const 
     st16(r, (uint32_t)(row0 * D * 2 + 1024 * i + 16 * l), *(const u32x4*)((const char*)pad + 1024 * i + 16 * l));
 }
 
+// The same to rows `ld` elements apart: D / 8 lanes store one row's chunks.
+template <int D>
+__device__ inline void store_block32_strided(__amdgpu_buffer_rsrc_t r, void* pad, const f32x16 (&acc)[D / 32], float scale,
+                                             int row0, int l, uint32_t ld) {
+  unsigned short* p = (unsigned short*)pad + 4 * (l >> 5) * D + (l & 31);
+  asm volatile("" ::: "memory");  // after the pad's previous reads
+#pragma unroll
+  for (int nb = 0; nb < D / 32; ++nb)
+#pragma unroll
+    for (int k = 0; k < 16; ++k) p[(8 * (k >> 2) + (k & 3)) * D + 32 * nb] = to_bf16(acc[nb][k] * scale);
+  asm volatile("" ::: "memory");  // lanes read what other lanes wrote
+  constexpr int CPR = D / 8, RPI = 64 / CPR;  // chunks per row, rows per instruction
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+    st16(r, (uint32_t)(row0 + RPI * i + l / CPR) * ld * 2 + 16 * (l % CPR), *(const u32x4*)((const char*)pad + 1024 * i + 16 * l));
+}
+
 // Launch a main-kernel instantiation on the persistent grid.  Shift and
 // Symmetric Shift chains wait on each other in a cycle, so every workgroup of
 // their grid must be resident at once: they launch cooperatively, and a grid

@@ -28,6 +28,7 @@
 #include "kernels.h"
 #include "bwd_common.h"
 #include "lds_layout.h"
+#include "packed_chain.h"
 
 namespace dash {
 
@@ -48,8 +49,14 @@ struct MainSmem {
   int item;
 };
 
-template <int D, bool CAUSAL, int MODE, bool STATS = false>
-__global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
+// Args: BwdArgs for a dense batch, PackedBwdArgs for packed sequences.  The latter
+// take their chains from PackedChain in place of the step table; a chain visits every
+// query head of its K/V head's group, so that dK and dV sum over them in registers.
+template <int D, bool CAUSAL, int MODE, bool STATS = false, typename Args = BwdArgs>
+__global__ __launch_bounds__(256) void bwd_main_kernel(Args a) {
+  constexpr bool PACKED = std::is_same_v<Args, PackedBwdArgs>;
+  static_assert(!PACKED || MODE == kModeOrdered, "packed sequences: the ordered reduction");
+  using Blk = std::conditional_t<PACKED, PackedBlk, int>;  // a query block (dense: of the chain's head)
   constexpr int BC = kTileKV;   // KV rows per tile (128 for d = 64 and 128)
   constexpr int NW = BC / 32;   // waves, 32 KV rows each
   constexpr int NT = 64 * NW;   // threads
@@ -83,7 +90,9 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
   // lines that workgroups on other CUs have since overwritten in the L2.
   constexpr bool xcd = MODE == kModeOrderedXcd;
   const int xq = xcd ? xcc_id() : 0;
-  const int total = xcd ? (xq < a.nxcd ? xcd_heads(a.bh, a.nxcd, xq) * G.chains : 0) : a.bh * G.chains;
+  int total_items = 0;
+  if constexpr (PACKED) total_items = a.ctrl[kCtrlItems] * a.p.heads_kv;
+  const int total = PACKED ? total_items : xcd ? (xq < a.nxcd ? xcd_heads(a.bh, a.nxcd, xq) * G.chains : 0) : a.bh * G.chains;
   int* const ticket = &a.ctrl[xcd ? kCtrlXcdTicket + xq : kCtrlTicket];
   const int* const order = a.order + (xcd ? 2 * xq * a.xcd_cap : 0);
   // LDS byte addresses for the direct copies: the base once, offsets as
@@ -94,7 +103,7 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
   // it at least one step later, so the counter release can wait until the
   // second MFMA run of the next step, by which time the accumulator stores
   // have drained without a wait of their own.
-  const bool deferred = G.sched == S_SHIFT || G.sched == S_SYMSHIFT;
+  const bool deferred = !PACKED && (G.sched == S_SHIFT || G.sched == S_SYMSHIFT);
   bool failed = false;  // this wave hit a wait timeout: skip further waits
   WaitStats wst;
   if constexpr (STATS) stats_wave_begin(wst);
@@ -106,15 +115,22 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
     if (item >= total) break;
     // (head, chain) of the ticket from bwd_pre's table; wave-uniform, so the
     // head's buffer descriptors stay in SGPRs
-    const int bh = __builtin_amdgcn_readfirstlane(order[2 * item]);
-    const int wch = __builtin_amdgcn_readfirstlane(order[2 * item + 1]);
+    std::conditional_t<PACKED, PackedChain<D, BC>, NoChain> ch(a);
+    if constexpr (PACKED) {
+      if (!ch.init(item)) {
+        __syncthreads();  // sm.item is rewritten by the next ticket
+        continue;
+      }
+    }
+    const int bh = PACKED ? 0 : __builtin_amdgcn_readfirstlane(order[2 * item]);
+    const int wch = PACKED ? 0 : __builtin_amdgcn_readfirstlane(order[2 * item + 1]);
     const size_t head = (size_t)bh * N * D;
     const auto rq = make_rsrc((const __bf16*)a.q + head, hbytes);
     const auto rk = make_rsrc((const __bf16*)a.k + head, hbytes);
     const auto rv = make_rsrc((const __bf16*)a.v + head, hbytes);
     const auto rdo = make_rsrc((const __bf16*)a.dO + head, hbytes);
     const auto racc = make_rsrc(a.dqacc + (size_t)bh * a.nblk * BM * D, (uint32_t)a.nblk * BM * D * 4);
-    int* ctr_head = a.counters + (size_t)bh * a.nblk * kCtrStride;
+    int* ctr_head = PACKED ? a.counters : a.counters + (size_t)bh * a.nblk * kCtrStride;
     const auto rctr = make_rsrc(ctr_head, (uint32_t)a.nblk * kCtrStride * 4);
     // L * log2(e) and D of this head's N rows: the padded rows of a ragged
     // last block read 0, so P = 1 there, multiplied by Q and dO rows that
@@ -123,11 +139,16 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
     const auto rds = make_rsrc(a.dvec + (size_t)bh * N, (uint32_t)N * 4);
 
     const unsigned* tab = a.steps + (size_t)wch * a.step_cap;
-    const int nsteps = __builtin_amdgcn_readfirstlane((int)tab[0]);
-    // the chain's schedule (computed by bwd_pre) into LDS; the previous
-    // chain's readers all passed the barrier after the ticket
-    for (int st = tid; st < nsteps; st += NT) sm.steps[st] = tab[1 + st];
-    __syncthreads();
+    int nsteps;
+    if constexpr (PACKED) {
+      nsteps = ch.steps();
+    } else {
+      nsteps = __builtin_amdgcn_readfirstlane((int)tab[0]);
+      // the chain's schedule (computed by bwd_pre) into LDS; the previous
+      // chain's readers all passed the barrier after the ticket
+      for (int st = tid; st < nsteps; st += NT) sm.steps[st] = tab[1 + st];
+      __syncthreads();
+    }
     int cur_j = -1;
     bf16x8 kreg[KS], vreg[KS], ktreg[KSC];  // K, V rows (B of S = Q K^T, dP = dO V^T), K^T (A of dQ^T = K^T dS^T)
     f32x16 dkacc[NB], dvacc[NB];
@@ -142,26 +163,45 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
 
     auto step_at = [&](int st) -> unsigned { return __builtin_amdgcn_readfirstlane(sm.steps[st]); };
     auto next_valid = [&](int st) {
-      while (st < nsteps && step_at(st) == kNoStep) ++st;
+      if constexpr (!PACKED)
+        while (st < nsteps && step_at(st) == kNoStep) ++st;
       return st;
+    };
+    // number of a block's counter (and, packed, of its accumulator)
+    auto ctr_at = [&](Blk b) {
+      if constexpr (PACKED) return ch.index(b);
+      else return b;
     };
     // Q / dO / L / D of block pb into LDS buffer b (asynchronous, vmcnt)
     // Part k of a block is rows 16k (D = 128; 32k at D = 64) further down, i.e.
     // 4 KB further in both the global tile and the LDS tile, with the same
     // swizzle (tile_swz repeats every 16 / 32 rows).
     static_assert((NT / CPR) * D * 2 == 4096 && NT * 16 == 4096, "a part is 4 KB");
-    auto load_part = [&](int pb, int b, int k) {  // part k < QLD of the Q and dO rows
-      const int r = tid / CPR, c = (tid % CPR) ^ tile_swz<D>(r);
-      const uint32_t off = (uint32_t)((pb * BM + r) * D + 8 * c) * 2;
+    auto load_part = [&](Blk pb, int b, int k) {  // part k < QLD of the Q and dO rows
       const uint32_t at = lds_of(&sm.qs[b][64 * w * 8]) + 4096u * k;
-      dma16_pair(rq, rdo, at, at + (uint32_t)sizeof(sm.qs), off, 4096u * k);
+      if constexpr (PACKED) {
+        // (offsets of strided rows are rebuilt where they are used: kept, they spill)
+        const int t0 = 64 * w + fresh_lane(), r = t0 / CPR, c = (t0 % CPR) ^ tile_swz<D>(r);
+        dma16(ch.q(pb), at, ch.at(a.p.qs, r + k * (NT / CPR), 8 * c));
+        dma16(ch.dO(pb), at + (uint32_t)sizeof(sm.qs), ch.at(a.dos, r + k * (NT / CPR), 8 * c));
+      } else {
+        const int r = tid / CPR, c = (tid % CPR) ^ tile_swz<D>(r);
+        const uint32_t off = (uint32_t)((pb * BM + r) * D + 8 * c) * 2;
+        dma16_pair(rq, rdo, at, at + (uint32_t)sizeof(sm.qs), off, 4096u * k);
+      }
     };
-    auto load_ld = [&](int pb, int b) {  // L * log2(e) and D of the block's rows
-      const uint32_t row = (uint32_t)(pb * BM + fresh_lane());
-      if (w == 0) dma4(rls, lds_of(&sm.ls[b][0]), row * 4);
-      if (w == 1) dma4(rds, lds_of(&sm.ds[b][0]), row * 4);
+    auto load_ld = [&](Blk pb, int b) {  // L * log2(e) and D of the block's rows
+      if constexpr (PACKED) {
+        const uint32_t row = (uint32_t)fresh_lane();
+        if (w == 0) dma4(ch.vec(a.lse2, pb), lds_of(&sm.ls[b][0]), row * 4);
+        if (w == 1) dma4(ch.vec(a.dvec, pb), lds_of(&sm.ds[b][0]), row * 4);
+      } else {
+        const uint32_t row = (uint32_t)(pb * BM + fresh_lane());
+        if (w == 0) dma4(rls, lds_of(&sm.ls[b][0]), row * 4);
+        if (w == 1) dma4(rds, lds_of(&sm.ds[b][0]), row * 4);
+      }
     };
-    auto load_block = [&](int pb, int b) {
+    auto load_block = [&](Blk pb, int b) {
 #pragma unroll
       for (int k = 0; k < QLD; ++k) load_part(pb, b, k);
       load_ld(pb, b);
@@ -173,19 +213,39 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
     // of lane l at k*256 + 4l holds row 32 (qh0 + k/4) + l%32, columns
     // 32 dblk + 8rb + 4(l/32) .. +3.
     float* acc_w = &sm.acc[w * DQT * 1024];
-    auto acc_off = [&](int pb, int k) { return (uint32_t)(pb * BM * D + w * DQT * 1024 + k * 256 + 4 * l) * 4; };
+    auto acc_rsrc = [&](Blk pb) {
+      if constexpr (PACKED) return ch.acc(pb);
+      else return racc;
+    };
+    auto acc_off = [&](Blk pb, int k) {
+      if constexpr (PACKED) return (uint32_t)(w * DQT * 1024 + k * 256 + 4 * l) * 4;  // (within the block)
+      else return (uint32_t)(pb * BM * D + w * DQT * 1024 + k * 256 + 4 * l) * 4;
+    };
     // block pb's counter into this wave's poll slot.  The counters stay
     // device-coherent under XCD-local placement too: the atomic adds are
     // performed past the L2, so an L2 read of a counter can stay stale.
-    auto poll_copy = [&](int pb) { dma4_coherent(rctr, lds_of(&sm.poll[w][0]), (uint32_t)pb * kCtrStride * 4); };
-    auto acc_copy = [&](int pb, int k4) {  // chunks 4 k4 .. 4 k4 + 3 of the slice into its landing pad
-      dma16x4_coherent(racc, lds_of(&acc_w[k4 * 1024]), acc_off(pb, 0), 4096u * k4);
+    auto poll_copy = [&](Blk pb) { dma4_coherent(rctr, lds_of(&sm.poll[w][0]), (uint32_t)ctr_at(pb) * kCtrStride * 4); };
+    auto acc_copy = [&](Blk pb, int k4) {  // chunks 4 k4 .. 4 k4 + 3 of the slice into its landing pad
+      dma16x4_coherent(acc_rsrc(pb), lds_of(&acc_w[k4 * 1024]), acc_off(pb, 0), 4096u * k4);
     };
-    auto load_acc = [&](int pb) {
+    auto load_acc = [&](Blk pb) {
 #pragma unroll
       for (int k4 = 0; k4 < NACC / 4; ++k4) acc_copy(pb, k4);
     };
     auto store_dkdv = [&](int j) {
+      if constexpr (PACKED) {
+        const auto rdk = ch.tile(a.dk, a.dks), rdv = ch.tile(a.dv, a.dvs);
+        const int lf = fresh_lane(), g = lf >> 5, lc = lf & 31;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int kv = 32 * w + 8 * (r >> 2) + 4 * g + (r & 3);
+            st2(rdv, ch.at(a.dvs, kv, 32 * nb + lc), to_bf16(dvacc[nb][r]));
+            st2(rdk, ch.at(a.dks, kv, 32 * nb + lc), to_bf16(dkacc[nb][r] * a.scale));
+          }
+        return;
+      }
       const auto rdk = make_rsrc((__bf16*)a.dk + head, hbytes);
       const auto rdv = make_rsrc((__bf16*)a.dv + head, hbytes);
       const int kv0 = j * BC;
@@ -209,34 +269,72 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
 
     int st = next_valid(0);
     int buf = 0;
+    Blk cur{};  // packed: the step's block
+    if constexpr (PACKED) {
+      cur = ch.first();
+      if (nsteps == 0) {  // no query sees the tile
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) dkacc[nb][r] = dvacc[nb][r] = 0.f;
+        cur_j = ch.j;
+      }
+    }
     if (st < nsteps) {
-      const int pb0 = step_at(st) & 0xfff;
+      Blk pb0;
+      if constexpr (PACKED) pb0 = cur;
+      else pb0 = step_at(st) & 0xfff;
       load_block(pb0, buf);
       if (ordered) poll_copy(pb0);
     }
 
     for (; st < nsteps;) {
-      const unsigned e = step_at(st);
-      const int pb = e & 0xfff, j = (e >> 12) & 0x1ff, rank = (e >> 21) & 0x3ff;
-      const bool last = (e >> 31) != 0;
-      const int q0 = pb * BM;
+      Blk pb;
+      int j, rank, q0;
+      bool last;
+      if constexpr (PACKED) {
+        pb = cur;
+        j = rank = ch.j;
+        last = ch.last(pb);
+        q0 = pb.pb * BM + ch.sg.off();  // (as the causal mask counts)
+      } else {
+        const unsigned e = step_at(st);
+        pb = e & 0xfff;
+        j = (e >> 12) & 0x1ff;
+        rank = (e >> 21) & 0x3ff;
+        last = (e >> 31) != 0;
+        q0 = pb * BM;
+      }
 
       if (j != cur_j) {  // new KV tile: flush the previous one, load K/V operands
         if (cur_j >= 0) store_dkdv(cur_j);
         cur_j = j;
         const int kv0 = j * BC;
+        auto k_rsrc = [&]() {
+          if constexpr (PACKED) return ch.tile(a.k, a.p.ks);
+          else return rk;
+        };
+        auto v_rsrc = [&]() {
+          if constexpr (PACKED) return ch.tile(a.v, a.p.vs);
+          else return rv;
+        };
+        const int lf = PACKED ? fresh_lane() : l, g = lf >> 5, lc = lf & 31;
         const int kvr = kv0 + 32 * w + lc;
+        auto kv_at = [&](bool of_k, int row, int col) {  // row of the call (dense) or of the tile (packed)
+          if constexpr (PACKED) return ch.at(of_k ? a.p.ks : a.p.vs, row - kv0, col);
+          else return (uint32_t)(row * D + col) * 2;
+        };
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          kreg[ks] = as_bf16x8(ld16(rk, (uint32_t)(kvr * D + 16 * ks + 8 * g) * 2));
-          vreg[ks] = as_bf16x8(ld16(rv, (uint32_t)(kvr * D + 16 * ks + 8 * g) * 2));
+          kreg[ks] = as_bf16x8(ld16(k_rsrc(), kv_at(true, kvr, 16 * ks + 8 * g)));
+          vreg[ks] = as_bf16x8(ld16(v_rsrc(), kv_at(false, kvr, 16 * ks + 8 * g)));
         }
         // K^T operand: lane holds column d = 32 dblk + lc of K over keys 16ks + 8g .. +7
 #pragma unroll
         for (int ks = 0; ks < KSC; ++ks) {
           unsigned short t[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) t[e] = ld2(rk, (uint32_t)((kv0 + 16 * ks + 8 * g + e) * D + 32 * dblk + lc) * 2);
+          for (int e = 0; e < 8; ++e) t[e] = ld2(k_rsrc(), kv_at(true, kv0 + 16 * ks + 8 * g + e, 32 * dblk + lc));
           ktreg[ks] = as_bf16x8(u32x4{t[0] | ((unsigned)t[1] << 16), t[2] | ((unsigned)t[3] << 16),
                                       t[4] | ((unsigned)t[5] << 16), t[6] | ((unsigned)t[7] << 16)});
         }
@@ -267,12 +365,15 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
 
       // ---- the next valid block (prefetched into the other buffer below)
       const int nst = next_valid(st + 1);
-      const int pb_next = nst < nsteps ? (int)(step_at(nst) & 0xfff) : -1;
+      const bool has_next = nst < nsteps;
+      Blk pb_next;
+      if constexpr (PACKED) pb_next = ch.next(pb);
+      else pb_next = has_next ? (int)(step_at(nst) & 0xfff) : -1;
       // the chain moves to another KV tile after this step (Symmetric Shift,
       // between its two tiles)
-      const bool tile_ends = nst < nsteps && (int)((step_at(nst) >> 12) & 0x1ff) != j;
+      const bool tile_ends = !PACKED && nst < nsteps && (int)((step_at(nst) >> 12) & 0x1ff) != j;
 
-      int* ctr = ctr_head + (size_t)pb * kCtrStride;
+      int* ctr = ctr_head + (size_t)ctr_at(pb) * kCtrStride;
       bool have_turn = false;
 
       const __bf16* qs = sm.qs[buf];
@@ -402,11 +503,11 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
 
       // run 1: S/dP of half 0, with the next block's Q / dO / L / D prefetch
       sdp(0, [&](int k) { rd_rows(1, k); }, [&](int ks) {
-        if (pb_next < 0) return;
+        if (!has_next) return;
         if (ks < QLD) load_part(pb_next, buf ^ 1, ks);
         if (ks == 0) load_ld(pb_next, buf ^ 1);
       });
-      if (pb_next >= 0) {
+      if (has_next) {
         const int n = kBlockLoads + (w < 2 ? 1 : 0);
         vm_poll += n;
         vm_rel += n;
@@ -494,7 +595,7 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
         }
         // dq[t][r] <-> query 32 (qh0 + t) + lc, column d = 32 dblk + 8(r/4) + 4g + r%4
 
-        if (a.partials) {
+        if (!PACKED && a.partials) {
           const auto rp = make_rsrc(a.partials + ((size_t)bh * a.tc + j) * N * D, hbytes * 2);
   #pragma unroll
           for (int t = 0; t < DQT; ++t)
@@ -525,7 +626,7 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
         vm_wait<0>();
         vm_poll = vm_rel = 0;
         // copy the next block's counter now, ahead of the stores below
-        if (ordered && pb_next >= 0) poll_copy(pb_next);
+        if (ordered && has_next) poll_copy(pb_next);
         if constexpr (ordered) {
           // ---- add this wave's partial into its slice straight from registers:
           //      the accumulator is stored in this wave's register order, so the
@@ -546,12 +647,18 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
               f32x4 v = {dq[t][4 * rb], dq[t][4 * rb + 1], dq[t][4 * rb + 2], dq[t][4 * rb + 3]};
               if constexpr (kAdd) v = old[k] + v;
               if constexpr (kLast) {
-                const auto rdq = make_rsrc((__bf16*)a.dq + head, hbytes);
-                const uint32_t off = (uint32_t)((q0 + 32 * (qh0 + t) + lc) * D + 32 * dblk + 8 * rb + 4 * g);
-                st8(rdq, off * 2, u32x2{pack_bf16(v[0] * a.scale, v[1] * a.scale), pack_bf16(v[2] * a.scale, v[3] * a.scale)});
-                if (a.dq_accum) st16(make_rsrc(a.dq_accum + head, hbytes * 2), off * 4, __builtin_bit_cast(u32x4, v));
+                if constexpr (PACKED) {
+                  const int lf = fresh_lane();
+                  st8(ch.dq(pb), ch.at(a.dqs, 32 * (qh0 + t) + (lf & 31), 32 * dblk + 8 * rb + 4 * (lf >> 5)),
+                      u32x2{pack_bf16(v[0] * a.scale, v[1] * a.scale), pack_bf16(v[2] * a.scale, v[3] * a.scale)});
+                } else {
+                  const auto rdq = make_rsrc((__bf16*)a.dq + head, hbytes);
+                  const uint32_t off = (uint32_t)((q0 + 32 * (qh0 + t) + lc) * D + 32 * dblk + 8 * rb + 4 * g);
+                  st8(rdq, off * 2, u32x2{pack_bf16(v[0] * a.scale, v[1] * a.scale), pack_bf16(v[2] * a.scale, v[3] * a.scale)});
+                  if (a.dq_accum) st16(make_rsrc(a.dq_accum + head, hbytes * 2), off * 4, __builtin_bit_cast(u32x4, v));
+                }
               } else {
-                st16_coherent(racc, acc_off(pb, k), __builtin_bit_cast(u32x4, v));
+                st16_coherent(acc_rsrc(pb), acc_off(pb, k), __builtin_bit_cast(u32x4, v));
               }
             }
           };
@@ -565,7 +672,7 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
               if (add) finish(T_{}, T_{});
               else finish(F_{}, T_{});
             }
-            vm_poll += last ? (a.dq_accum ? 2 * NACC : NACC) : NACC;
+            vm_poll += last ? (!PACKED && a.dq_accum ? 2 * NACC : NACC) : NACC;
           }
         } else if constexpr (MODE == kModePartials) {
           // ---- partials variant: the partial goes to KV tile j's own buffer, in
@@ -603,9 +710,11 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
           }
         }
         if (ordered) {
-          if (tid == 0 && a.witness && rank < a.tc) a.witness[((size_t)bh * a.nblk + pb) * a.tc + rank] = j;
-          if (w == 0 && a.witness && rank < a.tc) vm_poll += 1;
-          pend_ctr = pb;
+          if constexpr (!PACKED) {
+            if (tid == 0 && a.witness && rank < a.tc) a.witness[((size_t)bh * a.nblk + pb) * a.tc + rank] = j;
+            if (w == 0 && a.witness && rank < a.tc) vm_poll += 1;
+          }
+          pend_ctr = ctr_at(pb);
           // at the end of the chain or of its KV tile the release comes now: the
           // tile switch (dK, dV stores, K, V loads) would hold it back, and under
           // Symmetric Shift every later contributor of the block, one task behind
@@ -620,6 +729,7 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(BwdArgs a) {
       }
       buf ^= 1;
       st = nst;
+      if constexpr (PACKED) cur = pb_next;
     }
     if (cur_j >= 0) store_dkdv(cur_j);
     __syncthreads();  // sm.item is rewritten by the next ticket
@@ -642,6 +752,13 @@ hipError_t launch_main_mask(const BwdArgs& a, int grid, hipStream_t stream) {
 template <int D>
 hipError_t launch_main(const BwdArgs& a, int grid_main, hipStream_t stream) {
   return a.G.causal ? launch_main_mask<D, true>(a, grid_main, stream) : launch_main_mask<D, false>(a, grid_main, stream);
+}
+
+template <int D>
+hipError_t launch_packed_main(const PackedBwdArgs& a, int grid, hipStream_t stream) {
+  if (a.p.causal) hipLaunchKernelGGL((bwd_main_kernel<D, true, kModeOrdered, false, PackedBwdArgs>), dim3(grid), dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((bwd_main_kernel<D, false, kModeOrdered, false, PackedBwdArgs>), dim3(grid), dim3(256), 0, stream, a);
+  return hipGetLastError();
 }
 
 template <int D>

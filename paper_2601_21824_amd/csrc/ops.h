@@ -71,4 +71,22 @@ struct PackedArgs {
 };
 hipError_t launch_packed_fwd(const PackedArgs& a, int d, hipStream_t stream);
 
+// The backward's main kernels run on BwdArgs; of those, a packed call uses q, k, v, o,
+// dO, lse, dq, dk, dv, dqacc, dvec and lse2 ([heads_q][total_q]), counters (one per 64-row
+// slot and query head), ctrl, order (start order -> sequence, KV tile), scale,
+// spin_limit, poison and status.
+struct PackedBwdArgs : BwdArgs {
+  PackedArgs p;
+  Strides dos, dqs, dks, dvs;
+  int bc;               // rows of a KV tile
+  int slots_q, slots_k;  // 64-row query slots, KV-tile slots
+};
+constexpr int kCtrlItems = 48;  // ctrl[] slot: KV tiles of all sequences
+// rows of a KV tile for a packed call
+int packed_tile_rows(int d, int total_q, int total_k, int batch, int heads_kv);
+hipError_t launch_packed_bwd(const PackedBwdArgs& a, int d, int cus, hipStream_t stream);
+hipError_t launch_packed_main64(const PackedBwdArgs& a, int grid, hipStream_t stream);   // attn_bwd_d64.hip
+hipError_t launch_packed_main128(const PackedBwdArgs& a, int grid, hipStream_t stream);  // attn_bwd.hip
+hipError_t launch_packed_mainw(const PackedBwdArgs& a, int d, int grid, hipStream_t stream);  // attn_bwdw.hip
+
 }  // namespace dash

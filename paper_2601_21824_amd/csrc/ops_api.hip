@@ -194,6 +194,8 @@ int check_packed(const dash_packed_t* p, float* scale, const void* q, const void
     return fail(DASH_ERR_INVALID_ARG, "total_q and total_k must be in 0 .. 2^28");
   if ((int64_t)(p->total_q / 64 + p->batch) * p->heads_q >= (1 << 24))
     return fail(DASH_ERR_UNSUPPORTED, "(total_q / 64 + batch) * heads_q must be below 2^24");
+  if ((int64_t)(p->total_k / 128 + p->batch) * p->heads_kv >= (1 << 30))
+    return fail(DASH_ERR_UNSUPPORTED, "(total_k / 128 + batch) * heads_kv must be below 2^30");
   *work = p->batch > 0 && (p->total_q > 0 || p->total_k > 0);
   if (!*work) return DASH_OK;
   if (!p->cu_q) return fail(DASH_ERR_INVALID_ARG, "null cu_q");
@@ -222,6 +224,88 @@ int attn_packed_fwd(const dash_packed_t* p, const void* q, const void* k, const 
   if ((rc = device_info(&di))) return rc;
   const hipError_t e = dash::launch_packed_fwd(packed_args(p, scale, q, k, v, o, lse), p->d, (hipStream_t)stream);
   return e == hipSuccess ? DASH_OK : hip_fail(e, "packed forward launch");
+}
+
+struct PackedLayout {
+  int slots_q, slots_k;
+  size_t ctrl, dqacc, dvec, lse2, counters, order, total;
+};
+// ctrl first, where dash_bwd_check looks; KV-tile slots for the narrowest tiles
+PackedLayout packed_layout(int batch, int total_q, int total_k, int heads_q, int d) {
+  PackedLayout L;
+  L.slots_q = total_q / dash::kBlockRows + batch;
+  L.slots_k = total_k / 128 + batch;
+  const size_t blocks = (size_t)L.slots_q * heads_q, rows = (size_t)total_q * heads_q;
+  size_t off = 0;
+  L.ctrl = off;
+  off += dash::kCtrlBytes;
+  L.dqacc = off;
+  off += align256(blocks * dash::kBlockRows * d * sizeof(float));
+  L.dvec = off;
+  off += align256(rows * sizeof(float));
+  L.lse2 = off;
+  off += align256(rows * sizeof(float));
+  L.counters = off;
+  off += align256(blocks * dash::kCtrStride * sizeof(int));
+  L.order = off;
+  off += align256((size_t)L.slots_k * 2 * sizeof(int));
+  L.total = off;
+  return L;
+}
+
+int attn_packed_bwd(const dash_packed_t* p, const void* q, const void* k, const void* v, const void* o, const void* dO,
+                    const float* lse, void* dq, void* dk, void* dv, void* workspace, size_t ws_bytes, int* status, void* stream) {
+  bool work = false;
+  float scale = 0.f;
+  int rc = check_packed(p, &scale, q, k, v, o, false, lse, &work);
+  if (rc) return rc;
+  if (!work) {
+    int* flag = workspace && ws_bytes >= dash::kCtrlBytes ? (int*)workspace + dash::kCtrlError : nullptr;
+    return dash::api::clear_flags(flag, status, stream);
+  }
+  const int64_t nq = p->total_q, nk = p->total_k;
+  if (nq && (rc = check_tensor("dO", dO, nq, p->heads_q, p->d, p->do_row_stride, p->do_head_stride, 8, false))) return rc;
+  if (nq && (rc = check_tensor("dq", dq, nq, p->heads_q, p->d, p->dq_row_stride, p->dq_head_stride, 8, true))) return rc;
+  if (nk && (rc = check_tensor("dk", dk, nk, p->heads_kv, p->d, p->dk_row_stride, p->dk_head_stride, 8, true))) return rc;
+  if (nk && (rc = check_tensor("dv", dv, nk, p->heads_kv, p->d, p->dv_row_stride, p->dv_head_stride, 8, true))) return rc;
+  const PackedLayout L = packed_layout(p->batch, p->total_q, p->total_k, p->heads_q, p->d);
+  if (!workspace || ws_bytes < L.total)
+    return fail(DASH_ERR_INVALID_ARG, "workspace missing or smaller than dash_packed_workspace_size()");
+  if (((uintptr_t)workspace & 255) != 0) return fail(DASH_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  DeviceInfo di;
+  if ((rc = device_info(&di))) return rc;
+  char* ws = (char*)workspace;
+  dash::PackedBwdArgs a{};
+  a.p = packed_args(p, scale, q, k, v, const_cast<void*>(o), const_cast<float*>(lse));
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.o = o;
+  a.dO = dO;
+  a.lse = lse;
+  a.dq = dq;
+  a.dk = dk;
+  a.dv = dv;
+  a.dqacc = (float*)(ws + L.dqacc);
+  a.dvec = (float*)(ws + L.dvec);
+  a.lse2 = (float*)(ws + L.lse2);
+  a.counters = (int*)(ws + L.counters);
+  a.ctrl = (int*)(ws + L.ctrl);
+  a.order = (int*)(ws + L.order);
+  a.bh = 1;
+  a.nblk = L.slots_q * p->heads_q;  // counters
+  a.scale = scale;
+  a.spin_limit = 1 << 24;
+  a.status = status;
+  a.dos = {p->do_row_stride, p->do_head_stride};
+  a.dqs = {p->dq_row_stride, p->dq_head_stride};
+  a.dks = {p->dk_row_stride, p->dk_head_stride};
+  a.dvs = {p->dv_row_stride, p->dv_head_stride};
+  a.bc = dash::packed_tile_rows(p->d, p->total_q, p->total_k, p->batch, p->heads_kv);
+  a.slots_q = L.slots_q;
+  a.slots_k = p->total_k / a.bc + p->batch;
+  const hipError_t e = dash::launch_packed_bwd(a, p->d, di.cus, (hipStream_t)stream);
+  return e == hipSuccess ? DASH_OK : hip_fail(e, "packed backward launch");
 }
 
 // no C++ exception (an error message that finds no memory) crosses the interface
@@ -264,6 +348,21 @@ int dash_attn_decode(const dash_paged_cache_t* cache, const void* q, int64_t q_r
 
 int dash_attn_packed_fwd(const dash_packed_t* p, const void* q, const void* k, const void* v, void* o, float* lse, void* stream) {
   return guarded([&] { return attn_packed_fwd(p, q, k, v, o, lse, stream); });
+}
+
+size_t dash_packed_workspace_size(int batch, int total_q, int total_k, int heads_q, int heads_kv, int d) {
+  size_t bytes = 0;
+  guarded([&] {
+    if (check_heads(batch, heads_q, heads_kv, d) == DASH_OK && total_q >= 0 && total_k >= 0 && total_q <= kMaxRows && total_k <= kMaxRows)
+      bytes = packed_layout(batch, total_q, total_k, heads_q, d).total;
+    return 0;
+  });
+  return bytes;
+}
+
+int dash_attn_packed_bwd(const dash_packed_t* p, const void* q, const void* k, const void* v, const void* o, const void* dO,
+                         const float* lse, void* dq, void* dk, void* dv, void* workspace, size_t ws_bytes, int* status, void* stream) {
+  return guarded([&] { return attn_packed_bwd(p, q, k, v, o, dO, lse, dq, dk, dv, workspace, ws_bytes, status, stream); });
 }
 
 }  // extern "C"

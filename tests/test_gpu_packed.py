@@ -84,3 +84,218 @@ def test_forward_equals_the_dense_forward():
     do, dl = dash.attn_fwd(*dense, True)
     assert torch.equal(o.reshape(B, N, H, d).transpose(1, 2), do)
     assert torch.equal(lse.reshape(H, B, N).transpose(0, 1), dl)
+
+
+# ------------------------------------------------------------------ backward
+def like(x, fill=7.0):
+    """A tensor of x's shape and strides, filled."""
+    return torch.full_like(x, fill, memory_format=torch.preserve_format) if x.is_contiguous() else \
+        torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device).fill_(fill)
+
+
+def train(q, k, v, do, cu_q, cu_k, causal, scale=None, status=None):
+    o, lse = like(q), torch.full((q.shape[1], q.shape[0]), 7.0, device="cuda")
+    dash.dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k, causal, scale)
+    dq, dk, dv = like(do), like(k.contiguous()), like(v.contiguous())
+    ws = torch.full((dash.dash_packed_workspace_size(cu_q.numel() - 1, q.shape[0], k.shape[0], q.shape[1], k.shape[1], q.shape[2]),),
+                    255, dtype=torch.uint8, device="cuda")
+    dash.dash_attn_packed_bwd(q, k, v, o, do, lse, dq, dk, dv, cu_q, cu_k, causal, scale, ws, status)
+    assert dash.dash_bwd_check(ws) == dash.DASH_OK
+    return dq, dk, dv
+
+
+@pytest.mark.parametrize("d,hq,hkv,qlens,klens,causal,layout", CASES, ids=map(ids, CASES))
+def test_backward(d, hq, hkv, qlens, klens, causal, layout):
+    tail = 5
+    q, k, v, do = packed_inputs(qlens, klens, hq, hkv, d, layout, tail)
+    status = torch.full((1,), 9, dtype=torch.int32, device="cuda")
+    scale = 0.7 / math.sqrt(d)
+    cu_q, cu_k = cu_of(qlens), None if qlens == klens else cu_of(klens)
+    dq, dk, dv = train(q, k, v, do, cu_q, cu_k, causal, scale, status)
+    assert int(status) == 0
+    ref = reference(q, k, v, do, qlens, klens, causal, scale)
+    for name, got, lens in (("q", dq, qlens), ("k", dk, klens), ("v", dv, klens)):
+        n = sum(lens)
+        assert over(got[:n], ref["d" + name][:n], ref["t" + name][:n]) <= 0, "d" + name
+        assert bool((got[n:] == 7).all()), "rows behind the last sequence"
+    none = (ref["lse"] == -math.inf).t()[:sum(qlens)]
+    assert bool((dq[:sum(qlens)][none] == 0).all())
+    again = train(q, k, v, do, cu_q, cu_k, causal, scale)
+    for a, b in zip((dq, dk, dv), again):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+# wide KV tiles at d = 128, many chains per sequence, several workgroups' rounds
+@pytest.mark.parametrize("d,hq,hkv,lens,causal", [
+    (128, 16, 8, [4000, 1, 3000, 700, 600], True), (128, 8, 8, [2500, 513, 0, 6000], False), (128, 32, 8, [8192], True),
+    (64, 32, 8, [2000, 900, 300, 1100], True), (256, 8, 4, [1500, 100, 2400], True), (256, 4, 4, [1025, 900], False)])
+def test_backward_large(d, hq, hkv, lens, causal):
+    q, k, v, do = packed_inputs(lens, lens, hq, hkv, d, "fused")
+    out = train(q, k, v, do, cu_of(lens), None, causal)
+    ref = reference(q, k, v, do, lens, lens, causal, 1 / math.sqrt(d))
+    for name, got in zip("qkv", out):
+        e = (got.double() - ref["d" + name])
+        # (the elementwise bounds grow with the length; this is the repository's tolerance)
+        assert float(e.norm() / ref["d" + name].norm()) <= 5e-3
+        assert float(e.abs().max() / ref["d" + name].abs().max()) <= 2e-2
+    for _ in range(8):
+        again = train(q, k, v, do, cu_of(lens), None, causal)
+        assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(out, again))
+
+
+def test_gradients_against_differences():
+    """The gradients of sum(O * dO) against central differences of the float64
+    definition's forward, along random directions (the forward itself is checked above)."""
+    lens, hq, hkv, d, eps = [40, 3, 70], 4, 2, 64, 1e-4
+    q, k, v, do = packed_inputs(lens, lens, hq, hkv, d)
+    dq, dk, dv = train(q, k, v, do, cu_of(lens), None, True)
+    base = [x.double() for x in (q, k, v)]
+    for which, grad in ((0, dq), (1, dk), (2, dv)):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(which)
+        for _ in range(3):
+            u = torch.randn(base[which].shape, generator=g, device="cuda", dtype=torch.float64)
+
+            def value(sign):
+                x = list(base)
+                x[which] = x[which] + sign * eps * u
+                r = reference(*x, do, lens, lens, True, 1 / math.sqrt(d))
+                return (r["o"] * do.double()).sum()
+
+            slope = float((value(1) - value(-1)) / (2 * eps))
+            got = float((grad.double() * u).sum())
+            # the gradient's bf16 errors (u8 of each value and of P, dS) along a random
+            # direction add up like their 2-norm; six times that, and the difference's eps^2
+            size = float((grad.double() * u).norm())
+            assert abs(got - slope) <= 6 * 4 * 2.0 ** -8 * size + 1e-3
+
+
+def test_backward_equals_the_dense_backward():
+    """Equal lengths, a head each, narrow tiles: dQ is summed over the same KV tiles in the
+    same order as by Descending, and has its bits.  dK and dV have them under a full mask;
+    under a causal one the dense call visits 128-row query tiles from the last one down but
+    the two 64-row blocks of each upwards, so that their sums are ordered differently."""
+    for d, causal in ((64, True), (128, True), (128, False)):
+        B, H, N = 2, 3, 500
+        q, k, v, do = packed_inputs([N] * B, [N] * B, H, H, d)
+        o, lse = dash.attn_packed_fwd(q, k, v, cu_of([N] * B), causal=causal)
+        got = dash.attn_packed_bwd(q, k, v, o, do, lse, cu_of([N] * B), causal=causal)
+        dense = [x.reshape(B, N, H, d).transpose(1, 2).contiguous() for x in (q, k, v, do)]
+        od, ld = dash.attn_fwd(*dense[:3], causal)
+        want = dash.attn_bwd(*dense[:3], od, dense[3], ld, causal, "descending")
+        for a, b in list(zip(got, want))[:1 if causal else 3]:
+            assert torch.equal(a.reshape(B, N, H, d).transpose(1, 2).contiguous().view(torch.int16), b.view(torch.int16))
+
+
+def test_training_step_captured_and_replayed_with_other_lengths():
+    """Forward and backward in two graphs on one workspace, replayed in turn with offsets
+    that change between replays and eager calls between them: the eager bits every time."""
+    d, hq, hkv, T, B = 128, 8, 2, 700, 4
+    splits = ([100, 200, 0, 400], [700, 0, 0, 0], [1, 1, 1, 300], [350, 350, 0, 0])
+    ws = torch.empty(dash.dash_packed_workspace_size(B, T, T, hq, hkv, d), dtype=torch.uint8, device="cuda")
+
+    def step(b):
+        dash.dash_attn_packed_fwd(b["q"], b["k"], b["v"], b["o"], b["lse"], b["cu"])
+        dash.dash_attn_packed_bwd(b["q"], b["k"], b["v"], b["o"], b["do"], b["lse"], b["dq"], b["dk"], b["dv"], b["cu"],
+                                  workspace=ws)
+
+    def buffers(seed):
+        q, k, v, do = packed_inputs([T], [T], hq, hkv, d, seed=seed)
+        return dict(q=q, k=k, v=v, do=do, o=torch.zeros_like(q), lse=torch.zeros((hq, T), device="cuda"), dq=torch.zeros_like(q),
+                    dk=torch.zeros_like(k), dv=torch.zeros_like(v), cu=cu_of(splits[0]))
+
+    graphs = []
+    for seed in (1, 2):
+        b = buffers(seed)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step(b)
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step(b)
+        graphs.append((graph, b))
+    names = ("o", "lse", "dq", "dk", "dv")
+    for lens in splits + splits:
+        n = sum(lens)
+        for graph, b in graphs:
+            b["cu"].copy_(cu_of(lens))
+            for x in names:
+                b[x].fill_(7)
+            graph.replay()
+            torch.cuda.synchronize()
+            got = {x: b[x].clone() for x in names}
+            eager = dict(b, **{x: torch.full_like(b[x], 7) for x in names})
+            step(eager)  # eager, on the same workspace, between the replays
+            assert dash.dash_bwd_check(ws) == dash.DASH_OK
+            assert all(torch.equal(got[x], eager[x]) for x in names)
+            assert bool((got["dq"][n:] == 7).all()) and bool((got["dk"][n:] == 7).all())
+
+
+def test_two_streams_with_their_own_workspaces():
+    lens = [300, 1200, 64]
+    q, k, v, do = packed_inputs(lens, lens, 8, 2, 128)
+    cu = cu_of(lens)
+    o, lse = dash.attn_packed_fwd(q, k, v, cu)
+    want = dash.attn_packed_bwd(q, k, v, o, do, lse, cu)
+    torch.cuda.synchronize()
+    n = dash.dash_packed_workspace_size(3, sum(lens), sum(lens), 8, 2, 128)
+    work = [(torch.cuda.Stream(), torch.empty(n, dtype=torch.uint8, device="cuda"),
+             [[torch.zeros_like(x) for x in want] for _ in range(4)]) for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(4):
+        for s, ws, outs in work:
+            dash.dash_attn_packed_bwd(q, k, v, o, do, lse, *outs[i], cu, workspace=ws, stream=s)
+    torch.cuda.synchronize()
+    for _, _, outs in work:
+        assert all(torch.equal(a, b) for got in outs for a, b in zip(got, want))
+
+
+def test_from_prompt_to_answer():
+    """As a model's attention layer uses the operators: a prompt's queries and keys rotated
+    and its keys stored, attention over the prompt, then tokens one by one over the
+    cache.  Each token's output equals the packed forward's over the whole text so far."""
+    d, hq, hkv, page, prompt, more = 128, 8, 2, 16, [37, 5, 120], 4
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    total = [n + more for n in prompt]
+    qkv = [torch.randn((n, hq + 2 * hkv, d), generator=g, device="cuda").to(BF) for n in total]
+    inv = (10000.0 ** (-torch.arange(0, d, 2, device="cuda") / d)).float()
+    width = max(total) // page + 1
+    table = torch.arange(3 * width, dtype=torch.int32, device="cuda").reshape(3, width)
+    kc, vc = (torch.full((3 * width, hkv, page, d), float("nan"), device="cuda").to(BF) for _ in range(2))
+    lens = torch.zeros(3, dtype=torch.int32, device="cuda")
+    x = torch.cat([t[:n] for t, n in zip(qkv, prompt)])
+    q, k, v = x.split([hq, hkv, hkv], dim=1)
+    qr, kr = torch.empty_like(q), torch.empty_like(k)
+    cu = cu_of(prompt)
+    dash.dash_kv_append(k, v, kc, vc, table, lens, cu=cu, q=q, q_out=qr, k_out=kr, inv_freq=inv)
+    lens += torch.tensor(prompt, dtype=torch.int32, device="cuda")
+    first, _ = dash.attn_packed_fwd(qr, kr, v, cu)
+    answers = []
+    for t in range(more):
+        x = torch.stack([s[n + t] for s, n in zip(qkv, prompt)])
+        q, k, v = x.split([hq, hkv, hkv], dim=1)
+        qt = torch.empty_like(q)
+        dash.dash_kv_append(k, v, kc, vc, table, lens, q=q, q_out=qt, inv_freq=inv)
+        lens += 1
+        answers.append(dash.attn_decode(qt, kc, vc, table, lens))
+    # the whole texts at once
+    x = torch.cat(qkv)
+    q, k, v = x.split([hq, hkv, hkv], dim=1)
+    qr, kr = torch.empty_like(q), torch.empty_like(k)
+    kc2, vc2 = torch.zeros_like(kc), torch.zeros_like(vc)
+    cu = cu_of(total)
+    dash.dash_kv_append(k, v, kc2, vc2, table, torch.zeros_like(lens), cu=cu, q=q, q_out=qr, k_out=kr, inv_freq=inv)
+    whole, _ = dash.attn_packed_fwd(qr, kr, v, cu)
+    ref = reference(qr, kr, v, torch.zeros_like(qr), total, total, True, 1 / math.sqrt(d))
+    at, a = cu.tolist(), 0
+    for s, n in enumerate(prompt):
+        rows = slice(at[s], at[s] + n)
+        assert over(first[a:a + n], ref["o"][rows], ref["to"][rows]) <= 0
+        a += n
+        for t in range(more):
+            row = at[s] + n + t
+            assert over(answers[t][s], ref["o"][row], ref["to"][row]) <= 0
+            assert over(whole[row], ref["o"][row], ref["to"][row]) <= 0
