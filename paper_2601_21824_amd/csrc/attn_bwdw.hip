@@ -123,7 +123,7 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
   const bool xcd = !PACKED && a.nxcd > 0;
   const int xq = xcd ? xcc_id() : 0;
   int total_items = 0;
-  if constexpr (PACKED) total_items = a.ctrl[kCtrlItems] * a.p.heads_kv;
+  if constexpr (PACKED) total_items = PackedChain<D, BC>::items(a);
   const int total = PACKED ? total_items : xcd ? (xq < a.nxcd ? xcd_heads(a.bh, a.nxcd, xq) * G.chains : 0) : a.bh * G.chains;
   int* const ticket = &a.ctrl[xcd ? kCtrlXcdTicket + xq : kCtrlTicket];
   const int* const order = a.order + (xcd ? 2 * xq * a.xcd_cap : 0);
@@ -396,9 +396,6 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
       };
       const auto rdk = dkv_rsrc(a.dk, true);
       const auto rdv = dkv_rsrc(a.dv, false);
-      const int row0 = PACKED ? 0 : j * BC;  // row of the tile's first key in those
-      int64_t ldk = D, ldv = D;
-      if constexpr (PACKED) ldk = a.dks.row, ldv = a.dvs.row;
       char* pad = (char*)sm.kt + w * 16384;
       const int lf = fresh_lane();
 #pragma unroll
@@ -409,11 +406,11 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
           acc_settle(dkacc[kb][nb]);
         }
         if constexpr (PACKED) {
-          store_block32_strided<D>(rdv, pad, dvacc[kb], 1.f, row0 + 32 * (NKB * w + kb), lf, (uint32_t)ldv);
-          store_block32_strided<D>(rdk, pad, dkacc[kb], a.scale, row0 + 32 * (NKB * w + kb), lf, (uint32_t)ldk);
+          store_block32_packed<D, 128>(rdv, (uint32_t)a.dvs.row, ch.partial(1), ch.split, pad, dvacc[kb], 1.f, 32 * (NKB * w + kb));
+          store_block32_packed<D, 128>(rdk, (uint32_t)a.dks.row, ch.partial(0), ch.split, pad, dkacc[kb], a.scale, 32 * (NKB * w + kb));
         } else {
-          store_block32<D>(rdv, pad, dvacc[kb], 1.f, row0 + 32 * (NKB * w + kb), lf);
-          store_block32<D>(rdk, pad, dkacc[kb], a.scale, row0 + 32 * (NKB * w + kb), lf);
+          store_block32<D>(rdv, pad, dvacc[kb], 1.f, j * BC + 32 * (NKB * w + kb), lf);
+          store_block32<D>(rdk, pad, dkacc[kb], a.scale, j * BC + 32 * (NKB * w + kb), lf);
         }
       }
     };

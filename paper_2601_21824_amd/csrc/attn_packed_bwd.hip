@@ -94,21 +94,79 @@ __global__ __launch_bounds__(256) void packed_pre_kernel(PackedBwdArgs a) {
   const int j = slot - first_slot(p.cu_k, s, p.total_k, a.bc);
   const int length = g.chain(j);
   int place = 0, total = 0;
+  long steps = 0;
   for (int b = 0; b < p.batch; b += 64) {
     const int o = b + l;
     if (o < p.batch) {
       const SeqGeom og = geom(o);
       place += order_part(og, o, s, j, length);
       total += og.tiles();
+      steps += og.steps();
     }
   }
   place = wave_sum(place);
-  total = wave_sum(total);
+  if (slot == 0) {  // the wave of the first slot counts
+    total = wave_sum(total);
+    total = total < a.slots_k ? total : a.slots_k;
+    steps = ((long)wave_sum((int)(steps >> 20)) << 20) + wave_sum((int)(steps & 0xfffff));
+    int n_long = 0;
+    const int group = p.heads_q / p.heads_kv;
+    if (group > 1) {
+      const long above = split_above(steps, p.heads_q, group);
+      for (int b = 0; b < p.batch; b += 64)
+        if (b + l < p.batch) n_long += geom(b + l).tiles_from(above < (1 << 30) ? (int)above + 1 : 1 << 30);
+      n_long = wave_sum(n_long);
+      n_long = n_long < a.split_cap ? n_long : a.split_cap;
+      n_long = n_long < total ? n_long : total;
+    }
+    if (l == 0) {
+      a.ctrl[kCtrlItems] = total;
+      a.ctrl[kCtrlLong] = n_long;
+    }
+  }
   if (l != 0) return;
-  if (slot == 0) a.ctrl[kCtrlItems] = total < a.slots_k ? total : a.slots_k;
   if (j >= 0 && j < g.tiles() && place < a.slots_k) {
     a.order[2 * (size_t)place] = s;
     a.order[2 * (size_t)place + 1] = j;
+  }
+}
+
+// dK, dV of the split tiles: the partials of the group's query heads, in order of the
+// head.  One workgroup per 32 rows of a tile, K/V head and tensor.
+template <int D>
+__global__ __launch_bounds__(256) void packed_sum_kernel(PackedBwdArgs a) {
+  const PackedArgs& p = a.p;
+  const int tid = threadIdx.x, G = p.heads_q / p.heads_kv, rbs = a.bc / 32;
+  int x = (int)blockIdx.x;
+  const int which = x & 1;  // 0: dK, 1: dV
+  x >>= 1;
+  const int rb = x % rbs;
+  x /= rbs;
+  const int hk = x % p.heads_kv, place = x / p.heads_kv;
+  if (place >= a.ctrl[kCtrlLong]) return;
+  const int s = a.order[2 * (size_t)place], j = a.order[2 * (size_t)place + 1];
+  if ((unsigned)s >= (unsigned)p.batch) return;
+  const Span k = span_of(p.cu_k, s, p.total_k);
+  const int row0 = j * a.bc + 32 * rb;
+  if (j < 0 || row0 >= k.len) return;
+  const size_t part = (size_t)a.bc * D;
+  const float* src = a.dkv_part + (((size_t)place * p.heads_q + hk * G) * 2 + which) * part + 32 * rb * D;
+  const float scale = which ? 1.f : a.scale;
+  const Strides& st = which ? a.dvs : a.dks;
+  __bf16* out = (__bf16*)(which ? a.dv : a.dk) + ((int64_t)k.start + row0) * st.row + hk * st.head;
+  const int rows = k.len - row0 < 32 ? k.len - row0 : 32;
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    const int e = tid + 256 * i, r = e / (D / 8), c = e % (D / 8) * 8;
+    f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+    for (int g = 0; g < G; ++g) {
+      const float* at = src + g * (2 * part) + r * D + c;
+      lo += *(const f32x4*)at;
+      hi += *(const f32x4*)(at + 4);
+    }
+    lo *= scale, hi *= scale;
+    if (r < rows)
+      *(u32x4*)(out + r * st.row + c) = u32x4{pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3])};
   }
 }
 
@@ -116,15 +174,19 @@ template <int D>
 hipError_t launch(const PackedBwdArgs& a, int cus, hipStream_t stream) {
   const unsigned grid = (unsigned)(a.slots_q * a.p.heads_q + (a.slots_k + 3) / 4);
   hipLaunchKernelGGL(packed_pre_kernel<D>, dim3(grid), dim3(256), 0, stream, a);
-  const hipError_t e = hipGetLastError();
+  hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // persistent workgroups: as many as stay resident (two per CU at d = 64, else one).
   // A chain waits only on chains that took an earlier ticket, so any count is safe.
-  const long items = (long)a.slots_k * a.p.heads_kv, cap = (long)cus * (D == 64 ? 2 : 1);
+  const long items = (long)a.slots_k * a.p.heads_q, cap = (long)cus * (D == 64 ? 2 : 1);
   const int g = (int)(items < cap ? items : cap);
-  if constexpr (D == 64) return launch_packed_main64(a, g, stream);
-  else if constexpr (D == 256) return launch_packed_mainw(a, D, g, stream);
-  else return a.bc == 256 ? launch_packed_mainw(a, D, g, stream) : launch_packed_main128(a, g, stream);
+  if constexpr (D == 64) e = launch_packed_main64(a, g, stream);
+  else if constexpr (D == 256) e = launch_packed_mainw(a, D, g, stream);
+  else e = a.bc == 256 ? launch_packed_mainw(a, D, g, stream) : launch_packed_main128(a, g, stream);
+  if (e != hipSuccess || a.p.heads_q == a.p.heads_kv) return e;
+  const unsigned sums = (unsigned)a.split_cap * a.p.heads_kv * (a.bc / 32) * 2;
+  hipLaunchKernelGGL(packed_sum_kernel<D>, dim3(sums), dim3(256), 0, stream, a);
+  return hipGetLastError();
 }
 
 }  // namespace

@@ -193,21 +193,40 @@ __device__ inline void store_block32(__amdgpu_buffer_rsrc_t r, void* pad, const 
     st16(r, (uint32_t)(row0 * D * 2 + 1024 * i + 16 * l), *(const u32x4*)((const char*)pad + 1024 * i + 16 * l));
 }
 
-// The same to rows `ld` elements apart: D / 8 lanes store one row's chunks.
-template <int D>
-__device__ inline void store_block32_strided(__amdgpu_buffer_rsrc_t r, void* pad, const f32x16 (&acc)[D / 32], float scale,
-                                             int row0, int l, uint32_t ld) {
-  unsigned short* p = (unsigned short*)pad + 4 * (l >> 5) * D + (l & 31);
-  asm volatile("" ::: "memory");  // after the pad's previous reads
+// The same for a packed call, W columns at a time through `pad` (wave-private LDS, 128 W
+// bytes): to rows `ld` elements apart of `out`, bf16 times scale; or, where a tile's
+// chain is split by query heads, fp32 as it is to rows of D of `part`.
+template <int D, int W>
+__device__ inline void store_block32_packed(__amdgpu_buffer_rsrc_t out, uint32_t ld, __amdgpu_buffer_rsrc_t part, bool split,
+                                            void* pad, const f32x16 (&acc)[D / 32], float scale, int row0) {
 #pragma unroll
-  for (int nb = 0; nb < D / 32; ++nb)
+  for (int c0 = 0; c0 < D; c0 += W) {
+    const int l = fresh_lane();
+    float* p = (float*)pad + 4 * (l >> 5) * W + (l & 31);
+    asm volatile("" ::: "memory");  // after the pad's previous reads
 #pragma unroll
-    for (int k = 0; k < 16; ++k) p[(8 * (k >> 2) + (k & 3)) * D + 32 * nb] = to_bf16(acc[nb][k] * scale);
-  asm volatile("" ::: "memory");  // lanes read what other lanes wrote
-  constexpr int CPR = D / 8, RPI = 64 / CPR;  // chunks per row, rows per instruction
+    for (int nb = 0; nb < W / 32; ++nb)
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i)
-    st16(r, (uint32_t)(row0 + RPI * i + l / CPR) * ld * 2 + 16 * (l % CPR), *(const u32x4*)((const char*)pad + 1024 * i + 16 * l));
+      for (int k = 0; k < 16; ++k) p[(8 * (k >> 2) + (k & 3)) * W + 32 * nb] = acc[c0 / 32 + nb][k];
+    asm volatile("" ::: "memory");  // lanes read what other lanes wrote
+    __builtin_amdgcn_sched_barrier(0);
+    const float* src = (const float*)pad;
+    if (split) {
+#pragma unroll
+      for (int i = 0; i < W / 8; ++i) {
+        const int e = 64 * i + l, r = e / (W / 4), c = e % (W / 4) * 4;
+        st16(part, (uint32_t)((row0 + r) * D + c0 + c) * 4, *(const u32x4*)(src + r * W + c));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < W / 16; ++i) {
+        const int e = 64 * i + l, r = e / (W / 8), c = e % (W / 8) * 8;
+        const f32x4 x = *(const f32x4*)(src + r * W + c) * scale, y = *(const f32x4*)(src + r * W + c + 4) * scale;
+        st16(out, (uint32_t)(row0 + r) * ld * 2 + (uint32_t)(c0 + c) * 2,
+             u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])});
+      }
+    }
+  }
 }
 
 // Launch a main-kernel instantiation on the persistent grid.  Shift and

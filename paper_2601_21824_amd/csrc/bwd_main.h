@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(Args a) {
   constexpr bool xcd = MODE == kModeOrderedXcd;
   const int xq = xcd ? xcc_id() : 0;
   int total_items = 0;
-  if constexpr (PACKED) total_items = a.ctrl[kCtrlItems] * a.p.heads_kv;
+  if constexpr (PACKED) total_items = PackedChain<D, BC>::items(a);
   const int total = PACKED ? total_items : xcd ? (xq < a.nxcd ? xcd_heads(a.bh, a.nxcd, xq) * G.chains : 0) : a.bh * G.chains;
   int* const ticket = &a.ctrl[xcd ? kCtrlXcdTicket + xq : kCtrlTicket];
   const int* const order = a.order + (xcd ? 2 * xq * a.xcd_cap : 0);
@@ -234,16 +234,11 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(Args a) {
     };
     auto store_dkdv = [&](int j) {
       if constexpr (PACKED) {
-        const auto rdk = ch.tile(a.dk, a.dks), rdv = ch.tile(a.dv, a.dvs);
-        const int lf = fresh_lane(), g = lf >> 5, lc = lf & 31;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int kv = 32 * w + 8 * (r >> 2) + 4 * g + (r & 3);
-            st2(rdv, ch.at(a.dvs, kv, 32 * nb + lc), to_bf16(dvacc[nb][r]));
-            st2(rdk, ch.at(a.dks, kv, 32 * nb + lc), to_bf16(dkacc[nb][r] * a.scale));
-          }
+        // every wave is past its reads of the Q blocks (the barrier before the last step's
+        // dQ^T): each takes a quarter as its store pad
+        char* pad = (char*)sm.qs + w * (sizeof(sm.qs) / NW);
+        store_block32_packed<D, D / 2>(ch.tile(a.dv, a.dvs), (uint32_t)a.dvs.row, ch.partial(1), ch.split, pad, dvacc, 1.f, 32 * w);
+        store_block32_packed<D, D / 2>(ch.tile(a.dk, a.dks), (uint32_t)a.dks.row, ch.partial(0), ch.split, pad, dkacc, a.scale, 32 * w);
         return;
       }
       const auto rdk = make_rsrc((__bf16*)a.dk + head, hbytes);

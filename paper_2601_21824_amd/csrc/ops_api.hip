@@ -9,6 +9,7 @@
 #include "api.h"
 #include "dash.h"
 #include "ops.h"
+#include "packed_order.h"
 
 namespace {
 
@@ -194,8 +195,8 @@ int check_packed(const dash_packed_t* p, float* scale, const void* q, const void
     return fail(DASH_ERR_INVALID_ARG, "total_q and total_k must be in 0 .. 2^28");
   if ((int64_t)(p->total_q / 64 + p->batch) * p->heads_q >= (1 << 24))
     return fail(DASH_ERR_UNSUPPORTED, "(total_q / 64 + batch) * heads_q must be below 2^24");
-  if ((int64_t)(p->total_k / 128 + p->batch) * p->heads_kv >= (1 << 30))
-    return fail(DASH_ERR_UNSUPPORTED, "(total_k / 128 + batch) * heads_kv must be below 2^30");
+  if ((int64_t)(p->total_k / 128 + p->batch) * p->heads_q >= (1 << 30))
+    return fail(DASH_ERR_UNSUPPORTED, "(total_k / 128 + batch) * heads_q must be below 2^30");
   *work = p->batch > 0 && (p->total_q > 0 || p->total_k > 0);
   if (!*work) return DASH_OK;
   if (!p->cu_q) return fail(DASH_ERR_INVALID_ARG, "null cu_q");
@@ -227,14 +228,16 @@ int attn_packed_fwd(const dash_packed_t* p, const void* q, const void* k, const 
 }
 
 struct PackedLayout {
-  int slots_q, slots_k;
-  size_t ctrl, dqacc, dvec, lse2, counters, order, total;
+  int bc, slots_q, slots_k, split_cap;
+  size_t ctrl, dqacc, dvec, lse2, counters, order, dkv_part, total;
 };
-// ctrl first, where dash_bwd_check looks; KV-tile slots for the narrowest tiles
-PackedLayout packed_layout(int batch, int total_q, int total_k, int heads_q, int d) {
+// ctrl first, where dash_bwd_check looks
+PackedLayout packed_layout(int batch, int total_q, int total_k, int heads_q, int heads_kv, int d) {
   PackedLayout L;
+  L.bc = dash::packed_tile_rows(d, total_q, total_k, batch, heads_kv);
   L.slots_q = total_q / dash::kBlockRows + batch;
-  L.slots_k = total_k / 128 + batch;
+  L.slots_k = total_k / L.bc + batch;
+  L.split_cap = heads_q == heads_kv ? 0 : dash::split_tiles(L.slots_k, heads_kv);
   const size_t blocks = (size_t)L.slots_q * heads_q, rows = (size_t)total_q * heads_q;
   size_t off = 0;
   L.ctrl = off;
@@ -249,6 +252,8 @@ PackedLayout packed_layout(int batch, int total_q, int total_k, int heads_q, int
   off += align256(blocks * dash::kCtrStride * sizeof(int));
   L.order = off;
   off += align256((size_t)L.slots_k * 2 * sizeof(int));
+  L.dkv_part = off;
+  off += (size_t)L.split_cap * heads_q * 2 * L.bc * d * sizeof(float);
   L.total = off;
   return L;
 }
@@ -268,7 +273,7 @@ int attn_packed_bwd(const dash_packed_t* p, const void* q, const void* k, const 
   if (nq && (rc = check_tensor("dq", dq, nq, p->heads_q, p->d, p->dq_row_stride, p->dq_head_stride, 8, true))) return rc;
   if (nk && (rc = check_tensor("dk", dk, nk, p->heads_kv, p->d, p->dk_row_stride, p->dk_head_stride, 8, true))) return rc;
   if (nk && (rc = check_tensor("dv", dv, nk, p->heads_kv, p->d, p->dv_row_stride, p->dv_head_stride, 8, true))) return rc;
-  const PackedLayout L = packed_layout(p->batch, p->total_q, p->total_k, p->heads_q, p->d);
+  const PackedLayout L = packed_layout(p->batch, p->total_q, p->total_k, p->heads_q, p->heads_kv, p->d);
   if (!workspace || ws_bytes < L.total)
     return fail(DASH_ERR_INVALID_ARG, "workspace missing or smaller than dash_packed_workspace_size()");
   if (((uintptr_t)workspace & 255) != 0) return fail(DASH_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
@@ -301,9 +306,11 @@ int attn_packed_bwd(const dash_packed_t* p, const void* q, const void* k, const 
   a.dqs = {p->dq_row_stride, p->dq_head_stride};
   a.dks = {p->dk_row_stride, p->dk_head_stride};
   a.dvs = {p->dv_row_stride, p->dv_head_stride};
-  a.bc = dash::packed_tile_rows(p->d, p->total_q, p->total_k, p->batch, p->heads_kv);
+  a.bc = L.bc;
   a.slots_q = L.slots_q;
-  a.slots_k = p->total_k / a.bc + p->batch;
+  a.slots_k = L.slots_k;
+  a.split_cap = L.split_cap;
+  a.dkv_part = (float*)(ws + L.dkv_part);
   const hipError_t e = dash::launch_packed_bwd(a, p->d, di.cus, (hipStream_t)stream);
   return e == hipSuccess ? DASH_OK : hip_fail(e, "packed backward launch");
 }
@@ -354,7 +361,7 @@ size_t dash_packed_workspace_size(int batch, int total_q, int total_k, int heads
   size_t bytes = 0;
   guarded([&] {
     if (check_heads(batch, heads_q, heads_kv, d) == DASH_OK && total_q >= 0 && total_k >= 0 && total_q <= kMaxRows && total_k <= kMaxRows)
-      bytes = packed_layout(batch, total_q, total_k, heads_q, d).total;
+      bytes = packed_layout(batch, total_q, total_k, heads_q, heads_kv, d).total;
     return 0;
   });
   return bytes;

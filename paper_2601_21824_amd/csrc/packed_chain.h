@@ -26,17 +26,31 @@ struct PackedChain {
   const PackedBwdArgs& a;
   SeqGeom sg;
   int j, hk, G;
+  int place;                  // the tile's place in the order
+  int h0, hn;                 // the chain's query heads of the group: all, or one of a split tile
+  bool split;
   int qstart, kstart, slot0;  // slot0: the sequence's first accumulator slot
   int pb0;                    // the chain's last (lowest) block
 
   __device__ explicit PackedChain(const PackedBwdArgs& args) : a(args) {}
   // the work item's chain; false: no such chain (an order table that cu does not match)
   __device__ bool init(int item) {
-    const int i = item / a.p.heads_kv;
-    hk = item - i * a.p.heads_kv;
     G = a.p.heads_q / a.p.heads_kv;
-    const int s = __builtin_amdgcn_readfirstlane(a.order[2 * i]);
-    j = __builtin_amdgcn_readfirstlane(a.order[2 * i + 1]);
+    const int n_long = __builtin_amdgcn_readfirstlane(a.ctrl[kCtrlLong]), of_long = n_long * a.p.heads_q;
+    split = item < of_long;
+    h0 = 0, hn = G;
+    if (split) {
+      place = item / a.p.heads_q;
+      const int h = item - place * a.p.heads_q;
+      hk = h / G;
+      h0 = h - hk * G, hn = 1;
+    } else {
+      place = (item - of_long) / a.p.heads_kv;
+      hk = item - of_long - place * a.p.heads_kv;
+      place += n_long;
+    }
+    const int s = __builtin_amdgcn_readfirstlane(a.order[2 * place]);
+    j = __builtin_amdgcn_readfirstlane(a.order[2 * place + 1]);
     if ((unsigned)s >= (unsigned)a.p.batch) return false;
     const Span q = span_of(a.p.cu_q, s, a.p.total_q), k = span_of(a.p.cu_k, s, a.p.total_k);
     qstart = __builtin_amdgcn_readfirstlane(q.start);
@@ -47,9 +61,18 @@ struct PackedChain {
     pb0 = sg.first_block(j);
     return true;
   }
-  __device__ int steps() const { return (sg.blocks() - pb0) * G; }
-  __device__ PackedBlk first() const { return {sg.blocks() - 1, G - 1}; }
-  __device__ PackedBlk next(PackedBlk b) const { return b.h > 0 ? PackedBlk{b.pb, b.h - 1} : PackedBlk{b.pb - 1, G - 1}; }
+  // items of the call
+  __device__ static int items(const PackedBwdArgs& a) {
+    const int n = a.ctrl[kCtrlItems], n_long = a.ctrl[kCtrlLong];
+    return n_long * a.p.heads_q + (n - n_long) * a.p.heads_kv;
+  }
+  __device__ int steps() const { return (sg.blocks() - pb0) * hn; }
+  __device__ PackedBlk first() const { return {sg.blocks() - 1, h0 + hn - 1}; }
+  __device__ PackedBlk next(PackedBlk b) const { return b.h > h0 ? PackedBlk{b.pb, b.h - 1} : PackedBlk{b.pb - 1, h0 + hn - 1}; }
+  // a split tile's fp32 partials of this head: dK (0) or dV (1), BC rows of D
+  __device__ __amdgpu_buffer_rsrc_t partial(int which) const {
+    return make_rsrc(a.dkv_part + (((size_t)place * a.p.heads_q + hk * G + h0) * 2 + which) * (BC * D), BC * D * 4);
+  }
   __device__ bool last(PackedBlk b) const { return sg.last_tile(b.pb) == j; }
 
   // accumulator block and ordering counter

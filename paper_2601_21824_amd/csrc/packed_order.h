@@ -53,7 +53,33 @@ struct SeqGeom {
     const int t = (int)(key / bc) + 1;
     return t < tiles() ? t : tiles();
   }
+  // block steps of the sequence's chains per query head, about: visible pairs over a
+  // step's, and half a step more for every block and tile that the border cuts
+  DASH_ORDER_HD long steps() const {
+    const long m = nq, n = nk;
+    if (m == 0 || n == 0) return 0;
+    if (!causal) return (long)blocks() * tiles();
+    const long pairs = n >= m ? m * (n - m) + m * (m + 1) / 2 : n * (n + 1) / 2;
+    return pairs / (64L * bc) + (blocks() + tiles()) / 2;
+  }
 };
+
+// Where a group has several query heads, a long tile's chain is split into one chain
+// per query head, whose dK and dV partials a further kernel adds in order of the head:
+// a chain of all heads of a long tile would outlast the rest of the call.  A tile is
+// long where its chain has more than split_above blocks, i.e. more than half of a
+// worker's share of all steps.  kSplitWorkers is a constant, so that the sums' order
+// depends on the lengths alone.  Long tiles times K/V heads are then fewer than
+// 2 kSplitWorkers (each has more than 1 / (2 kSplitWorkers) of the steps).
+constexpr int kSplitWorkers = 256;
+DASH_ORDER_HD long split_above(long steps_per_head, int heads_q, int group) {
+  return steps_per_head * heads_q / (2L * kSplitWorkers) / group;
+}
+// room for the partials of this many tiles
+DASH_ORDER_HD int split_tiles(int slots, int heads_kv) {
+  const int most = (2 * kSplitWorkers + heads_kv - 1) / heads_kv;
+  return slots < most ? slots : most;
+}
 
 // Chains start in descending order of their length, equal ones by sequence: the
 // part of tile (s, j)'s place that sequence `other` (number o) adds.  Within one sequence

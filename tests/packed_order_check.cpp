@@ -53,6 +53,21 @@ int main() {
             CHECK(g.tiles_from(n) == m);
           }
         }
+        // a chain is split only where few of all tiles can be
+        for (int hkv : {1, 3, 8})
+          for (int group : {2, 4, 32}) {
+            long steps = 0;
+            for (const SeqGeom& g : q) {
+              steps += g.steps();
+              long exact = 0;
+              for (int j = 0; j < g.tiles(); ++j) exact += g.chain(j);
+              CHECK(g.steps() <= exact + g.blocks() + g.tiles() && exact <= g.steps() + g.blocks() + g.tiles());
+            }
+            const long above = split_above(steps, hkv * group, group);
+            int n_long = 0;
+            for (const SeqGeom& g : q) n_long += g.tiles_from((int)above + 1);
+            CHECK(above >= 0 && n_long <= total && split_tiles(total, hkv) <= total);
+          }
         std::vector<int> seen(total, 0), length(total, -1), seq(total, -1), tile(total, -1);
         for (int s = 0; s < batch; ++s)
           for (int j = 0; j < q[s].tiles(); ++j) {
