@@ -188,17 +188,19 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
     };
     // number of a block's counter (and, packed, of its accumulator)
     auto ctr_at = [&](Blk b) {
-      if constexpr (PACKED) return ch.index(b);
+      if constexpr (PACKED) return b.x;
       else return b;
     };
     // part k of the Q and dO rows of half h of block pb into buffer h
-    auto load_part = [&](Blk pb, int h, int k) {
+    // (packed: the resources of the step's block and of the next one, built once a step)
+    __amdgpu_buffer_rsrc_t blk_q[2], blk_do[2];
+    auto load_part = [&](Blk pb, int h, int k, int nxt = 0) {
       const int t0 = 64 * w + fresh_lane();
       const int r = t0 / CPR + k * (NT / CPR), c = (t0 % CPR) ^ tile_swz<D>(r);
       const uint32_t at = lds_of(&sm.qs[h][0]) + 1024u * w + 4096u * k;
       if constexpr (PACKED) {
-        dma16(ch.q(pb), at, ch.at(a.p.qs, SQ * h + r, 8 * c));
-        dma16(ch.dO(pb), at + (uint32_t)sizeof(sm.qs), ch.at(a.dos, SQ * h + r, 8 * c));
+        dma16(blk_q[nxt], at, ch.at(a.p.qs, SQ * h + r, 8 * c));
+        dma16(blk_do[nxt], at + (uint32_t)sizeof(sm.qs), ch.at(a.dos, SQ * h + r, 8 * c));
       } else {
         dma16_pair(rq, rdo, at, at + (uint32_t)sizeof(sm.qs), (uint32_t)((pb * BM + SQ * h + r) * D + 8 * c) * 2, 0);
       }
@@ -419,6 +421,8 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
     Blk cur{};  // packed: the step's block
     if constexpr (PACKED) {
       cur = ch.first();
+      blk_q[0] = ch.q(cur);
+      blk_do[0] = ch.dO(cur);
       if (nsteps == 0) {  // no query sees the tile: dK = dV = 0
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb)
@@ -426,7 +430,7 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int r = 0; r < 16; ++r) dkacc[kb][nb][r] = dvacc[kb][nb][r] = 0.f;
-        store_dkdv(ch.j);
+        cur_j = ch.j;
       }
     }
     if (st < nsteps) {
@@ -474,9 +478,11 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks)
             vreg[kb][ks] = as_bf16x8(ld16(rv, kv_at(false, 32 * (NKB * w + kb) + (lf & 31), 16 * ks + 8 * (lf >> 5))));
-        if (cur_j >= 0) {  // (the V loads above are on their way meanwhile)
-          flush();
-          store_dkdv(cur_j);
+        if constexpr (!PACKED) {  // (one tile per chain)
+          if (cur_j >= 0) {  // (the V loads above are on their way meanwhile)
+            flush();
+            store_dkdv(cur_j);
+          }
         }
         cur_j = j;
         __syncthreads();  // every wave is done with its store pad (and, in a new chain, with the K tile)
@@ -578,7 +584,7 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
             } else if (has_next) {
               if (ks == 0 && ordered) poll_copy(pb_next);
               if (ks == 0) load_ld(pb_next, bpar ^ 1);
-              if (ks % GAP == 1 && ks / GAP < QP) load_part(pb_next, 0, ks / GAP);
+              if (ks % GAP == 1 && ks / GAP < QP) load_part(pb_next, 0, ks / GAP, 1);
             }
             if (h == 1 && ks == KS - 3 && look2) load_old(pb, 0, add);
             // phase 2's addresses and first reads
@@ -591,6 +597,8 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
           if constexpr (h == 0) {
             has_next = nst < nsteps;
             pb_next = ch.next(pb);
+            blk_q[1] = ch.q(pb_next);
+            blk_do[1] = ch.dO(pb_next);
           }
         } else if constexpr (h == 0) {
           nst = st + 1;
@@ -751,10 +759,14 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
       bpar ^= 1;
       st = nst;
       e = e_next;
-      if constexpr (PACKED) cur = pb_next;
+      if constexpr (PACKED) {
+        cur = pb_next;
+        blk_q[0] = blk_q[1];
+        blk_do[0] = blk_do[1];
+      }
     }
     if (cur_j >= 0) {
-      flush();
+      if (!PACKED || nsteps > 0) flush();
       store_dkdv(cur_j);
     }
     __syncthreads();  // sm.item is rewritten by the next ticket

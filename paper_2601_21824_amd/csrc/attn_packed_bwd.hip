@@ -132,42 +132,48 @@ __global__ __launch_bounds__(256) void packed_pre_kernel(PackedBwdArgs a) {
 }
 
 // dK, dV of the split tiles: the partials of the group's query heads, in order of the
-// head.  One workgroup per 32 rows of a tile, K/V head and tensor.
+// head.  A thread sums 8 columns of a row, a workgroup 2048 / D rows of a tile, K/V head
+// and tensor; eight heads' loads are in flight at once.
 template <int D>
 __global__ __launch_bounds__(256) void packed_sum_kernel(PackedBwdArgs a) {
+  constexpr int RPW = 2048 / D;
   const PackedArgs& p = a.p;
-  const int tid = threadIdx.x, G = p.heads_q / p.heads_kv, rbs = a.bc / 32;
+  const int tid = threadIdx.x, G = p.heads_q / p.heads_kv, pieces = a.bc / RPW;
   int x = (int)blockIdx.x;
+  const int piece = x % pieces;
+  x /= pieces;
   const int which = x & 1;  // 0: dK, 1: dV
   x >>= 1;
-  const int rb = x % rbs;
-  x /= rbs;
   const int hk = x % p.heads_kv, place = x / p.heads_kv;
   if (place >= a.ctrl[kCtrlLong]) return;
   const int s = a.order[2 * (size_t)place], j = a.order[2 * (size_t)place + 1];
   if ((unsigned)s >= (unsigned)p.batch) return;
   const Span k = span_of(p.cu_k, s, p.total_k);
-  const int row0 = j * a.bc + 32 * rb;
-  if (j < 0 || row0 >= k.len) return;
+  const int r = piece * RPW + tid / (D / 8), c = tid % (D / 8) * 8;  // row of the tile, first column
+  if (j < 0 || j * a.bc + r >= k.len) return;
   const size_t part = (size_t)a.bc * D;
-  const float* src = a.dkv_part + (((size_t)place * p.heads_q + hk * G) * 2 + which) * part + 32 * rb * D;
-  const float scale = which ? 1.f : a.scale;
-  const Strides& st = which ? a.dvs : a.dks;
-  __bf16* out = (__bf16*)(which ? a.dv : a.dk) + ((int64_t)k.start + row0) * st.row + hk * st.head;
-  const int rows = k.len - row0 < 32 ? k.len - row0 : 32;
+  const float* src = a.dkv_part + (((size_t)place * p.heads_q + hk * G) * 2 + which) * part + (size_t)r * D + c;
+  f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+  int g = 0;
+  for (; g + 8 <= G; g += 8) {
+    f32x4 x0[8], x1[8];
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) {
-    const int e = tid + 256 * i, r = e / (D / 8), c = e % (D / 8) * 8;
-    f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
-    for (int g = 0; g < G; ++g) {
-      const float* at = src + g * (2 * part) + r * D + c;
-      lo += *(const f32x4*)at;
-      hi += *(const f32x4*)(at + 4);
+    for (int i = 0; i < 8; ++i) {
+      x0[i] = *(const f32x4*)(src + (g + i) * (2 * part));
+      x1[i] = *(const f32x4*)(src + (g + i) * (2 * part) + 4);
     }
-    lo *= scale, hi *= scale;
-    if (r < rows)
-      *(u32x4*)(out + r * st.row + c) = u32x4{pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3])};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) lo += x0[i], hi += x1[i];
   }
+  for (; g < G; ++g) {
+    lo += *(const f32x4*)(src + g * (2 * part));
+    hi += *(const f32x4*)(src + g * (2 * part) + 4);
+  }
+  const float scale = which ? 1.f : a.scale;
+  lo *= scale, hi *= scale;
+  const Strides& st = which ? a.dvs : a.dks;
+  __bf16* out = (__bf16*)(which ? a.dv : a.dk) + ((int64_t)k.start + j * a.bc + r) * st.row + hk * st.head + c;
+  *(u32x4*)out = u32x4{pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3])};
 }
 
 template <int D>
@@ -184,7 +190,7 @@ hipError_t launch(const PackedBwdArgs& a, int cus, hipStream_t stream) {
   else if constexpr (D == 256) e = launch_packed_mainw(a, D, g, stream);
   else e = a.bc == 256 ? launch_packed_mainw(a, D, g, stream) : launch_packed_main128(a, g, stream);
   if (e != hipSuccess || a.p.heads_q == a.p.heads_kv) return e;
-  const unsigned sums = (unsigned)a.split_cap * a.p.heads_kv * (a.bc / 32) * 2;
+  const unsigned sums = (unsigned)a.split_cap * a.p.heads_kv * 2 * (a.bc / (2048 / D));
   hipLaunchKernelGGL(packed_sum_kernel<D>, dim3(sums), dim3(256), 0, stream, a);
   return hipGetLastError();
 }

@@ -2,6 +2,8 @@
 // ordering wait, transposed LDS reads, direct global->LDS loads and the
 // packed per-chain step table.
 #pragma once
+#include <type_traits>
+
 #include "common.h"
 #include "kernels.h"
 
@@ -197,10 +199,11 @@ __device__ inline void store_block32(__amdgpu_buffer_rsrc_t r, void* pad, const 
 // bytes): to rows `ld` elements apart of `out`, bf16 times scale; or, where a tile's
 // chain is split by query heads, fp32 as it is to rows of D of `part`.
 template <int D, int W>
-__device__ inline void store_block32_packed(__amdgpu_buffer_rsrc_t out, uint32_t ld, __amdgpu_buffer_rsrc_t part, bool split,
+__device__ __attribute__((always_inline)) inline void store_block32_packed(__amdgpu_buffer_rsrc_t out, uint32_t ld, __amdgpu_buffer_rsrc_t part, bool split,
                                             void* pad, const f32x16 (&acc)[D / 32], float scale, int row0) {
-#pragma unroll
-  for (int c0 = 0; c0 < D; c0 += W) {
+  static_assert(D == W || D == 2 * W, "one or two passes");
+  auto pass = [&](auto c0_c) __attribute__((always_inline)) {  // (a loop of passes is not unrolled, which puts acc into memory)
+    constexpr int c0 = decltype(c0_c)::value;
     const int l = fresh_lane();
     float* p = (float*)pad + 4 * (l >> 5) * W + (l & 31);
     asm volatile("" ::: "memory");  // after the pad's previous reads
@@ -226,7 +229,9 @@ __device__ inline void store_block32_packed(__amdgpu_buffer_rsrc_t out, uint32_t
              u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])});
       }
     }
-  }
+  };
+  pass(std::integral_constant<int, 0>{});
+  if constexpr (D > W) pass(std::integral_constant<int, W>{});
 }
 
 // Launch a main-kernel instantiation on the persistent grid.  Shift and

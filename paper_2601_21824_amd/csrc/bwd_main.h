@@ -169,7 +169,7 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(Args a) {
     };
     // number of a block's counter (and, packed, of its accumulator)
     auto ctr_at = [&](Blk b) {
-      if constexpr (PACKED) return ch.index(b);
+      if constexpr (PACKED) return b.x;
       else return b;
     };
     // Q / dO / L / D of block pb into LDS buffer b (asynchronous, vmcnt)
@@ -177,13 +177,15 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(Args a) {
     // 4 KB further in both the global tile and the LDS tile, with the same
     // swizzle (tile_swz repeats every 16 / 32 rows).
     static_assert((NT / CPR) * D * 2 == 4096 && NT * 16 == 4096, "a part is 4 KB");
+    // (packed: the resources of a block's copies, built once a step)
+    __amdgpu_buffer_rsrc_t blk_q, blk_do;
     auto load_part = [&](Blk pb, int b, int k) {  // part k < QLD of the Q and dO rows
       const uint32_t at = lds_of(&sm.qs[b][64 * w * 8]) + 4096u * k;
       if constexpr (PACKED) {
         // (offsets of strided rows are rebuilt where they are used: kept, they spill)
         const int t0 = 64 * w + fresh_lane(), r = t0 / CPR, c = (t0 % CPR) ^ tile_swz<D>(r);
-        dma16(ch.q(pb), at, ch.at(a.p.qs, r + k * (NT / CPR), 8 * c));
-        dma16(ch.dO(pb), at + (uint32_t)sizeof(sm.qs), ch.at(a.dos, r + k * (NT / CPR), 8 * c));
+        dma16(blk_q, at, ch.at(a.p.qs, r + k * (NT / CPR), 8 * c));
+        dma16(blk_do, at + (uint32_t)sizeof(sm.qs), ch.at(a.dos, r + k * (NT / CPR), 8 * c));
       } else {
         const int r = tid / CPR, c = (tid % CPR) ^ tile_swz<D>(r);
         const uint32_t off = (uint32_t)((pb * BM + r) * D + 8 * c) * 2;
@@ -277,8 +279,13 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(Args a) {
     }
     if (st < nsteps) {
       Blk pb0;
-      if constexpr (PACKED) pb0 = cur;
-      else pb0 = step_at(st) & 0xfff;
+      if constexpr (PACKED) {
+        pb0 = cur;
+        blk_q = ch.q(cur);
+        blk_do = ch.dO(cur);
+      } else {
+        pb0 = step_at(st) & 0xfff;
+      }
       load_block(pb0, buf);
       if (ordered) poll_copy(pb0);
     }
@@ -302,7 +309,9 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(Args a) {
       }
 
       if (j != cur_j) {  // new KV tile: flush the previous one, load K/V operands
-        if (cur_j >= 0) store_dkdv(cur_j);
+        if constexpr (!PACKED) {  // (one tile per chain)
+          if (cur_j >= 0) store_dkdv(cur_j);
+        }
         cur_j = j;
         const int kv0 = j * BC;
         auto k_rsrc = [&]() {
@@ -362,8 +371,11 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(Args a) {
       const int nst = next_valid(st + 1);
       const bool has_next = nst < nsteps;
       Blk pb_next;
-      if constexpr (PACKED) pb_next = ch.next(pb);
-      else pb_next = has_next ? (int)(step_at(nst) & 0xfff) : -1;
+      if constexpr (PACKED) {
+        pb_next = ch.next(pb);
+        blk_q = ch.q(pb_next);
+        blk_do = ch.dO(pb_next);
+      } else pb_next = has_next ? (int)(step_at(nst) & 0xfff) : -1;
       // the chain moves to another KV tile after this step (Symmetric Shift,
       // between its two tiles)
       const bool tile_ends = !PACKED && nst < nsteps && (int)((step_at(nst) >> 12) & 0x1ff) != j;

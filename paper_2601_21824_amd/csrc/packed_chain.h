@@ -14,6 +14,7 @@ namespace dash {
 // a 64-row query block of one query head of the group
 struct PackedBlk {
   int pb, h;
+  int x;  // number of its accumulator and ordering counter
 };
 
 struct NoChain {
@@ -67,18 +68,21 @@ struct PackedChain {
     return n_long * a.p.heads_q + (n - n_long) * a.p.heads_kv;
   }
   __device__ int steps() const { return (sg.blocks() - pb0) * hn; }
-  __device__ PackedBlk first() const { return {sg.blocks() - 1, h0 + hn - 1}; }
-  __device__ PackedBlk next(PackedBlk b) const { return b.h > h0 ? PackedBlk{b.pb, b.h - 1} : PackedBlk{b.pb - 1, h0 + hn - 1}; }
+  __device__ PackedBlk first() const {
+    const int pb = sg.blocks() - 1, h = h0 + hn - 1;
+    return {pb, h, (slot0 + pb) * a.p.heads_q + hk * G + h};
+  }
+  __device__ PackedBlk next(PackedBlk b) const {
+    return b.h > h0 ? PackedBlk{b.pb, b.h - 1, b.x - 1} : PackedBlk{b.pb - 1, h0 + hn - 1, b.x - a.p.heads_q + hn - 1};
+  }
   // a split tile's fp32 partials of this head: dK (0) or dV (1), BC rows of D
   __device__ __amdgpu_buffer_rsrc_t partial(int which) const {
     return make_rsrc(a.dkv_part + (((size_t)place * a.p.heads_q + hk * G + h0) * 2 + which) * (BC * D), BC * D * 4);
   }
   __device__ bool last(PackedBlk b) const { return sg.last_tile(b.pb) == j; }
 
-  // accumulator block and ordering counter
-  __device__ int index(PackedBlk b) const { return (slot0 + b.pb) * a.p.heads_q + hk * G + b.h; }
   __device__ __amdgpu_buffer_rsrc_t acc(PackedBlk b, bool on = true) const {
-    return make_rsrc(a.dqacc + (size_t)index(b) * (kBlockRows * D), on ? kBlockRows * D * 4 : 0);
+    return make_rsrc(a.dqacc + (size_t)b.x * (kBlockRows * D), on ? kBlockRows * D * 4 : 0);
   }
 
   __device__ static __amdgpu_buffer_rsrc_t rows(const void* p, int64_t first, const Strides& s, int head, int n, int most) {

@@ -67,17 +67,17 @@ struct SeqGeom {
 // Where a group has several query heads, a long tile's chain is split into one chain
 // per query head, whose dK and dV partials a further kernel adds in order of the head:
 // a chain of all heads of a long tile would outlast the rest of the call.  A tile is
-// long where its chain has more than split_above blocks, i.e. more than half of a
-// worker's share of all steps.  kSplitWorkers is a constant, so that the sums' order
-// depends on the lengths alone.  Long tiles times K/V heads are then fewer than
-// 2 kSplitWorkers (each has more than 1 / (2 kSplitWorkers) of the steps).
-constexpr int kSplitWorkers = 256;
+// long where its chain has more than split_above blocks, i.e. more than a
+// kSplitShare-th of a worker's share of all steps.  The constants do not ask the device,
+// so that the sums' order depends on the lengths alone.  Long tiles times K/V heads are
+// then fewer than kSplitShare kSplitWorkers (each has more than that part of the steps).
+constexpr int kSplitWorkers = 256, kSplitShare = 8;
 DASH_ORDER_HD long split_above(long steps_per_head, int heads_q, int group) {
-  return steps_per_head * heads_q / (2L * kSplitWorkers) / group;
+  return steps_per_head * heads_q / ((long)kSplitShare * kSplitWorkers) / group;
 }
 // room for the partials of this many tiles
 DASH_ORDER_HD int split_tiles(int slots, int heads_kv) {
-  const int most = (2 * kSplitWorkers + heads_kv - 1) / heads_kv;
+  const int most = (kSplitShare * kSplitWorkers + heads_kv - 1) / heads_kv;
   return slots < most ? slots : most;
 }
 
