@@ -109,19 +109,52 @@ __global__ __launch_bounds__(256) void packed_pre_kernel(PackedBwdArgs a) {
     total = wave_sum(total);
     total = total < a.slots_k ? total : a.slots_k;
     steps = ((long)wave_sum((int)(steps >> 20)) << 20) + wave_sum((int)(steps & 0xfffff));
-    int n_long = 0;
+    // the cheapest split: lane l weighs limit l % 8 with parts l / 8
     const int group = p.heads_q / p.heads_kv;
+    int n_long = 0, heads = group;
     if (group > 1) {
-      const long above = split_above(steps, p.heads_q, group);
+      const long share = steps * p.heads_q / kSplitWorkers;
+      int longest = 0, mine = 0;
+#pragma unroll
+      for (int i = 0; i < kSplitLimits; ++i) {
+        const long above = split_above(share, group, i);
+        const int from = above < (1 << 30) ? (int)above + 1 : 1 << 30;
+        int n = 0;
+        for (int b = 0; b < p.batch; b += 64)
+          if (b + l < p.batch) n += geom(b + l).tiles_from(from);
+        n = wave_sum(n);
+        mine = (l & 7) == i ? n : mine;
+      }
       for (int b = 0; b < p.batch; b += 64)
-        if (b + l < p.batch) n_long += geom(b + l).tiles_from(above < (1 << 30) ? (int)above + 1 : 1 << 30);
-      n_long = wave_sum(n_long);
-      n_long = n_long < a.split_cap ? n_long : a.split_cap;
+        if (b + l < p.batch) {
+          const SeqGeom og = geom(b + l);
+          const int x = og.tiles() > 0 ? og.chain(0) : 0;
+          longest = x > longest ? x : longest;
+        }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {
+        const int x = __shfl_xor(longest, o);
+        longest = x > longest ? x : longest;
+      }
+      const int per = split_heads(group, l >> 3);
+      long cost = split_cost(share, longest, split_above(share, group, l & 7), mine, per, group, p.heads_kv);
+      if (per < group && (long)mine * p.heads_kv * split_parts(group, per) > a.split_room) cost = 1L << 48;
+      cost = cost << 6 | l;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {
+        const long x = __shfl_xor(cost, o);
+        cost = x < cost ? x : cost;
+      }
+      const int best = (int)(cost & 63);
+      heads = split_heads(group, best >> 3);
+      n_long = __shfl(mine, best);
+      if (heads >= group) n_long = 0;
       n_long = n_long < total ? n_long : total;
     }
     if (l == 0) {
       a.ctrl[kCtrlItems] = total;
       a.ctrl[kCtrlLong] = n_long;
+      a.ctrl[kCtrlHeads] = heads;
     }
   }
   if (l != 0) return;
@@ -131,49 +164,49 @@ __global__ __launch_bounds__(256) void packed_pre_kernel(PackedBwdArgs a) {
   }
 }
 
-// dK, dV of the split tiles: the partials of the group's query heads, in order of the
-// head.  A thread sums 8 columns of a row, a workgroup 2048 / D rows of a tile, K/V head
-// and tensor; eight heads' loads are in flight at once.
+// dK, dV of the split tiles: the parts' partials, in order.  A thread sums 8 columns of
+// a row, a workgroup 2048 / D rows of a tile, K/V head and tensor; eight parts' loads are
+// in flight at once.  A fixed grid takes the pieces in turn, as their number is only
+// known on the device.
 template <int D>
 __global__ __launch_bounds__(256) void packed_sum_kernel(PackedBwdArgs a) {
   constexpr int RPW = 2048 / D;
   const PackedArgs& p = a.p;
-  const int tid = threadIdx.x, G = p.heads_q / p.heads_kv, pieces = a.bc / RPW;
-  int x = (int)blockIdx.x;
-  const int piece = x % pieces;
-  x /= pieces;
-  const int which = x & 1;  // 0: dK, 1: dV
-  x >>= 1;
-  const int hk = x % p.heads_kv, place = x / p.heads_kv;
-  if (place >= a.ctrl[kCtrlLong]) return;
-  const int s = a.order[2 * (size_t)place], j = a.order[2 * (size_t)place + 1];
-  if ((unsigned)s >= (unsigned)p.batch) return;
-  const Span k = span_of(p.cu_k, s, p.total_k);
-  const int r = piece * RPW + tid / (D / 8), c = tid % (D / 8) * 8;  // row of the tile, first column
-  if (j < 0 || j * a.bc + r >= k.len) return;
-  const size_t part = (size_t)a.bc * D;
-  const float* src = a.dkv_part + (((size_t)place * p.heads_q + hk * G) * 2 + which) * part + (size_t)r * D + c;
-  f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
-  int g = 0;
-  for (; g + 8 <= G; g += 8) {
-    f32x4 x0[8], x1[8];
+  const int tid = threadIdx.x, pieces = a.bc / RPW;
+  const int n_long = a.ctrl[kCtrlLong], parts = split_parts(p.heads_q / p.heads_kv, a.ctrl[kCtrlHeads]);
+  const long todo = (long)n_long * p.heads_kv * 2 * pieces;
+  for (long x = blockIdx.x; x < todo; x += gridDim.x) {
+    const int piece = (int)(x % pieces), which = (int)(x / pieces) & 1;  // 0: dK, 1: dV
+    const int tile = (int)(x / (2 * pieces)), hk = tile % p.heads_kv, place = tile / p.heads_kv;
+    const int s = a.order[2 * (size_t)place], j = a.order[2 * (size_t)place + 1];
+    if ((unsigned)s >= (unsigned)p.batch) continue;
+    const Span k = span_of(p.cu_k, s, p.total_k);
+    const int r = piece * RPW + tid / (D / 8), c = tid % (D / 8) * 8;  // row of the tile, first column
+    if (j < 0 || j * a.bc + r >= k.len) continue;
+    const size_t step = (size_t)a.bc * D;
+    const float* src = a.dkv_part + ((size_t)tile * parts * 2 + which) * step + (size_t)r * D + c;
+    f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+    int g = 0;
+    for (; g + 8 <= parts; g += 8) {
+      f32x4 x0[8], x1[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      x0[i] = *(const f32x4*)(src + (g + i) * (2 * part));
-      x1[i] = *(const f32x4*)(src + (g + i) * (2 * part) + 4);
+      for (int i = 0; i < 8; ++i) {
+        x0[i] = *(const f32x4*)(src + (g + i) * (2 * step));
+        x1[i] = *(const f32x4*)(src + (g + i) * (2 * step) + 4);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) lo += x0[i], hi += x1[i];
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) lo += x0[i], hi += x1[i];
+    for (; g < parts; ++g) {
+      lo += *(const f32x4*)(src + g * (2 * step));
+      hi += *(const f32x4*)(src + g * (2 * step) + 4);
+    }
+    const float scale = which ? 1.f : a.scale;
+    lo *= scale, hi *= scale;
+    const Strides& st = which ? a.dvs : a.dks;
+    __bf16* out = (__bf16*)(which ? a.dv : a.dk) + ((int64_t)k.start + j * a.bc + r) * st.row + hk * st.head + c;
+    *(u32x4*)out = u32x4{pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3])};
   }
-  for (; g < G; ++g) {
-    lo += *(const f32x4*)(src + g * (2 * part));
-    hi += *(const f32x4*)(src + g * (2 * part) + 4);
-  }
-  const float scale = which ? 1.f : a.scale;
-  lo *= scale, hi *= scale;
-  const Strides& st = which ? a.dvs : a.dks;
-  __bf16* out = (__bf16*)(which ? a.dv : a.dk) + ((int64_t)k.start + j * a.bc + r) * st.row + hk * st.head + c;
-  *(u32x4*)out = u32x4{pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3])};
 }
 
 template <int D>
@@ -190,7 +223,8 @@ hipError_t launch(const PackedBwdArgs& a, int cus, hipStream_t stream) {
   else if constexpr (D == 256) e = launch_packed_mainw(a, D, g, stream);
   else e = a.bc == 256 ? launch_packed_mainw(a, D, g, stream) : launch_packed_main128(a, g, stream);
   if (e != hipSuccess || a.p.heads_q == a.p.heads_kv) return e;
-  const unsigned sums = (unsigned)a.split_cap * a.p.heads_kv * 2 * (a.bc / (2048 / D));
+  const long most = (long)a.split_room * 2 * (a.bc / (2048 / D));  // (2 parts at least to a sum)
+  const unsigned sums = (unsigned)(most / 2 < 8L * cus ? most / 2 : 8L * cus);
   hipLaunchKernelGGL(packed_sum_kernel<D>, dim3(sums), dim3(256), 0, stream, a);
   return hipGetLastError();
 }

@@ -80,11 +80,12 @@ struct PackedBwdArgs : BwdArgs {
   Strides dos, dqs, dks, dvs;
   int bc;               // rows of a KV tile
   int slots_q, slots_k;  // 64-row query slots, KV-tile slots
-  int split_cap;         // tiles that dkv_part has room for
-  float* dkv_part;       // partials of split tiles: [place][heads_q][dK, dV][bc * d]
+  int split_room;        // parts that dkv_part has room for
+  float* dkv_part;       // split tiles: [place][K/V head][part][dK, dV][bc][d]
 };
 constexpr int kCtrlItems = 48;  // ctrl[] slot: KV tiles of all sequences
 constexpr int kCtrlLong = 49;   // ctrl[] slot: how many of them, from the first on, are split
+constexpr int kCtrlHeads = 50;  // ctrl[] slot: query heads of a part of those
 // rows of a KV tile for a packed call
 int packed_tile_rows(int d, int total_q, int total_k, int batch, int heads_kv);
 hipError_t launch_packed_bwd(const PackedBwdArgs& a, int d, int cus, hipStream_t stream);

@@ -228,7 +228,7 @@ int attn_packed_fwd(const dash_packed_t* p, const void* q, const void* k, const 
 }
 
 struct PackedLayout {
-  int bc, slots_q, slots_k, split_cap;
+  int bc, slots_q, slots_k, split_room;
   size_t ctrl, dqacc, dvec, lse2, counters, order, dkv_part, total;
 };
 // ctrl first, where dash_bwd_check looks
@@ -237,7 +237,7 @@ PackedLayout packed_layout(int batch, int total_q, int total_k, int heads_q, int
   L.bc = dash::packed_tile_rows(d, total_q, total_k, batch, heads_kv);
   L.slots_q = total_q / dash::kBlockRows + batch;
   L.slots_k = total_k / L.bc + batch;
-  L.split_cap = heads_q == heads_kv ? 0 : dash::split_tiles(L.slots_k, heads_kv);
+  L.split_room = heads_q == heads_kv ? 0 : dash::split_room(L.slots_k, heads_q);
   const size_t blocks = (size_t)L.slots_q * heads_q, rows = (size_t)total_q * heads_q;
   size_t off = 0;
   L.ctrl = off;
@@ -253,7 +253,7 @@ PackedLayout packed_layout(int batch, int total_q, int total_k, int heads_q, int
   L.order = off;
   off += align256((size_t)L.slots_k * 2 * sizeof(int));
   L.dkv_part = off;
-  off += (size_t)L.split_cap * heads_q * 2 * L.bc * d * sizeof(float);
+  off += (size_t)L.split_room * 2 * L.bc * d * sizeof(float);
   L.total = off;
   return L;
 }
@@ -309,7 +309,7 @@ int attn_packed_bwd(const dash_packed_t* p, const void* q, const void* k, const 
   a.bc = L.bc;
   a.slots_q = L.slots_q;
   a.slots_k = L.slots_k;
-  a.split_cap = L.split_cap;
+  a.split_room = L.split_room;
   a.dkv_part = (float*)(ws + L.dkv_part);
   const hipError_t e = dash::launch_packed_bwd(a, p->d, di.cus, (hipStream_t)stream);
   return e == hipSuccess ? DASH_OK : hip_fail(e, "packed backward launch");

@@ -28,8 +28,9 @@ struct PackedChain {
   SeqGeom sg;
   int j, hk, G;
   int place;                  // the tile's place in the order
-  int h0, hn;                 // the chain's query heads of the group: all, or one of a split tile
+  int h0, hn;                 // the chain's query heads of the group: all, or a part's of a split tile
   bool split;
+  int part;                   // the part's number
   int qstart, kstart, slot0;  // slot0: the sequence's first accumulator slot
   int pb0;                    // the chain's last (lowest) block
 
@@ -37,14 +38,18 @@ struct PackedChain {
   // the work item's chain; false: no such chain (an order table that cu does not match)
   __device__ bool init(int item) {
     G = a.p.heads_q / a.p.heads_kv;
-    const int n_long = __builtin_amdgcn_readfirstlane(a.ctrl[kCtrlLong]), of_long = n_long * a.p.heads_q;
+    const int n_long = __builtin_amdgcn_readfirstlane(a.ctrl[kCtrlLong]);
+    const int per = __builtin_amdgcn_readfirstlane(a.ctrl[kCtrlHeads]), parts = split_parts(G, per);
+    const int of_long = n_long * a.p.heads_kv * parts;
     split = item < of_long;
     h0 = 0, hn = G;
+    part = item;
     if (split) {
-      place = item / a.p.heads_q;
-      const int h = item - place * a.p.heads_q;
-      hk = h / G;
-      h0 = h - hk * G, hn = 1;
+      place = item / (a.p.heads_kv * parts);
+      const int x = item - place * (a.p.heads_kv * parts);
+      hk = x / parts;
+      h0 = (x - hk * parts) * per;
+      hn = h0 + per < G ? per : G - h0;
     } else {
       place = (item - of_long) / a.p.heads_kv;
       hk = item - of_long - place * a.p.heads_kv;
@@ -65,7 +70,8 @@ struct PackedChain {
   // items of the call
   __device__ static int items(const PackedBwdArgs& a) {
     const int n = a.ctrl[kCtrlItems], n_long = a.ctrl[kCtrlLong];
-    return n_long * a.p.heads_q + (n - n_long) * a.p.heads_kv;
+    const int parts = split_parts(a.p.heads_q / a.p.heads_kv, a.ctrl[kCtrlHeads]);
+    return (n_long * parts + n - n_long) * a.p.heads_kv;
   }
   __device__ int steps() const { return (sg.blocks() - pb0) * hn; }
   __device__ PackedBlk first() const {
@@ -75,9 +81,9 @@ struct PackedChain {
   __device__ PackedBlk next(PackedBlk b) const {
     return b.h > h0 ? PackedBlk{b.pb, b.h - 1, b.x - 1} : PackedBlk{b.pb - 1, h0 + hn - 1, b.x - a.p.heads_q + hn - 1};
   }
-  // a split tile's fp32 partials of this head: dK (0) or dV (1), BC rows of D
+  // a part's fp32 partials: dK (0) or dV (1), BC rows of D
   __device__ __amdgpu_buffer_rsrc_t partial(int which) const {
-    return make_rsrc(a.dkv_part + (((size_t)place * a.p.heads_q + hk * G + h0) * 2 + which) * (BC * D), BC * D * 4);
+    return make_rsrc(a.dkv_part + ((size_t)part * 2 + which) * (BC * D), BC * D * 4);
   }
   __device__ bool last(PackedBlk b) const { return sg.last_tile(b.pb) == j; }
 

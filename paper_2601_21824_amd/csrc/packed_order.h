@@ -64,21 +64,41 @@ struct SeqGeom {
   }
 };
 
-// Where a group has several query heads, a long tile's chain is split into one chain
-// per query head, whose dK and dV partials a further kernel adds in order of the head:
-// a chain of all heads of a long tile would outlast the rest of the call.  A tile is
-// long where its chain has more than split_above blocks, i.e. more than a
-// kSplitShare-th of a worker's share of all steps.  The constants do not ask the device,
-// so that the sums' order depends on the lengths alone.  Long tiles times K/V heads are
-// then fewer than kSplitShare kSplitWorkers (each has more than that part of the steps).
-constexpr int kSplitWorkers = 256, kSplitShare = 8;
-DASH_ORDER_HD long split_above(long steps_per_head, int heads_q, int group) {
-  return steps_per_head * heads_q / ((long)kSplitShare * kSplitWorkers) / group;
+// Where a group has several query heads, a long tile's chain can be split into chains
+// of fewer heads each, whose dK and dV partials a further kernel adds in order: as
+// one chain it would outlast the rest of the call.  A split is `parts` chains of up
+// to ceil(group / parts) heads for every tile whose chain has more than `above` blocks.
+// Which one: the least of split_cost over kSplits choices, in block steps of a worker.
+// It asks the lengths and the constant kSplitWorkers, not the device, so that the
+// sums' order depends on the lengths alone.
+constexpr int kSplitWorkers = 256;
+constexpr int kSplitLimits = 8, kSplitParts = 8, kSplits = kSplitLimits * kSplitParts;
+// limit i: a tile is long whose whole chain is over 2^-i of a worker's share
+DASH_ORDER_HD long split_above(long share, int group, int i) { return (share >> i) / group; }
+DASH_ORDER_HD int split_heads(int group, int i) {  // heads per part, choice i: group / 2^i
+  const int h = (group + (1 << i) - 1) >> i;
+  return h < 1 ? 1 : h;
 }
-// room for the partials of this many tiles
-DASH_ORDER_HD int split_tiles(int slots, int heads_kv) {
-  const int most = (kSplitShare * kSplitWorkers + heads_kv - 1) / heads_kv;
-  return slots < most ? slots : most;
+DASH_ORDER_HD int split_parts(int group, int heads) { return (group + heads - 1) / heads; }
+// share: steps of all chains over the workers; longest: blocks of the longest chain;
+// n_long: tiles with more than `above` blocks; heads: per part (group: none is split).
+// Unsplit chains start last, so that on average half of one stands over at the end;
+// writing and reading a part's partials takes about as long as 3 steps.
+DASH_ORDER_HD long split_cost(long share, long longest, long above, long n_long, int heads, int group, int heads_kv) {
+  const bool whole = heads >= group;
+  const long tail = (whole || above > longest ? longest : above) * group;
+  long t = share + tail / 2;
+  t = t > tail ? t : tail;
+  if (whole) return t;
+  const long part = longest > above ? longest * heads : 0;
+  t = t > part ? t : part;
+  return t + 3 * n_long * heads_kv * split_parts(group, heads) / kSplitWorkers;
+}
+// Partials there is room for (each of a part's dK and dV): a tile is never split finer
+// than costs less than its steps, i.e. more than `share` steps' worth of partials in all.
+DASH_ORDER_HD int split_room(int slots, int heads_q) {
+  const long all = (long)slots * heads_q;
+  return all < 8 * kSplitWorkers ? (int)all : 8 * kSplitWorkers;
 }
 
 // Chains start in descending order of their length, equal ones by sequence: the

@@ -63,10 +63,20 @@ int main() {
               for (int j = 0; j < g.tiles(); ++j) exact += g.chain(j);
               CHECK(g.steps() <= exact + g.blocks() + g.tiles() && exact <= g.steps() + g.blocks() + g.tiles());
             }
-            const long above = split_above(steps, hkv * group, group);
-            int n_long = 0;
-            for (const SeqGeom& g : q) n_long += g.tiles_from((int)above + 1);
-            CHECK(above >= 0 && n_long <= total && split_tiles(total, hkv) <= total);
+            // every choice of a split covers the group's heads once
+            for (int i = 0; i < kSplitParts; ++i) {
+              const int heads = split_heads(group, i), parts = split_parts(group, heads);
+              CHECK(heads >= 1 && heads <= group && (parts - 1) * heads < group && parts * heads >= group);
+              CHECK(i > 0 || heads == group);
+            }
+            const long share = steps * hkv * group / kSplitWorkers;
+            for (int i = 0; i < kSplitLimits; ++i) {
+              const long above = split_above(share, group, i);
+              CHECK(above >= 0 && (i == 0 || above <= split_above(share, group, i - 1)));
+              int n_long = 0;
+              for (const SeqGeom& g : q) n_long += g.tiles_from((int)above + 1);
+              CHECK(n_long <= total);
+            }
           }
         std::vector<int> seen(total, 0), length(total, -1), seq(total, -1), tile(total, -1);
         for (int s = 0; s < batch; ++s)
