@@ -457,11 +457,18 @@ typedef struct {
   int64_t dq_row_stride, dq_head_stride, dk_row_stride, dk_head_stride, dv_row_stride, dv_head_stride;
 } dash_packed_t;
 
+/* Bytes of workspace with which dash_attn_packed_fwd may split the keys, under either
+   mask (0: this call is not split, or the arguments are invalid). */
+size_t dash_packed_fwd_workspace_size(int batch, int total_q, int total_k, int heads_q, int heads_kv, int d);
+
 /* Forward over packed sequences: q, o bf16 [total_q][heads_q][d], k, v bf16
    [total_k][heads_kv][d], lse fp32 [heads_q][total_q] contiguous.  Asynchronous on
-   `stream`. */
+   `stream`.  A call with few query rows for the GPU and long sequences is faster split over
+   the keys, for which it needs a workspace of dash_packed_fwd_workspace_size bytes
+   (256-byte aligned, any contents, not used by another call until this one has
+   finished); with NULL it is not split.  Both give the same result up to rounding. */
 int dash_attn_packed_fwd(const dash_packed_t* p, const void* q, const void* k, const void* v, void* o, float* lse,
-                         void* stream);
+                         void* workspace, size_t ws_bytes, void* stream);
 
 /* Bytes of workspace for dash_attn_packed_bwd (0 if the arguments are invalid). */
 size_t dash_packed_workspace_size(int batch, int total_q, int total_k, int heads_q, int heads_kv, int d);
@@ -471,8 +478,9 @@ size_t dash_packed_workspace_size(int batch, int total_q, int total_k, int heads
  * (each K/V head's gradient is the sum over its query heads).  Deterministic: dK and dV
  * are summed by one workgroup, dQ over the KV tiles in ascending order by the ordered
  * reduction of dash_attn_bwd_ex (Descending Q-Tile Iteration, Section 3.3, over the
- * blocks of all query heads of a group).  The KV tile, and with it the order of the
- * sums, depends on total_k and heads_kv at d = 128.  Asynchronous on `stream`, launched
+ * blocks of all query heads of a group).  The KV tile at d = 128, and with it the order of
+ * the sums, depends on total_k, batch, heads_q and the mask; how a group's query heads
+ * are summed into dK and dV depends on all sequences' lengths.  Asynchronous on `stream`, launched
  * without cooperation: its waits only point to work that started earlier.
  * Workspace of ws_bytes >= dash_packed_workspace_size(...) bytes, 256-byte aligned, any
  * contents, not used by another call until this one has finished.  A wait timeout is

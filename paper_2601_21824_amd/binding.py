@@ -31,7 +31,7 @@ EXPORTS = ("dash_attn_fwd", "dash_attn_fwd_ex", "dash_attn_bwd", "dash_bwd_works
            "dash_bwd_placement", "dash_mfma_peak", "dash_last_error", "dash_release_workspace",
            "dash_auto_schedule", "dash_model_makespan", "dash_kv_append", "dash_attn_decode",
            "dash_decode_workspace_size", "dash_attn_packed_fwd", "dash_attn_packed_bwd",
-           "dash_packed_workspace_size")
+           "dash_packed_workspace_size", "dash_packed_fwd_workspace_size")
 DASH_CACHE_BF16, DASH_CACHE_E4M3 = 0, 1
 
 
@@ -110,7 +110,9 @@ def load():
         lib.dash_attn_packed_bwd.argtypes = [ctypes.POINTER(dash_packed_t)] + [vp] * 10 + [sz, vp, vp]
         lib.dash_packed_workspace_size.argtypes = [ci] * 6
         lib.dash_packed_workspace_size.restype = sz
-        lib.dash_attn_packed_fwd.argtypes = [ctypes.POINTER(dash_packed_t)] + [vp] * 6
+        lib.dash_attn_packed_fwd.argtypes = [ctypes.POINTER(dash_packed_t)] + [vp] * 6 + [sz, vp]
+        lib.dash_packed_fwd_workspace_size.argtypes = [ci] * 6
+        lib.dash_packed_fwd_workspace_size.restype = sz
         lib.dash_decode_workspace_size.restype = sz
         lib.dash_last_error.restype = ctypes.c_char_p
         lib.dash_release_workspace.restype = None
@@ -457,11 +459,17 @@ def _packed(q, k, cu_q, cu_k, causal, scale):
                          _flat("cu_q", cu_q, torch.int32, dev, batch + 1), _flat("cu_k", cu_k, torch.int32, dev, batch + 1)), dev
 
 
-def dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k=None, causal: bool = True, scale=None, stream=None):
+def dash_packed_fwd_workspace_size(batch: int, total_q: int, total_k: int, heads_q: int, heads_kv: int, d: int) -> int:
+    return int(load().dash_packed_fwd_workspace_size(batch, total_q, total_k, heads_q, heads_kv, d))
+
+
+def dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k=None, causal: bool = True, scale=None, workspace=None, stream=None):
     """O and L of attention over packed sequences into o (bf16 [total_q, heads_q, d]) and
     lse (fp32 [heads_q, total_q]); q like o, k and v [total_k, heads_kv, d], any row and
     head strides.  ``cu_q``, ``cu_k``: int32 [batch + 1], where each sequence's queries and
-    keys begin (the same without ``cu_k``); a causal mask is aligned to the last key."""
+    keys begin (the same without ``cu_k``); a causal mask is aligned to the last key.
+    ``workspace``: None, or a uint8 device tensor of dash_packed_fwd_workspace_size bytes with
+    which a call of few rows is split over its keys."""
     import torch
     p, dev = _packed(q, k, cu_q, cu_k, causal, scale)
     bf = torch.bfloat16
@@ -469,16 +477,20 @@ def dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k=None, causal: bool = True, 
     b, p.k_row_stride, p.k_head_stride = _rows("k", k, bf, dev, p.total_k, p.heads_kv, p.d)
     c, p.v_row_stride, p.v_head_stride = _rows("v", v, bf, dev, p.total_k, p.heads_kv, p.d)
     e, p.o_row_stride, p.o_head_stride = _rows("o", o, bf, dev, p.total_q, p.heads_q, p.d)
+    ws, n = (None, 0) if workspace is None else (_flat("workspace", workspace, torch.uint8, dev, workspace.numel()), workspace.numel())
     with _On(dev):
         _check(load().dash_attn_packed_fwd(ctypes.byref(p), a, b, c, e, _flat("lse", lse, torch.float32, dev, p.heads_q * p.total_q),
-                                           _stream_of(stream, dev)))
+                                           ws, n, _stream_of(stream, dev)))
 
 
 def attn_packed_fwd(q, k, v, cu_q, cu_k=None, causal: bool = True, scale=None):
     import torch
     o = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
     lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
-    dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k, causal, scale)
+    n = 0 if q.dim() != 3 or k.dim() != 3 else dash_packed_fwd_workspace_size(cu_q.numel() - 1, q.shape[0], k.shape[0],
+                                                                               q.shape[1], k.shape[1], q.shape[2])
+    ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k, causal, scale, ws)
     return o, lse
 
 

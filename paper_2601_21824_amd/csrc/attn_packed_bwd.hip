@@ -231,10 +231,19 @@ hipError_t launch(const PackedBwdArgs& a, int cus, hipStream_t stream) {
 
 }  // namespace
 
-int packed_tile_rows(int d, int total_q, int total_k, int batch, int heads_kv) {
-  (void)total_q;
-  (void)batch;
-  return d == 128 && (long)(total_k / 256) * heads_kv >= 256 ? 256 : 128;
+// d = 128 has both tiles.  Wide ones need chains enough for 256 CUs (split by query
+// head, total_k / 256 times heads_q; longer ones weigh more under a causal mask) and
+// sequences that fill them.  Measured (us, narrow / wide; heads_q over heads_kv):
+//   causal  352 chains of one of 3000 385 / 348, 384 (4096, 24 over 8) 511 / 466, 512 (2048
+//           64 over 8) 360 / 312; 256 (4096, 16 over 16) 345 / 367, (8192, 8 over 1) 673 / 721,
+//           (2 of 1024, 32 over 8) 136 / 138
+//   full    192 (2048, 24 over 24) 303 / 258, 256 (4096, 16 over 4) 674 / 525; 128 (4096, 8 over 8,
+//           causal) 264 / 363
+//   length  1024 chains of 16 of 512 292 / 272; 24 of 384 233 / 314, 32 of 256 159 / 226, 10 of 409
+//           on average 180 / 200
+int packed_tile_rows(int d, int total_k, int batch, int heads_q, int causal) {
+  const long chains = (long)(total_k / 256) * heads_q;
+  return d == 128 && chains >= (causal ? 320 : 160) && total_k >= 480L * batch ? 256 : 128;
 }
 
 hipError_t launch_packed_bwd(const PackedBwdArgs& a, int d, int cus, hipStream_t stream) {

@@ -58,7 +58,12 @@ struct DenseView {
   __device__ __amdgpu_buffer_rsrc_t o() const { return make_rsrc((__bf16*)a.o + head, hbytes); }
   __device__ __amdgpu_buffer_rsrc_t lse() const { return make_rsrc(a.lse + (size_t)bh * nq, (uint32_t)nq * 4); }
   __device__ uint32_t q_at(int row, int col) const { return (uint32_t)(row * D + col) * 2; }
-  __device__ uint32_t o_at(int row, int col) const { return (uint32_t)(row * D + col) * 2; }
+  __device__ uint32_t l_at(int row) const { return (uint32_t)row * 4; }
+  // columns col .. col + 3 of a row of O
+  __device__ void put_o(__amdgpu_buffer_rsrc_t r, int row, int col, float a0, float a1, float a2, float a3) const {
+    const u32x2 t = {pack_bf16(a0, a1), pack_bf16(a2, a3)};
+    st8(r, (uint32_t)(row * D + col) * 2, t);
+  }
   // row `row` of the tile whose first key is k0
   __device__ uint32_t k_at(int k0, int row, int col) const { return (uint32_t)((k0 + row) * D + col) * 2; }
   __device__ uint32_t v_at(int k0, int row, int col) const { return (uint32_t)((k0 + row) * D + col) * 2; }
@@ -194,13 +199,11 @@ __device__ void far_rows(const V& view, int causal, float scale, int row0) {
 #pragma unroll
     for (int db = 0; db < 2; ++db)
 #pragma unroll
-      for (int rb = 0; rb < 4; ++rb) {
-        const u32x2 t = {pack_bf16(o[db][4 * rb] * inv, o[db][4 * rb + 1] * inv),
-                         pack_bf16(o[db][4 * rb + 2] * inv, o[db][4 * rb + 3] * inv)};
-        st8(ro, view.o_at(qrow, d0 + 32 * db + 8 * rb + 4 * g), t);
-      }
+      for (int rb = 0; rb < 4; ++rb)
+        view.put_o(ro, qrow, d0 + 32 * db + 8 * rb + 4 * g, o[db][4 * rb] * inv, o[db][4 * rb + 1] * inv, o[db][4 * rb + 2] * inv,
+                   o[db][4 * rb + 3] * inv);
     if (d0 == 0 && g == 0)
-      st4f(view.lse(), (uint32_t)qrow * 4, (m + __log2f(sum)) * kLn2);
+      st4f(view.lse(), view.l_at(qrow), (m + __log2f(sum)) * kLn2);
   }
 }
 
@@ -559,10 +562,9 @@ __device__ __attribute__((always_inline)) inline void attn_fwd_rows(const V& vie
 #pragma unroll
       for (int rb = 0; rb < 4; ++rb) {
         const f32x16& o = oacc[qg][db];
-        u32x2 t = {pack_bf16(o[4 * rb] * inv, o[4 * rb + 1] * inv), pack_bf16(o[4 * rb + 2] * inv, o[4 * rb + 3] * inv)};
-        st8(ro, view.o_at(qrow, 32 * db + 8 * rb + 4 * g), t);
+        view.put_o(ro, qrow, 32 * db + 8 * rb + 4 * g, o[4 * rb] * inv, o[4 * rb + 1] * inv, o[4 * rb + 2] * inv, o[4 * rb + 3] * inv);
       }
-    if (g == 0) st4f(rl, (uint32_t)qrow * 4, (m[qg] + __log2f(sum)) * kLn2);
+    if (g == 0) st4f(rl, view.l_at(qrow), (m[qg] + __log2f(sum)) * kLn2);
   }
 }
 

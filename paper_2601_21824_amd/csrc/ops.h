@@ -68,7 +68,14 @@ struct PackedArgs {
   int batch, heads_q, heads_kv, total_q, total_k, causal;
   float scale;
   Strides qs, ks, vs, os;
+  // the forward's split over the keys: runs at most, and their O and L (packed_part_rows)
+  int splits;
+  float* part_o;
+  float* part_l;
 };
+int packed_splits(int d, int total_q, int total_k, int batch, int heads_q, int causal);
+// rows of part_l, and of d columns of part_o
+size_t packed_part_rows(int total_q, int batch, int heads_q, int splits);
 hipError_t launch_packed_fwd(const PackedArgs& a, int d, hipStream_t stream);
 
 // The backward's main kernels run on BwdArgs; of those, a packed call uses q, k, v, o,
@@ -87,7 +94,7 @@ constexpr int kCtrlItems = 48;  // ctrl[] slot: KV tiles of all sequences
 constexpr int kCtrlLong = 49;   // ctrl[] slot: how many of them, from the first on, are split
 constexpr int kCtrlHeads = 50;  // ctrl[] slot: query heads of a part of those
 // rows of a KV tile for a packed call
-int packed_tile_rows(int d, int total_q, int total_k, int batch, int heads_kv);
+int packed_tile_rows(int d, int total_k, int batch, int heads_q, int causal);
 hipError_t launch_packed_bwd(const PackedBwdArgs& a, int d, int cus, hipStream_t stream);
 hipError_t launch_packed_main64(const PackedBwdArgs& a, int grid, hipStream_t stream);   // attn_bwd_d64.hip
 hipError_t launch_packed_main128(const PackedBwdArgs& a, int grid, hipStream_t stream);  // attn_bwd.hip

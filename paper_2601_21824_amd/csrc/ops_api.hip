@@ -213,17 +213,42 @@ int check_packed(const dash_packed_t* p, float* scale, const void* q, const void
 dash::PackedArgs packed_args(const dash_packed_t* p, float scale, const void* q, const void* k, const void* v, void* o, float* lse) {
   return {q, k, v, o, lse, p->cu_q, p->cu_k ? p->cu_k : p->cu_q, p->batch, p->heads_q, p->heads_kv, p->total_q, p->total_k,
           p->causal ? 1 : 0, scale, {p->q_row_stride, p->q_head_stride}, {p->k_row_stride, p->k_head_stride},
-          {p->v_row_stride, p->v_head_stride}, {p->o_row_stride, p->o_head_stride}};
+          {p->v_row_stride, p->v_head_stride}, {p->o_row_stride, p->o_head_stride}, 1, nullptr, nullptr};
 }
 
-int attn_packed_fwd(const dash_packed_t* p, const void* q, const void* k, const void* v, void* o, float* lse, void* stream) {
+struct FwdLayout {
+  int splits;
+  size_t part_o, part_l, total;
+};
+FwdLayout fwd_layout(int batch, int total_q, int total_k, int heads_q, int d, int causal) {
+  FwdLayout L;
+  L.splits = batch > 0 ? dash::packed_splits(d, total_q, total_k, batch, heads_q, causal) : 1;
+  const size_t rows = dash::packed_part_rows(total_q, batch, heads_q, L.splits);
+  L.part_o = 0;
+  L.part_l = rows * d * sizeof(float);
+  L.total = L.part_l + align256(rows * sizeof(float));
+  return L;
+}
+
+int attn_packed_fwd(const dash_packed_t* p, const void* q, const void* k, const void* v, void* o, float* lse, void* workspace,
+                    size_t ws_bytes, void* stream) {
   bool work = false;
   float scale = 0.f;
   int rc = check_packed(p, &scale, q, k, v, o, true, lse, &work);
   if (rc || !work || p->total_q == 0) return rc;
+  dash::PackedArgs a = packed_args(p, scale, q, k, v, o, lse);
+  const FwdLayout L = fwd_layout(p->batch, p->total_q, p->total_k, p->heads_q, p->d, a.causal);
+  if (L.splits > 1 && workspace) {
+    if (ws_bytes < dash_packed_fwd_workspace_size(p->batch, p->total_q, p->total_k, p->heads_q, p->heads_kv, p->d))
+      return fail(DASH_ERR_INVALID_ARG, "workspace smaller than dash_packed_fwd_workspace_size()");
+    if (((uintptr_t)workspace & 255) != 0) return fail(DASH_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    a.splits = L.splits;
+    a.part_o = (float*)((char*)workspace + L.part_o);
+    a.part_l = (float*)((char*)workspace + L.part_l);
+  }
   DeviceInfo di;
   if ((rc = device_info(&di))) return rc;
-  const hipError_t e = dash::launch_packed_fwd(packed_args(p, scale, q, k, v, o, lse), p->d, (hipStream_t)stream);
+  const hipError_t e = dash::launch_packed_fwd(a, p->d, (hipStream_t)stream);
   return e == hipSuccess ? DASH_OK : hip_fail(e, "packed forward launch");
 }
 
@@ -231,10 +256,10 @@ struct PackedLayout {
   int bc, slots_q, slots_k, split_room;
   size_t ctrl, dqacc, dvec, lse2, counters, order, dkv_part, total;
 };
-// ctrl first, where dash_bwd_check looks
-PackedLayout packed_layout(int batch, int total_q, int total_k, int heads_q, int heads_kv, int d) {
+// ctrl first, where dash_bwd_check looks; bc: rows of the KV tiles
+PackedLayout packed_layout(int batch, int total_q, int total_k, int heads_q, int heads_kv, int d, int bc) {
   PackedLayout L;
-  L.bc = dash::packed_tile_rows(d, total_q, total_k, batch, heads_kv);
+  L.bc = bc;
   L.slots_q = total_q / dash::kBlockRows + batch;
   L.slots_k = total_k / L.bc + batch;
   L.split_room = heads_q == heads_kv ? 0 : dash::split_room(L.slots_k, heads_q);
@@ -273,8 +298,9 @@ int attn_packed_bwd(const dash_packed_t* p, const void* q, const void* k, const 
   if (nq && (rc = check_tensor("dq", dq, nq, p->heads_q, p->d, p->dq_row_stride, p->dq_head_stride, 8, true))) return rc;
   if (nk && (rc = check_tensor("dk", dk, nk, p->heads_kv, p->d, p->dk_row_stride, p->dk_head_stride, 8, true))) return rc;
   if (nk && (rc = check_tensor("dv", dv, nk, p->heads_kv, p->d, p->dv_row_stride, p->dv_head_stride, 8, true))) return rc;
-  const PackedLayout L = packed_layout(p->batch, p->total_q, p->total_k, p->heads_q, p->heads_kv, p->d);
-  if (!workspace || ws_bytes < L.total)
+  const PackedLayout L = packed_layout(p->batch, p->total_q, p->total_k, p->heads_q, p->heads_kv, p->d,
+                                       dash::packed_tile_rows(p->d, p->total_k, p->batch, p->heads_q, p->causal != 0));
+  if (!workspace || ws_bytes < dash_packed_workspace_size(p->batch, p->total_q, p->total_k, p->heads_q, p->heads_kv, p->d))
     return fail(DASH_ERR_INVALID_ARG, "workspace missing or smaller than dash_packed_workspace_size()");
   if (((uintptr_t)workspace & 255) != 0) return fail(DASH_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
   DeviceInfo di;
@@ -353,15 +379,28 @@ int dash_attn_decode(const dash_paged_cache_t* cache, const void* q, int64_t q_r
   });
 }
 
-int dash_attn_packed_fwd(const dash_packed_t* p, const void* q, const void* k, const void* v, void* o, float* lse, void* stream) {
-  return guarded([&] { return attn_packed_fwd(p, q, k, v, o, lse, stream); });
+size_t dash_packed_fwd_workspace_size(int batch, int total_q, int total_k, int heads_q, int heads_kv, int d) {
+  size_t bytes = 0;
+  guarded([&] {
+    if (check_heads(batch, heads_q, heads_kv, d) == DASH_OK && total_q >= 0 && total_k >= 0 && total_q <= kMaxRows && total_k <= kMaxRows)
+      bytes = std::max(fwd_layout(batch, total_q, total_k, heads_q, d, 0).total, fwd_layout(batch, total_q, total_k, heads_q, d, 1).total);
+    return 0;
+  });
+  return bytes;
+}
+
+int dash_attn_packed_fwd(const dash_packed_t* p, const void* q, const void* k, const void* v, void* o, float* lse, void* workspace,
+                         size_t ws_bytes, void* stream) {
+  return guarded([&] { return attn_packed_fwd(p, q, k, v, o, lse, workspace, ws_bytes, stream); });
 }
 
 size_t dash_packed_workspace_size(int batch, int total_q, int total_k, int heads_q, int heads_kv, int d) {
   size_t bytes = 0;
   guarded([&] {
     if (check_heads(batch, heads_q, heads_kv, d) == DASH_OK && total_q >= 0 && total_k >= 0 && total_q <= kMaxRows && total_k <= kMaxRows)
-      bytes = packed_layout(batch, total_q, total_k, heads_q, heads_kv, d).total;
+      for (int causal = 0; causal < 2; ++causal)  // either mask
+        bytes = std::max(bytes, packed_layout(batch, total_q, total_k, heads_q, heads_kv, d,
+                                              dash::packed_tile_rows(d, total_k, batch, heads_q, causal)).total);
     return 0;
   });
   return bytes;

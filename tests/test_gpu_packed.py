@@ -50,6 +50,55 @@ def test_forward(d, hq, hkv, qlens, klens, causal, layout):
     assert torch.equal(o[:n].view(torch.int16), o2[:n].view(torch.int16)) and torch.equal(lse[:, :n], lse2[:, :n])
 
 
+# few query rows on many keys: split over the keys, evenly and not, beside sequences too
+# short to be, and past the keys that a causal row sees
+SPLITS = [(d, hq, hkv, q, k, causal) for d in (64, 128, 256) for causal in (True, False)
+          for hq, hkv, q, k in ((2, 1, [1], [4097]), (4, 2, [130, 3], [5000, 700]), (8, 8, [64, 0, 200], [1023, 300, 3333]),
+                                (2, 2, [2000], [2000]), (1, 1, [300, 5], [512, 6000]))]
+
+
+@pytest.mark.parametrize("d,hq,hkv,qlens,klens,causal", SPLITS)
+def test_forward_split(d, hq, hkv, qlens, klens, causal):
+    tail = 3
+    q, k, v, do = packed_inputs(qlens, klens, hq, hkv, d, "packed", tail, spread=2.0)
+    cu_q, cu_k = cu_of(qlens), cu_of(klens)
+    n, T, K = sum(qlens), sum(qlens) + tail, sum(klens) + tail
+    size = dash.dash_packed_fwd_workspace_size(len(qlens), T, K, hq, hkv, d)
+    assert size > 0
+    ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")  # NaN, if it were read before it is written
+    o, lse = torch.full_like(q, 7.0), torch.full((hq, T), 7.0, device="cuda")
+    dash.dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k, causal, workspace=ws)
+    ref = reference(q, k, v, do, qlens, klens, causal, 1 / math.sqrt(d))
+    assert over(o[:n], ref["o"][:n], ref["to"][:n]) <= 0
+    rl = ref["lse"][:, :n]
+    assert bool(rl.isfinite().all()) and over(lse[:, :n], rl, 2e-5 * rl.abs().clamp(min=1)) <= 0
+    assert bool((o[n:] == 7).all()) and bool((lse[:, n:] == 7).all())
+    o1, lse1 = dash.attn_packed_fwd(q, k, v, cu_q, cu_k, causal)  # allocates its own
+    assert torch.equal(o[:n].view(torch.int16), o1[:n].view(torch.int16)) and torch.equal(lse[:, :n], lse1[:, :n])
+    o2, lse2 = torch.empty_like(o), torch.empty_like(lse)
+    dash.dash_attn_packed_fwd(q, k, v, o2, lse2, cu_q, cu_k, causal)  # not split
+    assert over(o2[:n], ref["o"][:n], ref["to"][:n]) <= 0 and over(lse2[:, :n], rl, 2e-5 * rl.abs().clamp(min=1)) <= 0
+
+
+def test_forward_split_far_scores():
+    """Runs whose keys all score -inf or far below the others: no weight, no NaN."""
+    q, k, v, _ = packed_inputs([100], [4000], 2, 2, 128)
+    q[..., 0] = 1
+    for shift, lo, hi in ((float("-inf"), 0, 1500), (-1e30, 1000, 3000), (float("-inf"), 2500, 4000)):
+        k2 = k.clone()
+        k2[lo:hi, :, 0] = shift
+        keep = torch.tensor([j for j in range(4000) if not lo <= j < hi], device="cuda")
+        o, lse = dash.attn_packed_fwd(q, k2, v, cu_of([100]), cu_of([4000]), causal=False)
+        for h in range(2):
+            s = q[:, h].double() @ k2[keep, h].double().t() / math.sqrt(128)
+            want = torch.softmax(s, -1) @ v[keep, h].double()
+            assert float((o[:, h].double() - want).norm() / want.norm()) <= 5e-3
+            assert float((lse[h].double() - torch.logsumexp(s, -1)).abs().max()) <= 1e-4
+    k2[..., 0] = float("-inf")
+    o, lse = dash.attn_packed_fwd(q, k2, v, cu_of([100]), cu_of([4000]), causal=False)
+    assert bool((o == 0).all()) and bool((lse == -math.inf).all())
+
+
 @pytest.mark.parametrize("shift", [-1e30, -3e9, float("-inf")])
 @pytest.mark.parametrize("d", [64, 128, 256])
 def test_forward_far_scores(d, shift):

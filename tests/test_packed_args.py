@@ -19,8 +19,8 @@ def problem(**kw):
     return p
 
 
-def fwd(p, ptrs=(P,) * 4, lse=P):
-    return b.load().dash_attn_packed_fwd(None if p is None else ctypes.byref(p), *ptrs, lse, None)
+def fwd(p, ptrs=(P,) * 4, lse=P, ws=None, ws_bytes=0):
+    return b.load().dash_attn_packed_fwd(None if p is None else ctypes.byref(p), *ptrs, lse, ws, ws_bytes, None)
 
 
 def bwd(p, ptrs=(P,) * 9, ws=P, ws_bytes=1 << 40):
@@ -74,6 +74,15 @@ def test_pointers_and_workspace():
         assert bwd(problem(), ws=ws, ws_bytes=n) == b.DASH_ERR_INVALID_ARG and "workspace" in b.dash_last_error()
     for bad in ((2, 300, 300, 8, 3, 128), (2, 300, 300, 8, 2, 100), (-1, 300, 300, 8, 2, 128), (2, -1, 300, 8, 2, 128)):
         assert b.dash_packed_workspace_size(*bad) == 0
+
+
+def test_forward_workspace():
+    big = dict(total_k=30000, cu_k=P)
+    need = b.dash_packed_fwd_workspace_size(2, 300, 30000, 8, 2, 128)
+    assert need > 0 and b.dash_packed_fwd_workspace_size(2, 300, 300, 8, 2, 128) == 0
+    assert b.dash_packed_fwd_workspace_size(2, 300, 30000, 8, 3, 128) == 0
+    for ws, n in ((P, need - 1), (P + 16, need)):
+        assert fwd(problem(**big), ws=ws, ws_bytes=n) == b.DASH_ERR_INVALID_ARG and "workspace" in b.dash_last_error()
 
 
 def test_too_many_blocks():
