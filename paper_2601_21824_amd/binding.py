@@ -287,82 +287,86 @@ def dash_schedule_table(schedule, N: int, d: int, causal: bool, placement=DASH_P
 
 
 # ----------------------------------------------------------------- sequences of different lengths
+# These calls are short on the GPU, so their checks are written to be quick: the
+# strides go into the C structs by position, and the raw stream is asked for.
 def _bad(msg: str):
     raise DashError(DASH_ERR_INVALID_ARG, msg)
 
 
-def _rows(name, t, dtype, device, rows, heads, d):
-    """A [rows, heads, d] tensor whose heads are contiguous: its pointer and strides."""
-    if t.dtype is not dtype or t.device != device or t.shape != (rows, heads, d):
-        _bad(f"{name} must be a {dtype} [{rows}, {heads}, {d}] tensor on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+def _rows(name, t, dtype, dev, rows, heads, d):
+    """A [rows, heads, d] tensor on GPU `dev` whose heads are contiguous: its pointer and strides."""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != (rows, heads, d):
+        _bad(f"{name} must be a {dtype} [{rows}, {heads}, {d}] tensor on cuda:{dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     row, head, one = t.stride()
-    if one != 1:
+    if one != 1 and d > 1:
         _bad(f"{name}: the last dimension must be contiguous")
     return t.data_ptr(), row, head
 
 
-def _flat(name, t, dtype, device, n):
-    """A contiguous tensor of n values, or None: its pointer."""
+def _flat(name, t, dtype, dev, n):
+    """A contiguous tensor of n values on GPU `dev`, or None: its pointer."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.device != device or t.numel() != n or not t.is_contiguous():
-        _bad(f"{name} must be a contiguous {dtype} tensor of {n} values on {device}")
+    if t.dtype is not dtype or t.get_device() != dev or t.numel() != n or not t.is_contiguous():
+        _bad(f"{name} must be a contiguous {dtype} tensor of {n} values on cuda:{dev}")
     return t.data_ptr()
 
 
-def _device(t):
-    """The device of a call's tensors: a GPU."""
-    if not t.is_cuda:
+def _gpu(t):
+    """The number of a tensor's GPU."""
+    dev = t.get_device()
+    if dev < 0:
         _bad("expected device tensors")
-    return t.device
+    return dev
 
 
-class _On:
-    """The call's device made current, as the library launches on the current one."""
-
-    def __init__(self, device):
-        import torch
-        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _space(workspace, need, dev, stream):
+    """A call's workspace (allocated if there is none, behind the current stream's work): pointer and bytes."""
+    import torch
+    if workspace is None:
+        if stream is not None:
+            _bad("a call on an explicit stream needs an explicit workspace")
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=torch.device("cuda", dev))
+    return _flat("workspace", workspace, torch.uint8, dev, workspace.numel()), workspace.numel(), workspace
 
 
-def _stream_of(stream, device):
+def _call(f, dev, stream, *args):
+    """f(*args, stream) with GPU `dev` current, as the library launches on the current one."""
+    import torch
+    if torch.cuda.current_device() != dev:
+        with torch.cuda.device(dev):
+            return _call(f, dev, stream, *args)
     if stream is None:
-        import torch
-        return torch.cuda.current_stream(device).cuda_stream
-    return stream if isinstance(stream, int) else stream.cuda_stream
+        stream = torch._C._cuda_getCurrentRawStream(dev)
+    elif not isinstance(stream, int):
+        stream = stream.cuda_stream
+    _check(f(*args, stream))
 
 
-def _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q):
+def _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q, dev):
     """dash_paged_cache_t of [pages, heads_kv, page_size, d] caches (any strides, contiguous rows)."""
     import torch
-    dev = _device(k_cache)
     dt = k_cache.dtype
     if dt is not torch.bfloat16 and dt is not torch.float8_e4m3fn:
         _bad("caches must be bfloat16 or float8_e4m3fn")
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or v_cache.dtype is not dt or v_cache.device != dev:
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or v_cache.dtype is not dt or v_cache.get_device() != dev:
         _bad("k_cache and v_cache must be [pages, heads_kv, page_size, d] tensors alike")
     pages, heads_kv, page, d = k_cache.shape
     (kp, kh, kr, k1), (vp, vh, vr, v1) = k_cache.stride(), v_cache.stride()
     if k1 != 1 or v1 != 1:
         _bad("the last dimension of the caches must be contiguous")
     batch = lens.numel()
-    if (block_table.dtype is not torch.int32 or block_table.device != dev or block_table.dim() != 2
-            or block_table.shape[0] != batch or (block_table.shape[1] > 1 and block_table.stride(1) != 1)):
-        _bad("block_table must be an int32 [batch, width] tensor with contiguous rows")
-    e4m3 = dt is torch.float8_e4m3fn
+    if block_table.dtype is not torch.int32 or block_table.get_device() != dev or block_table.dim() != 2:
+        _bad(f"block_table must be an int32 [batch, width] tensor on cuda:{dev}")
+    rows, width = block_table.shape
+    row, one = block_table.stride()
+    if rows != batch or (width > 1 and one != 1):
+        _bad("block_table must be [batch, width] with contiguous rows")
     return dash_paged_cache_t(
-        batch, heads_q, heads_kv, d, pages, page, block_table.shape[1], DASH_CACHE_E4M3 if e4m3 else DASH_CACHE_BF16,
-        k_cache.data_ptr(), v_cache.data_ptr(), kp, kh, kr, vp, vh, vr, block_table.data_ptr(),
-        block_table.stride(0) if batch > 1 else block_table.shape[1], _flat("lens", lens, torch.int32, dev, batch),
-        _flat("k_scale", k_scale, torch.float32, dev, heads_kv), _flat("v_scale", v_scale, torch.float32, dev, heads_kv))
+        batch, heads_q, heads_kv, d, pages, page, width, DASH_CACHE_BF16 if dt is torch.bfloat16 else DASH_CACHE_E4M3,
+        k_cache.data_ptr(), v_cache.data_ptr(), kp, kh, kr, vp, vh, vr, block_table.data_ptr(), row if batch > 1 else width,
+        _flat("lens", lens, torch.int32, dev, batch), _flat("k_scale", k_scale, torch.float32, dev, heads_kv),
+        _flat("v_scale", v_scale, torch.float32, dev, heads_kv))
 
 
 def dash_kv_append(k, v, k_cache, v_cache, block_table, lens, cu=None, q=None, q_out=None, k_out=None, inv_freq=None,
@@ -380,25 +384,23 @@ def dash_kv_append(k, v, k_cache, v_cache, block_table, lens, cu=None, q=None, q
         _bad("q and q_out come together")
     if q is not None and q.dim() != 3:
         _bad("q must be [tokens, heads_q, d]")
+    dev = _gpu(k_cache)
     tokens, heads_kv, d = k.shape
     heads_q = heads_kv if q is None else q.shape[1]
-    c = _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q)
-    dev = k_cache.device
-    bf = torch.bfloat16
-    if c.heads_kv != heads_kv or c.d != d:
+    c = _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q, dev)
+    bf, i32 = torch.bfloat16, torch.int32
+    if k_cache.shape[1] != heads_kv or k_cache.shape[3] != d:
         _bad("k and k_cache must have the same heads and head dim")
     none = (None, 0, 0)
-    kp, vp = _rows("k", k, bf, dev, tokens, heads_kv, d), _rows("v", v, bf, dev, tokens, heads_kv, d)
-    qp = none if q is None else _rows("q", q, bf, dev, tokens, heads_q, d)
-    qo = none if q is None else _rows("q_out", q_out, bf, dev, tokens, heads_q, d)
-    ko = none if k_out is None else _rows("k_out", k_out, bf, dev, tokens, heads_kv, d)
+    kp, *ks = _rows("k", k, bf, dev, tokens, heads_kv, d)
+    vp, *vs = _rows("v", v, bf, dev, tokens, heads_kv, d)
+    qp, *qs = none if q is None else _rows("q", q, bf, dev, tokens, heads_q, d)
+    qo, *qos = none if q is None else _rows("q_out", q_out, bf, dev, tokens, heads_q, d)
+    ko, *kos = none if k_out is None else _rows("k_out", k_out, bf, dev, tokens, heads_kv, d)
     rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-    x = dash_append_t(tokens, _flat("cu", cu, torch.int32, dev, c.batch + 1), kp[0], vp[0], qp[0], qo[0], ko[0], *kp[1:],
-                      *vp[1:], *qp[1:], *qo[1:], *ko[1:], _flat("inv_freq", inv_freq, torch.float32, dev, rot // 2), rot,
-                      int(interleaved))
-    with _On(dev):
-        _check(load().dash_kv_append(ctypes.byref(c), ctypes.byref(x), _flat("status", status, torch.int32, dev, 1),
-                                     _stream_of(stream, dev)))
+    x = dash_append_t(tokens, _flat("cu", cu, i32, dev, lens.numel() + 1), kp, vp, qp, qo, ko, *ks, *vs, *qs, *qos, *kos,
+                      _flat("inv_freq", inv_freq, torch.float32, dev, rot // 2), rot, interleaved)
+    _call(load().dash_kv_append, dev, stream, ctypes.byref(c), ctypes.byref(x), _flat("status", status, i32, dev, 1))
 
 
 def dash_decode_workspace_size(batch: int, heads_q: int, heads_kv: int, d: int, page_size: int, table_width: int) -> int:
@@ -415,48 +417,47 @@ def dash_attn_decode(q, k_cache, v_cache, block_table, lens, o, lse=None, scale=
     import torch
     if q.dim() != 3:
         _bad("q must be [batch, heads_q, d]")
+    dev = _gpu(k_cache)
     batch, heads_q, d = q.shape
-    c = _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q)
-    dev = k_cache.device
-    if c.batch != batch or c.d != d:
+    c = _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q, dev)
+    pages, heads_kv, page, cd = k_cache.shape
+    if lens.numel() != batch or cd != d:
         _bad("q, lens and the caches must have the same batch and head dim")
-    qp, op = _rows("q", q, torch.bfloat16, dev, batch, heads_q, d), _rows("o", o, torch.bfloat16, dev, batch, heads_q, d)
     lib = load()
-    if workspace is None:
-        if stream is not None:
-            _bad("a call on an explicit stream needs an explicit workspace")
-        n = lib.dash_decode_workspace_size(batch, heads_q, c.heads_kv, d, c.page_size, c.table_width)
-        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=dev)
-    ws = _flat("workspace", workspace, torch.uint8, dev, workspace.numel())
-    with _On(dev):
-        _check(lib.dash_attn_decode(ctypes.byref(c), qp[0], qp[1], qp[2], op[0], op[1], op[2],
-                                    _flat("lse", lse, torch.float32, dev, batch * heads_q),
-                                    0.0 if scale is None else float(scale), ws, workspace.numel(),
-                                    _flat("status", status, torch.int32, dev, 1), _stream_of(stream, dev)))
+    need = 0 if workspace is not None else lib.dash_decode_workspace_size(batch, heads_q, heads_kv, d, page, block_table.shape[1])
+    ws, size, workspace = _space(workspace, need, dev, stream)
+    _call(lib.dash_attn_decode, dev, stream, ctypes.byref(c), *_rows("q", q, torch.bfloat16, dev, batch, heads_q, d),
+          *_rows("o", o, torch.bfloat16, dev, batch, heads_q, d), _flat("lse", lse, torch.float32, dev, batch * heads_q),
+          0.0 if scale is None else scale, ws, size, _flat("status", status, torch.int32, dev, 1))
 
 
 def attn_decode(q, k_cache, v_cache, block_table, lens, scale=None, k_scale=None, v_scale=None, workspace=None,
                 status=None):
     import torch
-    o = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    o = torch.empty_like(q, memory_format=torch.contiguous_format)
     dash_attn_decode(q, k_cache, v_cache, block_table, lens, o, None, scale, k_scale, v_scale, workspace, status)
     return o
 
 
-def _packed(q, k, cu_q, cu_k, causal, scale):
-    """dash_packed_t of a packed call, the strides still to be set."""
+def _packed(q, k, v, o, cu_q, cu_k, causal, scale, dev, *rest):
+    """dash_packed_t of a packed call; `rest`: strides of the backward's tensors.  Returns
+    it with the pointers of q, k, v, o."""
     import torch
     if q.dim() != 3 or k.dim() != 3:
         _bad("q and k must be [tokens, heads, d]")
     (tq, hq, d), (tk, hkv, _) = q.shape, k.shape
-    dev = _device(q)
     if cu_q.dim() != 1 or cu_q.numel() < 1:
         _bad("cu_q must be int32 [batch + 1]")
-    batch = cu_q.numel() - 1
+    n = cu_q.numel()
     if cu_k is None and tk != tq:
         _bad("without cu_k, k must have as many rows as q")
-    return dash_packed_t(batch, hq, hkv, d, int(causal), tq, tk, 0.0 if scale is None else float(scale),
-                         _flat("cu_q", cu_q, torch.int32, dev, batch + 1), _flat("cu_k", cu_k, torch.int32, dev, batch + 1)), dev
+    bf, i32 = torch.bfloat16, torch.int32
+    qp, q0, q1 = _rows("q", q, bf, dev, tq, hq, d)
+    kp, k0, k1 = _rows("k", k, bf, dev, tk, hkv, d)
+    vp, v0, v1 = _rows("v", v, bf, dev, tk, hkv, d)
+    op, o0, o1 = _rows("o", o, bf, dev, tq, hq, d)
+    return dash_packed_t(n - 1, hq, hkv, d, causal, tq, tk, 0.0 if scale is None else scale, _flat("cu_q", cu_q, i32, dev, n),
+                         _flat("cu_k", cu_k, i32, dev, n), q0, q1, k0, k1, v0, v1, o0, o1, *rest), qp, kp, vp, op
 
 
 def dash_packed_fwd_workspace_size(batch: int, total_q: int, total_k: int, heads_q: int, heads_kv: int, d: int) -> int:
@@ -471,26 +472,23 @@ def dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k=None, causal: bool = True, 
     ``workspace``: None, or a uint8 device tensor of dash_packed_fwd_workspace_size bytes with
     which a call of few rows is split over its keys."""
     import torch
-    p, dev = _packed(q, k, cu_q, cu_k, causal, scale)
-    bf = torch.bfloat16
-    a, p.q_row_stride, p.q_head_stride = _rows("q", q, bf, dev, p.total_q, p.heads_q, p.d)
-    b, p.k_row_stride, p.k_head_stride = _rows("k", k, bf, dev, p.total_k, p.heads_kv, p.d)
-    c, p.v_row_stride, p.v_head_stride = _rows("v", v, bf, dev, p.total_k, p.heads_kv, p.d)
-    e, p.o_row_stride, p.o_head_stride = _rows("o", o, bf, dev, p.total_q, p.heads_q, p.d)
-    ws, n = (None, 0) if workspace is None else (_flat("workspace", workspace, torch.uint8, dev, workspace.numel()), workspace.numel())
-    with _On(dev):
-        _check(load().dash_attn_packed_fwd(ctypes.byref(p), a, b, c, e, _flat("lse", lse, torch.float32, dev, p.heads_q * p.total_q),
-                                           ws, n, _stream_of(stream, dev)))
+    dev = _gpu(q)
+    p, qp, kp, vp, op = _packed(q, k, v, o, cu_q, cu_k, causal, scale, dev)
+    ws, size = (None, 0) if workspace is None else _space(workspace, 0, dev, stream)[:2]
+    _call(load().dash_attn_packed_fwd, dev, stream, ctypes.byref(p), qp, kp, vp, op,
+          _flat("lse", lse, torch.float32, dev, q.shape[0] * q.shape[1]), ws, size)
 
 
 def attn_packed_fwd(q, k, v, cu_q, cu_k=None, causal: bool = True, scale=None):
     import torch
-    o = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-    lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
-    n = 0 if q.dim() != 3 or k.dim() != 3 else dash_packed_fwd_workspace_size(cu_q.numel() - 1, q.shape[0], k.shape[0],
-                                                                               q.shape[1], k.shape[1], q.shape[2])
-    ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-    dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k, causal, scale, ws)
+    dev = _gpu(q)
+    if q.dim() != 3 or k.dim() != 3:
+        _bad("q and k must be [tokens, heads, d]")
+    (tq, hq, d), (tk, hkv, _) = q.shape, k.shape
+    o = torch.empty_like(q, memory_format=torch.contiguous_format)
+    lse = q.new_empty((hq, tq), dtype=torch.float32)
+    n = load().dash_packed_fwd_workspace_size(cu_q.numel() - 1, tq, tk, hq, hkv, d)
+    dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k, causal, scale, _space(None, n, dev, None)[2] if n else None)
     return o, lse
 
 
@@ -505,33 +503,26 @@ def dash_attn_packed_bwd(q, k, v, o, dO, lse, dq, dk, dv, cu_q, cu_k=None, causa
     (without it one is allocated).  ``status``: optional int32 that receives 0, or 1
     after a wait timeout (offsets that do not rise)."""
     import torch
-    p, dev = _packed(q, k, cu_q, cu_k, causal, scale)
+    dev = _gpu(q)
+    if q.dim() != 3 or k.dim() != 3:
+        _bad("q and k must be [tokens, heads, d]")
+    (tq, hq, d), (tk, hkv, _) = q.shape, k.shape
     bf = torch.bfloat16
-    a, p.q_row_stride, p.q_head_stride = _rows("q", q, bf, dev, p.total_q, p.heads_q, p.d)
-    b, p.k_row_stride, p.k_head_stride = _rows("k", k, bf, dev, p.total_k, p.heads_kv, p.d)
-    c, p.v_row_stride, p.v_head_stride = _rows("v", v, bf, dev, p.total_k, p.heads_kv, p.d)
-    e, p.o_row_stride, p.o_head_stride = _rows("o", o, bf, dev, p.total_q, p.heads_q, p.d)
-    f, p.do_row_stride, p.do_head_stride = _rows("dO", dO, bf, dev, p.total_q, p.heads_q, p.d)
-    x, p.dq_row_stride, p.dq_head_stride = _rows("dq", dq, bf, dev, p.total_q, p.heads_q, p.d)
-    y, p.dk_row_stride, p.dk_head_stride = _rows("dk", dk, bf, dev, p.total_k, p.heads_kv, p.d)
-    z, p.dv_row_stride, p.dv_head_stride = _rows("dv", dv, bf, dev, p.total_k, p.heads_kv, p.d)
+    do, *dos = _rows("dO", dO, bf, dev, tq, hq, d)
+    a, *dqs = _rows("dq", dq, bf, dev, tq, hq, d)
+    b, *dks = _rows("dk", dk, bf, dev, tk, hkv, d)
+    c, *dvs = _rows("dv", dv, bf, dev, tk, hkv, d)
+    p, qp, kp, vp, op = _packed(q, k, v, o, cu_q, cu_k, causal, scale, dev, *dos, *dqs, *dks, *dvs)
     lib = load()
-    if workspace is None:
-        if stream is not None:
-            _bad("a call on an explicit stream needs an explicit workspace")
-        n = lib.dash_packed_workspace_size(p.batch, p.total_q, p.total_k, p.heads_q, p.heads_kv, p.d)
-        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=dev)
-    ws = _flat("workspace", workspace, torch.uint8, dev, workspace.numel())
-    with _On(dev):
-        _check(lib.dash_attn_packed_bwd(ctypes.byref(p), a, b, c, e, f,
-                                        _flat("lse", lse, torch.float32, dev, p.heads_q * p.total_q), x, y, z, ws,
-                                        workspace.numel(), _flat("status", status, torch.int32, dev, 1),
-                                        _stream_of(stream, dev)))
+    need = 0 if workspace is not None else lib.dash_packed_workspace_size(cu_q.numel() - 1, tq, tk, hq, hkv, d)
+    ws, size, workspace = _space(workspace, need, dev, stream)
+    _call(lib.dash_attn_packed_bwd, dev, stream, ctypes.byref(p), qp, kp, vp, op, do,
+          _flat("lse", lse, torch.float32, dev, hq * tq), a, b, c, ws, size, _flat("status", status, torch.int32, dev, 1))
 
 
 def attn_packed_bwd(q, k, v, o, dO, lse, cu_q, cu_k=None, causal: bool = True, scale=None, workspace=None):
     import torch
-    dq, dk, dv = (torch.empty(t.shape, dtype=torch.bfloat16, device=t.device) for t in (q, k, v))
+    dq, dk, dv = (torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, v))
     dash_attn_packed_bwd(q, k, v, o, dO, lse, dq, dk, dv, cu_q, cu_k, causal, scale, workspace)
     return dq, dk, dv
 
