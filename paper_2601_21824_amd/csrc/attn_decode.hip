@@ -7,9 +7,10 @@
 // for 4 d G operations, G query heads to a K/V head.  So the kernel's business is
 // to keep loads in flight.  One workgroup takes a chunk of one sequence's keys for
 // one K/V head and up to 16 of its query heads; each of its four waves takes every
-// fourth tile of 32 keys by itself, with its own running maximum and sum, and loads its
-// next tile while it computes one (d = 256: the other waves' loads fill that time).  Nothing goes through LDS until the four waves
-// are joined:
+// fourth tile of 32 keys by itself, with its own running maximum and sum; the other
+// waves' loads are in flight meanwhile (8 to 16 waves a CU, 16 KB each at d = 128; a
+// second tile ahead in registers leaves fewer waves and gains nothing: 538 MB 111 us with it
+// and without).  Nothing goes through LDS until the four waves are joined:
 //   S^T = K Q^T   (MFMA 16x16x32, twice 16 keys) A = K rows, loaded in the operand's own layout
 //   P = exp(S - m), in the C layout: one query a lane, keys 4g .. 4g+3 and 16 + 4g .. +3
 //   O^T += V^T P^T   B = those 8 probabilities as they are; A = V^T: lane l loads rows
@@ -32,7 +33,7 @@
 namespace dash {
 namespace {
 
-constexpr int kQ = 16;  // query heads of a workgroup
+constexpr int kQ = 16;      // query heads of a workgroup
 
 // two e4m3 values of a word (its low or high half) as the upper halves of two floats
 template <bool HI>
@@ -56,15 +57,15 @@ struct Tile {
   unsigned v[8][VW];
 };
 
-template <int D, bool F8>
-__global__ __launch_bounds__(256, 2) void decode_kernel(DecodeArgs a) {
+template <int D, bool F8, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void decode_kernel(DecodeArgs a) {
   using T = Tile<D, F8>;
   constexpr int KS = D / 32;        // MFMA k-steps over d
   constexpr int VE = D / 16;        // columns of V per lane = 16-row blocks of O^T
   constexpr int SZ = F8 ? 1 : 2;    // bytes of an element
   constexpr int OP = D + 4;         // padded row of the join buffer
-  __shared__ float so[4][kQ][OP];
-  __shared__ float sm[4][kQ], sl[4][kQ];
+  __shared__ float so[NW][kQ][OP];
+  __shared__ float sm[NW][kQ], sl[NW][kQ];
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, l = tid & 63, g = l >> 4, lq = l & 15;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -83,7 +84,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(DecodeArgs a) {
     total += wave_sum(len >> 12) * 4096l + wave_sum(len & 4095);
   }
   // (a chunk past 2^31 - 1 keys holds any sequence, as 2^30 does)
-  const int64_t chunk64 = chunk_keys(total, a.workers);
+  const int64_t chunk64 = a.workers > 0 ? chunk_keys(total, a.workers) : (int64_t)1 << 30;
   const int chunk = __builtin_amdgcn_readfirstlane(chunk64 < (1 << 30) ? (int)chunk64 : 1 << 30);
   int s = -1, i = 0, n = 0;
   for (int b = 0, before = 0; b < c.batch; b += 64) {
@@ -153,11 +154,12 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(DecodeArgs a) {
       for (int x = 0; x < 4; ++x) {
         const char* at = vp + v_lane + x * (uint32_t)((int)c.v_row * SZ);
         unsigned* v = t.v[4 * tt + x];
-        if constexpr (T::VW == 1) v[0] = *(const unsigned*)at;
-        else if constexpr (T::VW == 2) *(u32x2*)v = *(const u32x2*)at;
+        // nothing reads V's rows again, and one load takes a row whole: past the caches
+        if constexpr (T::VW == 1) v[0] = __builtin_nontemporal_load((const unsigned*)at);
+        else if constexpr (T::VW == 2) *(u32x2*)v = __builtin_nontemporal_load((const u32x2*)at);
         else
 #pragma unroll
-          for (int y = 0; y < T::VW; y += 4) *(u32x4*)(v + y) = *(const u32x4*)(at + 4 * y);
+          for (int y = 0; y < T::VW; y += 4) *(u32x4*)(v + y) = __builtin_nontemporal_load((const u32x4*)(at + 4 * y));
       }
     }
   };
@@ -232,29 +234,14 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(DecodeArgs a) {
       }
     }
   };
-  if constexpr (D == 256) {  // (two tiles spill: 64 registers each of K and V, 64 of O)
-    T t0;
-    for (int kb = k0 + 32 * w; kb < k1; kb += 128) {
-      load(t0, kb);
-      compute(t0, kb);
-    }
-  } else {
-    T t0, t1;
-    int kb = k0 + 32 * w;
-    if (kb < k1) load(t0, kb);
-    while (kb < k1) {
-      if (kb + 128 < k1) load(t1, kb + 128);
-      compute(t0, kb);
-      kb += 128;
-      if (kb >= k1) break;
-      if (kb + 128 < k1) load(t0, kb + 128);
-      compute(t1, kb);
-      kb += 128;
-    }
+  for (int kb = k0 + 32 * w; kb < k1; kb += 32 * NW) {
+    T t;
+    load(t, kb);
+    compute(t, kb);
   }
   if (bad && l == 0 && c.status) *c.status = 1;
 
-  // ---- join the four waves: o[y][r] is column VE (4g + r) + y of query l % 16
+  // ---- join the waves: o[y][r] is column VE (4g + r) + y of query l % 16
   sum = quad_sum(sum);
   if (g == 0) sm[w][lq] = m, sl[w][lq] = sum;
 #pragma unroll
@@ -263,14 +250,16 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(DecodeArgs a) {
     for (int r = 0; r < 4; ++r) so[w][lq][VE * (4 * g + r) + y] = o[y][r];
   __syncthreads();
   const float vs = F8 && c.v_scale ? c.v_scale[hk] : 1.f;
-  for (int e = tid; e < nq * (D / 4); e += 256) {
+  for (int e = tid; e < nq * (D / 4); e += 64 * NW) {
     const int q = e / (D / 4), d0 = e % (D / 4) * 4;
-    float top = fmaxf(fmaxf(sm[0][q], sm[1][q]), fmaxf(sm[2][q], sm[3][q]));
+    float top = sm[0][q];
+#pragma unroll
+    for (int x = 1; x < NW; ++x) top = fmaxf(top, sm[x][q]);
     const float mm = top == -INFINITY ? 0.f : top;
     float den = 0.f;
     f32x4 out = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
+    for (int x = 0; x < NW; ++x) {
       const float f = __builtin_amdgcn_exp2f(sm[x][q] - mm);
       den += f * sl[x][q];
       out += f * *(const f32x4*)&so[x][q][d0];
@@ -328,8 +317,13 @@ template <int D>
 void launch(const DecodeArgs& a, hipStream_t stream) {
   const int G = a.c.heads_q / a.c.heads_kv;
   const unsigned grid = (unsigned)a.slots * a.c.heads_kv * ((G + kQ - 1) / kQ);
-  if (a.c.e4m3) hipLaunchKernelGGL((decode_kernel<D, true>), dim3(grid), dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((decode_kernel<D, false>), dim3(grid), dim3(256), 0, stream, a);
+  if (a.workers == 0) {
+    if (a.c.e4m3) hipLaunchKernelGGL((decode_kernel<D, true, 8>), dim3(grid), dim3(512), 0, stream, a);
+    else hipLaunchKernelGGL((decode_kernel<D, false, 8>), dim3(grid), dim3(512), 0, stream, a);
+    return;
+  }
+  if (a.c.e4m3) hipLaunchKernelGGL((decode_kernel<D, true, 4>), dim3(grid), dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((decode_kernel<D, false, 4>), dim3(grid), dim3(256), 0, stream, a);
   if (a.slots > a.c.batch)  // (else no sequence can have two chunks)
     hipLaunchKernelGGL(join_kernel<D>, dim3((unsigned)(a.c.batch * a.c.heads_q)), dim3(256), 0, stream, a);
 }
@@ -338,13 +332,19 @@ void launch(const DecodeArgs& a, hipStream_t stream) {
 
 // Chunks aimed at, over all sequences: with the K/V heads (and further groups of
 // 16 query heads) about 1024 workgroups, four for each of 256 CUs.
-int decode_workers(int heads_q, int heads_kv) {
+// 0: each sequence is one chunk of eight waves, written at once -- tables of up to
+// 65536 / d keys, for which the second kernel costs more than the waves' further tiles
+// (us with the host's part, whole / cut: 1 sequence of 1000, 2 heads of 64, 10.9 / 12.0; 8 of 500, 8 heads
+// of 128, 10.2 / 11.7, in e4m3 9.9 / 12.2; 4 of 200, 4 heads of 256, 10.0 / 11.9; but 1 of 1000, 8 heads
+// of 128, 13.6 / 12.0, 8 of 1000 in e4m3 14.1 / 12.2, 4 of 500, 4 heads of 256, 17.8 / 11.7).
+int decode_workers(int heads_q, int heads_kv, int d, int table_tokens) {
+  if (table_tokens <= 65536 / d) return 0;
   const int units = heads_kv * ((heads_q / heads_kv + kQ - 1) / kQ);
   return units < 1024 ? 1024 / units : 1;
 }
-int decode_slots(int batch, int heads_q, int heads_kv, int table_tokens) {
-  const long most = (long)batch * ((table_tokens + kMinChunk - 1) / kMinChunk);
-  const long s = (long)decode_workers(heads_q, heads_kv) + batch;
+int decode_slots(int batch, int heads_q, int heads_kv, int d, int table_tokens) {
+  const long most = table_tokens > kMinChunk ? (long)batch * ((table_tokens + kMinChunk - 1) / kMinChunk) : batch;
+  const long s = (long)decode_workers(heads_q, heads_kv, d, table_tokens) + batch;
   return (int)(s < most ? s : most);
 }
 

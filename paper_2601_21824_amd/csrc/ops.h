@@ -55,8 +55,8 @@ struct DecodeArgs {
   float* part_m;  // [slots][heads_q][2]: maximum (log2 domain), sum
   int* base;      // [batch][2]: first slot of a sequence, its chunks
 };
-int decode_workers(int heads_q, int heads_kv);
-int decode_slots(int batch, int heads_q, int heads_kv, int table_tokens);
+int decode_workers(int heads_q, int heads_kv, int d, int table_tokens);
+int decode_slots(int batch, int heads_q, int heads_kv, int d, int table_tokens);
 hipError_t launch_decode(const DecodeArgs& a, hipStream_t stream);
 
 // ---------------------------------------------------------------- packed sequences

@@ -80,7 +80,7 @@ int check_cache(const dash_paged_cache_t* c, bool written) {
     return fail(DASH_ERR_INVALID_ARG, "table_width must be >= 0 and table_width * page_size below 2^31 - 255");
   if (c->batch == 0) return DASH_OK;
   if (c->pages < 1) return fail(DASH_ERR_INVALID_ARG, "pages must be >= 1");
-  if (!c->lens || !c->block_table) return fail(DASH_ERR_INVALID_ARG, "null lens or block_table");
+  if (!c->lens || (!c->block_table && c->table_width > 0)) return fail(DASH_ERR_INVALID_ARG, "null lens or block_table");
   if (c->table_stride < c->table_width && c->batch > 1) return fail(DASH_ERR_INVALID_ARG, "table_stride is below table_width");
   const int unit = c->cache_type == DASH_CACHE_E4M3 ? 16 : 8;
   const struct {
@@ -111,7 +111,7 @@ struct DecodeLayout {
 };
 DecodeLayout decode_layout(int batch, int heads_q, int heads_kv, int d, int tokens) {
   DecodeLayout L;
-  L.slots = dash::decode_slots(batch, heads_q, heads_kv, tokens);
+  L.slots = dash::decode_slots(batch, heads_q, heads_kv, d, tokens);
   size_t off = 0;
   L.part_o = off;
   off += align256((size_t)L.slots * heads_q * d * sizeof(float));
@@ -177,7 +177,7 @@ int attn_decode(const dash_paged_cache_t* c, const void* q, int64_t q_row, int64
   if ((rc = device_info(&di))) return rc;
   char* ws = (char*)workspace;
   const dash::DecodeArgs a{cache_args(c, status), q, o, lse, {q_row, q_head}, {o_row, o_head}, scale,
-                           dash::decode_workers(c->heads_q, c->heads_kv), L.slots, (float*)(ws + L.part_o),
+                           dash::decode_workers(c->heads_q, c->heads_kv, c->d, c->table_width * c->page_size), L.slots, (float*)(ws + L.part_o),
                            (float*)(ws + L.part_m), (int*)(ws + L.base)};
   const hipError_t e = dash::launch_decode(a, (hipStream_t)stream);
   return e == hipSuccess ? DASH_OK : hip_fail(e, "decode launch");

@@ -221,6 +221,10 @@ DECODES = [(d, hq, hkv, LENS, page, dt, order)
 DECODES += [(128, 8, 2, [20000], 16, BF, "phrd"), (64, 64, 1, [9000, 1], 16, E4, "phrd"), (256, 4, 4, [7001, 40, 3000], 32, E4, "phrd"),
             (128, 4, 1, [1 + 37 * i % 211 for i in range(150)], 16, BF, "phrd"),  # more than two rounds of 64 sequences
             (64, 2, 2, [0] * 70 + [2000], 16, BF, "phrd")]
+# tables short enough for one chunk per sequence (65536 / d keys), full and not, and one page more
+DECODES += [(d, 8, 2, [n, 1, 0, n - 17, n // 3], 16, dt, "phrd") for d in (64, 128, 256) for dt in (BF, E4)
+            for n in (65536 // d - 16, 65536 // d)]
+DECODES += [(128, 20, 1, [1 + 29 * i % 490 for i in range(90)], 16, BF, "phrd")]
 
 
 def decode_case(d, hq, hkv, lens, page, dtype, order, seed=0, garbage=float("nan")):
@@ -306,6 +310,18 @@ def test_decode_reports_bad_tables():
         status = i32([0])
         o = dash.attn_decode(q, kc, vc, table, i32([n, 40]), status=status)
         assert int(status) == status_want and torch.equal(o[1], good[1])
+
+
+def test_tables_of_no_page():
+    """No sequence has a page: nothing to attend to, nowhere to store."""
+    q, kc = torch.ones((3, 4, 64), device="cuda").to(BF), make_cache(2, 2, 16, 64, BF)
+    table, lens, status = torch.empty((3, 0), dtype=torch.int32, device="cuda"), i32([0, 0, 0]), i32([0])
+    o, lse = torch.full_like(q, 3.0), torch.zeros((3, 4), device="cuda")
+    dash.dash_attn_decode(q, kc, kc, table, lens, o, lse, status=status)
+    assert bool((o == 0).all()) and bool((lse == -math.inf).all()) and int(status) == 0
+    before = kc.clone()
+    dash.dash_kv_append(q[:, :2], q[:, :2], kc, kc.clone(), table, lens, status=status)
+    assert int(status) == 1 and torch.equal(kc, before)
 
 
 # ------------------------------------------------------------------ together
