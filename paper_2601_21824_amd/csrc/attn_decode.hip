@@ -90,12 +90,7 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(DecodeArgs a) {
   for (int b = 0, before = 0; b < c.batch; b += 64) {
     if (c.batch > 64) len = b + l < c.batch ? clamp_len(c.lens[b + l], c.table_width, c.page_size) : 0;
     const int mine = b + l < c.batch ? chunks_of(len, chunk) : 0;
-    int upto = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(upto, o);
-      if (l >= o) upto += x;
-    }
+    const int upto = wave_scan(mine);
     const unsigned long long here = __ballot(before + upto > slot);
     if (here) {
       const int at = __builtin_ctzll(here);

@@ -36,20 +36,20 @@ __device__ inline Run run_of(int kv_end, int splits, int i) {
   return {a * KT, (b * KT < kv_end ? b * KT : kv_end) - a * KT, n};
 }
 
-// The rows of a slot: its sequence s, first row q0 and their number (<= 0: none), the keys that
-// the rows see at most.
+// The rows of a slot: first row q0 and their number (<= 0: none), the keys that they
+// see at most.
 struct Rows {
-  int s, q0, n, kv_end;
+  int q0, n, kv_end;
   Span q, k;
 };
 template <int QROWS>
 __device__ inline Rows rows_of(const PackedArgs& a, int slot, int l) {
   Rows r;
-  r.s = __builtin_amdgcn_readfirstlane(
+  const int s = __builtin_amdgcn_readfirstlane(
       find_last(a.batch, slot, l, [&](int x) { return first_slot(a.cu_q, x, a.total_q, QROWS); }));
-  r.q = span_of(a.cu_q, r.s, a.total_q);
-  r.k = span_of(a.cu_k, r.s, a.total_k);
-  r.q0 = (slot - first_slot(a.cu_q, r.s, a.total_q, QROWS)) * QROWS;
+  r.q = span_of(a.cu_q, s, a.total_q);
+  r.k = span_of(a.cu_k, s, a.total_k);
+  r.q0 = (slot - first_slot(a.cu_q, s, a.total_q, QROWS)) * QROWS;
   r.n = r.q0 < 0 ? 0 : r.q.len - r.q0 < QROWS ? r.q.len - r.q0 : QROWS;
   r.kv_end = r.k.len;
   if (a.causal) {
@@ -113,7 +113,9 @@ __global__ __launch_bounds__(256, WPS) void packed_fwd_kernel(PackedArgs a) {
   const int split = in / (slots * G);
   int slot = in / G % slots;
   // causal: a sequence's longest blocks (last rows) first; where a run ends inside a
-  // head, from both ends in turn, so that every run holds like work
+  // head, from both ends in turn, so that every run holds like work.  (Longest first over
+  // all sequences, found by a search, costs more than the tail that it saves: 16 sequences of
+  // 512 67 -> 73 us, 12 of 8192 in all 111 -> 112.)
   if (a.causal) slot = (a.heads_kv & 7) == 0 ? slots - 1 - slot : (slot & 1) ? slot >> 1 : slots - 1 - (slot >> 1);
   const Rows r = rows_of<QROWS>(a, slot, tid & 63);
   if (r.n <= 0) return;

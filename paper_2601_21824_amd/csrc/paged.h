@@ -46,12 +46,19 @@ __device__ inline Span span_of(const int32_t* cu, int s, int total) {
 // those between two sequences' blocks are empty.
 __device__ inline int first_slot(const int32_t* cu, int s, int total, int rows) { return clamp_row(cu[s], total) / rows + s; }
 
-// sum over the 64 lanes, all lanes receive it
-__device__ inline int wave_sum(int x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+// x plus the lanes before it: four shifts inside rows of 16 lanes, then the last lane
+// of a row, and of the lower half, to those behind it.  All lanes active.
+__device__ inline int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);   // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);   // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);   // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
   return x;
 }
+// sum over the 64 lanes, wave-uniform
+__device__ inline int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
 
 // Over the four lanes l % 16 + 16 i.  The swaps exchange the upper half (every odd
 // row of 16) of one register with the lower half (even row) of another, here two
