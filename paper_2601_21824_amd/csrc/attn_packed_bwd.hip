@@ -4,11 +4,12 @@
 // 128, 128 at d = 256) on the chains of packed_chain.h, with the ordered dQ reduction
 // of the dense calls in Descending order.
 //
-// packed_pre: per 64-row query block and head, D = rowsum(dO o O) and L log2(e) (+inf for
-// a row that sees nothing, so that its P is 0); the block's ordering counter; dQ = 0
-// where no KV tile sees the block.  Further waves put the KV tiles' chains in the order
-// in which they start (packed_order.h): longest first over all sequences, each
-// sequence's own in ascending order.  Memory-bound, as bwd_pre: O and dO once.
+// packed_pre: D = rowsum(dO o O) and L log2(e) (+inf for a row that sees nothing, so that
+// its P is 0) for every row and head, of no sequence too; the ordering counters; dQ = 0
+// where no KV tile sees a 64-row block; and the KV tiles' chains in the order in which
+// they start (packed_order.h): longest first over all sequences, each sequence's own in
+// ascending order.  Workgroups of three kinds, by blockIdx, the rows' last.  Memory-bound, as bwd_pre: O
+// and dO once.
 #include "common.h"
 #include "ops.h"
 #include "packed_order.h"
@@ -19,148 +20,159 @@ namespace {
 
 constexpr int BM = kBlockRows;
 
-template <int D>
+// H query heads of 64 rows a workgroup, their bytes side by side in a packed layout.
+template <int D, int H>
 __global__ __launch_bounds__(256) void packed_pre_kernel(PackedBwdArgs a) {
-  constexpr int TPR = D / 8;        // threads per row, 8 elements each
-  constexpr int RPP = 256 / TPR;    // rows per pass
-  constexpr int U = BM / RPP;       // passes
+  constexpr int TPR = D / 8;           // threads per row and head, 8 elements each
+  constexpr int RPP = 256 / TPR / H;   // rows per pass
+  constexpr int U = BM / RPP < 4 ? BM / RPP : 4;  // passes whose loads are in flight together
+  static_assert(RPP >= 1 && BM % (RPP * U) == 0, "passes");
   const PackedArgs& p = a.p;
   const int tid = threadIdx.x, l = tid & 63;
   const bool causal = p.causal != 0;
-  const int blocks = a.slots_q * p.heads_q;
-  if ((int)blockIdx.x < blocks) {
-    const int slot = (int)blockIdx.x / p.heads_q, h = (int)blockIdx.x % p.heads_q;
-    if (blockIdx.x == 0 && tid == 0) {
+  const int groups = p.heads_q / H, order = (a.slots_k + 3) / 4;
+  int x = (int)blockIdx.x;
+  if (x < order) {  // ---- one wave per KV-tile slot; first, as one of them counts longest
+    const int slot = __builtin_amdgcn_readfirstlane(x * 4 + (tid >> 6));
+    if (slot >= a.slots_k) return;
+    const int s = __builtin_amdgcn_readfirstlane(
+        find_last(p.batch, slot, l, [&](int x) { return first_slot(p.cu_k, x, p.total_k, a.bc); }));
+    auto geom = [&](int x) {
+      return SeqGeom{span_of(p.cu_q, x, p.total_q).len, span_of(p.cu_k, x, p.total_k).len, causal, a.bc};
+    };
+    const SeqGeom g = geom(s);
+    const int j = slot - first_slot(p.cu_k, s, p.total_k, a.bc);
+    const int length = g.chain(j);
+    int place = 0, total = 0;
+    long steps = 0;
+    for (int b = 0; b < p.batch; b += 64) {
+      const int o = b + l;
+      if (o < p.batch) {
+        const SeqGeom og = geom(o);
+        place += order_part(og, o, s, j, length);
+        total += og.tiles();
+        steps += og.steps();
+      }
+    }
+    place = wave_sum(place);
+    if (slot == 0) {  // the wave of the first slot counts
+      total = wave_sum(total);
+      total = total < a.slots_k ? total : a.slots_k;
+      steps = ((long)wave_sum((int)(steps >> 20)) << 20) + wave_sum((int)(steps & 0xfffff));
+      // the cheapest split: lane l weighs limit l % 8 with parts l / 8
+      const int group = p.heads_q / p.heads_kv;
+      int n_long = 0, heads = group;
+      if (group > 1) {
+        const long share = steps * p.heads_q / kSplitWorkers;
+        int longest = 0, mine = 0;
+#pragma unroll
+        for (int i = 0; i < kSplitLimits; ++i) {
+          const long above = split_above(share, group, i);
+          const int from = above < (1 << 30) ? (int)above + 1 : 1 << 30;
+          int n = 0;
+          for (int b = 0; b < p.batch; b += 64)
+            if (b + l < p.batch) n += geom(b + l).tiles_from(from);
+          n = wave_sum(n);
+          mine = (l & 7) == i ? n : mine;
+        }
+        for (int b = 0; b < p.batch; b += 64)
+          if (b + l < p.batch) {
+            const SeqGeom og = geom(b + l);
+            const int x = og.tiles() > 0 ? og.chain(0) : 0;
+            longest = x > longest ? x : longest;
+          }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+          const int x = __shfl_xor(longest, o);
+          longest = x > longest ? x : longest;
+        }
+        const int per = split_heads(group, l >> 3);
+        long cost = split_cost(share, longest, split_above(share, group, l & 7), mine, per, group, p.heads_kv);
+        if (per < group && (long)mine * p.heads_kv * split_parts(group, per) > a.split_room) cost = 1L << 48;
+        cost = cost << 6 | l;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+          const long x = __shfl_xor(cost, o);
+          cost = x < cost ? x : cost;
+        }
+        const int best = (int)(cost & 63);
+        heads = split_heads(group, best >> 3);
+        n_long = __shfl(mine, best);
+        if (heads >= group) n_long = 0;
+        n_long = n_long < total ? n_long : total;
+      }
+      if (l == 0) {
+        a.ctrl[kCtrlItems] = total;
+        a.ctrl[kCtrlLong] = n_long;
+        a.ctrl[kCtrlHeads] = heads;
+      }
+    }
+    if (l != 0) return;
+    if (j >= 0 && j < g.tiles() && place < a.slots_k) {
+      a.order[2 * (size_t)place] = s;
+      a.order[2 * (size_t)place + 1] = j;
+    }
+    return;
+  }
+  x -= order;
+  if (x < a.slots_q) {  // ---- a slot's counters, and dQ where nothing else writes it
+    if (x == 0 && tid == 0) {
       a.ctrl[kCtrlTicket] = 0;
       a.ctrl[kCtrlError] = 0;
       if (a.status) *a.status = 0;
     }
+    for (int h = tid; h < p.heads_q; h += 256) a.counters[((size_t)x * p.heads_q + h) * kCtrStride] = a.poison ? kPoison : 0;
     const int s = __builtin_amdgcn_readfirstlane(
-        find_last(p.batch, slot, l, [&](int x) { return first_slot(p.cu_q, x, p.total_q, BM); }));
+        find_last(p.batch, x, l, [&](int i) { return first_slot(p.cu_q, i, p.total_q, BM); }));
     const Span q = span_of(p.cu_q, s, p.total_q), k = span_of(p.cu_k, s, p.total_k);
-    const int pb = slot - first_slot(p.cu_q, s, p.total_q, BM);
+    const int pb = x - first_slot(p.cu_q, s, p.total_q, BM);
     if (pb < 0 || pb * BM >= q.len) return;
+    const SeqGeom g{q.len, k.len, causal, a.bc};
+    if (g.last_tile(pb) >= 0) return;
     const int rows = q.len - pb * BM < BM ? q.len - pb * BM : BM;
-    const int64_t row0 = (int64_t)q.start + pb * BM;
-    const int c = tid % TPR, r0 = tid / TPR;
-    u32x4 x[U], y[U];
+    for (int e = tid; e < rows * p.heads_q * TPR; e += 256) {
+      const int r = e / (p.heads_q * TPR), h = e / TPR % p.heads_q;
+      *(u32x4*)((__bf16*)a.dq + ((int64_t)q.start + pb * BM + r) * a.dqs.row + h * a.dqs.head + 8 * (e % TPR)) = u32x4{0, 0, 0, 0};
+    }
+    return;
+  }
+  x -= a.slots_q;
+  // ---- D and L of 64 rows
+  const int row0 = x / groups * BM, hg = x % groups * H;
+  const int rows = p.total_q - row0 < BM ? p.total_q - row0 : BM;
+  const int c = tid % TPR, h = hg + tid / TPR % H, r0 = tid / (TPR * H);
+  const int64_t vec = (int64_t)h * p.total_q + row0;
+  const __bf16* dO = (const __bf16*)a.dO + row0 * a.dos.row + h * a.dos.head + 8 * c;
+  const __bf16* O = (const __bf16*)a.o + row0 * p.os.row + h * p.os.head + 8 * c;
+  for (int b = r0; b < rows; b += RPP * U) {
+    u32x4 u0[U], u1[U];
+    float L[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      int r = r0 + u * RPP;
+      int r = b + u * RPP;
       r = r < rows ? r : rows - 1;  // (read, not written)
-      x[u] = *(const u32x4*)((const __bf16*)a.dO + (row0 + r) * a.dos.row + h * a.dos.head + 8 * c);
-      y[u] = *(const u32x4*)((const __bf16*)a.o + (row0 + r) * p.os.row + h * p.os.head + 8 * c);
+      u0[u] = *(const u32x4*)(dO + r * a.dos.row);
+      u1[u] = __builtin_nontemporal_load((const u32x4*)(O + r * p.os.row));  // (nothing reads O again)
+      L[u] = p.lse[vec + r];
     }
-    const int64_t vec = (int64_t)h * p.total_q + row0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float acc = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float xf = bf16_to_f32((unsigned short)(x[u][e >> 1] >> (16 * (e & 1))));
-        const float yf = bf16_to_f32((unsigned short)(y[u][e >> 1] >> (16 * (e & 1))));
+        const float xf = bf16_to_f32((unsigned short)(u0[u][e >> 1] >> (16 * (e & 1))));
+        const float yf = bf16_to_f32((unsigned short)(u1[u][e >> 1] >> (16 * (e & 1))));
         acc = __builtin_fmaf(xf, yf, acc);
       }
       // butterfly over the TPR lanes of a row, as in bwd_pre
 #pragma unroll
       for (int o = 1; o < TPR; o <<= 1) acc += __shfl_xor(acc, o);
-      const int r = r0 + u * RPP;
+      const int r = b + u * RPP;
       if (c == 0 && r < rows) {
         a.dvec[vec + r] = acc;
-        const float L = p.lse[vec + r];
-        a.lse2[vec + r] = L == -INFINITY ? INFINITY : L * kLog2e;
+        a.lse2[vec + r] = L[u] == -INFINITY ? INFINITY : L[u] * kLog2e;
       }
     }
-    if (tid == 0) a.counters[((size_t)slot * p.heads_q + h) * kCtrStride] = a.poison ? kPoison : 0;
-    const SeqGeom g{q.len, k.len, causal, a.bc};
-    if (g.last_tile(pb) < 0) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int r = r0 + u * RPP;
-        if (r < rows) *(u32x4*)((__bf16*)a.dq + (row0 + r) * a.dqs.row + h * a.dqs.head + 8 * c) = u32x4{0, 0, 0, 0};
-      }
-    }
-    return;
-  }
-  // ---- one wave per KV-tile slot
-  const int slot = __builtin_amdgcn_readfirstlane(((int)blockIdx.x - blocks) * 4 + (tid >> 6));
-  if (slot >= a.slots_k) return;
-  const int s = __builtin_amdgcn_readfirstlane(
-      find_last(p.batch, slot, l, [&](int x) { return first_slot(p.cu_k, x, p.total_k, a.bc); }));
-  auto geom = [&](int x) {
-    return SeqGeom{span_of(p.cu_q, x, p.total_q).len, span_of(p.cu_k, x, p.total_k).len, causal, a.bc};
-  };
-  const SeqGeom g = geom(s);
-  const int j = slot - first_slot(p.cu_k, s, p.total_k, a.bc);
-  const int length = g.chain(j);
-  int place = 0, total = 0;
-  long steps = 0;
-  for (int b = 0; b < p.batch; b += 64) {
-    const int o = b + l;
-    if (o < p.batch) {
-      const SeqGeom og = geom(o);
-      place += order_part(og, o, s, j, length);
-      total += og.tiles();
-      steps += og.steps();
-    }
-  }
-  place = wave_sum(place);
-  if (slot == 0) {  // the wave of the first slot counts
-    total = wave_sum(total);
-    total = total < a.slots_k ? total : a.slots_k;
-    steps = ((long)wave_sum((int)(steps >> 20)) << 20) + wave_sum((int)(steps & 0xfffff));
-    // the cheapest split: lane l weighs limit l % 8 with parts l / 8
-    const int group = p.heads_q / p.heads_kv;
-    int n_long = 0, heads = group;
-    if (group > 1) {
-      const long share = steps * p.heads_q / kSplitWorkers;
-      int longest = 0, mine = 0;
-#pragma unroll
-      for (int i = 0; i < kSplitLimits; ++i) {
-        const long above = split_above(share, group, i);
-        const int from = above < (1 << 30) ? (int)above + 1 : 1 << 30;
-        int n = 0;
-        for (int b = 0; b < p.batch; b += 64)
-          if (b + l < p.batch) n += geom(b + l).tiles_from(from);
-        n = wave_sum(n);
-        mine = (l & 7) == i ? n : mine;
-      }
-      for (int b = 0; b < p.batch; b += 64)
-        if (b + l < p.batch) {
-          const SeqGeom og = geom(b + l);
-          const int x = og.tiles() > 0 ? og.chain(0) : 0;
-          longest = x > longest ? x : longest;
-        }
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) {
-        const int x = __shfl_xor(longest, o);
-        longest = x > longest ? x : longest;
-      }
-      const int per = split_heads(group, l >> 3);
-      long cost = split_cost(share, longest, split_above(share, group, l & 7), mine, per, group, p.heads_kv);
-      if (per < group && (long)mine * p.heads_kv * split_parts(group, per) > a.split_room) cost = 1L << 48;
-      cost = cost << 6 | l;
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) {
-        const long x = __shfl_xor(cost, o);
-        cost = x < cost ? x : cost;
-      }
-      const int best = (int)(cost & 63);
-      heads = split_heads(group, best >> 3);
-      n_long = __shfl(mine, best);
-      if (heads >= group) n_long = 0;
-      n_long = n_long < total ? n_long : total;
-    }
-    if (l == 0) {
-      a.ctrl[kCtrlItems] = total;
-      a.ctrl[kCtrlLong] = n_long;
-      a.ctrl[kCtrlHeads] = heads;
-    }
-  }
-  if (l != 0) return;
-  if (j >= 0 && j < g.tiles() && place < a.slots_k) {
-    a.order[2 * (size_t)place] = s;
-    a.order[2 * (size_t)place + 1] = j;
   }
 }
 
@@ -211,8 +223,13 @@ __global__ __launch_bounds__(256) void packed_sum_kernel(PackedBwdArgs a) {
 
 template <int D>
 hipError_t launch(const PackedBwdArgs& a, int cus, hipStream_t stream) {
-  const unsigned grid = (unsigned)(a.slots_q * a.p.heads_q + (a.slots_k + 3) / 4);
-  hipLaunchKernelGGL(packed_pre_kernel<D>, dim3(grid), dim3(256), 0, stream, a);
+  // several heads a workgroup where that leaves workgroups enough
+  const int rows = (a.p.total_q + BM - 1) / BM, rest = a.slots_q + (a.slots_k + 3) / 4;
+  constexpr int H = D == 256 ? 2 : 4;
+  if (a.p.heads_q % H == 0 && (long)rows * a.p.heads_q >= 4096)
+    hipLaunchKernelGGL((packed_pre_kernel<D, H>), dim3((unsigned)(rows * (a.p.heads_q / H) + rest)), dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL((packed_pre_kernel<D, 1>), dim3((unsigned)(rows * a.p.heads_q + rest)), dim3(256), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // persistent workgroups: as many as stay resident (two per CU at d = 64, else one).

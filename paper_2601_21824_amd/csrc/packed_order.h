@@ -83,7 +83,8 @@ DASH_ORDER_HD int split_parts(int group, int heads) { return (group + heads - 1)
 // share: steps of all chains over the workers; longest: blocks of the longest chain;
 // n_long: tiles with more than `above` blocks; heads: per part (group: none is split).
 // Unsplit chains start last, so that on average half of one stands over at the end;
-// writing and reading a part's partials takes about as long as 3 steps.
+// writing and reading a part's partials costs 6 steps (by 3, 12 sequences of 8192 tokens, 32
+// heads over 8, took one head a part, 474 us, by 5 to 12 two, 420).
 DASH_ORDER_HD long split_cost(long share, long longest, long above, long n_long, int heads, int group, int heads_kv) {
   const bool whole = heads >= group;
   const long tail = (whole || above > longest ? longest : above) * group;
@@ -92,7 +93,7 @@ DASH_ORDER_HD long split_cost(long share, long longest, long above, long n_long,
   if (whole) return t;
   const long part = longest > above ? longest * heads : 0;
   t = t > part ? t : part;
-  return t + 3 * n_long * heads_kv * split_parts(group, heads) / kSplitWorkers;
+  return t + 6 * n_long * heads_kv * split_parts(group, heads) / kSplitWorkers;
 }
 // Partials there is room for (each of a part's dK and dV): a tile is never split finer
 // than costs less than its steps, i.e. more than `share` steps' worth of partials in all.
