@@ -11,9 +11,9 @@
 //
 // Bound by memory for prompts (q, k, v in, q and the cache rows out) and by the
 // launch for single tokens.  One wave per token: it takes sine and cosine of every
-// pair once (through LDS, for all heads), then 64 items of 16 components a round --
-// the 8 pairs 8j .. 8j+7 of a head, which in both pairings are two 16-byte chunks, so
-// that a lane never needs another lane's data and q_out may be q.  Calls with few
+// pair once (through LDS, for all heads), then 64 items a round: two 16-byte chunks of
+// a head that hold 8 whole pairs, so that a lane never needs another lane's data and
+// q_out may be q.  Calls with few
 // tokens give each wave one round only, and the waves of a token redo its sines.
 #include "common.h"
 #include "ops.h"
@@ -37,7 +37,9 @@ __device__ inline unsigned pack_e4m3(const float* x) {
   return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], r, true);
 }
 
-template <int D>
+// ONCE: inputs larger than the last-level cache can hold behind the kernel that made
+// them are read past the caches.
+template <int D, bool ONCE>
 __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, int rounds) {
   constexpr int IPH = D / 16;    // items per head
   constexpr int HPR = 64 / IPH;  // heads per round
@@ -77,18 +79,28 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, in
   const PageRow to = page_row(c.table + s * c.table_stride, c.table_width, c.page_size, c.pages, old < 0 ? -1 : at_place);
   if (!to.ok && l == 0 && c.status) *c.status = 1;
 
-  const int j = l % IPH;
-  const bool rot = 8 * j < pairs;
-  const bool split = rot && !a.interleaved;
-  // element offsets of the item's two chunks
-  const int e0 = split ? 8 * j : 16 * j, e1 = split ? e0 + pairs : e0 + 8;
+  // The item's two 16-byte chunks (element offsets e0, e1) and their sines: neighbouring
+  // lanes hold neighbouring chunks, so that a load is whole lines
+  const int j = l % IPH, rot = 2 * pairs;
+  const bool split = !a.interleaved && 16 * j < rot;  // chunks of the two halves of 8 pairs
+  int e0 = 8 * j, e1 = 8 * j + D / 2;
+  if (split) {
+    e1 = 8 * j + pairs;
+  } else if (!a.interleaved) {  // components that are not rotated
+    e0 = rot + 8 * (j - rot / 16);
+    e1 = e0 + (D - rot) / 2;
+  }
   float cs[8], sn[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float2 x = rot ? turn[w][8 * j + i] : make_float2(1.f, 0.f);
+    // split: pairs 8j .. 8j+7; interleaved: the four of chunk e0 and the four of e1
+    const int at = split ? 8 * j + i : (i < 4 ? e0 : e1) / 2 + (i & 3);
+    const bool on = split || (a.interleaved && (i < 4 ? e0 : e1) < rot);
+    const float2 x = on ? turn[w][at] : make_float2(1.f, 0.f);
     cs[i] = x.x;
     sn[i] = x.y;
   }
+  const bool turned = split || (a.interleaved && e0 < rot);  // (e1 < rot only if e0 is)
   for (int r = first; r < first + rounds; ++r) {
     const int h = r * HPR + l / IPH;
     if (h >= heads) return;
@@ -97,7 +109,8 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, in
     const __bf16* src = kind == 0   ? (const __bf16*)a.q + t * a.qs.row + h * a.qs.head
                         : kind == 1 ? (const __bf16*)a.k + t * a.ks.row + hk * a.ks.head
                                     : (const __bf16*)a.v + t * a.vs.row + hk * a.vs.head;
-    u32x4 x0 = *(const u32x4*)(src + e0), x1 = *(const u32x4*)(src + e1);
+    u32x4 x0 = ONCE ? __builtin_nontemporal_load((const u32x4*)(src + e0)) : *(const u32x4*)(src + e0);
+    u32x4 x1 = ONCE ? __builtin_nontemporal_load((const u32x4*)(src + e1)) : *(const u32x4*)(src + e1);
     float y0[8], y1[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -106,7 +119,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, in
       y1[2 * i] = bf_lo(x1[i]);
       y1[2 * i + 1] = bf_hi(x1[i]);
     }
-    if (kind != 2 && rot) {
+    if (kind != 2 && turned) {
       if (split) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -170,7 +183,13 @@ void launch(const AppendArgs& a, hipStream_t stream) {
   // rounds as a token has
   const int rounds = (long)a.tokens * total <= 4096 ? 1 : total;
   const long waves = (long)a.tokens * ((total + rounds - 1) / rounds);
-  hipLaunchKernelGGL(kv_append_kernel<D>, dim3((unsigned)((waves + kWaves - 1) / kWaves)), dim3(64 * kWaves), 0, stream, a, rounds);
+  const dim3 grid((unsigned)((waves + kWaves - 1) / kWaves));
+  // past the caches from 64 MB of q, k and v on (us, through / past them: 8192 tokens, 32 heads
+  // over 8 of 128, 100 MB, 44.2 / 40.3; 16 over 4 of 64, 25 MB, where the cache still holds them, 14.0 / 17.5)
+  if ((long)a.tokens * heads * D * 2 >= 64L << 20)
+    hipLaunchKernelGGL((kv_append_kernel<D, true>), grid, dim3(64 * kWaves), 0, stream, a, rounds);
+  else
+    hipLaunchKernelGGL((kv_append_kernel<D, false>), grid, dim3(64 * kWaves), 0, stream, a, rounds);
 }
 
 }  // namespace
