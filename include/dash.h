@@ -364,7 +364,7 @@ typedef enum {
 
 /* A paged key-value cache: `pages` pages of page_size rows for each of heads_kv
    heads, and for each of `batch` sequences the pages that hold its rows in order.
-   page_size is a multiple of 16.  Key j of sequence s is row j % page_size
+   page_size is a multiple of 16.  Sequences may share pages that no call writes.  Key j of sequence s is row j % page_size
    of page block_table[s * table_stride + j / page_size]. */
 typedef struct {
   int batch, heads_q, heads_kv, d;
@@ -442,9 +442,10 @@ int dash_attn_decode(const dash_paged_cache_t* cache, const void* q, int64_t q_r
    (keys: cu_k, k and v); offsets rise from 0.  Rows from cu_q[batch] (cu_k[batch]) on
    belong to nobody: what they hold is not read into any result, and outputs are left
    alone there.  With m queries and n keys and causal != 0, query i of a sequence sees
-   key j iff j - i <= n - m (the last query sees every key); else all n.  A NaN or an
-   infinity in V reaches, under a causal mask, queries before it as well where they share a
-   tile with it (0 * NaN): up to 31 rows back in O, a KV tile in dQ; one in K the latter. */
+   key j iff j - i <= n - m (the last query sees every key); else all n.  Under a causal
+   mask a NaN or an infinity in V reaches queries before it as well where they share a tile
+   with it (0 * NaN): up to 63 rows back in O, a KV tile and a query block (319 rows) in dQ;
+   one in K does so in dQ. */
 typedef struct {
   int batch, heads_q, heads_kv, d, causal;
   int total_q, total_k; /* rows of the tensors */
@@ -483,9 +484,10 @@ size_t dash_packed_workspace_size(int batch, int total_q, int total_k, int heads
  * are summed into dK and dV depends on all sequences' lengths.  Asynchronous on `stream`, launched
  * without cooperation: its waits only point to work that started earlier.
  * Workspace of ws_bytes >= dash_packed_workspace_size(...) bytes, 256-byte aligned, any
- * contents, not used by another call until this one has finished.  A wait timeout is
- * recorded there (dash_bwd_check) and in status (NULL or a device int that the call sets
- * to 0, or 1 after a timeout): it can only happen where cu_q or cu_k do not rise.
+ * contents, not used by another call until this one has finished.  Offsets that do not
+ * rise within 0 .. total_q (total_k) are found on the device: the gradients are then
+ * undefined, and dash_bwd_check on the workspace gives DASH_ERR_TIMEOUT, as after a wait
+ * that timed out.  status: NULL or a device int that the call sets to 0, or 1 in these cases.
  */
 int dash_attn_packed_bwd(const dash_packed_t* p, const void* q, const void* k, const void* v, const void* o,
                          const void* dO, const float* lse, void* dq, void* dk, void* dv, void* workspace,

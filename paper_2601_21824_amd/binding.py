@@ -501,7 +501,7 @@ def dash_attn_packed_bwd(q, k, v, o, dO, lse, dq, dk, dv, cu_q, cu_k=None, causa
     """Backward of dash_attn_packed_fwd into dq (like q), dk and dv (like k), from its o
     and lse.  ``workspace``: a uint8 device tensor of dash_packed_workspace_size bytes
     (without it one is allocated).  ``status``: optional int32 that receives 0, or 1
-    after a wait timeout (offsets that do not rise)."""
+    for offsets that do not rise (or after a wait timeout)."""
     import torch
     dev = _gpu(q)
     if q.dim() != 3 or k.dim() != 3:

@@ -55,7 +55,12 @@ __global__ __launch_bounds__(256) void packed_pre_kernel(PackedBwdArgs a) {
       }
     }
     place = wave_sum(place);
-    if (slot == 0) {  // the wave of the first slot counts
+    if (slot == 0) {  // the wave of the first slot counts, and looks the offsets over
+      bool bad = false;
+      for (int b = l; b < p.batch; b += 64)
+        bad |= p.cu_q[b] < 0 || p.cu_q[b + 1] < p.cu_q[b] || p.cu_q[b + 1] > p.total_q || p.cu_k[b] < 0 ||
+               p.cu_k[b + 1] < p.cu_k[b] || p.cu_k[b + 1] > p.total_k;
+      bad = __any(bad);
       total = wave_sum(total);
       total = total < a.slots_k ? total : a.slots_k;
       steps = ((long)wave_sum((int)(steps >> 20)) << 20) + wave_sum((int)(steps & 0xfffff));
@@ -102,13 +107,18 @@ __global__ __launch_bounds__(256) void packed_pre_kernel(PackedBwdArgs a) {
         n_long = n_long < total ? n_long : total;
       }
       if (l == 0) {
+        a.ctrl[kCtrlTicket] = 0;
+        a.ctrl[kCtrlError] = bad ? 1 : 0;
+        if (a.status) *a.status = bad ? 1 : 0;
+        // chains of sequences that overlap would wait for one another in vain
+        if (bad) total = n_long = 0;
         a.ctrl[kCtrlItems] = total;
         a.ctrl[kCtrlLong] = n_long;
         a.ctrl[kCtrlHeads] = heads;
       }
     }
     if (l != 0) return;
-    if (j >= 0 && j < g.tiles() && place < a.slots_k) {
+    if (j >= 0 && j < g.tiles() && (unsigned)place < (unsigned)a.slots_k) {
       a.order[2 * (size_t)place] = s;
       a.order[2 * (size_t)place + 1] = j;
     }
@@ -116,11 +126,6 @@ __global__ __launch_bounds__(256) void packed_pre_kernel(PackedBwdArgs a) {
   }
   x -= order;
   if (x < a.slots_q) {  // ---- a slot's counters, and dQ where nothing else writes it
-    if (x == 0 && tid == 0) {
-      a.ctrl[kCtrlTicket] = 0;
-      a.ctrl[kCtrlError] = 0;
-      if (a.status) *a.status = 0;
-    }
     for (int h = tid; h < p.heads_q; h += 256) a.counters[((size_t)x * p.heads_q + h) * kCtrStride] = a.poison ? kPoison : 0;
     const int s = __builtin_amdgcn_readfirstlane(
         find_last(p.batch, x, l, [&](int i) { return first_slot(p.cu_q, i, p.total_q, BM); }));

@@ -210,10 +210,16 @@ int check_packed(const dash_packed_t* p, float* scale, const void* q, const void
   return DASH_OK;
 }
 
+// The stride of a single row means nothing (a broadcast's is 0), but the kernels find the
+// end of a tensor's rows by it.
+int64_t row_stride(int64_t stride, int rows, int d) { return rows > 1 ? stride : d; }
+
 dash::PackedArgs packed_args(const dash_packed_t* p, float scale, const void* q, const void* k, const void* v, void* o, float* lse) {
+  const auto row_q = [&](int64_t s) { return row_stride(s, p->total_q, p->d); };
+  const auto row_k = [&](int64_t s) { return row_stride(s, p->total_k, p->d); };
   return {q, k, v, o, lse, p->cu_q, p->cu_k ? p->cu_k : p->cu_q, p->batch, p->heads_q, p->heads_kv, p->total_q, p->total_k,
-          p->causal ? 1 : 0, scale, {p->q_row_stride, p->q_head_stride}, {p->k_row_stride, p->k_head_stride},
-          {p->v_row_stride, p->v_head_stride}, {p->o_row_stride, p->o_head_stride}, 1, nullptr, nullptr};
+          p->causal ? 1 : 0, scale, {row_q(p->q_row_stride), p->q_head_stride}, {row_k(p->k_row_stride), p->k_head_stride},
+          {row_k(p->v_row_stride), p->v_head_stride}, {row_q(p->o_row_stride), p->o_head_stride}, 1, nullptr, nullptr};
 }
 
 struct FwdLayout {
@@ -328,10 +334,10 @@ int attn_packed_bwd(const dash_packed_t* p, const void* q, const void* k, const 
   a.scale = scale;
   a.spin_limit = 1 << 24;
   a.status = status;
-  a.dos = {p->do_row_stride, p->do_head_stride};
-  a.dqs = {p->dq_row_stride, p->dq_head_stride};
-  a.dks = {p->dk_row_stride, p->dk_head_stride};
-  a.dvs = {p->dv_row_stride, p->dv_head_stride};
+  a.dos = {row_stride(p->do_row_stride, p->total_q, p->d), p->do_head_stride};
+  a.dqs = {row_stride(p->dq_row_stride, p->total_q, p->d), p->dq_head_stride};
+  a.dks = {row_stride(p->dk_row_stride, p->total_k, p->d), p->dk_head_stride};
+  a.dvs = {row_stride(p->dv_row_stride, p->total_k, p->d), p->dv_head_stride};
   a.bc = L.bc;
   a.slots_q = L.slots_q;
   a.slots_k = L.slots_k;

@@ -192,6 +192,73 @@ def test_backward_large(d, hq, hkv, lens, causal):
         assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(out, again))
 
 
+def test_no_queries_no_keys_one_row():
+    """Tensors of no rows on either side; one row, whose strides say nothing (a broadcast)."""
+    kv = torch.randn((300, 2, 64), device="cuda").to(BF)
+    none = kv[:0, :1].expand(0, 4, 64)
+    o, lse = dash.attn_packed_fwd(none, kv, kv, cu_of([0, 0]), cu_of([100, 200]))
+    dq, dk, dv = dash.attn_packed_bwd(none, kv, kv, o, none.contiguous(), lse, cu_of([0, 0]), cu_of([100, 200]))
+    assert bool((dk == 0).all()) and bool((dv == 0).all()) and dq.numel() == 0
+    q = torch.randn((300, 4, 64), device="cuda").to(BF)
+    empty = torch.empty((0, 2, 64), dtype=BF, device="cuda")
+    o, lse = dash.attn_packed_fwd(q, empty, empty, cu_of([100, 200]), cu_of([0, 0]))
+    assert bool((o == 0).all()) and bool((lse == -math.inf).all())
+    dq, dk, dv = dash.attn_packed_bwd(q, empty, empty, o, q, lse, cu_of([100, 200]), cu_of([0, 0]))
+    assert bool((dq == 0).all())
+    for d in (64, 128, 256):
+        one = torch.randn((1, 1, d), device="cuda").to(BF).as_strided((1, 2, d), (0, 0, 1))  # strides of 0
+        qq = torch.randn((70, 4, d), device="cuda").to(BF)
+        do = torch.randn_like(qq)
+        want = reference(qq, one, one, do, [70], [1], False, 1 / math.sqrt(d))
+        o, lse = dash.attn_packed_fwd(qq, one, one, cu_of([70]), cu_of([1]), causal=False)
+        assert over(o, want["o"], want["to"]) <= 0
+        dq, dk, dv = dash.attn_packed_bwd(qq, one, one, o, do, lse, cu_of([70]), cu_of([1]), causal=False)
+        assert over(dq, want["dq"], want["tq"]) <= 0 and over(dk, want["dk"], want["tk"]) <= 0 and over(dv, want["dv"], want["tv"]) <= 0
+
+
+def test_offsets_that_do_not_rise_are_reported():
+    q, k, v, do = packed_inputs([200, 100], [200, 100], 4, 2, 64)
+    good = cu_of([200, 100])
+    o, lse = dash.attn_packed_fwd(q, k, v, good)
+    want = dash.attn_packed_bwd(q, k, v, o, do, lse, good)
+    ws = torch.empty(dash.dash_packed_workspace_size(2, 300, 300, 4, 2, 64), dtype=torch.uint8, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for bad in ([0, 301, 300], [0, 200, 100], [-1, 200, 300], [0, 300, 2 ** 31 - 1], [300, 0, 300]):
+        for cu_q, cu_k in ((bad, [0, 200, 300]), ([0, 200, 300], bad), (bad, bad)):
+            a, b = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (cu_q, cu_k))
+            out = [torch.empty_like(x) for x in (q, k, v)]
+            dash.dash_attn_packed_bwd(q, k, v, o, do, lse, *out, a, b, workspace=ws, status=status)
+            assert int(status) == 1 and dash.dash_bwd_check(ws) == dash.DASH_ERR_TIMEOUT
+            dash.attn_packed_fwd(q, k, v, a, b)  # some result, within the tensors
+    dash.dash_attn_packed_bwd(q, k, v, o, do, lse, *out, good, workspace=ws, status=status)
+    assert int(status) == 0 and dash.dash_bwd_check(ws) == dash.DASH_OK
+    assert all(torch.equal(x, y) for x, y in zip(out, want))
+
+
+def test_broadcast_heads():
+    """K and V of one head read by all through a head stride of 0, gradients for each."""
+    lens = [90, 40]
+    q, k, v, do = packed_inputs(lens, lens, 4, 1, 128)
+    kb, vb = k.expand(-1, 4, -1), v.expand(-1, 4, -1)
+    cu = cu_of(lens)
+    o, lse = dash.attn_packed_fwd(q, kb, vb, cu)
+    got = dash.attn_packed_bwd(q, kb, vb, o, do, lse, cu)
+    o2, lse2 = dash.attn_packed_fwd(q, kb.contiguous(), vb.contiguous(), cu)
+    want = dash.attn_packed_bwd(q, kb.contiguous(), vb.contiguous(), o2, do, lse2, cu)
+    assert torch.equal(o, o2) and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_many_sequences_and_heads():
+    """More than 64 sequences (two rounds of a wave), empty ones among them; 34 heads over 2."""
+    lens = [(37 * i) % 150 for i in range(140)]
+    for d, hq, hkv in ((64, 4, 2), (128, 34, 2)):
+        q, k, v, do = packed_inputs(lens, lens, hq, hkv, d)
+        out = train(q, k, v, do, cu_of(lens), None, True)
+        ref = reference(q, k, v, do, lens, lens, True, 1 / math.sqrt(d))
+        for name, got in zip("qkv", out):
+            assert over(got, ref["d" + name], ref["t" + name]) <= 0, "d" + name
+
+
 def test_gradients_against_differences():
     """The gradients of sum(O * dO) against central differences of the float64
     definition's forward, along random directions (the forward itself is checked above)."""
