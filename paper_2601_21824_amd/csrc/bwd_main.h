@@ -369,13 +369,19 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(Args a) {
 
       // ---- the next valid block (prefetched into the other buffer below)
       const int nst = next_valid(st + 1);
-      const bool has_next = nst < nsteps;
       Blk pb_next;
       if constexpr (PACKED) {
         pb_next = ch.next(pb);
         blk_q = ch.q(pb_next);
         blk_do = ch.dO(pb_next);
-      } else pb_next = has_next ? (int)(step_at(nst) & 0xfff) : -1;
+      } else {
+        pb_next = nst < nsteps ? (int)(step_at(nst) & 0xfff) : -1;
+      }
+      // negative after the last step (a dense call's next block itself: a flag beside it is
+      // kept in a vector register and costs 1% of a causal call)
+      int more;
+      if constexpr (PACKED) more = nst < nsteps ? 0 : -1;
+      else more = pb_next;
       // the chain moves to another KV tile after this step (Symmetric Shift,
       // between its two tiles)
       const bool tile_ends = !PACKED && nst < nsteps && (int)((step_at(nst) >> 12) & 0x1ff) != j;
@@ -510,11 +516,11 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(Args a) {
 
       // run 1: S/dP of half 0, with the next block's Q / dO / L / D prefetch
       sdp(0, [&](int k) { rd_rows(1, k); }, [&](int ks) {
-        if (!has_next) return;
+        if (more < 0) return;
         if (ks < QLD) load_part(pb_next, buf ^ 1, ks);
         if (ks == 0) load_ld(pb_next, buf ^ 1);
       });
-      if (has_next) {
+      if (more >= 0) {
         const int n = kBlockLoads + (w < 2 ? 1 : 0);
         vm_poll += n;
         vm_rel += n;
@@ -633,7 +639,7 @@ __global__ __launch_bounds__(256) void bwd_main_kernel(Args a) {
         vm_wait<0>();
         vm_poll = vm_rel = 0;
         // copy the next block's counter now, ahead of the stores below
-        if (ordered && has_next) poll_copy(pb_next);
+        if (ordered && more >= 0) poll_copy(pb_next);
         if constexpr (ordered) {
           // ---- add this wave's partial into its slice straight from registers:
           //      the accumulator is stored in this wave's register order, so the
