@@ -224,9 +224,8 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
     // T*1024, chunk rb of lane l at rb*256 + 4l: row 32 half + l%32 of the block,
     // columns 32 (d block) + 8rb + 4(l/32) .. +3.  Wave w: d blocks w DQT ...
     auto acc_off = [&](Blk pb, int h, int k) {  // wave-uniform part (packed: within the block)
-      int at = (2 * (w * DQT + (k >> 2)) + h) * 1024 + (k & 3) * 256;
-      if constexpr (!PACKED) at += pb * BM * D;
-      return (uint32_t)at * 4;
+      if constexpr (PACKED) return (uint32_t)((2 * (w * DQT + (k >> 2)) + h) * 1024 + (k & 3) * 256) * 4;
+      else return (uint32_t)(pb * BM * D + (2 * (w * DQT + (k >> 2)) + h) * 1024 + (k & 3) * 256) * 4;
     };
     // An accumulator slice is loaded and stored by straight-line code in every
     // sub-step: where there is nothing to load or store, the descriptor covers 0
@@ -510,7 +509,7 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
 
       int nst = st + 1;  // the next block (looked up in the first sub-step)
       Blk pb_next{};
-      bool has_next = false;
+      int more = -1;  // negative after the last step (dense: the next block itself, as in bwd_main.h)
       unsigned e_next = 0;
       bool turn = !ordered;  // this block's turn
 
@@ -581,7 +580,7 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
             if (h == 0) {
               if (ks == 0 && ordered && !turn) poll_copy(pb);
               if (ks % GAP == 1 && ks / GAP < QP) load_part(pb, 1, ks / GAP);
-            } else if (has_next) {
+            } else if (more >= 0) {
               if (ks == 0 && ordered) poll_copy(pb_next);
               if (ks == 0) load_ld(pb_next, bpar ^ 1);
               if (ks % GAP == 1 && ks / GAP < QP) load_part(pb_next, 0, ks / GAP, 1);
@@ -595,7 +594,7 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
         }
         if constexpr (PACKED) {
           if constexpr (h == 0) {
-            has_next = nst < nsteps;
+            more = nst < nsteps ? 0 : -1;
             pb_next = ch.next(pb);
             blk_q[1] = ch.q(pb_next);
             blk_do[1] = ch.dO(pb_next);
@@ -609,12 +608,11 @@ __global__ __launch_bounds__(NT) void bwd_mainw_kernel(Args a) {
               if (nst < nsteps) e_next = step_at(nst);
             }
           }
-          has_next = nst < nsteps;
-          pb_next = (int)(e_next & 0xfff);
+          more = pb_next = nst < nsteps ? (int)(e_next & 0xfff) : -1;
         }
         // deferred release of the block whose second half was stored a sub-step ago
         if (ordered && h == 1 && rel_pb >= 0) {
-          vm_wait_few(has_next ? 2 * QP : 0);  // (the copies issued since)
+          vm_wait_few(more >= 0 ? 2 * QP : 0);  // (the copies issued since)
           release();
         }
 
