@@ -276,7 +276,7 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(DecodeArgs a) {
 // take every NG-th chunk and are added in order of the group.
 template <int D>
 __global__ __launch_bounds__(256) void join_kernel(DecodeArgs a) {
-  constexpr int NG = 256 / (D / 4);
+  constexpr int NG = 256 / (D / 4), U = 8;  // U chunks' loads in flight together
   __shared__ f32x4 acc[NG][D / 4];
   __shared__ float dens[NG];
   const int hq = a.c.heads_q, s = (int)blockIdx.x / hq, h = (int)blockIdx.x % hq;
@@ -291,10 +291,23 @@ __global__ __launch_bounds__(256) void join_kernel(DecodeArgs a) {
   const float mm = top == -INFINITY ? 0.f : top;
   float den = 0.f;
   f32x4 out = {0.f, 0.f, 0.f, 0.f};
-  for (int i = grp; i < n; i += NG) {
-    const float f = __builtin_amdgcn_exp2f(pm[2 * (size_t)i * hq] - mm);
-    den += f * pm[2 * (size_t)i * hq + 1];
-    out += f * *(const f32x4*)(a.part_o + ((size_t)(first + i) * hq + h) * D + 4 * d4);
+  for (int i = grp; i < n; i += U * NG) {
+    float m[U], e[U];
+    f32x4 o[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int iu = i + u * NG < n ? i + u * NG : i;  // (read again, not added)
+      m[u] = pm[2 * (size_t)iu * hq];
+      e[u] = pm[2 * (size_t)iu * hq + 1];
+      o[u] = *(const f32x4*)(a.part_o + ((size_t)(first + iu) * hq + h) * D + 4 * d4);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i + u * NG < n) {
+        const float f = __builtin_amdgcn_exp2f(m[u] - mm);
+        den += f * e[u];
+        out += f * o[u];
+      }
   }
   acc[grp][d4] = out;
   if (d4 == 0) dens[grp] = den;

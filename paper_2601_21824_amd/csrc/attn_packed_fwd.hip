@@ -134,12 +134,13 @@ __global__ __launch_bounds__(256, WPS) void packed_fwd_kernel(PackedArgs a) {
   attn_fwd_rows<D, QG>(view, a.causal, a.scale, r.q0);
 }
 
-// The runs of a slot's rows, in order: one workgroup per 32 rows and head, D / 4 lanes a row.
+// The runs of a slot's rows, in order: one workgroup per two passes of rows and head, D / 4
+// lanes a row.
 template <int D, int QROWS>
 __global__ __launch_bounds__(256) void join_kernel(PackedArgs a) {
-  constexpr int KT = D == 256 ? 32 : 64, RPP = 1024 / D;  // rows a pass
+  constexpr int KT = D == 256 ? 32 : 64, RPP = 1024 / D, RWG = 2 * RPP;  // rows a pass, rows a workgroup
   const int tid = threadIdx.x;
-  const int x = (int)blockIdx.x / (QROWS / 32), r0 = (int)blockIdx.x % (QROWS / 32) * 32;
+  const int x = (int)blockIdx.x / (QROWS / RWG), r0 = (int)blockIdx.x % (QROWS / RWG) * RWG;
   const int slot = x / a.heads_q, h = x % a.heads_q;
   const Rows r = rows_of<QROWS>(a, slot, tid & 63);
   if (r0 >= r.n || r.kv_end <= 0) return;
@@ -147,7 +148,7 @@ __global__ __launch_bounds__(256) void join_kernel(PackedArgs a) {
   if (n == 1) return;  // the result is there
   const int64_t part = ((int64_t)slot * a.heads_q + h) * a.splits;
   const int c = tid % (D / 4) * 4;
-  for (int row = r0 + tid / (D / 4); row < r0 + 32 && row < r.n; row += RPP) {
+  for (int row = r0 + tid / (D / 4); row < r0 + RWG && row < r.n; row += RPP) {
     float top = -INFINITY;
     for (int i = 0; i < n; ++i) top = fmaxf(top, a.part_l[(part + i) * QROWS + row]);
     const float at = top == -INFINITY ? 0.f : top;
@@ -170,7 +171,7 @@ void launch(const PackedArgs& a, hipStream_t stream) {
   constexpr int QROWS = 128 * QG;
   const long blocks = (long)(a.total_q / QROWS + a.batch) * a.heads_q, items = blocks * a.splits;
   hipLaunchKernelGGL((packed_fwd_kernel<D, QG, WPS>), dim3((unsigned)((items + 7) / 8 * 8)), dim3(256), 0, stream, a);
-  if (a.splits > 1) hipLaunchKernelGGL((join_kernel<D, QROWS>), dim3((unsigned)(blocks * (QROWS / 32))), dim3(256), 0, stream, a);
+  if (a.splits > 1) hipLaunchKernelGGL((join_kernel<D, QROWS>), dim3((unsigned)(blocks * (QROWS / (2048 / D)))), dim3(256), 0, stream, a);
 }
 
 }  // namespace
