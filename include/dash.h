@@ -479,7 +479,7 @@ size_t dash_packed_workspace_size(int batch, int total_q, int total_k, int heads
  * (each K/V head's gradient is the sum over its query heads).  Deterministic: dK and dV
  * are summed by one workgroup, dQ over the KV tiles in ascending order by the ordered
  * reduction of dash_attn_bwd_ex (Descending Q-Tile Iteration, Section 3.3, over the
- * blocks of all query heads of a group).  The KV tile at d = 128, and with it the order of
+ * blocks of all query heads of a group).  The KV tile at d = 64 and 128, and with it the order of
  * the sums, depends on total_k, batch, heads_q and the mask; how a group's query heads
  * are summed into dK and dV depends on all sequences' lengths.  Asynchronous on `stream`, launched
  * without cooperation: its waits only point to work that started earlier.

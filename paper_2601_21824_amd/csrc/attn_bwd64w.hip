@@ -22,6 +22,7 @@
 #include "kernels.h"
 #include "bwd_common.h"
 #include "lds_layout.h"
+#include "packed_chain.h"
 
 namespace dash {
 
@@ -43,8 +44,12 @@ struct Smem64w {
   int item;
 };
 
-template <bool CAUSAL, int MODE, bool STATS = false>
-__global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
+// Args: as in bwd_main.h
+template <bool CAUSAL, int MODE, bool STATS = false, typename Args = BwdArgs>
+__global__ __launch_bounds__(256) void bwd_main64w_kernel(Args a) {
+  constexpr bool PACKED = std::is_same_v<Args, PackedBwdArgs>;
+  static_assert(!PACKED || MODE == kModeOrdered, "packed sequences: the ordered reduction");
+  using Blk = std::conditional_t<PACKED, PackedBlk, int>;  // a query block (dense: of the chain's head)
   constexpr int D = 64;
   constexpr int BC = kW64Rows;
   constexpr int NW = 4;          // waves
@@ -72,7 +77,9 @@ __global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
   constexpr bool ordered = MODE == kModeOrdered || MODE == kModeOrderedXcd;
   constexpr bool xcd = MODE == kModeOrderedXcd;
   const int xq = xcd ? xcc_id() : 0;
-  const int total = xcd ? (xq < a.nxcd ? xcd_heads(a.bh, a.nxcd, xq) * G.chains : 0) : a.bh * G.chains;
+  int total_items = 0;
+  if constexpr (PACKED) total_items = PackedChain<D, BC>::items(a);
+  const int total = PACKED ? total_items : xcd ? (xq < a.nxcd ? xcd_heads(a.bh, a.nxcd, xq) * G.chains : 0) : a.bh * G.chains;
   int* const ticket = &a.ctrl[xcd ? kCtrlXcdTicket + xq : kCtrlTicket];
   const int* const order = a.order + (xcd ? 2 * xq * a.xcd_cap : 0);
   const uint32_t sm_lds = lds_base(&sm);
@@ -80,7 +87,7 @@ __global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
   // Shift-type orders: the next contributor to a block reaches it a step or
   // more later, so the counter release waits until the second run of the
   // next step, when the stores have drained without a wait of their own
-  const bool deferred = G.sched == S_SHIFT || G.sched == S_SYMSHIFT;
+  const bool deferred = !PACKED && (G.sched == S_SHIFT || G.sched == S_SYMSHIFT);
   bool failed = false;
   WaitStats wst;
   if constexpr (STATS) stats_wave_begin(wst);
@@ -90,15 +97,22 @@ __global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
     __syncthreads();
     const int item = __builtin_amdgcn_readfirstlane(sm.item);
     if (item >= total) break;
-    const int bh = __builtin_amdgcn_readfirstlane(order[2 * item]);
-    const int wch = __builtin_amdgcn_readfirstlane(order[2 * item + 1]);
+    std::conditional_t<PACKED, PackedChain<D, BC>, NoChain> ch(a);
+    if constexpr (PACKED) {
+      if (!ch.init(item)) {
+        __syncthreads();  // sm.item is rewritten by the next ticket
+        continue;
+      }
+    }
+    const int bh = PACKED ? 0 : __builtin_amdgcn_readfirstlane(order[2 * item]);
+    const int wch = PACKED ? 0 : __builtin_amdgcn_readfirstlane(order[2 * item + 1]);
     const size_t head = (size_t)bh * N * D;
     const auto rq = make_rsrc((const __bf16*)a.q + head, hbytes);
     const auto rk = make_rsrc((const __bf16*)a.k + head, hbytes);
     const auto rv = make_rsrc((const __bf16*)a.v + head, hbytes);
     const auto rdo = make_rsrc((const __bf16*)a.dO + head, hbytes);
     const auto racc = make_rsrc(a.dqacc + (size_t)bh * a.nblk * BM * D, (uint32_t)a.nblk * BM * D * 4);
-    int* ctr_head = a.counters + (size_t)bh * a.nblk * kCtrStride;
+    int* ctr_head = PACKED ? a.counters : a.counters + (size_t)bh * a.nblk * kCtrStride;
     const auto rctr = make_rsrc(ctr_head, (uint32_t)a.nblk * kCtrStride * 4);
     // padded rows of a ragged last block read L = D = 0 (P = 1 there), and
     // their Q and dO rows read 0: they add nothing to dK and dV
@@ -106,9 +120,14 @@ __global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
     const auto rds = make_rsrc(a.dvec + (size_t)bh * N, (uint32_t)N * 4);
 
     const unsigned* tab = a.steps + (size_t)wch * a.step_cap;
-    const int nsteps = __builtin_amdgcn_readfirstlane((int)tab[0]);
-    for (int st = tid; st < nsteps; st += NT) sm.steps[st] = tab[1 + st];
-    __syncthreads();
+    int nsteps;
+    if constexpr (PACKED) {
+      nsteps = ch.steps();
+    } else {
+      nsteps = __builtin_amdgcn_readfirstlane((int)tab[0]);
+      for (int st = tid; st < nsteps; st += NT) sm.steps[st] = tab[1 + st];
+      __syncthreads();
+    }
     int cur_j = -1;
     bf16x8 kreg[KB][KS], vreg[KB][KS];  // K, V rows of the wave's key blocks (B of S = Q K^T, dP = dO V^T)
     f32x16 dkacc[KB][NB], dvacc[KB][NB];
@@ -118,23 +137,43 @@ __global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
 
     auto step_at = [&](int st) -> unsigned { return __builtin_amdgcn_readfirstlane(sm.steps[st]); };
     auto next_valid = [&](int st) {
-      while (st < nsteps && step_at(st) == kNoStep) ++st;
+      if constexpr (!PACKED)
+        while (st < nsteps && step_at(st) == kNoStep) ++st;
       return st;
     };
+    // number of a block's counter (and, packed, of its accumulator)
+    auto ctr_at = [&](Blk b) {
+      if constexpr (PACKED) return b.x;
+      else return b;
+    };
+    // (packed: the resources of a block's copies, built once a step)
+    __amdgpu_buffer_rsrc_t blk_q, blk_do;
     // part k of block pb's Q and dO rows (32 rows, 4 KB each) into buffer b
     static_assert((NT / CPR) * D * 2 == 4096, "a part is 4 KB");
-    auto load_part = [&](int pb, int b, int k) {
-      const int r = tid / CPR, c = (tid % CPR) ^ tile_swz<D>(r);
-      const uint32_t off = (uint32_t)((pb * BM + r) * D + 8 * c) * 2;
+    auto load_part = [&](Blk pb, int b, int k) {
       const uint32_t at = lds_of(&sm.qs[b][64 * w * 8]) + 4096u * k;
-      dma16_pair(rq, rdo, at, at + (uint32_t)sizeof(sm.qs), off, 4096u * k);
+      if constexpr (PACKED) {
+        const int t0 = 64 * w + fresh_lane(), r = t0 / CPR, c = (t0 % CPR) ^ tile_swz<D>(r);
+        dma16(blk_q, at, ch.at(a.p.qs, r + k * (NT / CPR), 8 * c));
+        dma16(blk_do, at + (uint32_t)sizeof(sm.qs), ch.at(a.dos, r + k * (NT / CPR), 8 * c));
+      } else {
+        const int r = tid / CPR, c = (tid % CPR) ^ tile_swz<D>(r);
+        const uint32_t off = (uint32_t)((pb * BM + r) * D + 8 * c) * 2;
+        dma16_pair(rq, rdo, at, at + (uint32_t)sizeof(sm.qs), off, 4096u * k);
+      }
     };
-    auto load_ld = [&](int pb, int b) {
-      const uint32_t row = (uint32_t)(pb * BM + fresh_lane());
-      if (w == 0) dma4(rls, lds_of(&sm.ls[b][0]), row * 4);
-      if (w == 1) dma4(rds, lds_of(&sm.ds[b][0]), row * 4);
+    auto load_ld = [&](Blk pb, int b) {
+      if constexpr (PACKED) {
+        const uint32_t row = (uint32_t)fresh_lane();
+        if (w == 0) dma4(ch.vec(a.lse2, pb), lds_of(&sm.ls[b][0]), row * 4);
+        if (w == 1) dma4(ch.vec(a.dvec, pb), lds_of(&sm.ds[b][0]), row * 4);
+      } else {
+        const uint32_t row = (uint32_t)(pb * BM + fresh_lane());
+        if (w == 0) dma4(rls, lds_of(&sm.ls[b][0]), row * 4);
+        if (w == 1) dma4(rds, lds_of(&sm.ds[b][0]), row * 4);
+      }
     };
-    auto load_block = [&](int pb, int b) {
+    auto load_block = [&](Blk pb, int b) {
 #pragma unroll
       for (int k = 0; k < QLD; ++k) load_part(pb, b, k);
       load_ld(pb, b);
@@ -144,10 +183,28 @@ __global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
     // pb*BM*D, wave w's 32 x 32 tile at w*1024, its chunk k of lane l at k*256 + 4l
     // (row 32 qh0 + l%32 of the block, columns 32 dblk + 8k + 4(l/32) .. +3)
     float* acc_w = &sm.acc[w * 1024];
-    auto acc_off = [&](int pb, int k) { return (uint32_t)(pb * BM * D + w * 1024 + k * 256 + 4 * l) * 4; };
-    auto poll_copy = [&](int pb) { dma4_coherent(rctr, lds_of(&sm.poll[w][0]), (uint32_t)pb * kCtrStride * 4); };
-    auto load_acc = [&](int pb) { dma16x4_coherent(racc, lds_of(acc_w), acc_off(pb, 0), 0u); };
+    auto acc_rsrc = [&](Blk pb) {
+      if constexpr (PACKED) return ch.acc(pb);
+      else return racc;
+    };
+    auto acc_off = [&](Blk pb, int k) {
+      if constexpr (PACKED) return (uint32_t)(w * 1024 + k * 256 + 4 * l) * 4;  // (within the block)
+      else return (uint32_t)(pb * BM * D + w * 1024 + k * 256 + 4 * l) * 4;
+    };
+    auto poll_copy = [&](Blk pb) { dma4_coherent(rctr, lds_of(&sm.poll[w][0]), (uint32_t)ctr_at(pb) * kCtrStride * 4); };
+    auto load_acc = [&](Blk pb) { dma16x4_coherent(acc_rsrc(pb), lds_of(acc_w), acc_off(pb, 0), 0u); };
     auto store_dkdv = [&](int j) {
+      if constexpr (PACKED) {
+        // every wave is past its reads of the Q blocks (the barrier before the last step's
+        // dQ^T): each takes a quarter as its store pad
+        char* pad = (char*)sm.qs + w * (sizeof(sm.qs) / NW);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          store_block32_packed<D, D / 2>(ch.tile(a.dv, a.dvs), (uint32_t)a.dvs.row, ch.partial(1), ch.split, pad, dvacc[kb], 1.f, 64 * w + 32 * kb);
+          store_block32_packed<D, D / 2>(ch.tile(a.dk, a.dks), (uint32_t)a.dks.row, ch.partial(0), ch.split, pad, dkacc[kb], a.scale, 64 * w + 32 * kb);
+        }
+        return;
+      }
       const auto rdk = make_rsrc((__bf16*)a.dk + head, hbytes);
       const auto rdv = make_rsrc((__bf16*)a.dv + head, hbytes);
       const int kv0 = j * BC;
@@ -171,39 +228,85 @@ __global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
 
     int st = next_valid(0);
     int buf = 0;
+    Blk cur{};  // packed: the step's block
+    if constexpr (PACKED) {
+      cur = ch.first();
+      if (nsteps == 0) {  // no query sees the tile
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dkacc[kb][nb][r] = dvacc[kb][nb][r] = 0.f;
+        cur_j = ch.j;
+      }
+    }
     if (st < nsteps) {
-      const int pb0 = step_at(st) & 0xfff;
+      Blk pb0;
+      if constexpr (PACKED) {
+        pb0 = cur;
+        blk_q = ch.q(cur);
+        blk_do = ch.dO(cur);
+      } else {
+        pb0 = step_at(st) & 0xfff;
+      }
       load_block(pb0, buf);
       if (ordered) poll_copy(pb0);
     }
 
     for (; st < nsteps;) {
-      const unsigned e = step_at(st);
-      const int pb = e & 0xfff, j = (e >> 12) & 0x1ff, rank = (e >> 21) & 0x3ff;
-      const bool last = (e >> 31) != 0;
-      const int q0 = pb * BM;
+      Blk pb;
+      int j, rank, q0;
+      bool last;
+      if constexpr (PACKED) {
+        pb = cur;
+        j = rank = ch.j;
+        last = ch.last(pb);
+        q0 = pb.pb * BM + ch.sg.off();  // (as the causal mask counts)
+      } else {
+        const unsigned e = step_at(st);
+        pb = e & 0xfff;
+        j = (e >> 12) & 0x1ff;
+        rank = (e >> 21) & 0x3ff;
+        last = (e >> 31) != 0;
+        q0 = pb * BM;
+      }
 
       if (j != cur_j) {  // new KV tile: flush the previous one, load K / V and the K tile
-        if (cur_j >= 0) store_dkdv(cur_j);
+        if constexpr (!PACKED) {  // (one tile per chain)
+          if (cur_j >= 0) store_dkdv(cur_j);
+        }
         cur_j = j;
         const int kv0 = j * BC;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
-          const int kvr = kv0 + 64 * w + 32 * kb + lc;
+          if constexpr (PACKED) {
+            const int lf = fresh_lane(), row = 64 * w + 32 * kb + (lf & 31);
+            const auto tk = ch.tile(a.k, a.p.ks), tv = ch.tile(a.v, a.p.vs);
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) {
-            kreg[kb][ks] = as_bf16x8(ld16(rk, (uint32_t)(kvr * D + 16 * ks + 8 * g) * 2));
-            vreg[kb][ks] = as_bf16x8(ld16(rv, (uint32_t)(kvr * D + 16 * ks + 8 * g) * 2));
+            for (int ks = 0; ks < KS; ++ks) {
+              kreg[kb][ks] = as_bf16x8(ld16(tk, ch.at(a.p.ks, row, 16 * ks + 8 * (lf >> 5))));
+              vreg[kb][ks] = as_bf16x8(ld16(tv, ch.at(a.p.vs, row, 16 * ks + 8 * (lf >> 5))));
+            }
+          } else {
+            const int kvr = kv0 + 64 * w + 32 * kb + lc;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+              kreg[kb][ks] = as_bf16x8(ld16(rk, (uint32_t)(kvr * D + 16 * ks + 8 * g) * 2));
+              vreg[kb][ks] = as_bf16x8(ld16(rv, (uint32_t)(kvr * D + 16 * ks + 8 * g) * 2));
+            }
           }
         }
         // every wave is past its last dQ^T reads of the previous tile's copy
         __syncthreads();
         {
-          const int r = tid / CPR, c = (tid % CPR) ^ tile_swz<D>(r);
+          const int t0 = PACKED ? 64 * w + fresh_lane() : tid, r = t0 / CPR, c = (t0 % CPR) ^ tile_swz<D>(r);
           const uint32_t at = lds_of(&sm.kt[64 * w * 8]);
 #pragma unroll
-          for (int k = 0; k < KLD; ++k)  // rows 32k + r (the swizzle repeats every 16 rows)
-            dma16(rk, at + 4096u * k, (uint32_t)((kv0 + 32 * k + r) * D + 8 * c) * 2);
+          for (int k = 0; k < KLD; ++k) {  // rows 32k + r (the swizzle repeats every 16 rows)
+            if constexpr (PACKED) dma16(ch.tile(a.k, a.p.ks), at + 4096u * k, ch.at(a.p.ks, 32 * k + r, 8 * c));
+            else dma16(rk, at + 4096u * k, (uint32_t)((kv0 + 32 * k + r) * D + 8 * c) * 2);
+          }
         }
         // wait for the operands here: the K tile is published by the
         // barrier at the top of the step
@@ -232,11 +335,20 @@ __global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
       __syncthreads();
 
       const int nst = next_valid(st + 1);
-      const int pb_next = nst < nsteps ? (int)(step_at(nst) & 0xfff) : -1;
+      Blk pb_next;
+      int more;  // negative after the last step (dense: the next block itself, as in bwd_main.h)
+      if constexpr (PACKED) {
+        pb_next = ch.next(pb);
+        blk_q = ch.q(pb_next);
+        blk_do = ch.dO(pb_next);
+        more = nst < nsteps ? 0 : -1;
+      } else {
+        more = pb_next = nst < nsteps ? (int)(step_at(nst) & 0xfff) : -1;
+      }
       // the chain moves to another KV tile after this step (Symmetric Shift,
       // between its two tiles)
-      const bool tile_ends = nst < nsteps && (int)((step_at(nst) >> 12) & 0x1ff) != j;
-      int* ctr = ctr_head + (size_t)pb * kCtrStride;
+      const bool tile_ends = !PACKED && nst < nsteps && (int)((step_at(nst) >> 12) & 0x1ff) != j;
+      int* ctr = ctr_head + (size_t)ctr_at(pb) * kCtrStride;
       bool have_turn = false;
       const __bf16* qs = sm.qs[buf];
       const __bf16* dos = sm.dos[buf];
@@ -395,12 +507,12 @@ __global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
         // run 1: S/dP of half 0 (key block 0: with the next block's Q / dO /
         // L / D prefetch)
         sdp(0, kb, [&](int k) { rd_rows(1, k); }, [&](int ks) {
-          if (kb > 0 || pb_next < 0) return;
+          if (kb > 0 || more < 0) return;
           if (ks < QLD) load_part(pb_next, buf ^ 1, ks);
           if (ks == 0) load_ld(pb_next, buf ^ 1);
         });
         if (kb == 0) {
-          if (pb_next >= 0) {
+          if (more >= 0) {
             const int n = kBlockLoads + (w < 2 ? 1 : 0);
             vm_poll += n;
             vm_rel += n;
@@ -483,7 +595,7 @@ __global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
         }
         // dq[r] <-> query 32 qh0 + lc, column d = 32 dblk + 8(r/4) + 4g + r%4
 
-        if (a.partials) {
+        if (!PACKED && a.partials) {
           const auto rp = make_rsrc(a.partials + ((size_t)bh * a.tc + j) * N * D, hbytes * 2);
 #pragma unroll
           for (int rb = 0; rb < 4; ++rb)
@@ -511,7 +623,7 @@ __global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
         // this wave's slice (and the next block's Q / dO) have landed
         vm_wait<0>();
         vm_poll = vm_rel = 0;
-        if (ordered && pb_next >= 0) poll_copy(pb_next);
+        if (ordered && more >= 0) poll_copy(pb_next);
         if constexpr (ordered) {
           // ---- add the partial into the slice from registers, one lane per
           //      element: the sum order is the schedule's
@@ -527,12 +639,18 @@ __global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
               f32x4 v = {dq[4 * k], dq[4 * k + 1], dq[4 * k + 2], dq[4 * k + 3]};
               if constexpr (kAdd) v = old[k] + v;
               if constexpr (kLast) {
-                const auto rdq = make_rsrc((__bf16*)a.dq + head, hbytes);
-                const uint32_t off = (uint32_t)((q0 + 32 * qh0 + lc) * D + 32 * dblk + 8 * k + 4 * g);
-                st8(rdq, off * 2, u32x2{pack_bf16(v[0] * a.scale, v[1] * a.scale), pack_bf16(v[2] * a.scale, v[3] * a.scale)});
-                if (a.dq_accum) st16(make_rsrc(a.dq_accum + head, hbytes * 2), off * 4, __builtin_bit_cast(u32x4, v));
+                if constexpr (PACKED) {
+                  const int lf = fresh_lane();
+                  st8(ch.dq(pb), ch.at(a.dqs, 32 * qh0 + (lf & 31), 32 * dblk + 8 * k + 4 * (lf >> 5)),
+                      u32x2{pack_bf16(v[0] * a.scale, v[1] * a.scale), pack_bf16(v[2] * a.scale, v[3] * a.scale)});
+                } else {
+                  const auto rdq = make_rsrc((__bf16*)a.dq + head, hbytes);
+                  const uint32_t off = (uint32_t)((q0 + 32 * qh0 + lc) * D + 32 * dblk + 8 * k + 4 * g);
+                  st8(rdq, off * 2, u32x2{pack_bf16(v[0] * a.scale, v[1] * a.scale), pack_bf16(v[2] * a.scale, v[3] * a.scale)});
+                  if (a.dq_accum) st16(make_rsrc(a.dq_accum + head, hbytes * 2), off * 4, __builtin_bit_cast(u32x4, v));
+                }
               } else {
-                st16_coherent(racc, acc_off(pb, k), __builtin_bit_cast(u32x4, v));
+                st16_coherent(acc_rsrc(pb), acc_off(pb, k), __builtin_bit_cast(u32x4, v));
               }
             }
           };
@@ -546,7 +664,7 @@ __global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
               if (add) finish(T_{}, T_{});
               else finish(F_{}, T_{});
             }
-            vm_poll += last ? (a.dq_accum ? 2 * NACC : NACC) : NACC;
+            vm_poll += last ? (!PACKED && a.dq_accum ? 2 * NACC : NACC) : NACC;
           }
         } else if constexpr (MODE == kModePartials) {
           // ---- the partial goes to KV tile j's own buffer, in the ordered
@@ -579,9 +697,11 @@ __global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
           }
         }
         if (ordered) {
-          if (tid == 0 && a.witness && rank < a.tc) a.witness[((size_t)bh * a.nblk + pb) * a.tc + rank] = j;
-          if (w == 0 && a.witness && rank < a.tc) vm_poll += 1;
-          pend_ctr = pb;
+          if constexpr (!PACKED) {
+            if (tid == 0 && a.witness && rank < a.tc) a.witness[((size_t)bh * a.nblk + pb) * a.tc + rank] = j;
+            if (w == 0 && a.witness && rank < a.tc) vm_poll += 1;
+          }
+          pend_ctr = ctr_at(pb);
           // at the end of the chain or of its KV tile the release comes now: the
           // tile switch (dK, dV stores, K, V loads) would hold it back, and under
           // Symmetric Shift every later contributor of the block, one task behind
@@ -596,6 +716,7 @@ __global__ __launch_bounds__(256) void bwd_main64w_kernel(BwdArgs a) {
       }
       buf ^= 1;
       st = nst;
+      if constexpr (PACKED) cur = pb_next;
     }
     if (cur_j >= 0) store_dkdv(cur_j);
     __syncthreads();  // sm.item is rewritten by the next ticket
@@ -619,6 +740,12 @@ hipError_t launch_mask(const BwdArgs& a, int grid, hipStream_t stream) {
 
 hipError_t launch_main64w(const BwdArgs& a, int grid_main, hipStream_t stream) {
   return a.G.causal ? launch_mask<true>(a, grid_main, stream) : launch_mask<false>(a, grid_main, stream);
+}
+
+hipError_t launch_packed_main64w(const PackedBwdArgs& a, int grid, hipStream_t stream) {
+  if (a.p.causal) hipLaunchKernelGGL((bwd_main64w_kernel<true, kModeOrdered, false, PackedBwdArgs>), dim3(grid), dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((bwd_main64w_kernel<false, kModeOrdered, false, PackedBwdArgs>), dim3(grid), dim3(256), 0, stream, a);
+  return hipGetLastError();
 }
 
 int bwd_main64w_occupancy() {

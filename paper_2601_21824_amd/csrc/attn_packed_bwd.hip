@@ -1,7 +1,7 @@
 // attn_packed_bwd.hip -- the deterministic backward over packed sequences: the kernel
 // before the main kernel, and the launch sequence of a call.  The main kernels are
-// bwd_main.h (128-row KV tiles at d = 64 and 128) and attn_bwdw.hip (256 rows at d =
-// 128, 128 at d = 256) on the chains of packed_chain.h, with the ordered dQ reduction
+// bwd_main.h (128-row KV tiles at d = 64 and 128), attn_bwd64w.hip (256 rows at d = 64) and
+// attn_bwdw.hip (256 rows at d = 128, 128 at d = 256) on the chains of packed_chain.h, with the ordered dQ reduction
 // of the dense calls in Descending order.
 //
 // packed_pre: D = rowsum(dO o O) and L log2(e) (+inf for a row that sees nothing, so that
@@ -237,11 +237,11 @@ hipError_t launch(const PackedBwdArgs& a, int cus, hipStream_t stream) {
     hipLaunchKernelGGL((packed_pre_kernel<D, 1>), dim3((unsigned)(rows * a.p.heads_q + rest)), dim3(256), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  // persistent workgroups: as many as stay resident (two per CU at d = 64, else one).
+  // persistent workgroups: as many as stay resident (two per CU at d = 64 and 128 rows, else one).
   // A chain waits only on chains that took an earlier ticket, so any count is safe.
-  const long items = (long)a.slots_k * a.p.heads_q, cap = (long)cus * (D == 64 ? 2 : 1);
+  const long items = (long)a.slots_k * a.p.heads_q, cap = (long)cus * (D == 64 && a.bc == 128 ? 2 : 1);
   const int g = (int)(items < cap ? items : cap);
-  if constexpr (D == 64) e = launch_packed_main64(a, g, stream);
+  if constexpr (D == 64) e = a.bc == 256 ? launch_packed_main64w(a, g, stream) : launch_packed_main64(a, g, stream);
   else if constexpr (D == 256) e = launch_packed_mainw(a, D, g, stream);
   else e = a.bc == 256 ? launch_packed_mainw(a, D, g, stream) : launch_packed_main128(a, g, stream);
   if (e != hipSuccess || a.p.heads_q == a.p.heads_kv) return e;
@@ -253,7 +253,7 @@ hipError_t launch(const PackedBwdArgs& a, int cus, hipStream_t stream) {
 
 }  // namespace
 
-// d = 128 has both tiles.  Wide ones need chains enough for 256 CUs (split by query
+// d = 64 and 128 have both tiles.  Wide ones at d = 128 need chains enough for 256 CUs (split by query
 // head, total_k / 256 times heads_q; longer ones weigh more under a causal mask) and
 // sequences that fill them.  Measured (us, narrow / wide; heads_q over heads_kv):
 //   causal  352 chains of one of 3000 385 / 348, 384 (4096, 24 over 8) 511 / 466, 512 (2048
@@ -263,9 +263,18 @@ hipError_t launch(const PackedBwdArgs& a, int cus, hipStream_t stream) {
 //           causal) 264 / 363
 //   length  1024 chains of 16 of 512 292 / 272; 24 of 384 233 / 314, 32 of 256 159 / 226, 10 of 409
 //           on average 180 / 200
+// d = 64 likewise, for longer causal sequences:
+//   causal  512 chains (4096, 32 over 8) 421 / 354, 384 (2048, 48 over 8) 192 / 172, 380 (5000, 20 over 4)
+//           408 / 354; 320 (4096, 20 over 4) 285 / 313, 256 (8192, 8 over 1) 463 / 541
+//   full    176 (3000, 16 over 4) 285 / 260, 256 (2048, 32 over 32) 202 / 175; 128 (4096, 8 over 8) 265 / 329
+//   length  causal 8 of 1024 255 / 219, 4 of 2048 414 / 360; 11 of 768 202 / 228, 14 of 600 180 / 203 (but 13
+//           of 640, 32 over 32, 201 / 183); full 32 of 256 122 / 98, 24 of 341 on average 279 / 262, 40 of 200
+//           158 / 161 (but 16 of 520 313 / 328)
 int packed_tile_rows(int d, int total_k, int batch, int heads_q, int causal) {
   const long chains = (long)(total_k / 256) * heads_q;
-  return d == 128 && chains >= (causal ? 320 : 160) && total_k >= 480L * batch ? 256 : 128;
+  if (d == 128) return chains >= (causal ? 320 : 160) && total_k >= 480L * batch ? 256 : 128;
+  if (d == 64) return chains >= (causal ? 352 : 160) && total_k >= (causal ? 800L : 256L) * batch ? 256 : 128;
+  return 128;
 }
 
 hipError_t launch_packed_bwd(const PackedBwdArgs& a, int d, int cus, hipStream_t stream) {

@@ -97,6 +97,7 @@ constexpr int kCtrlHeads = 50;  // ctrl[] slot: query heads of a part of those
 int packed_tile_rows(int d, int total_k, int batch, int heads_q, int causal);
 hipError_t launch_packed_bwd(const PackedBwdArgs& a, int d, int cus, hipStream_t stream);
 hipError_t launch_packed_main64(const PackedBwdArgs& a, int grid, hipStream_t stream);   // attn_bwd_d64.hip
+hipError_t launch_packed_main64w(const PackedBwdArgs& a, int grid, hipStream_t stream);  // attn_bwd64w.hip
 hipError_t launch_packed_main128(const PackedBwdArgs& a, int grid, hipStream_t stream);  // attn_bwd.hip
 hipError_t launch_packed_mainw(const PackedBwdArgs& a, int d, int grid, hipStream_t stream);  // attn_bwdw.hip
 

@@ -192,6 +192,29 @@ def test_backward_large(d, hq, hkv, lens, causal):
         assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(out, again))
 
 
+# 256-row KV tiles at d = 64: queries other than keys (rows that see nothing, keys that none
+# sees), lengths at a tile's edges, split chains, the tile's last rows past a sequence
+@pytest.mark.parametrize("hq,hkv,qlens,klens,causal,layout", [
+    (32, 32, [1023, 1281, 1, 1500], [1023, 1281, 1, 1500], True, "packed"), (48, 8, [2049, 640], [2049, 640], True, "fused"),
+    (64, 4, [257, 900, 31], [1700, 900, 900], True, "packed"), (64, 64, [1500, 700], [1100, 1000], True, "packed"),
+    (20, 20, [300, 0, 256, 700], [257, 600, 256, 1300], False, "heads"), (40, 8, [64, 1000], [1025, 512], False, "packed")])
+def test_backward_wide_d64(hq, hkv, qlens, klens, causal, layout):
+    same = qlens == klens
+    q, k, v, do = packed_inputs(qlens, klens, hq, hkv, 64, layout, tail=5)
+    cu_q, cu_k = cu_of(qlens), None if same else cu_of(klens)
+    out = train(q, k, v, do, cu_q, cu_k, causal)
+    ref = reference(q, k, v, do, qlens, klens, causal, 1 / math.sqrt(64))
+    for name, got, n in zip("qkv", out, (sum(qlens), sum(klens), sum(klens))):
+        assert bool((got[n:] == 7).all()), "rows behind the last sequence"
+        e = (got.double() - ref["d" + name])[:n]
+        # (the repository's tolerance, as above)
+        assert float(e.norm() / ref["d" + name].norm()) <= 5e-3
+        assert float(e.abs().max() / ref["d" + name].abs().max()) <= 2e-2
+    for _ in range(4):
+        again = train(q, k, v, do, cu_q, cu_k, causal)
+        assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(out, again))
+
+
 def test_no_queries_no_keys_one_row():
     """Tensors of no rows on either side; one row, whose strides say nothing (a broadcast)."""
     kv = torch.randn((300, 2, 64), device="cuda").to(BF)
