@@ -2,17 +2,19 @@
  * dash.h -- C ABI of libdash: deterministic FlashAttention backward for
  * AMD Instinct MI355X (gfx950), with the dQ reduction order scheduled as in
  * "DASH: Deterministic Attention Scheduling for High-throughput Reproducible
- * LLM Training" (arXiv 2601.21824).
+ * LLM Training" (arXiv 2601.21824), over dense batches and over packed sequences
+ * of different lengths; and attention over a paged key-value cache.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
  *  - All tensor pointers are DEVICE pointers owned by the caller.  The library
  *    keeps no pointer after a call returns.
- *  - q, k, v, o, dO, dq, dk, dv: bf16 values (stored as uint16_t), layout
+ *  - q, k, v, o, dO, dq, dk, dv: bf16 values (stored as uint16_t), in the dense calls
+ *    (those with B, H and N; the others' layouts stand in their section) of layout
  *    [B][H][N][d], row-major and contiguous (one head = an N x d matrix).
  *  - lse: fp32 [B][H][N], the natural-log logsumexp of the scaled scores of
  *    each query row (the "logsumexp vector L" that Algorithm 1 takes as input).
- *  - Self-attention only: N queries attend to N keys.  With causal != 0,
+ *  - Dense calls are self-attention only: N queries attend to N keys.  With causal != 0,
  *    query i sees key j iff j <= i.
  *  - d must be 64, 128 or 256.  N >= 0 is arbitrary (ragged last tiles are masked);
  *    B, H >= 0, B*H*N < 2^30.  A problem with B*H*N == 0 is a successful no-op.

@@ -21,10 +21,14 @@
 // the softmax scale and V's into the output.
 //
 // The keys of all sequences are cut into chunks of one size, found on the device
-// from lens (so that a captured call follows them): the sum over `workers`, at
-// least 128.  A sequence of one chunk is written at once; the others' chunks leave
+// from lens (so that a captured call follows them): the sum over `workers`.  A sequence of one chunk is written at once; the others' chunks leave
 // (m, sum, O) in fp32 and join_kernel adds them in order.  The chunk size, and so
 // the order of the sums, is fixed by lens and the call's shape, never by timing.
+// (Chunks of at least 128 keys: one tile for each wave.)
+//
+// Measured, 32 heads over 8 of 128: 131072 keys of 64 sequences in bf16 97 us, 5.5 TB/s,
+// and 5 us of joins; of one sequence in e4m3 43 us, 6.2 TB/s, and 6.4; 901 keys, 8 heads over 2 of
+// 64, whole, 8.9 us (four tiles a wave, one after the other).
 #include "common.h"
 #include "ops.h"
 #include "page_index.h"
@@ -273,7 +277,8 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(DecodeArgs a) {
 }
 
 // The chunks of one sequence and query head, in order: thread groups of D/4 lanes
-// take every NG-th chunk and are added in order of the group.
+// take every NG-th chunk and are added in order of the group.  Bound by latency: 128 chunks
+// of 32 heads 8.6 us with one chunk's loads in flight, 6.7 with four, 6.4 with eight.
 template <int D>
 __global__ __launch_bounds__(256) void join_kernel(DecodeArgs a) {
   constexpr int NG = 256 / (D / 4), U = 8;  // U chunks' loads in flight together

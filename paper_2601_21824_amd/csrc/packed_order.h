@@ -69,8 +69,8 @@ struct SeqGeom {
 // one chain it would outlast the rest of the call.  A split is `parts` chains of up
 // to ceil(group / parts) heads for every tile whose chain has more than `above` blocks.
 // Which one: the least of split_cost over kSplits choices, in block steps of a worker.
-// It asks the lengths and the constant kSplitWorkers, not the device, so that the
-// sums' order depends on the lengths alone.
+// It asks the lengths and a constant number of workers (the 256 CUs), not the device, so
+// that the sums' order depends on the lengths alone.
 constexpr int kSplitWorkers = 256;
 constexpr int kSplitLimits = 8, kSplitParts = 8, kSplits = kSplitLimits * kSplitParts;
 // limit i: a tile is long whose whole chain is over 2^-i of a worker's share
@@ -83,7 +83,7 @@ DASH_ORDER_HD int split_parts(int group, int heads) { return (group + heads - 1)
 // share: steps of all chains over the workers; longest: blocks of the longest chain;
 // n_long: tiles with more than `above` blocks; heads: per part (group: none is split).
 // Unsplit chains start last, so that on average half of one stands over at the end;
-// writing and reading a part's partials costs 6 steps (by 3, 12 sequences of 8192 tokens, 32
+// writing and reading a part's partials counts as 6 steps (by 3, 12 sequences of 8192 tokens, 32
 // heads over 8, took one head a part, 474 us, by 5 to 12 two, 420).
 DASH_ORDER_HD long split_cost(long share, long longest, long above, long n_long, int heads, int group, int heads_kv) {
   const bool whole = heads >= group;
@@ -95,8 +95,8 @@ DASH_ORDER_HD long split_cost(long share, long longest, long above, long n_long,
   t = t > part ? t : part;
   return t + 6 * n_long * heads_kv * split_parts(group, heads) / kSplitWorkers;
 }
-// Partials there is room for (each of a part's dK and dV): a tile is never split finer
-// than costs less than its steps, i.e. more than `share` steps' worth of partials in all.
+// Parts there is room for (a part is its dK and its dV); a choice that needs more is not
+// taken: all chains in parts of one head where those are few, else eight for every worker.
 DASH_ORDER_HD int split_room(int slots, int heads_q) {
   const long all = (long)slots * heads_q;
   return all < 8 * kSplitWorkers ? (int)all : 8 * kSplitWorkers;
