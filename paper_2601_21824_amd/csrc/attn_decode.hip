@@ -87,9 +87,7 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(DecodeArgs a) {
     len = b + l < c.batch ? clamp_len(c.lens[b + l], c.table_width, c.page_size) : 0;
     total += wave_sum(len >> 12) * 4096l + wave_sum(len & 4095);
   }
-  // (a chunk past 2^31 - 1 keys holds any sequence, as 2^30 does)
-  const int64_t chunk64 = a.workers > 0 ? chunk_keys(total, a.workers) : (int64_t)1 << 30;
-  const int chunk = __builtin_amdgcn_readfirstlane(chunk64 < (1 << 30) ? (int)chunk64 : 1 << 30);
+  const int chunk = __builtin_amdgcn_readfirstlane(chunk_size(total, a.workers));
   int s = -1, i = 0, n = 0;
   for (int b = 0, before = 0; b < c.batch; b += 64) {
     if (c.batch > 64) len = b + l < c.batch ? clamp_len(c.lens[b + l], c.table_width, c.page_size) : 0;

@@ -10,6 +10,7 @@
 #include "dash.h"
 #include "ops.h"
 #include "packed_order.h"
+#include "page_index.h"
 
 namespace {
 
@@ -76,7 +77,7 @@ int check_cache(const dash_paged_cache_t* c, bool written) {
     return fail(DASH_ERR_INVALID_ARG, "k_scale and v_scale are for E4M3 caches");
   if (c->page_size < 16 || c->page_size % 16 || c->page_size > 65536)
     return fail(DASH_ERR_INVALID_ARG, "page_size must be a multiple of 16, at most 65536");
-  if (c->table_width < 0 || (int64_t)c->table_width * c->page_size > 0x7fffff00)
+  if (c->table_width < 0 || (int64_t)c->table_width * c->page_size > dash::kMaxKeys)
     return fail(DASH_ERR_INVALID_ARG, "table_width must be >= 0 and table_width * page_size below 2^31 - 255");
   if (c->batch == 0) return DASH_OK;
   if (c->pages < 1) return fail(DASH_ERR_INVALID_ARG, "pages must be >= 1");
@@ -369,7 +370,7 @@ size_t dash_decode_workspace_size(int batch, int heads_q, int heads_kv, int d, i
   size_t bytes = 0;
   guarded([&] {
     if (check_heads(batch, heads_q, heads_kv, d) == DASH_OK && page_size >= 16 && page_size % 16 == 0 && page_size <= 65536 &&
-        table_width >= 0 && (int64_t)table_width * page_size <= 0x7fffff00)
+        table_width >= 0 && (int64_t)table_width * page_size <= dash::kMaxKeys)
       bytes = decode_layout(batch, heads_q, heads_kv, d, table_width * page_size).total;
     return 0;
   });

@@ -42,6 +42,13 @@ DASH_PAGE_HD int64_t chunk_keys(int64_t total, int workers) {
   const int64_t c = (per + kMinChunk - 1) / kMinChunk * kMinChunk;
   return c < kMinChunk ? kMinChunk : c;
 }
+// What a call takes: no table holds more than kMaxKeys, so a chunk of as many is any
+// sequence whole, and the bound holds for longer ones as well.  workers 0: all whole.
+constexpr int kMaxKeys = 0x7fffff00;
+DASH_PAGE_HD int chunk_size(int64_t total, int workers) {
+  const int64_t c = workers > 0 ? chunk_keys(total, workers) : kMaxKeys;
+  return c < kMaxKeys ? (int)c : kMaxKeys;
+}
 DASH_PAGE_HD int chunks_of(int len, int64_t chunk) { return len > 0 ? (int)((len + chunk - 1) / chunk) : 1; }
 
 }  // namespace dash

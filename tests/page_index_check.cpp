@@ -52,6 +52,15 @@ int main() {
     CHECK(slots <= (int64_t)workers + batch);
   }
   CHECK(chunk_keys((int64_t)1 << 50, 1) == (int64_t)1 << 50);
+  // sequences as long as a table can hold (they may share pages): the slots still suffice
+  for (int batch : {1, 3, 70, 200})
+    for (int workers : {0, 1, 2, 128, 1024}) {
+      const int len = kMaxKeys - batch % 3;
+      const int chunk = chunk_size((int64_t)batch * len, workers);
+      CHECK(chunk % 128 == 0);
+      CHECK((int64_t)batch * chunks_of(len, chunk) <= (int64_t)workers + batch);
+    }
+  CHECK(chunk_size(1000, 4) == chunk_keys(1000, 4) && chunk_size((int64_t)1 << 50, 1) == kMaxKeys);
   std::printf("%s\n", bad ? "FAILED" : "ok");
   return bad != 0;
 }
