@@ -119,8 +119,7 @@ def load():
         for f in ("dash_attn_fwd", "dash_attn_fwd_ex", "dash_attn_bwd", "dash_attn_bwd_ex", "dash_attn_bwd_noalloc",
                   "dash_bwd_check", "dash_resolve_schedule", "dash_schedule_table", "dash_bwd_placement",
                   "dash_mfma_peak", "dash_auto_schedule", "dash_model_makespan", "dash_kv_append", "dash_attn_decode",
-                  "dash_attn_packed_fwd", "dash_attn_packed_bwd",
-           "dash_packed_workspace_size"):
+                  "dash_attn_packed_fwd", "dash_attn_packed_bwd"):
             getattr(lib, f).restype = ci
         _lib = lib
     return _lib

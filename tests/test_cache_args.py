@@ -85,6 +85,7 @@ def test_decode_arguments():
     assert need > 0
     for ws, n in ((None, need), (P, need - 1), (P + 16, need)):
         assert run_decode(cache(), ws=ws, ws_bytes=n) == b.DASH_ERR_INVALID_ARG and "workspace" in b.dash_last_error()
+    assert b.dash_decode_workspace_size(1 << 16, 64, 64, 256, 16, 1 << 20) >= (1 << 16) * 64 * 256 * 4  # past 2^31
     assert b.dash_decode_workspace_size(2, 8, 3, 128, 16, 4) == 0
     assert b.dash_decode_workspace_size(2, 8, 2, 96, 16, 4) == 0
     assert b.dash_decode_workspace_size(2, 8, 2, 128, 8, 4) == 0

@@ -215,6 +215,21 @@ def test_backward_wide_d64(hq, hkv, qlens, klens, causal, layout):
         assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(out, again))
 
 
+def test_backward_accumulators_past_2_gib():
+    """130 sequences of 1000, 32 heads over 8: dQ's fp32 blocks alone are 2.2 GB.  The last two
+    sequences against the definition."""
+    lens, hq, hkv, d = [1000] * 130, 32, 8, 128
+    q, k, v, do = packed_inputs(lens, lens, hq, hkv, d)
+    assert dash.dash_packed_workspace_size(len(lens), sum(lens), sum(lens), hq, hkv, d) > 1 << 31
+    out = train(q, k, v, do, cu_of(lens), None, True)
+    ref = reference(*(x[-2000:] for x in (q, k, v, do)), lens[-2:], lens[-2:], True, 1 / math.sqrt(d))
+    for name, got in zip("qkv", out):
+        e = got[-2000:].double() - ref["d" + name]
+        assert float(e.norm() / ref["d" + name].norm()) <= 5e-3
+        assert float(e.abs().max() / ref["d" + name].abs().max()) <= 2e-2
+        assert bool(got.isfinite().all())
+
+
 def test_no_queries_no_keys_one_row():
     """Tensors of no rows on either side; one row, whose strides say nothing (a broadcast)."""
     kv = torch.randn((300, 2, 64), device="cuda").to(BF)

@@ -74,6 +74,8 @@ def test_pointers_and_workspace():
         assert bwd(problem(), ws=ws, ws_bytes=n) == b.DASH_ERR_INVALID_ARG and "workspace" in b.dash_last_error()
     for bad in ((2, 300, 300, 8, 3, 128), (2, 300, 300, 8, 2, 100), (-1, 300, 300, 8, 2, 128), (2, -1, 300, 8, 2, 128)):
         assert b.dash_packed_workspace_size(*bad) == 0
+    # sizes past 2^31 bytes come through whole
+    assert b.dash_packed_workspace_size(64, 1 << 20, 1 << 20, 32, 8, 128) >= (1 << 20) * 32 * 128 * 4
 
 
 def test_forward_workspace():
