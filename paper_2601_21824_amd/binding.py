@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -75,6 +76,24 @@ class dash_packed_t(ctypes.Structure):
     _fields_ += [(f"{t}_{s}_stride", _I64) for t in ("q", "k", "v", "o", "do", "dq", "dk", "dv") for s in ("row", "head")]
 
 
+def _packer(cls):
+    """A function from a C struct's values, by position, to its bytes, in a third of the time
+    that ctypes takes for its fields.  Pointers are ints here, 0 for none."""
+    code = {_CI: "i", ctypes.c_float: "f", _I64: "q", _VP: "P"}
+    fmt = struct.Struct("@" + "".join(code[t] for _, t in cls._fields_))
+    for i, (name, t) in enumerate(cls._fields_):  # the same layout
+        head = struct.calcsize("@" + "".join(code[u] for _, u in cls._fields_[:i]) + "0" + code[t])
+        assert getattr(cls, name).offset == head and fmt.size <= ctypes.sizeof(cls)
+
+    def pack(*values):
+        try:
+            return fmt.pack(*values)
+        except (struct.error, OverflowError) as e:
+            _bad(f"{cls.__name__}: {e}")
+    return pack
+
+
+_pack_cache, _pack_append, _pack_packed = map(_packer, (dash_paged_cache_t, dash_append_t, dash_packed_t))
 _lib = None
 
 
@@ -103,14 +122,15 @@ def load():
         dp = ctypes.POINTER(ctypes.c_double)
         lib.dash_auto_schedule.argtypes = [ci] * 6 + [ip, dp]
         lib.dash_model_makespan.argtypes = [ci] * 9 + [ctypes.c_double, ctypes.c_double, dp]
-        lib.dash_kv_append.argtypes = [ctypes.POINTER(dash_paged_cache_t), ctypes.POINTER(dash_append_t), vp, vp]
-        lib.dash_attn_decode.argtypes = [ctypes.POINTER(dash_paged_cache_t), vp, _I64, _I64, vp, _I64, _I64, vp, cf, vp,
+        # (the structs as void pointers: bytes are one as well)
+        lib.dash_kv_append.argtypes = [vp, vp, vp, vp]
+        lib.dash_attn_decode.argtypes = [vp, vp, _I64, _I64, vp, _I64, _I64, vp, cf, vp,
                                          sz, vp, vp]
         lib.dash_decode_workspace_size.argtypes = [ci] * 6
-        lib.dash_attn_packed_bwd.argtypes = [ctypes.POINTER(dash_packed_t)] + [vp] * 10 + [sz, vp, vp]
+        lib.dash_attn_packed_bwd.argtypes = [vp] * 11 + [sz, vp, vp]
         lib.dash_packed_workspace_size.argtypes = [ci] * 6
         lib.dash_packed_workspace_size.restype = sz
-        lib.dash_attn_packed_fwd.argtypes = [ctypes.POINTER(dash_packed_t)] + [vp] * 6 + [sz, vp]
+        lib.dash_attn_packed_fwd.argtypes = [vp] * 7 + [sz, vp]
         lib.dash_packed_fwd_workspace_size.argtypes = [ci] * 6
         lib.dash_packed_fwd_workspace_size.restype = sz
         lib.dash_decode_workspace_size.restype = sz
@@ -303,9 +323,9 @@ def _rows(name, t, dtype, dev, rows, heads, d):
 
 
 def _flat(name, t, dtype, dev, n):
-    """A contiguous tensor of n values on GPU `dev`, or None: its pointer."""
+    """A contiguous tensor of n values on GPU `dev`, or None: its pointer (0 for None)."""
     if t is None:
-        return None
+        return 0
     if t.dtype is not dtype or t.get_device() != dev or t.numel() != n or not t.is_contiguous():
         _bad(f"{name} must be a contiguous {dtype} tensor of {n} values on cuda:{dev}")
     return t.data_ptr()
@@ -319,20 +339,24 @@ def _gpu(t):
     return dev
 
 
-def _space(workspace, need, dev, stream):
-    """A call's workspace (allocated if there is none, behind the current stream's work): pointer and bytes."""
+def _space(workspace, need, like, dev, stream):
+    """A call's workspace (allocated beside `like` if there is none, behind the current
+    stream's work): pointer, bytes and tensor."""
     import torch
     if workspace is None:
         if stream is not None:
             _bad("a call on an explicit stream needs an explicit workspace")
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=torch.device("cuda", dev))
-    return _flat("workspace", workspace, torch.uint8, dev, workspace.numel()), workspace.numel(), workspace
+        need = need if need > 256 else 256
+        workspace = like.new_empty(need, dtype=torch.uint8)
+        return workspace.data_ptr(), need, workspace
+    n = workspace.numel()
+    return _flat("workspace", workspace, torch.uint8, dev, n), n, workspace
 
 
 def _call(f, dev, stream, *args):
     """f(*args, stream) with GPU `dev` current, as the library launches on the current one."""
     import torch
-    if torch.cuda.current_device() != dev:
+    if torch._C._cuda_getDevice() != dev:
         with torch.cuda.device(dev):
             return _call(f, dev, stream, *args)
     if stream is None:
@@ -361,7 +385,7 @@ def _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q, dev):
     row, one = block_table.stride()
     if rows != batch or (width > 1 and one != 1):
         _bad("block_table must be [batch, width] with contiguous rows")
-    return dash_paged_cache_t(
+    return _pack_cache(
         batch, heads_q, heads_kv, d, pages, page, width, DASH_CACHE_BF16 if dt is torch.bfloat16 else DASH_CACHE_E4M3,
         k_cache.data_ptr(), v_cache.data_ptr(), kp, kh, kr, vp, vh, vr, block_table.data_ptr(), row if batch > 1 else width,
         _flat("lens", lens, torch.int32, dev, batch), _flat("k_scale", k_scale, torch.float32, dev, heads_kv),
@@ -390,16 +414,16 @@ def dash_kv_append(k, v, k_cache, v_cache, block_table, lens, cu=None, q=None, q
     bf, i32 = torch.bfloat16, torch.int32
     if k_cache.shape[1] != heads_kv or k_cache.shape[3] != d:
         _bad("k and k_cache must have the same heads and head dim")
-    none = (None, 0, 0)
+    none = (0, 0, 0)
     kp, *ks = _rows("k", k, bf, dev, tokens, heads_kv, d)
     vp, *vs = _rows("v", v, bf, dev, tokens, heads_kv, d)
     qp, *qs = none if q is None else _rows("q", q, bf, dev, tokens, heads_q, d)
     qo, *qos = none if q is None else _rows("q_out", q_out, bf, dev, tokens, heads_q, d)
     ko, *kos = none if k_out is None else _rows("k_out", k_out, bf, dev, tokens, heads_kv, d)
     rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-    x = dash_append_t(tokens, _flat("cu", cu, i32, dev, lens.numel() + 1), kp, vp, qp, qo, ko, *ks, *vs, *qs, *qos, *kos,
-                      _flat("inv_freq", inv_freq, torch.float32, dev, rot // 2), rot, interleaved)
-    _call(load().dash_kv_append, dev, stream, ctypes.byref(c), ctypes.byref(x), _flat("status", status, i32, dev, 1))
+    x = _pack_append(tokens, _flat("cu", cu, i32, dev, lens.numel() + 1), kp, vp, qp, qo, ko, *ks, *vs, *qs, *qos, *kos,
+                     _flat("inv_freq", inv_freq, torch.float32, dev, rot // 2), rot, interleaved)
+    _call(load().dash_kv_append, dev, stream, c, x, _flat("status", status, i32, dev, 1))
 
 
 def dash_decode_workspace_size(batch: int, heads_q: int, heads_kv: int, d: int, page_size: int, table_width: int) -> int:
@@ -424,8 +448,8 @@ def dash_attn_decode(q, k_cache, v_cache, block_table, lens, o, lse=None, scale=
         _bad("q, lens and the caches must have the same batch and head dim")
     lib = load()
     need = 0 if workspace is not None else lib.dash_decode_workspace_size(batch, heads_q, heads_kv, d, page, block_table.shape[1])
-    ws, size, workspace = _space(workspace, need, dev, stream)
-    _call(lib.dash_attn_decode, dev, stream, ctypes.byref(c), *_rows("q", q, torch.bfloat16, dev, batch, heads_q, d),
+    ws, size, workspace = _space(workspace, need, q, dev, stream)
+    _call(lib.dash_attn_decode, dev, stream, c, *_rows("q", q, torch.bfloat16, dev, batch, heads_q, d),
           *_rows("o", o, torch.bfloat16, dev, batch, heads_q, d), _flat("lse", lse, torch.float32, dev, batch * heads_q),
           0.0 if scale is None else scale, ws, size, _flat("status", status, torch.int32, dev, 1))
 
@@ -436,6 +460,9 @@ def attn_decode(q, k_cache, v_cache, block_table, lens, scale=None, k_scale=None
     o = torch.empty_like(q, memory_format=torch.contiguous_format)
     dash_attn_decode(q, k_cache, v_cache, block_table, lens, o, None, scale, k_scale, v_scale, workspace, status)
     return o
+
+
+_NO_STRIDES = (0,) * 8
 
 
 def _packed(q, k, v, o, cu_q, cu_k, causal, scale, dev, *rest):
@@ -455,8 +482,8 @@ def _packed(q, k, v, o, cu_q, cu_k, causal, scale, dev, *rest):
     kp, k0, k1 = _rows("k", k, bf, dev, tk, hkv, d)
     vp, v0, v1 = _rows("v", v, bf, dev, tk, hkv, d)
     op, o0, o1 = _rows("o", o, bf, dev, tq, hq, d)
-    return dash_packed_t(n - 1, hq, hkv, d, causal, tq, tk, 0.0 if scale is None else scale, _flat("cu_q", cu_q, i32, dev, n),
-                         _flat("cu_k", cu_k, i32, dev, n), q0, q1, k0, k1, v0, v1, o0, o1, *rest), qp, kp, vp, op
+    return _pack_packed(n - 1, hq, hkv, d, causal, tq, tk, 0.0 if scale is None else scale, _flat("cu_q", cu_q, i32, dev, n),
+                        _flat("cu_k", cu_k, i32, dev, n), q0, q1, k0, k1, v0, v1, o0, o1, *(rest or _NO_STRIDES)), qp, kp, vp, op
 
 
 def dash_packed_fwd_workspace_size(batch: int, total_q: int, total_k: int, heads_q: int, heads_kv: int, d: int) -> int:
@@ -473,8 +500,8 @@ def dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k=None, causal: bool = True, 
     import torch
     dev = _gpu(q)
     p, qp, kp, vp, op = _packed(q, k, v, o, cu_q, cu_k, causal, scale, dev)
-    ws, size = (None, 0) if workspace is None else _space(workspace, 0, dev, stream)[:2]
-    _call(load().dash_attn_packed_fwd, dev, stream, ctypes.byref(p), qp, kp, vp, op,
+    ws, size = (0, 0) if workspace is None else _space(workspace, 0, q, dev, stream)[:2]
+    _call(load().dash_attn_packed_fwd, dev, stream, p, qp, kp, vp, op,
           _flat("lse", lse, torch.float32, dev, q.shape[0] * q.shape[1]), ws, size)
 
 
@@ -487,7 +514,7 @@ def attn_packed_fwd(q, k, v, cu_q, cu_k=None, causal: bool = True, scale=None):
     o = torch.empty_like(q, memory_format=torch.contiguous_format)
     lse = q.new_empty((hq, tq), dtype=torch.float32)
     n = load().dash_packed_fwd_workspace_size(cu_q.numel() - 1, tq, tk, hq, hkv, d)
-    dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k, causal, scale, _space(None, n, dev, None)[2] if n else None)
+    dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k, causal, scale, _space(None, n, q, dev, None)[2] if n else None)
     return o, lse
 
 
@@ -514,8 +541,8 @@ def dash_attn_packed_bwd(q, k, v, o, dO, lse, dq, dk, dv, cu_q, cu_k=None, causa
     p, qp, kp, vp, op = _packed(q, k, v, o, cu_q, cu_k, causal, scale, dev, *dos, *dqs, *dks, *dvs)
     lib = load()
     need = 0 if workspace is not None else lib.dash_packed_workspace_size(cu_q.numel() - 1, tq, tk, hq, hkv, d)
-    ws, size, workspace = _space(workspace, need, dev, stream)
-    _call(lib.dash_attn_packed_bwd, dev, stream, ctypes.byref(p), qp, kp, vp, op, do,
+    ws, size, workspace = _space(workspace, need, q, dev, stream)
+    _call(lib.dash_attn_packed_bwd, dev, stream, p, qp, kp, vp, op, do,
           _flat("lse", lse, torch.float32, dev, hq * tq), a, b, c, ws, size, _flat("status", status, torch.int32, dev, 1))
 
 
