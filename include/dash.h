@@ -390,9 +390,10 @@ typedef struct {
 /* New tokens of dash_kv_append. */
 typedef struct {
   int tokens;
-  /* [batch + 1]: the tokens of sequence s are rows cu[s] .. cu[s+1]-1.  Rows from
-     cu[batch] on are left alone, in q_out and k_out too.  NULL: one token per
-     sequence (tokens == batch). */
+  /* [batch + 1], rising from 0 or more: the tokens of sequence s are rows cu[s] ..
+     cu[s+1]-1.  Rows before cu[0] and from cu[batch] on belong to nobody: they are not
+     stored, and left alone in q_out and k_out.  So are rows between offsets that do not
+     rise, as far as no sequence holds them.  NULL: one token per sequence (tokens == batch). */
   const int32_t* cu;
   const void* k; /* bf16 [tokens][heads_kv][d] */
   const void* v;
@@ -418,7 +419,8 @@ typedef struct {
  * saturated at 448.  status: NULL or a device int that the call sets to 1
  * when a token's place lies outside its row of block_table or in a page
  * outside 0 .. pages-1 (that token is not stored; its q_out and k_out are still
- * written).  The call never sets it to 0.
+ * written), or when offsets that do not rise leave a row without a sequence.  The call
+ * never sets it to 0.
  */
 int dash_kv_append(const dash_paged_cache_t* cache, const dash_append_t* x, int* status, void* stream);
 

@@ -60,8 +60,13 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, in
   int s = t, place = 0;
   if (a.cu) {
     s = find_sequence(a.cu, c.batch, t, l);
-    if (s < 0) return;  // behind the last sequence
-    place = t - a.cu[s];
+    if (s < 0) return;  // before the first sequence or behind the last
+    const int start = a.cu[s], end = a.cu[s + 1];
+    if (start < 0 || t < start || t >= end) {  // offsets that do not rise from 0 on: nobody's row
+      if (l == 0 && c.status) *c.status = 1;
+      return;
+    }
+    place = t - start;
   }
   const int old = c.lens[s];
   const int64_t at_place = (int64_t)place + old;

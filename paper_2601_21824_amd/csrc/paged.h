@@ -23,9 +23,10 @@ __device__ inline int find_last(int n, int t, int l, Key&& key) {
   return lo;
 }
 
-// The sequence that row t lies in, -1 where t is at or behind cu[batch].
+// The sequence that row t lies in, -1 where t is before cu[0] or at or behind cu[batch].
+// Offsets that do not rise give some sequence, which need not hold t.
 __device__ inline int find_sequence(const int32_t* cu, int batch, int t, int l) {
-  if (t >= cu[batch]) return -1;
+  if (t < cu[0] || t >= cu[batch]) return -1;
   return find_last(batch, t, l, [&](int s) { return cu[s]; });
 }
 

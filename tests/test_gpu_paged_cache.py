@@ -189,6 +189,57 @@ def test_append_reports_missing_pages():
         assert int((kc == 1).sum()) == int((vc == 1).sum()) == stored * 64
 
 
+# (offsets, lengths before, page): rows before the first sequence, few of them and more than a
+# sequence has cached; one sequence; empty ones first; rows on both sides
+OUTSIDE = [([3, 8], [10], 16), ([1, 1, 5, 9], [40, 7, 0], 16), ([6, 6, 6, 20], [2, 90, 33], 32), ([700, 1100, 1500], [900, 64], 64)]
+
+
+@pytest.mark.parametrize("at,old,page", OUTSIDE)
+@pytest.mark.parametrize("dtype", [BF, E4])
+def test_append_leaves_rows_before_the_first_sequence_alone(at, old, page, dtype):
+    d, hq, hkv, tail = 128, 8, 2, 4
+    g = torch.Generator(device="cuda")
+    g.manual_seed(sum(at))
+    q, k, v = (torch.randn((at[-1] + tail, h, d), generator=g, device="cuda").to(BF) for h in (hq, hkv, hkv))
+    new = [b - a for a, b in zip(at, at[1:])]
+    table, pages = table_of([a + b for a, b in zip(old, new)], page)
+    kc, vc = (make_cache(pages, hkv, page, d, dtype, seed=i) for i in (1, 2))
+    inv = (10000.0 ** (-torch.arange(0, d, 2, device="cuda") / d)).float()
+
+    def call(q, k, v, kc, vc, at):
+        q_out, k_out, status = torch.full_like(q, 7.0), torch.full_like(k, 7.0), i32([0])
+        dash.dash_kv_append(k, v, kc, vc, table, i32(old), cu=i32(at), q=q, q_out=q_out, k_out=k_out, inv_freq=inv, status=status)
+        assert int(status) == 0
+        return q_out, k_out
+
+    # the same tokens alone, from row 0 on
+    own = slice(at[0], at[-1])
+    k1, v1 = kc.clone(), vc.clone()
+    q_want, k_want = call(q[own], k[own], v[own], k1, v1, [a - at[0] for a in at])
+    q_out, k_out = call(q, k, v, kc, vc, at)
+    assert torch.equal(kc.view(torch.uint8), k1.view(torch.uint8)) and torch.equal(vc.view(torch.uint8), v1.view(torch.uint8))
+    assert torch.equal(q_out[own], q_want) and torch.equal(k_out[own], k_want)
+    for x in (q_out, k_out):
+        assert bool((x[:at[0]] == 7).all()) and bool((x[at[-1]:] == 7).all())
+
+
+@pytest.mark.parametrize("at,reported", [([0, 8, 5, 10], 1), ([0, 20, 3, 12], 1), ([-2, 4, 8, 12], 1), ([-2 ** 31, 4, 8, 12], 1),
+                                         ([0, 2 ** 31 - 1, 3, 12], 1), ([4, 0, 12, 12], 0)])  # (the last: all in 0 .. 11)
+def test_append_offsets_that_do_not_rise(at, reported):
+    """Rows that no sequence holds are reported, and what the sequences have cached keeps its bits."""
+    old, d = [20, 30, 25], 64
+    k = torch.ones((12, 1, d), device="cuda").to(BF)
+    table, pages = table_of([n + 12 for n in old], 16)
+    kc, vc = (make_cache(pages, 1, 16, d, BF, seed=i) for i in (1, 2))
+    before = [[rows_of(c, table, s, n, 16) for c in (kc, vc)] for s, n in enumerate(old)]
+    status = i32([0])
+    dash.dash_kv_append(k, k, kc, vc, table, i32(old), cu=i32(at), status=status)
+    assert int(status) == reported
+    for s, n in enumerate(old):
+        for c, want in zip((kc, vc), before[s]):
+            assert torch.equal(rows_of(c, table, s, n, 16), want)
+
+
 # ------------------------------------------------------------------ one token
 def decode64(q, kc, vc, table, lens, page, scale, ks=None, vs=None):
     """o, lse and the bound on o's error, in float64."""
