@@ -108,7 +108,9 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, in
     cs[i] = x.x;
     sn[i] = x.y;
   }
-  const bool turned = split || (a.interleaved && e0 < rot);  // (e1 < rot only if e0 is)
+  // whether each chunk is rotated; one that is not keeps its bits (x cos 0 - y sin 0 makes NaN
+  // beside an infinity, and +0 of -0)
+  const bool turned0 = split || (a.interleaved && e0 < rot), turned1 = split || (a.interleaved && e1 < rot);
   for (int r = first; r < first + rounds; ++r) {
     const int h = r * HPR + l / IPH;
     if (h >= heads) return;
@@ -127,7 +129,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, in
       y1[2 * i] = bf_lo(x1[i]);
       y1[2 * i + 1] = bf_hi(x1[i]);
     }
-    if (kind != 2 && turned) {
+    if (kind != 2 && turned0) {  // (e1 < rot only if e0 is)
       if (split) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -138,18 +140,23 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, in
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float x = y0[2 * i], y = y0[2 * i + 1];
+          const float x = y0[2 * i], y = y0[2 * i + 1];
           y0[2 * i] = x * cs[i] - y * sn[i];
           y0[2 * i + 1] = x * sn[i] + y * cs[i];
-          x = y1[2 * i], y = y1[2 * i + 1];
-          y1[2 * i] = x * cs[4 + i] - y * sn[4 + i];
-          y1[2 * i + 1] = x * sn[4 + i] + y * cs[4 + i];
+        }
+        if (turned1) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float x = y1[2 * i], y = y1[2 * i + 1];
+            y1[2 * i] = x * cs[4 + i] - y * sn[4 + i];
+            y1[2 * i + 1] = x * sn[4 + i] + y * cs[4 + i];
+          }
         }
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         x0[i] = pack_bf16(y0[2 * i], y0[2 * i + 1]);
-        x1[i] = pack_bf16(y1[2 * i], y1[2 * i + 1]);
+        if (turned1) x1[i] = pack_bf16(y1[2 * i], y1[2 * i + 1]);
       }
     }
     __bf16* out = kind == 0                ? (__bf16*)a.q_out + t * a.qos.row + h * a.qos.head

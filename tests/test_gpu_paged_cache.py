@@ -154,6 +154,35 @@ def test_append(d, hq, hkv, new, old, page, dtype, rotary, interleaved, order, w
         assert torch.equal(c.transpose(1, 2)[keep].float(), c0.transpose(1, 2)[keep].float())
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", [BF, E4])
+@pytest.mark.parametrize("d,rotary", [(d, r) for d in (64, 128, 256) for r in (16, d // 2, d // 2 + 16, d - 16)])
+def test_append_keeps_the_components_behind_rotary_dim(d, rotary, dtype, interleaved):
+    """Infinities, NaN and -0 behind rotary_dim: q_out and k_out have their bits, the cache the same values."""
+    hq, hkv, T = 4, 2, 12
+    g = torch.Generator(device="cuda")
+    g.manual_seed(d + rotary)
+    q, k = (torch.randn((T, h, d), generator=g, device="cuda").to(BF) for h in (hq, hkv))
+    for i, odd in enumerate((float("inf"), float("-inf"), float("nan"), -0.0)):
+        for x in (q, k):  # each at every component once in a row of four tokens and heads, then by itself
+            x[i::4, :, rotary + i::4] = odd
+            x[i, 0, rotary:] = 1.0
+            x[i, 0, rotary + 4 + i] = odd
+    table, lens = torch.arange(T, dtype=torch.int32, device="cuda")[:, None], i32([1 + i % 5 for i in range(T)])
+    kc, vc = (make_cache(T, hkv, 16, d, dtype, fill=0.0) for _ in range(2))
+    inv = (10000.0 ** (-torch.arange(0, rotary, 2, device="cuda") / rotary)).float()
+    q_out, k_out = torch.empty_like(q), torch.empty_like(k)
+    dash.dash_kv_append(k, k, kc, vc, table, lens, q=q, q_out=q_out, k_out=k_out, inv_freq=inv, interleaved=interleaved)
+    for x, out in ((q, q_out), (k, k_out)):
+        assert torch.equal(out[..., rotary:].view(torch.int16), x[..., rotary:].view(torch.int16))
+        assert bool(out[..., :rotary].isfinite().all())
+    got = kc[torch.arange(T), :, lens.long()][..., rotary:]
+    want = k[..., rotary:] if dtype is BF else k[..., rotary:].float().clamp(-448, 448).to(E4)
+    bits = torch.int16 if dtype is BF else torch.uint8
+    same = (got.view(bits) == want.view(bits)) | (got.float().isnan() & want.float().isnan())
+    assert bool(same.all())
+
+
 def test_append_in_place_and_nan():
     """q_out = q and k_out = k; NaN and infinity pass (e4m3: infinity saturates, NaN stays)."""
     g = torch.Generator(device="cuda")
