@@ -10,8 +10,10 @@
 // row, so that a tile that reaches past it reads zeros, never a neighbour.
 //
 // Calls with few rows for the GPU split the keys as well (packed_splits): a
-// workgroup takes an equal run of the tiles that its rows see and leaves O and L of
-// those keys alone in fp32, and join_kernel adds the runs in order, weighted by exp(L_i - L).
+// workgroup takes an equal run of the tiles that its rows see and leaves, of those keys
+// alone and in fp32, O and each row's maximum m_i (log2 domain) and sum s_i; join_kernel adds
+// the runs in order, weighted by s_i 2^(m_i - m).  (Not by exp(L_i - L): an L far from 0
+// holds log s_i in few bits or none.)
 //
 // Bound, as the dense forward, by the issue of the MFMAs and of the softmax beside them.
 // Measured, causal, 32 heads over 8 of 128: one sequence of 8192 550-615 us, 890-1000 TFLOP/s; 12
@@ -89,11 +91,15 @@ struct PackedView {
     return rows(a.o, (int64_t)qstart + q0, a.os, h, nq - q0, QROWS);
   }
   __device__ __amdgpu_buffer_rsrc_t lse() const {
-    if (part >= 0) return make_rsrc(a.part_l + part * QROWS, QROWS * 4);
+    if (part >= 0) return make_rsrc(a.part_l + part * (2 * QROWS), QROWS * 8);
     const int n = nq - q0;
     return make_rsrc(a.lse + (int64_t)h * a.total_q + qstart + q0, (uint32_t)(n < QROWS ? n : QROWS) * 4);
   }
   __device__ uint32_t l_at(int row) const { return (uint32_t)(row - q0) * 4; }
+  __device__ void put_l(__amdgpu_buffer_rsrc_t r, int row, float m, float sum) const {
+    if (part >= 0) st8(r, (uint32_t)(row - q0) * 8, u32x2{__builtin_bit_cast(unsigned, m), __builtin_bit_cast(unsigned, sum)});
+    else st4f(r, l_at(row), (m + __log2f(sum)) * kLn2);
+  }
   __device__ void put_o(__amdgpu_buffer_rsrc_t r, int row, int col, float a0, float a1, float a2, float a3) const {
     if (part >= 0) st16(r, (uint32_t)((row - q0) * D + col) * 4, __builtin_bit_cast(u32x4, f32x4{a0, a1, a2, a3}));
     else st8(r, (uint32_t)(row - q0) * (uint32_t)a.os.row * 2 + col * 2, u32x2{pack_bf16(a0, a1), pack_bf16(a2, a3)});
@@ -154,20 +160,22 @@ __global__ __launch_bounds__(256) void join_kernel(PackedArgs a) {
   const int64_t part = ((int64_t)slot * a.heads_q + h) * a.splits;
   const int c = tid % (D / 4) * 4;
   for (int row = r0 + tid / (D / 4); row < r0 + RWG && row < r.n; row += RPP) {
+    const float2* stat = (const float2*)a.part_l;  // m, sum
     float top = -INFINITY;
-    for (int i = 0; i < n; ++i) top = fmaxf(top, a.part_l[(part + i) * QROWS + row]);
+    for (int i = 0; i < n; ++i) top = fmaxf(top, stat[(part + i) * QROWS + row].x);
     const float at = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     for (int i = 0; i < n; ++i) {
-      const float w = __builtin_amdgcn_exp2f((a.part_l[(part + i) * QROWS + row] - at) * kLog2e);
+      const float2 x = stat[(part + i) * QROWS + row];
+      const float w = x.y * __builtin_amdgcn_exp2f(x.x - at);
       sum += w;
       o += w * *(const f32x4*)(a.part_o + (part + i) * (QROWS * D) + row * D + c);
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (nothing but -inf: O 0)
     *(u32x2*)((__bf16*)a.o + ((int64_t)r.q.start + r.q0 + row) * a.os.row + h * a.os.head + c) =
         u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
-    if (c == 0) a.lse[(int64_t)h * a.total_q + r.q.start + r.q0 + row] = sum == 0.f ? -INFINITY : top + __log2f(sum) * kLn2;
+    if (c == 0) a.lse[(int64_t)h * a.total_q + r.q.start + r.q0 + row] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * kLn2;
   }
 }
 

@@ -64,6 +64,8 @@ struct DenseView {
     const u32x2 t = {pack_bf16(a0, a1), pack_bf16(a2, a3)};
     st8(r, (uint32_t)(row * D + col) * 2, t);
   }
+  // L of a row, from its maximum (log2 domain) and its sum of 2^(S log2(e) - m)
+  __device__ void put_l(__amdgpu_buffer_rsrc_t r, int row, float m, float sum) const { st4f(r, l_at(row), (m + __log2f(sum)) * kLn2); }
   // row `row` of the tile whose first key is k0
   __device__ uint32_t k_at(int k0, int row, int col) const { return (uint32_t)((k0 + row) * D + col) * 2; }
   __device__ uint32_t v_at(int k0, int row, int col) const { return (uint32_t)((k0 + row) * D + col) * 2; }
@@ -203,7 +205,7 @@ __device__ void far_rows(const V& view, int causal, float scale, int row0) {
         view.put_o(ro, qrow, d0 + 32 * db + 8 * rb + 4 * g, o[db][4 * rb] * inv, o[db][4 * rb + 1] * inv, o[db][4 * rb + 2] * inv,
                    o[db][4 * rb + 3] * inv);
     if (d0 == 0 && g == 0)
-      st4f(view.lse(), view.l_at(qrow), (m + __log2f(sum)) * kLn2);
+      view.put_l(view.lse(), qrow, m, sum);
   }
 }
 
@@ -564,7 +566,7 @@ __device__ __attribute__((always_inline)) inline void attn_fwd_rows(const V& vie
         const f32x16& o = oacc[qg][db];
         view.put_o(ro, qrow, 32 * db + 8 * rb + 4 * g, o[4 * rb] * inv, o[4 * rb + 1] * inv, o[4 * rb + 2] * inv, o[4 * rb + 3] * inv);
       }
-    if (g == 0) st4f(rl, view.l_at(qrow), (m[qg] + __log2f(sum)) * kLn2);
+    if (g == 0) view.put_l(rl, qrow, m[qg], sum);
   }
 }
 

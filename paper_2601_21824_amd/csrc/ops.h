@@ -68,13 +68,13 @@ struct PackedArgs {
   int batch, heads_q, heads_kv, total_q, total_k, causal;
   float scale;
   Strides qs, ks, vs, os;
-  // the forward's split over the keys: runs at most, and their O and L (packed_part_rows)
+  // the forward's split over the keys: runs at most, and their O, maxima and sums (packed_part_rows)
   int splits;
   float* part_o;
   float* part_l;
 };
 int packed_splits(int d, int total_q, int total_k, int batch, int heads_q, int causal);
-// rows of part_l, and of d columns of part_o
+// rows of part_l (maximum in the log2 domain, sum), and of d columns of part_o
 size_t packed_part_rows(int total_q, int batch, int heads_q, int splits);
 hipError_t launch_packed_fwd(const PackedArgs& a, int d, hipStream_t stream);
 

@@ -233,7 +233,7 @@ FwdLayout fwd_layout(int batch, int total_q, int total_k, int heads_q, int d, in
   const size_t rows = dash::packed_part_rows(total_q, batch, heads_q, L.splits);
   L.part_o = 0;
   L.part_l = rows * d * sizeof(float);
-  L.total = L.part_l + align256(rows * sizeof(float));
+  L.total = L.part_l + align256(rows * 2 * sizeof(float));
   return L;
 }
 

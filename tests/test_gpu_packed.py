@@ -99,6 +99,49 @@ def test_forward_split_far_scores():
     assert bool((o == 0).all()) and bool((lse == -math.inf).all())
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("at", [0.0, 98304.0, -98304.0, 2.0 ** 20, -2.0 ** 20, 2.0 ** 24, 1e30, -1e30])
+def test_forward_split_weighs_runs_by_their_keys(d, at):
+    """All keys but some score the same, however far from 0, and those nothing (-2 |at| - 2^30): every
+    run counts with as many keys as it has, one of them with a single one.
+
+    O is the mean of V.  A key's P is 2^e, e = S log2(e) - m with m rounded, |e| <= U24 |m|, or 1
+    where the rows are done again as far from 0: always from |m| = 2^20 on, and below it in a run
+    that begins with keys that score nothing.  So the keys of all other runs have one weight; P's
+    rounding makes a factor of it that is off by U8 at most.  With those of the one run that
+    begins among the keys of no weight and ends behind them (v[hi:b], b unknown) another
+    by d = U8 (1 + U8) + 2^(U24 |m|) - 1, O moves by d |sum over v[hi:b] of v - O| / n in first order,
+    (1 + d) of it with the second.  Then U8 for the rounding of O and 2 n U24 A for the sums.
+    L: log(n) added to S = at; the factor log2(e), the product, the sum with log2(n), the factor
+    log(2) and the last product round by U24 each."""
+    n, m = 4097, 3
+    q, k, v, _ = packed_inputs([m], [n], 2, 2, d)
+    q.zero_(), k.zero_()
+    q[..., 0], k[..., 0], q[..., 1] = 1, at, 1
+    U8, U24 = 2.0 ** -8, 2.0 ** -24
+    s = torch.tensor(at).to(BF).double().item()
+    size = dash.dash_packed_fwd_workspace_size(1, m, n, 2, 2, d)
+    assert size > 0
+    for lo, hi in ((0, 0), (1, 600), (n - 700, n - 1), (100, 4000)):
+        k2 = k.clone()
+        k2[lo:hi, :, 1] = -2 * abs(at) - 2.0 ** 30
+        keep = torch.ones(n, dtype=torch.bool, device="cuda")
+        keep[lo:hi] = False
+        w = v[keep].double()
+        want, top = w.mean(0), abs(s) / math.log(2)
+        bound = 2 * U8 * (1 + U8) * want.abs() + 2 * n * U24 * w.abs().mean(0)
+        if lo < hi and 0 < top < 2 ** 20:
+            off = U8 * (1 + U8) + 2 ** (U24 * top) - 1
+            bound = bound + off * (1 + off) * (v[hi:].double() - want).cumsum(0).abs().amax(0) / len(w)
+        o, lse = dash.attn_packed_fwd(q, k2, v, cu_of([m]), cu_of([n]), causal=False, scale=1.0)
+        o1, lse1 = torch.empty_like(o), torch.empty_like(lse)
+        dash.dash_attn_packed_fwd(q, k2, v, o1, lse1, cu_of([m]), cu_of([n]), False, 1.0)  # not split
+        L = s + math.log(int(keep.sum()))
+        for oo, ll in ((o1, lse1), (o, lse)):
+            assert over(oo, want.expand_as(oo), bound.expand_as(oo)) <= 0
+            assert over(ll, torch.full_like(ll, L, dtype=torch.float64), 5 * U24 * abs(s) + 2e-5) <= 0
+
+
 @pytest.mark.parametrize("shift", [-1e30, -3e9, float("-inf")])
 @pytest.mark.parametrize("d", [64, 128, 256])
 def test_forward_far_scores(d, shift):
