@@ -322,12 +322,14 @@ def _rows(name, t, dtype, dev, rows, heads, d):
     return t.data_ptr(), row, head
 
 
-def _flat(name, t, dtype, dev, n):
-    """A contiguous tensor of n values on GPU `dev`, or None: its pointer (0 for None)."""
+def _flat(name, t, dtype, dev, *shape):
+    """A contiguous tensor of this shape on GPU `dev`, or None: its pointer (0 for None).  A
+    vector may have further dimensions of 1."""
     if t is None:
         return 0
-    if t.dtype is not dtype or t.get_device() != dev or t.numel() != n or not t.is_contiguous():
-        _bad(f"{name} must be a contiguous {dtype} tensor of {n} values on cuda:{dev}")
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or t.shape != shape and (
+            len(shape) > 1 or t.numel() != shape[0] or t.numel() not in (1, *t.shape)):
+        _bad(f"{name} must be a contiguous {dtype} {list(shape)} tensor on cuda:{dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
@@ -349,8 +351,7 @@ def _space(workspace, need, like, dev, stream):
         need = need if need > 256 else 256
         workspace = like.new_empty(need, dtype=torch.uint8)
         return workspace.data_ptr(), need, workspace
-    n = workspace.numel()
-    return _flat("workspace", workspace, torch.uint8, dev, n), n, workspace
+    return _flat("workspace", workspace, torch.uint8, dev, *workspace.shape), workspace.numel(), workspace
 
 
 def _call(f, dev, stream, *args):
@@ -450,7 +451,7 @@ def dash_attn_decode(q, k_cache, v_cache, block_table, lens, o, lse=None, scale=
     need = 0 if workspace is not None else lib.dash_decode_workspace_size(batch, heads_q, heads_kv, d, page, block_table.shape[1])
     ws, size, workspace = _space(workspace, need, q, dev, stream)
     _call(lib.dash_attn_decode, dev, stream, c, *_rows("q", q, torch.bfloat16, dev, batch, heads_q, d),
-          *_rows("o", o, torch.bfloat16, dev, batch, heads_q, d), _flat("lse", lse, torch.float32, dev, batch * heads_q),
+          *_rows("o", o, torch.bfloat16, dev, batch, heads_q, d), _flat("lse", lse, torch.float32, dev, batch, heads_q),
           0.0 if scale is None else scale, ws, size, _flat("status", status, torch.int32, dev, 1))
 
 
@@ -502,7 +503,7 @@ def dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k=None, causal: bool = True, 
     p, qp, kp, vp, op = _packed(q, k, v, o, cu_q, cu_k, causal, scale, dev)
     ws, size = (0, 0) if workspace is None else _space(workspace, 0, q, dev, stream)[:2]
     _call(load().dash_attn_packed_fwd, dev, stream, p, qp, kp, vp, op,
-          _flat("lse", lse, torch.float32, dev, q.shape[0] * q.shape[1]), ws, size)
+          _flat("lse", lse, torch.float32, dev, q.shape[1], q.shape[0]), ws, size)
 
 
 def attn_packed_fwd(q, k, v, cu_q, cu_k=None, causal: bool = True, scale=None):
@@ -543,7 +544,7 @@ def dash_attn_packed_bwd(q, k, v, o, dO, lse, dq, dk, dv, cu_q, cu_k=None, causa
     need = 0 if workspace is not None else lib.dash_packed_workspace_size(cu_q.numel() - 1, tq, tk, hq, hkv, d)
     ws, size, workspace = _space(workspace, need, q, dev, stream)
     _call(lib.dash_attn_packed_bwd, dev, stream, p, qp, kp, vp, op, do,
-          _flat("lse", lse, torch.float32, dev, hq * tq), a, b, c, ws, size, _flat("status", status, torch.int32, dev, 1))
+          _flat("lse", lse, torch.float32, dev, hq, tq), a, b, c, ws, size, _flat("status", status, torch.int32, dev, 1))
 
 
 def attn_packed_bwd(q, k, v, o, dO, lse, cu_q, cu_k=None, causal: bool = True, scale=None, workspace=None):

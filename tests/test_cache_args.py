@@ -110,3 +110,27 @@ def test_binding_checks_tensors():
         with pytest.raises(b.DashError) as e:
             call()
         assert e.value.code == b.DASH_ERR_INVALID_ARG
+
+
+def test_binding_checks_shapes():
+    """A tensor of as many values in another shape: an L with its dimensions swapped, a matrix of lengths."""
+    import torch
+    f, i = torch.float32, torch.int32
+    at = b._flat  # (device -1: the CPU's)
+    for shape in ((3, 5), (1, 5), (3, 1), (0, 4)):
+        x = torch.zeros(shape, dtype=f)
+        assert at("lse", x, f, -1, *shape) == x.data_ptr()
+        for other in (shape[::-1], (shape[0] * shape[1],), (1, *shape)):
+            with pytest.raises(b.DashError, match="lse"):
+                at("lse", torch.zeros(other, dtype=f), f, -1, *shape)
+    for shape in ((6,), (6, 1), (1, 1, 6)):
+        assert at("lens", torch.zeros(shape, dtype=i), i, -1, 6) != 0
+    for shape in ((2, 3), (5,), (7, 1), (), (6, 0), (1, 2, 3)):
+        with pytest.raises(b.DashError, match="lens"):
+            at("lens", torch.zeros(shape, dtype=i), i, -1, 6)
+    for shape in ((), (1,), (1, 1)):
+        assert at("status", torch.zeros(shape, dtype=i), i, -1, 1) != 0
+    assert at("status", None, i, -1, 1) == 0
+    for bad in (torch.zeros(4, 2, dtype=i)[:, 0], torch.zeros(4, dtype=f)):
+        with pytest.raises(b.DashError, match="lens"):
+            at("lens", bad, i, -1, 4)

@@ -316,6 +316,20 @@ def test_offsets_that_do_not_rise_are_reported():
     assert all(torch.equal(x, y) for x, y in zip(out, want))
 
 
+def test_lse_of_another_shape_is_refused():
+    """[tokens, heads] holds as many values as [heads, tokens]: refused, not read as it."""
+    q, k, v, do = packed_inputs([90, 40], [90, 40], 4, 2, 64)
+    cu = cu_of([90, 40])
+    o, lse = dash.attn_packed_fwd(q, k, v, cu)
+    for bad in (lse.t().contiguous(), lse.flatten(), lse.reshape(2, 260), lse[None], lse.t()):
+        with pytest.raises(dash.DashError, match="lse"):
+            dash.dash_attn_packed_fwd(q, k, v, o, bad, cu)
+        with pytest.raises(dash.DashError, match="lse"):
+            dash.attn_packed_bwd(q, k, v, o, do, bad, cu)
+    with pytest.raises(dash.DashError, match="cu_k"):
+        dash.attn_packed_fwd(q, k, v, cu_of([90, 20, 20]), cu_of([90, 20, 20]).reshape(2, 2))
+
+
 def test_broadcast_heads():
     """K and V of one head read by all through a head stride of 0, gradients for each."""
     lens = [90, 40]

@@ -392,6 +392,25 @@ def test_decode_reports_bad_tables():
         assert int(status) == status_want and torch.equal(o[1], good[1])
 
 
+def test_lengths_and_scales_of_another_shape_are_refused():
+    q, kc, vc, table, ks, vs = decode_case(64, 8, 4, [5, 9, 20, 1], 16, E4, "phrd")
+    lens, o = i32([5, 9, 20, 1]), torch.empty_like(q)
+    want = dash.attn_decode(q, kc, vc, table, lens, k_scale=ks, v_scale=vs)
+    assert torch.equal(dash.attn_decode(q, kc, vc, table, lens[:, None], k_scale=ks[None, :, None], v_scale=vs), want)
+    lse = torch.empty((4, 8), device="cuda")
+    for word, kw in (("lens", dict(lens=lens.reshape(2, 2))), ("k_scale", dict(k_scale=ks.reshape(2, 2))),
+                     ("v_scale", dict(v_scale=vs.reshape(2, 2))), ("lse", dict(lse=lse.t().contiguous())),
+                     ("lse", dict(lse=lse.flatten()))):
+        args = dict(dict(lens=lens, lse=lse, k_scale=ks, v_scale=vs), **kw)
+        with pytest.raises(dash.DashError, match=word):
+            dash.dash_attn_decode(q, kc, vc, table, o=o, **args)
+    k = q[:, :4].contiguous()
+    for word, kw in (("lens", dict(lens=lens.reshape(2, 2))), ("k_scale", dict(k_scale=ks.reshape(2, 2))),
+                     ("inv_freq", dict(inv_freq=torch.ones((4, 4), device="cuda")))):
+        with pytest.raises(dash.DashError, match=word):
+            dash.dash_kv_append(k, k, kc, vc, table, **dict(dict(lens=lens, k_scale=ks, v_scale=vs), **kw))
+
+
 def test_tables_of_no_page():
     """No sequence has a page: nothing to attend to, nowhere to store."""
     q, kc = torch.ones((3, 4, 64), device="cuda").to(BF), make_cache(2, 2, 16, 64, BF)
