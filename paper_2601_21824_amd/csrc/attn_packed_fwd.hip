@@ -207,6 +207,11 @@ int packed_splits(int d, int total_q, int total_k, int batch, int heads_q, int c
   long s = blocks > 0 ? (triangle ? 2 : 1) * fit / blocks : 1;
   s = s < most ? s : most;
   if (triangle && d < 256 && s < 3) s = 1;
+  // Partial results have room for every slot: with far more sequences than queries (most of
+  // them empty) for nearly nothing but empty ones, so that their number is bounded (1.1 GB at d = 256;
+  // up to 2048 where batch <= total_q)
+  const long room = 8192 / ((total_q / 128 + (long)batch) * heads_q);
+  s = s < room ? s : room;
   return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
 }
 size_t packed_part_rows(int total_q, int batch, int heads_q, int splits) {

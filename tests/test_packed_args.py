@@ -87,6 +87,16 @@ def test_forward_workspace():
         assert fwd(problem(**big), ws=ws, ws_bytes=n) == b.DASH_ERR_INVALID_ARG and "workspace" in b.dash_last_error()
 
 
+def test_forward_workspace_of_mostly_empty_sequences():
+    """Room for the runs of rows that are there, not of every sequence that could have some."""
+    for batch, total_q, total_k, hq, hkv, d in ((1024, 8, 1 << 22, 32, 8, 128), (1 << 15, 1, 1 << 28, 8, 8, 256), (4096, 1, 1 << 24, 1, 1, 64)):
+        assert b.dash_packed_fwd_workspace_size(batch, total_q, total_k, hq, hkv, d) <= 8192 * 128 * (d + 2) * 4
+    # a token of each of 64 sequences, one of eight, and one alone: split as before
+    for batch, total_q, total_k, hq, splits in ((64, 64, 64 * 4096, 4, 2), (8, 1, 8 * 8192, 8, 16), (1, 1, 8192, 32, 16)):
+        rows = (total_q // 128 + batch) * hq * splits * 128
+        assert b.dash_packed_fwd_workspace_size(batch, total_q, total_k, hq, hq, 128) == rows * 130 * 4
+
+
 def test_too_many_blocks():
     big = dict(heads_q=4096, heads_kv=4096, total_q=1 << 20, total_k=1 << 20, cu_k=P)
     assert fwd(problem(**big)) == b.DASH_ERR_UNSUPPORTED and "2^24" in b.dash_last_error()
