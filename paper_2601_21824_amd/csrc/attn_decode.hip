@@ -359,6 +359,12 @@ int decode_slots(int batch, int heads_q, int heads_kv, int d, int table_tokens) 
   return (int)(s < most ? s : most);
 }
 
+int64_t decode_waves(const DecodeArgs& a) {
+  const int64_t G = a.c.heads_q / a.c.heads_kv, main = (int64_t)a.slots * a.c.heads_kv * ((G + kQ - 1) / kQ) * (a.workers == 0 ? 8 : 4);
+  const int64_t join = a.slots > a.c.batch ? (int64_t)a.c.batch * a.c.heads_q * 4 : 0;
+  return main > join ? main : join;
+}
+
 hipError_t launch_decode(const DecodeArgs& a, hipStream_t stream) {
   if (a.c.d == 64) launch<64>(a, stream);
   else if (a.c.d == 128) launch<128>(a, stream);

@@ -189,16 +189,23 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, in
   }
 }
 
-template <int D>
-void launch(const AppendArgs& a, hipStream_t stream) {
-  constexpr int HPR = 64 / (D / 16);
-  const int heads = (a.q ? a.c.heads_q : 0) + 2 * a.c.heads_kv;
-  const int total = (heads + HPR - 1) / HPR;
+// waves a token and their rounds
+struct Split {
+  int rounds, waves;
+};
+Split split_of(const AppendArgs& a) {
+  const int hpr = 64 / (a.c.d / 16), heads = (a.q ? a.c.heads_q : 0) + 2 * a.c.heads_kv;
+  const int total = (heads + hpr - 1) / hpr;
   // one round per wave until the waves fill the GPU (256 CUs of 16), then as many
   // rounds as a token has
   const int rounds = (long)a.tokens * total <= 4096 ? 1 : total;
-  const long waves = (long)a.tokens * ((total + rounds - 1) / rounds);
-  const dim3 grid((unsigned)((waves + kWaves - 1) / kWaves));
+  return {rounds, (total + rounds - 1) / rounds};
+}
+
+template <int D>
+void launch(const AppendArgs& a, hipStream_t stream) {
+  const int heads = (a.q ? a.c.heads_q : 0) + 2 * a.c.heads_kv, rounds = split_of(a).rounds;
+  const dim3 grid((unsigned)((append_waves(a) + kWaves - 1) / kWaves));
   // past the caches from 64 MB of q, k and v on (us, through / past them: 8192 tokens, 32 heads
   // over 8 of 128, 100 MB, 44.2 / 40.3; 16 over 4 of 64, 25 MB, where the cache still holds them, 14.0 / 17.5)
   if ((long)a.tokens * heads * D * 2 >= 64L << 20)
@@ -208,6 +215,8 @@ void launch(const AppendArgs& a, hipStream_t stream) {
 }
 
 }  // namespace
+
+int64_t append_waves(const AppendArgs& a) { return (int64_t)a.tokens * split_of(a).waves; }
 
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t stream) {
   if (a.c.d == 64) launch<64>(a, stream);

@@ -9,6 +9,9 @@
 
 namespace dash {
 
+// A launch takes fewer than 2^32 threads.
+constexpr int64_t kMaxWaves = ((int64_t)1 << 26) - 8;  // (whole workgroups of at most eight waves)
+
 // strides in elements
 struct Strides {
   int64_t row, head;
@@ -40,6 +43,8 @@ struct AppendArgs {
   const float* inv_freq;
   int rotary, interleaved;
 };
+// waves of the launch
+int64_t append_waves(const AppendArgs& a);
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t stream);
 
 struct DecodeArgs {
@@ -57,6 +62,8 @@ struct DecodeArgs {
 };
 int decode_workers(int heads_q, int heads_kv, int d, int table_tokens);
 int decode_slots(int batch, int heads_q, int heads_kv, int d, int table_tokens);
+// waves of the larger launch
+int64_t decode_waves(const DecodeArgs& a);
 hipError_t launch_decode(const DecodeArgs& a, hipStream_t stream);
 
 // ---------------------------------------------------------------- packed sequences

@@ -150,12 +150,13 @@ int kv_append(const dash_paged_cache_t* c, const dash_append_t* x, int* status, 
   if (x->k_out &&
       (rc = check_tensor("k_out", x->k_out, x->tokens, c->heads_kv, c->d, x->k_out_row_stride, x->k_out_head_stride, 8, true)))
     return rc;
-  DeviceInfo di;
-  if ((rc = device_info(&di))) return rc;
   const dash::AppendArgs a{cache_args(c, status), x->tokens, x->cu, x->k, x->v, x->q, x->q_out, x->k_out,
                            {x->k_row_stride, x->k_head_stride}, {x->v_row_stride, x->v_head_stride},
                            {x->q_row_stride, x->q_head_stride}, {x->q_out_row_stride, x->q_out_head_stride},
                            {x->k_out_row_stride, x->k_out_head_stride}, x->inv_freq, x->rotary_dim, x->interleaved ? 1 : 0};
+  if (dash::append_waves(a) > dash::kMaxWaves) return fail(DASH_ERR_UNSUPPORTED, "too many tokens for one call");
+  DeviceInfo di;
+  if ((rc = device_info(&di))) return rc;
   const hipError_t e = dash::launch_kv_append(a, (hipStream_t)stream);
   return e == hipSuccess ? DASH_OK : hip_fail(e, "append launch");
 }
@@ -172,14 +173,13 @@ int attn_decode(const dash_paged_cache_t* c, const void* q, int64_t q_row, int64
   if (!workspace || ws_bytes < L.total)
     return fail(DASH_ERR_INVALID_ARG, "workspace missing or smaller than dash_decode_workspace_size()");
   if (((uintptr_t)workspace & 255) != 0) return fail(DASH_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-  if ((int64_t)L.slots * c->heads_q >= ((int64_t)1 << 31) || (int64_t)c->batch * c->heads_q >= ((int64_t)1 << 31))
-    return fail(DASH_ERR_UNSUPPORTED, "batch * heads_q too large");
-  DeviceInfo di;
-  if ((rc = device_info(&di))) return rc;
   char* ws = (char*)workspace;
   const dash::DecodeArgs a{cache_args(c, status), q, o, lse, {q_row, q_head}, {o_row, o_head}, scale,
                            dash::decode_workers(c->heads_q, c->heads_kv, c->d, c->table_width * c->page_size), L.slots, (float*)(ws + L.part_o),
                            (float*)(ws + L.part_m), (int*)(ws + L.base)};
+  if (dash::decode_waves(a) > dash::kMaxWaves) return fail(DASH_ERR_UNSUPPORTED, "batch * heads_q too large for one call");
+  DeviceInfo di;
+  if ((rc = device_info(&di))) return rc;
   const hipError_t e = dash::launch_decode(a, (hipStream_t)stream);
   return e == hipSuccess ? DASH_OK : hip_fail(e, "decode launch");
 }

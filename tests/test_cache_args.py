@@ -92,6 +92,18 @@ def test_decode_arguments():
     assert b.dash_decode_workspace_size(2, 8, 2, 128, 16, 1 << 28) == 0
 
 
+def test_calls_too_large_for_a_launch():
+    """2^32 threads and more: refused by name, before any device work (cases that fit are not run here)."""
+    for c in (cache(batch=1 << 20, heads_q=64, heads_kv=64, table_width=1 << 16, table_stride=1 << 16),  # (main kernel and joins)
+              cache(batch=1 << 20, heads_q=16, heads_kv=1, table_width=1 << 16, table_stride=1 << 16),  # (joins alone)
+              cache(batch=1 << 20, heads_q=16, heads_kv=8)):  # (short tables: eight waves a workgroup)
+        assert run_decode(c, strides=(1 << 14, 128, 1 << 14, 128), ws_bytes=1 << 50) == b.DASH_ERR_UNSUPPORTED
+        assert "too large" in b.dash_last_error()
+    many = dict(tokens=(1 << 26) - 7, cu=P)
+    assert run_append(cache(), append(**many)) == b.DASH_ERR_UNSUPPORTED and "tokens" in b.dash_last_error()
+    assert run_append(cache(), append(q=None, q_out=None, **dict(many, tokens=(1 << 31) - 1))) == b.DASH_ERR_UNSUPPORTED
+
+
 def test_empty_calls_are_no_ops():
     assert run_append(cache(batch=0, lens=None, k_cache=None), append(tokens=0)) == b.DASH_OK
     assert run_append(cache(), append(tokens=0, cu=P, k=None)) == b.DASH_OK
