@@ -258,6 +258,34 @@ def test_backward_wide_d64(hq, hkv, qlens, klens, causal, layout):
         assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(out, again))
 
 
+# The same at d = 128, two key blocks a wave: sequences without queries and without keys, more
+# queries than keys, keys that no query sees, lengths around the tile, a group of one and more
+@pytest.mark.parametrize("hq,hkv,qlens,klens,causal,layout", [
+    (32, 32, [1023, 1281, 1, 1500], [1023, 1281, 1, 1500], True, "packed"), (48, 8, [2049, 640], [2049, 640], True, "fused"),
+    (64, 4, [257, 900, 0, 31], [1700, 900, 300, 900], True, "packed"), (64, 64, [1500, 700, 5], [1100, 1000, 0], True, "packed"),
+    (32, 8, [700, 900, 600, 80], [511, 512, 513, 1600], True, "heads"), (20, 20, [300, 0, 256, 700], [257, 600, 256, 1300], False, "heads"),
+    (40, 8, [64, 1000], [1025, 512], False, "packed"), (40, 10, [0, 700, 63], [255, 1280, 1], False, "packed")])
+def test_backward_wide_d128(hq, hkv, qlens, klens, causal, layout):
+    same, tail = qlens == klens, 5
+    q, k, v, do = packed_inputs(qlens, klens, hq, hkv, 128, layout, tail=tail)
+    # (packed_tile_rows' rule: 256-row tiles)
+    T = k.shape[0]
+    assert T // 256 * hq >= (320 if causal else 160) and T >= 480 * len(klens)
+    cu_q, cu_k = cu_of(qlens), None if same else cu_of(klens)
+    status = torch.full((1,), 9, dtype=torch.int32, device="cuda")
+    out = train(q, k, v, do, cu_q, cu_k, causal, status=status)
+    assert int(status) == 0
+    ref = reference(q, k, v, do, qlens, klens, causal, 1 / math.sqrt(128))
+    for name, got, n in zip("qkv", out, (sum(qlens), sum(klens), sum(klens))):
+        assert bool((got[n:] == 7).all()), "rows behind the last sequence"
+        assert over(got[:n], ref["d" + name][:n], ref["t" + name][:n]) <= 0, "d" + name
+    none = (ref["lse"] == -math.inf).t()[:sum(qlens)]
+    assert bool((out[0][:sum(qlens)][none] == 0).all())
+    for _ in range(4):
+        again = train(q, k, v, do, cu_q, cu_k, causal)
+        assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(out, again))
+
+
 def test_backward_accumulators_past_2_gib():
     """130 sequences of 1000, 32 heads over 8: dQ's fp32 blocks alone are 2.2 GB.  The last two
     sequences against the definition."""
@@ -328,6 +356,60 @@ def test_lse_of_another_shape_is_refused():
             dash.attn_packed_bwd(q, k, v, o, do, bad, cu)
     with pytest.raises(dash.DashError, match="cu_k"):
         dash.attn_packed_fwd(q, k, v, cu_of([90, 20, 20]), cu_of([90, 20, 20]).reshape(2, 2))
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_rows_before_the_first_sequence(d):
+    """Offsets that begin behind row 0: those rows are nobody's, like the ones behind the last sequence."""
+    skip, lens = 70, [200, 0, 90]
+    q, k, v, do = packed_inputs([skip, *lens], [skip, *lens], 4, 2, d, tail=3)
+    cu = cu_of([skip, *lens])[1:].contiguous()
+    own = slice(skip, skip + sum(lens))
+    for x in (q, k, v, do):
+        x[:skip] = float("nan")
+    o, lse = torch.full_like(q, 7.0), torch.full((4, q.shape[0]), 7.0, device="cuda")
+    dash.dash_attn_packed_fwd(q, k, v, o, lse, cu)
+    o0, lse0 = dash.attn_packed_fwd(q[own], k[own], v[own], cu_of(lens))
+    assert torch.equal(o[own], o0) and torch.equal(lse[:, own], lse0)
+    dq, dk, dv = train(q, k, v, do, cu, None, True)
+    want = train(q[own], k[own], v[own], do[own], cu_of(lens), None, True)
+    for got, w in zip((dq, dk, dv), want):
+        assert torch.equal(got[own], w)
+    for x in (o, dq, dk, dv):
+        assert bool((x[:skip] == 7).all()) and bool((x[own.stop:] == 7).all())
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_scores_that_overflow_to_minus_infinity(d):
+    """Finite q and k whose products pass fp32's range: the keys weigh nothing, and a row of nothing
+    else has O = 0, L = -inf and no gradient; the other rows and keys as without them."""
+    q, k, v, do = packed_inputs([200], [200], 2, 2, d)
+    q[:, :, 0], k[:, :, 0] = 2.0 ** 70, 0
+    q[:70, :, 0] = 2.0 ** 90
+    k[:100, :, 0] = -(2.0 ** 70)  # 2^160 and 2^140: -inf
+    o, lse = dash.attn_packed_fwd(q, k, v, cu_of([200]))
+    dq, dk, dv = dash.attn_packed_bwd(q, k, v, o, do, lse, cu_of([200]))
+    for x in (o[:100], dq[:100], dk[:100], dv[:100]):
+        assert bool((x == 0).all())
+    assert bool((lse[:, :100] == -math.inf).all())
+    o2, lse2 = dash.attn_packed_fwd(q[100:], k[100:], v[100:], cu_of([100]))
+    ref = reference(q[100:], k[100:], v[100:], do[100:], [100], [100], True, 1 / math.sqrt(d))
+    assert over(o[100:], ref["o"], ref["to"]) <= 0 and over(lse[:, 100:], ref["lse"], 2e-5 * ref["lse"].abs().clamp(min=1)) <= 0
+    # (dQ's first component is 0 times k's)
+    for name, got in (("q", dq), ("k", dk), ("v", dv)):
+        assert over(got[100:, :, 1:], ref["d" + name][..., 1:], ref["t" + name][..., 1:]) <= 0, "d" + name
+
+
+def test_thousands_of_sequences():
+    """2100 sequences of 0 to 12 tokens: many rounds of the searches and of the chains' order."""
+    lens = [(7 * i + i // 13) % 13 for i in range(2100)]
+    q, k, v, do = packed_inputs(lens, lens, 4, 2, 64)
+    o, lse = dash.attn_packed_fwd(q, k, v, cu_of(lens))
+    out = train(q, k, v, do, cu_of(lens), None, True)
+    ref = reference(q, k, v, do, lens, lens, True, 1 / math.sqrt(64))
+    assert over(o, ref["o"], ref["to"]) <= 0 and over(lse, ref["lse"], 2e-5 * ref["lse"].abs().clamp(min=1)) <= 0
+    for name, got in zip("qkv", out):
+        assert over(got, ref["d" + name], ref["t" + name]) <= 0, "d" + name
 
 
 def test_broadcast_heads():
