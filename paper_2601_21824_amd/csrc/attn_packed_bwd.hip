@@ -132,7 +132,7 @@ __global__ __launch_bounds__(256) void packed_pre_kernel(PackedBwdArgs a) {
   }
   x -= order;
   if (x < a.slots_q) {  // ---- a slot's counters, and dQ where nothing else writes it
-    for (int h = tid; h < p.heads_q; h += 256) a.counters[((size_t)x * p.heads_q + h) * kCtrStride] = a.poison ? kPoison : 0;
+    for (int h = tid; h < p.heads_q; h += 256) a.counters[((size_t)x * p.heads_q + h) * kCtrStride] = 0;
     const int s = __builtin_amdgcn_readfirstlane(
         find_last(p.batch, x, l, [&](int i) { return first_slot(p.cu_q, i, p.total_q, BM); }));
     const Span q = span_of(p.cu_q, s, p.total_q), k = span_of(p.cu_k, s, p.total_k);

@@ -25,6 +25,8 @@
 namespace dash {
 namespace {
 
+constexpr int kRows = 128;  // query rows of a workgroup
+
 // A workgroup's run of keys: the tiles of KT keys that its rows see, cut into n equal
 // runs of kMinRun keys at least (half of that where they are cut unevenly: more than
 // a workgroup's rows, so that under a causal mask every row sees a key of every run).
@@ -48,24 +50,23 @@ struct Rows {
   int q0, n, kv_end;
   Span q, k;
 };
-template <int QROWS>
 __device__ inline Rows rows_of(const PackedArgs& a, int slot, int l) {
   Rows r;
   const int s = __builtin_amdgcn_readfirstlane(
-      find_last(a.batch, slot, l, [&](int x) { return first_slot(a.cu_q, x, a.total_q, QROWS); }));
+      find_last(a.batch, slot, l, [&](int x) { return first_slot(a.cu_q, x, a.total_q, kRows); }));
   r.q = span_of(a.cu_q, s, a.total_q);
   r.k = span_of(a.cu_k, s, a.total_k);
-  r.q0 = (slot - first_slot(a.cu_q, s, a.total_q, QROWS)) * QROWS;
-  r.n = r.q0 < 0 ? 0 : r.q.len - r.q0 < QROWS ? r.q.len - r.q0 : QROWS;
+  r.q0 = (slot - first_slot(a.cu_q, s, a.total_q, kRows)) * kRows;
+  r.n = r.q0 < 0 ? 0 : r.q.len - r.q0 < kRows ? r.q.len - r.q0 : kRows;
   r.kv_end = r.k.len;
   if (a.causal) {
-    const int end = r.q0 + QROWS + r.k.len - r.q.len;
+    const int end = r.q0 + kRows + r.k.len - r.q.len;
     r.kv_end = end < r.kv_end ? end : r.kv_end;
   }
   return r;
 }
 
-template <int D, int QROWS>
+template <int D>
 struct PackedView {
   static constexpr bool kPacked = true;
   const PackedArgs& a;
@@ -74,26 +75,20 @@ struct PackedView {
   int qstart, kstart;
   int64_t part;  // number of the run's partial result; -1: the rows have one run, which is the result
   __device__ int off() const { return off_; }
-  // a resource over at most `most` rows of the n behind row r0
-  __device__ static __amdgpu_buffer_rsrc_t rows(const void* p, int64_t first, const Strides& s, int head, int n, int most) {
-    const int r = n < most ? n : most;
-    const uint32_t bytes = r > 0 ? (uint32_t)(r - 1) * (uint32_t)s.row * 2 + D * 2 : 0;
-    return make_rsrc((const __bf16*)p + first * s.row + head * s.head, bytes);
-  }
-  __device__ __amdgpu_buffer_rsrc_t q() const { return rows(a.q, (int64_t)qstart + q0, a.qs, h, nq - q0, QROWS); }
-  __device__ __amdgpu_buffer_rsrc_t k(int k0) const { return rows(a.k, (int64_t)kstart + k0, a.ks, hk, nk - k0, 64); }
-  __device__ __amdgpu_buffer_rsrc_t v(int k0) const { return rows(a.v, (int64_t)kstart + k0, a.vs, hk, nk - k0, 64); }
+  __device__ __amdgpu_buffer_rsrc_t q() const { return strided_rows<D>(a.q, (int64_t)qstart + q0, a.qs, h, nq - q0, kRows); }
+  __device__ __amdgpu_buffer_rsrc_t k(int k0) const { return strided_rows<D>(a.k, (int64_t)kstart + k0, a.ks, hk, nk - k0, 64); }
+  __device__ __amdgpu_buffer_rsrc_t v(int k0) const { return strided_rows<D>(a.v, (int64_t)kstart + k0, a.vs, hk, nk - k0, 64); }
   __device__ uint32_t q_at(int row, int col) const { return (uint32_t)(row - q0) * (uint32_t)a.qs.row * 2 + col * 2; }
   __device__ uint32_t k_at(int, int row, int col) const { return (uint32_t)row * (uint32_t)a.ks.row * 2 + col * 2; }
   __device__ uint32_t v_at(int, int row, int col) const { return (uint32_t)row * (uint32_t)a.vs.row * 2 + col * 2; }
   __device__ __amdgpu_buffer_rsrc_t o() const {
-    if (part >= 0) return make_rsrc(a.part_o + part * (QROWS * D), QROWS * D * 4);
-    return rows(a.o, (int64_t)qstart + q0, a.os, h, nq - q0, QROWS);
+    if (part >= 0) return make_rsrc(a.part_o + part * (kRows * D), kRows * D * 4);
+    return strided_rows<D>(a.o, (int64_t)qstart + q0, a.os, h, nq - q0, kRows);
   }
   __device__ __amdgpu_buffer_rsrc_t lse() const {
-    if (part >= 0) return make_rsrc(a.part_l + part * (2 * QROWS), QROWS * 8);
+    if (part >= 0) return make_rsrc(a.part_l + part * (2 * kRows), kRows * 8);
     const int n = nq - q0;
-    return make_rsrc(a.lse + (int64_t)h * a.total_q + qstart + q0, (uint32_t)(n < QROWS ? n : QROWS) * 4);
+    return make_rsrc(a.lse + (int64_t)h * a.total_q + qstart + q0, (uint32_t)(n < kRows ? n : kRows) * 4);
   }
   __device__ uint32_t l_at(int row) const { return (uint32_t)(row - q0) * 4; }
   __device__ void put_l(__amdgpu_buffer_rsrc_t r, int row, float m, float sum) const {
@@ -106,15 +101,15 @@ struct PackedView {
   }
 };
 
-template <int D, int QG, int WPS>
+template <int D, int WPS>
 __global__ __launch_bounds__(256, WPS) void packed_fwd_kernel(PackedArgs a) {
-  constexpr int QROWS = 128 * QG, KT = D == 256 ? 32 : 64;
+  constexpr int KT = D == 256 ? 32 : 64;
   const int tid = threadIdx.x;
   // Workgroup -> (K/V head, run of keys, slot, query head of the group).  Consecutive
   // workgroups go to the 8 XCDs in turn; each XCD takes a contiguous run, so that
   // the workgroups sharing an XCD's L2 read the same K and V.
   const int G = a.heads_q / a.heads_kv;
-  const int slots = a.total_q / QROWS + a.batch;
+  const int slots = a.total_q / kRows + a.batch;
   const int items = slots * a.heads_q * a.splits;
   const int per = (items + 7) >> 3;
   const int item = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
@@ -127,33 +122,33 @@ __global__ __launch_bounds__(256, WPS) void packed_fwd_kernel(PackedArgs a) {
   // all sequences, found by a search, costs more than the tail that it saves: 16 sequences of
   // 512 67 -> 73 us, 12 of 8192 in all 111 -> 112.)
   if (a.causal) slot = (a.heads_kv & 7) == 0 ? slots - 1 - slot : (slot & 1) ? slot >> 1 : slots - 1 - (slot >> 1);
-  const Rows r = rows_of<QROWS>(a, slot, tid & 63);
+  const Rows r = rows_of(a, slot, tid & 63);
   if (r.n <= 0) return;
   const int h = hk * G + in % G;
   Run run = {0, 0, 1};
   if (r.kv_end > 0) run = run_of<KT>(r.kv_end, a.splits, split);
   if (split >= run.n) return;
   const int64_t part = run.n > 1 ? ((int64_t)slot * a.heads_q + h) * a.splits + split : -1;
-  const PackedView<D, QROWS> view{a, h, hk, r.q0, r.q.len, run.keys, r.k.len - r.q.len - run.first, r.q.start, r.k.start + run.first, part};
+  const PackedView<D> view{a, h, hk, r.q0, r.q.len, run.keys, r.k.len - r.q.len - run.first, r.q.start, r.k.start + run.first, part};
   if (r.kv_end <= 0) {  // no row sees a key
     const auto ro = view.o(), rl = view.lse();
-    for (int e = tid; e < QROWS * (D / 4); e += 256) view.put_o(ro, r.q0 + e / (D / 4), 4 * (e % (D / 4)), 0.f, 0.f, 0.f, 0.f);
-    if (tid < QROWS) st4f(rl, view.l_at(r.q0 + tid), -INFINITY);
+    for (int e = tid; e < kRows * (D / 4); e += 256) view.put_o(ro, r.q0 + e / (D / 4), 4 * (e % (D / 4)), 0.f, 0.f, 0.f, 0.f);
+    if (tid < kRows) st4f(rl, view.l_at(r.q0 + tid), -INFINITY);
     return;
   }
-  attn_fwd_rows<D, QG>(view, a.causal, a.scale, r.q0);
+  attn_fwd_rows<D, 1>(view, a.causal, a.scale, r.q0);
 }
 
 // The runs of a slot's rows, in order: one workgroup per two passes of rows and head, D / 4
 // lanes a row: 1301 and 199 rows of 8 heads of 256 in two runs 7.6 us (8 passes a workgroup, one
 // after the other, 12.9).
-template <int D, int QROWS>
+template <int D>
 __global__ __launch_bounds__(256) void join_kernel(PackedArgs a) {
   constexpr int KT = D == 256 ? 32 : 64, RPP = 1024 / D, RWG = 2 * RPP;  // rows a pass, rows a workgroup
   const int tid = threadIdx.x;
-  const int x = (int)blockIdx.x / (QROWS / RWG), r0 = (int)blockIdx.x % (QROWS / RWG) * RWG;
+  const int x = (int)blockIdx.x / (kRows / RWG), r0 = (int)blockIdx.x % (kRows / RWG) * RWG;
   const int slot = x / a.heads_q, h = x % a.heads_q;
-  const Rows r = rows_of<QROWS>(a, slot, tid & 63);
+  const Rows r = rows_of(a, slot, tid & 63);
   if (r0 >= r.n || r.kv_end <= 0) return;
   const int n = run_of<KT>(r.kv_end, a.splits, 0).n;
   if (n == 1) return;  // the result is there
@@ -162,15 +157,15 @@ __global__ __launch_bounds__(256) void join_kernel(PackedArgs a) {
   for (int row = r0 + tid / (D / 4); row < r0 + RWG && row < r.n; row += RPP) {
     const float2* stat = (const float2*)a.part_l;  // m, sum
     float top = -INFINITY;
-    for (int i = 0; i < n; ++i) top = fmaxf(top, stat[(part + i) * QROWS + row].x);
+    for (int i = 0; i < n; ++i) top = fmaxf(top, stat[(part + i) * kRows + row].x);
     const float at = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     for (int i = 0; i < n; ++i) {
-      const float2 x = stat[(part + i) * QROWS + row];
+      const float2 x = stat[(part + i) * kRows + row];
       const float w = x.y * __builtin_amdgcn_exp2f(x.x - at);
       sum += w;
-      o += w * *(const f32x4*)(a.part_o + (part + i) * (QROWS * D) + row * D + c);
+      o += w * *(const f32x4*)(a.part_o + (part + i) * (kRows * D) + row * D + c);
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (nothing but -inf: O 0)
     *(u32x2*)((__bf16*)a.o + ((int64_t)r.q.start + r.q0 + row) * a.os.row + h * a.os.head + c) =
@@ -179,12 +174,11 @@ __global__ __launch_bounds__(256) void join_kernel(PackedArgs a) {
   }
 }
 
-template <int D, int QG, int WPS>
+template <int D, int WPS>
 void launch(const PackedArgs& a, hipStream_t stream) {
-  constexpr int QROWS = 128 * QG;
-  const long blocks = (long)(a.total_q / QROWS + a.batch) * a.heads_q, items = blocks * a.splits;
-  hipLaunchKernelGGL((packed_fwd_kernel<D, QG, WPS>), dim3((unsigned)((items + 7) / 8 * 8)), dim3(256), 0, stream, a);
-  if (a.splits > 1) hipLaunchKernelGGL((join_kernel<D, QROWS>), dim3((unsigned)(blocks * (QROWS / (2048 / D)))), dim3(256), 0, stream, a);
+  const long blocks = (long)(a.total_q / kRows + a.batch) * a.heads_q, items = blocks * a.splits;
+  hipLaunchKernelGGL((packed_fwd_kernel<D, WPS>), dim3((unsigned)((items + 7) / 8 * 8)), dim3(256), 0, stream, a);
+  if (a.splits > 1) hipLaunchKernelGGL((join_kernel<D>), dim3((unsigned)(blocks * (kRows / (2048 / D)))), dim3(256), 0, stream, a);
 }
 
 }  // namespace
@@ -219,9 +213,9 @@ size_t packed_part_rows(int total_q, int batch, int heads_q, int splits) {
 }
 
 hipError_t launch_packed_fwd(const PackedArgs& a, int d, hipStream_t stream) {
-  if (d == 64) launch<64, 1, 3>(a, stream);
-  else if (d == 128) launch<128, 1, 2>(a, stream);
-  else launch<256, 1, 1>(a, stream);
+  if (d == 64) launch<64, 3>(a, stream);
+  else if (d == 128) launch<128, 2>(a, stream);
+  else launch<256, 1>(a, stream);
   return hipGetLastError();
 }
 

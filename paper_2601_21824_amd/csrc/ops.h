@@ -88,7 +88,7 @@ hipError_t launch_packed_fwd(const PackedArgs& a, int d, hipStream_t stream);
 // The backward's main kernels run on BwdArgs; of those, a packed call uses q, k, v, o,
 // dO, lse, dq, dk, dv, dqacc, dvec and lse2 ([heads_q][total_q]), counters (one per 64-row
 // slot and query head), ctrl, order (start order -> sequence, KV tile), scale,
-// spin_limit, poison and status.
+// spin_limit and status.
 struct PackedBwdArgs : BwdArgs {
   PackedArgs p;
   Strides dos, dqs, dks, dvs;

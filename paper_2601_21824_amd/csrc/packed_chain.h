@@ -91,14 +91,9 @@ struct PackedChain {
     return make_rsrc(a.dqacc + (size_t)b.x * (kBlockRows * D), on ? kBlockRows * D * 4 : 0);
   }
 
-  __device__ static __amdgpu_buffer_rsrc_t rows(const void* p, int64_t first, const Strides& s, int head, int n, int most) {
-    const int r = n < most ? n : most;
-    const uint32_t bytes = r > 0 ? (uint32_t)(r - 1) * (uint32_t)s.row * 2 + D * 2 : 0;
-    return make_rsrc((const __bf16*)p + first * s.row + head * s.head, bytes);
-  }
   __device__ static uint32_t at(const Strides& s, int row, int col) { return (uint32_t)row * (uint32_t)s.row * 2 + (uint32_t)col * 2; }
   __device__ __amdgpu_buffer_rsrc_t block(const void* p, const Strides& s, PackedBlk b) const {
-    return rows(p, (int64_t)qstart + b.pb * kBlockRows, s, hk * G + b.h, sg.nq - b.pb * kBlockRows, kBlockRows);
+    return strided_rows<D>(p, (int64_t)qstart + b.pb * kBlockRows, s, hk * G + b.h, sg.nq - b.pb * kBlockRows, kBlockRows);
   }
   __device__ __amdgpu_buffer_rsrc_t q(PackedBlk b) const { return block(a.q, a.p.qs, b); }
   __device__ __amdgpu_buffer_rsrc_t dO(PackedBlk b) const { return block(a.dO, a.dos, b); }
@@ -109,7 +104,7 @@ struct PackedChain {
     return make_rsrc(p + (int64_t)(hk * G + b.h) * a.p.total_q + qstart + b.pb * kBlockRows, (uint32_t)(n < kBlockRows ? n : kBlockRows) * 4);
   }
   __device__ __amdgpu_buffer_rsrc_t tile(const void* p, const Strides& s) const {
-    return rows(p, (int64_t)kstart + j * BC, s, hk, sg.nk - j * BC, BC);
+    return strided_rows<D>(p, (int64_t)kstart + j * BC, s, hk, sg.nk - j * BC, BC);
   }
 };
 

@@ -1,7 +1,8 @@
 // paged.h -- device pieces shared by the variable-length operators: which
-// sequence a row belongs to, and reductions over the wave.
+// sequence a row belongs to, its resource, and reductions over the wave.
 #pragma once
 #include "common.h"
+#include "ops.h"
 
 namespace dash {
 
@@ -46,6 +47,15 @@ __device__ inline Span span_of(const int32_t* cu, int s, int total) {
 // (start + n) / rows - start / rows + 1 of them.)  At most total / rows + batch slots;
 // those between two sequences' blocks are empty.
 __device__ inline int first_slot(const int32_t* cu, int s, int total, int rows) { return clamp_row(cu[s], total) / rows + s; }
+
+// a resource over at most `most` of n rows from row `first` on: what lies past them reads 0 and
+// is not written
+template <int D>
+__device__ inline __amdgpu_buffer_rsrc_t strided_rows(const void* p, int64_t first, const Strides& s, int head, int n, int most) {
+  const int r = n < most ? n : most;
+  const uint32_t bytes = r > 0 ? (uint32_t)(r - 1) * (uint32_t)s.row * 2 + D * 2 : 0;
+  return make_rsrc((const __bf16*)p + first * s.row + head * s.head, bytes);
+}
 
 // x plus the lanes before it: four shifts inside rows of 16 lanes, then the last lane
 // of a row, and of the lower half, to those behind it.  All lanes active.
