@@ -355,8 +355,10 @@ void dash_release_workspace(void);
  *    clamped before use: no entry point reads or writes outside the tensors
  *    that its arguments describe.
  *  - A row whose keys are all masked, or all score -infinity, has O = 0, L = -infinity
- *    and no gradient.
- *  - Results are bitwise reproducible for the same call.
+ *    and no gradient (0; but 0 times an infinity that q or k itself holds is NaN in dK and dQ).
+ *  - Results are bitwise reproducible for the same call.  A sequence's bits may depend on the
+ *    other sequences of its call: how work is cut, and with it the order of sums, follows
+ *    from totals (each call says which).
  * ====================================================================== */
 
 typedef enum {
@@ -432,7 +434,8 @@ size_t dash_decode_workspace_size(int batch, int heads_q, int heads_kv, int d, i
  * [batch][heads_q][d]; lse NULL or fp32 [batch][heads_q].  scale as in
  * dash_attn_fwd_ex (0: 1/sqrt(d)), on top of k_scale.  A sequence of length 0
  * has O = 0, L = -infinity.  What the cache holds behind a sequence's last key does not
- * reach its result.  Asynchronous on `stream`; the workspace (256-byte
+ * reach its result.  Keys are summed in chunks whose size depends on all sequences' lengths
+ * together, heads_q, heads_kv, d and table_width * page_size.  Asynchronous on `stream`; the workspace (256-byte
  * aligned, any contents) must not be used by another call until this one has
  * finished.  status: NULL or a device int that the call sets to 1 when a length is
  * negative or more than table_width * page_size (clamped), or a page that it needs lies
@@ -471,7 +474,8 @@ size_t dash_packed_fwd_workspace_size(int batch, int total_q, int total_k, int h
    `stream`.  A call with few query rows for the GPU and long sequences is faster split over
    the keys, for which it needs a workspace of dash_packed_fwd_workspace_size bytes
    (256-byte aligned, any contents, not used by another call until this one has
-   finished); with NULL it is not split.  Both give the same result up to rounding. */
+   finished); with NULL it is not split.  Both give the same result up to rounding: the order
+   of the sums over a sequence's keys depends on d, total_q, total_k, batch, heads_q and the mask. */
 int dash_attn_packed_fwd(const dash_packed_t* p, const void* q, const void* k, const void* v, void* o, float* lse,
                          void* workspace, size_t ws_bytes, void* stream);
 

@@ -3,7 +3,8 @@
 //
 //   o_h = sum_j softmax_j(scale q_h . k_j) v_j over the lens[s] cached keys
 //
-// Bound by memory: K and V are read once, 4 d bytes a key and head (2 d in e4m3),
+// Bound by memory: K and V are read once for every 16 query heads of a K/V head (with more,
+// each 16 are a workgroup of their own), 4 d bytes a key and head (2 d in e4m3),
 // for 4 d G operations, G query heads to a K/V head.  So the kernel's business is
 // to keep loads in flight.  One workgroup takes a chunk of one sequence's keys for
 // one K/V head and up to 16 of its query heads; each of its four waves takes every
@@ -17,6 +18,9 @@
 //                 4g .. and 16 + 4g .. of V, D/16 columns each, and picks column by column
 // (g = l / 16).  The columns of V that one lane holds are D/16 neighbours, so that
 // 16 lanes read one whole row; O^T's rows come out in that order.
+// P goes into that product rounded to bf16, the MFMA's operand type: each weight by 2^-8 at most, as
+// much as O itself at the end.  Its sum takes it unrounded; sums, maxima and all that is
+// joined stay in fp32.
 // An e4m3 cache is widened to bf16, which holds every e4m3 value exactly; K's scale goes into
 // the softmax scale and V's into the output.
 //
@@ -151,7 +155,8 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kernel(DecodeArgs a) {
       for (int x = 0; x < 4; ++x) {
         const char* at = vp + v_lane + x * (uint32_t)((int)c.v_row * SZ);
         unsigned* v = t.v[4 * tt + x];
-        // nothing reads V's rows again, and one load takes a row whole: past the caches
+        // this workgroup does not read V's rows again (those of further 16 query heads do, from
+        // memory), and one load takes a row whole: past the caches
         if constexpr (T::VW == 1) v[0] = __builtin_nontemporal_load((const unsigned*)at);
         else if constexpr (T::VW == 2) *(u32x2*)v = __builtin_nontemporal_load((const u32x2*)at);
         else

@@ -2,7 +2,10 @@
 // before the main kernel, and the launch sequence of a call.  The main kernels are
 // bwd_main.h (128-row KV tiles at d = 64 and 128), attn_bwd64w.hip (256 rows at d = 64) and
 // attn_bwdw.hip (256 rows at d = 128, 128 at d = 256) on the chains of packed_chain.h, with the ordered dQ reduction
-// of the dense calls in Descending order.
+// of the dense calls in Descending order.  As there, P and dS are rounded to bf16, the MFMAs' operand
+// type, before the products that make dV, and dK and dQ (2^-8 of each term at most, as much as the
+// results' own rounding); scores, dP, D, L and every sum, the split chains' partials among them,
+// stay in fp32.
 //
 // packed_pre: D = rowsum(dO o O) and L log2(e) (+inf for a row that sees nothing, so that
 // its P is 0) for every row and head, of no sequence too; the ordering counters; dQ = 0

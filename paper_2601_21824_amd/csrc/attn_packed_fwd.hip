@@ -193,11 +193,15 @@ int packed_splits(int d, int total_q, int total_k, int batch, int heads_q, int c
   // workgroups with rows: whole slots, and one at least for each sequence
   const long rows = (total_q + 127) / 128 > batch ? (total_q + 127) / 128 : batch < total_q ? batch : total_q;
   const long blocks = rows * heads_q;
-  const long fit = d == 256 ? 256 : 512;  // workgroups that run at once on 256 CUs
+  // workgroups that run at once on 256 CUs: one a CU, or two (at d = 64, where three fit, two
+  // as well: the figures above were taken with this rule)
+  const long fit = d == 256 ? 256 : 512;
   // with as many queries as keys a causal block's work goes from one tile to all: runs
   // for two rounds level it, where two workgroups share a CU from three runs on
   const bool triangle = causal && total_k < 2L * total_q;
-  const long most = (long)total_k / batch / kMinRun;  // of a sequence of the average length
+  // of a sequence of the average length: the host knows no other, so that one long sequence among
+  // many short ones is split less than alone, or not at all
+  const long most = (long)total_k / batch / kMinRun;
   long s = blocks > 0 ? (triangle ? 2 : 1) * fit / blocks : 1;
   s = s < most ? s : most;
   if (triangle && d < 256 && s < 3) s = 1;

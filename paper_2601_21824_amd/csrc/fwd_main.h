@@ -6,7 +6,8 @@
 // units of 32 keys.  Per wave and unit: S^T = K Q^T on bf16 MFMA 32x32x16 (the
 // C layout then holds one query per lane, so row maxima and sums are in-lane up
 // to one swap of the lane halves), online softmax in the log2 domain, O^T += V^T P^T
-// with P^T fed to the MFMA straight from registers and V^T read from the
+// with P^T fed to the MFMA straight from registers (rounded to bf16, the MFMA's operand type: each
+// weight by 2^-8 at most, as much as O itself; the row sum takes P unrounded, in fp32) and V^T read from the
 // row-major tile by transposed LDS reads.  Deterministic: every reduction is
 // inside one wave in a fixed order.
 //
