@@ -398,9 +398,11 @@ def dash_kv_append(k, v, k_cache, v_cache, block_table, lens, cu=None, q=None, q
     """New keys and values (bf16 [tokens, heads_kv, d]) into a paged cache behind the
     ``lens`` rows that each sequence has, keys and queries rotated by their place
     (``inv_freq``: fp32, one per rotated pair).  ``cu``: int32 [batch + 1], where each
-    sequence's tokens begin; without it every sequence gets one token.  The rotated
+    sequence's tokens begin (rows before cu[0] and from cu[-1] on are left alone); without it every
+    sequence gets one token.  The rotated
     queries go to ``q_out`` and, if given, the rotated keys to ``k_out``.
-    ``status``: optional int32 that a token without a page sets to 1."""
+    ``status``: optional int32 that a token without a page, or a row between offsets that do
+    not rise, sets to 1."""
     import torch
     if k.dim() != 3:
         _bad("k must be [tokens, heads_kv, d]")
@@ -457,6 +459,7 @@ def dash_attn_decode(q, k_cache, v_cache, block_table, lens, o, lse=None, scale=
 
 def attn_decode(q, k_cache, v_cache, block_table, lens, scale=None, k_scale=None, v_scale=None, workspace=None,
                 status=None):
+    """dash_attn_decode into a new o."""
     import torch
     o = torch.empty_like(q, memory_format=torch.contiguous_format)
     dash_attn_decode(q, k_cache, v_cache, block_table, lens, o, None, scale, k_scale, v_scale, workspace, status)
@@ -507,6 +510,8 @@ def dash_attn_packed_fwd(q, k, v, o, lse, cu_q, cu_k=None, causal: bool = True, 
 
 
 def attn_packed_fwd(q, k, v, cu_q, cu_k=None, causal: bool = True, scale=None):
+    """dash_attn_packed_fwd into a new o and lse.  Rows that belong to no sequence (before
+    cu_q[0], from cu_q[-1] on) hold whatever the memory held."""
     import torch
     dev = _gpu(q)
     if q.dim() != 3 or k.dim() != 3:
@@ -548,6 +553,9 @@ def dash_attn_packed_bwd(q, k, v, o, dO, lse, dq, dk, dv, cu_q, cu_k=None, causa
 
 
 def attn_packed_bwd(q, k, v, o, dO, lse, cu_q, cu_k=None, causal: bool = True, scale=None, workspace=None):
+    """dash_attn_packed_bwd into new dq, dk and dv.  Rows that belong to no sequence hold
+    whatever the memory held: of a padded batch, take the sequences' rows alone, or give
+    dash_attn_packed_bwd gradients filled with zeros."""
     import torch
     dq, dk, dv = (torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, v))
     dash_attn_packed_bwd(q, k, v, o, dO, lse, dq, dk, dv, cu_q, cu_k, causal, scale, workspace)
