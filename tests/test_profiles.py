@@ -50,3 +50,18 @@ def test_bench_names_a_summary_of_the_kernel_it_runs():
     fields = dict(l.split(": ", 1) for l in text.splitlines() if ": " in l and not l.startswith(" "))
     assert os.path.isfile(os.path.join(ROOT, fields["source_file"]))
     assert float(fields["traffic_bytes_per_launch"]) > 0
+
+
+def test_summaries_are_of_the_sources_that_are_here():
+    """A summary whose kernel has changed since says so."""
+    import hashlib
+    for path in PROFILES:
+        text = open(path).read()
+        for src, sha in re.findall(r"Source of the kernel at measurement time: (\S+) sha256 prefix ([0-9a-f]{16})", text):
+            now = hashlib.sha256(open(os.path.join(ROOT, src), "rb").read()).hexdigest()[:16]
+            assert now == sha or "source has changed since" in text, (path, src)
+
+
+def test_bench_reports_traffic():
+    import bench
+    assert bench.measured_traffic() is not None
