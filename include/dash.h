@@ -421,8 +421,8 @@ typedef struct {
  * saturated at 448.  status: NULL or a device int that the call sets to 1
  * when a token's place lies outside its row of block_table or in a page
  * outside 0 .. pages-1 (that token is not stored; its q_out and k_out are still
- * written), or when offsets that do not rise leave a row without a sequence.  The call
- * never sets it to 0.
+ * written), or when offsets that do not rise leave a row of cu[0] .. cu[batch]-1 without a
+ * sequence.  The call never sets it to 0.
  */
 int dash_kv_append(const dash_paged_cache_t* cache, const dash_append_t* x, int* status, void* stream);
 
@@ -446,8 +446,8 @@ int dash_attn_decode(const dash_paged_cache_t* cache, const void* q, int64_t q_r
                      size_t ws_bytes, int* status, void* stream);
 
 /* Packed sequences: the queries of sequence s are rows cu_q[s] .. cu_q[s+1]-1 of q
-   (keys: cu_k, k and v); offsets rise from 0.  Rows from cu_q[batch] (cu_k[batch]) on
-   belong to nobody: what they hold is not read into any result, and outputs are left
+   (keys: cu_k, k and v); offsets rise from 0 or more.  Rows before cu_q[0] (cu_k[0]) and from
+   cu_q[batch] (cu_k[batch]) on belong to nobody: what they hold is not read into any result, and outputs are left
    alone there.  With m queries and n keys and causal != 0, query i of a sequence sees
    key j iff j - i <= n - m (the last query sees every key); else all n.  Under a causal
    mask a NaN or an infinity in V reaches queries before it as well where they share a tile
