@@ -3,7 +3,7 @@
  * AMD Instinct MI355X (gfx950), with the dQ reduction order scheduled as in
  * "DASH: Deterministic Attention Scheduling for High-throughput Reproducible
  * LLM Training" (arXiv 2601.21824), over dense batches and over packed sequences
- * of different lengths; and attention over a paged key-value cache.
+ * of different lengths; rotary positions; and attention over a paged key-value cache.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -341,8 +341,8 @@ const char* dash_last_error(void);
 void dash_release_workspace(void);
 
 /* ======================================================================
- * Sequences of different lengths: packed prompts, a paged key-value cache
- * and attention of one new token.
+ * Sequences of different lengths: packed prompts, rotary positions, a paged key-value
+ * cache and attention of one new token.
  *
  * Conventions of these entry points, beside the shared ones above:
  *  - Query head h reads K/V head h / (heads_q / heads_kv); heads_kv divides heads_q.
@@ -363,7 +363,11 @@ void dash_release_workspace(void);
 
 typedef enum {
   DASH_CACHE_BF16 = 0,
-  DASH_CACHE_E4M3 = 1 /* OCP 8-bit e4m3 */
+  DASH_CACHE_E4M3 = 1, /* OCP 8-bit e4m3 */
+  /* Microscaled (the OCP MX formats' elements and scales): 32 neighbouring components of a row
+     share a power of two 2^e, kept as the byte 127 + e.  e4m3, or two e2m1 a byte, the lower half first. */
+  DASH_CACHE_MXFP4 = 4,
+  DASH_CACHE_MXFP8 = 8
 } dash_cache_type_t;
 
 /* A paged key-value cache: `pages` pages of page_size rows for each of heads_kv
@@ -387,6 +391,11 @@ typedef struct {
      scale.  E4M3 only. */
   const float* k_scale;
   const float* v_scale;
+  /* MXFP8 and MXFP4 only (not looked at for the other types): the scale bytes, contiguous
+     [pages][heads_kv][page_size][d / 32], 16-byte aligned, written by dash_kv_append.  Strides of an MXFP4
+     cache are in bytes (a row has d / 2), multiples of 16. */
+  void* k_mx;
+  void* v_mx;
 } dash_paged_cache_t;
 
 /* New tokens of dash_kv_append. */
@@ -418,13 +427,83 @@ typedef struct {
  * query, into q_out) rotated by that place.  cache->lens holds the lengths before
  * the call and is not changed.  The angle is computed in 64 bits, the rest in 32 with
  * one rounding at the store; E4M3 stores value / scale rounded to nearest even and
- * saturated at 448.  status: NULL or a device int that the call sets to 1
+ * saturated at 448.  MXFP8 and MXFP4 rotate in 64 bits, round the key to fp32 and store value / 2^e
+ * rounded to nearest even, e the least exponent with which the block's largest value is at most
+ * 448 2^e (6 2^e), and at least -117; finite values from 1.5 2^127 on count as that, and a block that holds a
+ * NaN or an infinity has the scale byte 255: it reads as NaN.  status: NULL or a device int that the call sets to 1
  * when a token's place lies outside its row of block_table or in a page
  * outside 0 .. pages-1 (that token is not stored; its q_out and k_out are still
  * written), or when offsets that do not rise leave a row of cu[0] .. cu[batch]-1 without a
  * sequence.  The call never sets it to 0.
  */
 int dash_kv_append(const dash_paged_cache_t* cache, const dash_append_t* x, int* status, void* stream);
+
+/* Rows that dash_kv_read reads back. */
+typedef struct {
+  int rows; /* of k_out and v_out */
+  /* [batch + 1], rising from 0 or more: rows cu[s] .. cu[s+1]-1 receive keys first[s] ..
+     of sequence s.  Rows before cu[0] and from cu[batch] on are left alone. */
+  const int32_t* cu;
+  const int32_t* first; /* [batch]; NULL: 0 */
+  void* k_out;          /* bf16 [rows][heads_kv][d], or NULL */
+  void* v_out;
+  int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+} dash_read_t;
+
+/*
+ * Keys and values of a paged cache of any type as packed bf16 rows (what
+ * dash_attn_packed_fwd takes): the cached value (BF16), times its head's scale and
+ * rounded (E4M3), or times 2^e, which is exact (MXFP8, MXFP4).  A row whose key is negative, at or behind lens[s], or in a page outside 0 .. pages-1
+ * is left alone and sets status, NULL or a device int, to 1, and so do offsets that do not
+ * rise; the call never sets it to 0.
+ */
+int dash_kv_read(const dash_paged_cache_t* cache, const dash_read_t* x, int* status, void* stream);
+
+/* Rows of dash_rotary. */
+typedef struct {
+  int rows, heads_q, heads_k, d;
+  /* The position of each row: positions[t], or, where that is NULL, start[s] + t - cu[s] in sequence s
+     (cu [batch + 1], rising from 0 or more; start [batch], NULL: 0).  Rows that no
+     sequence holds are left alone. */
+  const int32_t* positions;
+  const int32_t* cu;
+  const int32_t* start;
+  int batch;
+  const void* q; /* bf16 [rows][heads_q][d], or NULL */
+  const void* k; /* bf16 [rows][heads_k][d], or NULL */
+  void* q_out;   /* (may be q, with the same strides) */
+  void* k_out;
+  int64_t q_row_stride, q_head_stride, k_row_stride, k_head_stride;
+  int64_t q_out_row_stride, q_out_head_stride, k_out_row_stride, k_out_head_stride;
+  const float* inv_freq; /* [rotary_dim / 2]: pair i at position p turns by p * inv_freq[i] */
+  int rotary_dim;        /* a multiple of 16, at most d; the components behind it are copied */
+  int interleaved;       /* 0: pairs (i, i + rotary_dim/2); else (2i, 2i + 1) */
+  float amplitude;       /* of the rotated components; 0: 1 */
+  int backward;          /* q and k are gradients of rotated ones: turned back, times the amplitude */
+} dash_rotary_t;
+
+/*
+ * Rotary positions: (x, y) of each pair becomes amplitude (x cos - y sin, x sin + y cos), or,
+ * backward, amplitude (x cos + y sin, y cos - x sin).  The angle is reduced in 64 bits, the rest is
+ * in 32 with one rounding at the store.  status: NULL or a device int that offsets that do not
+ * rise set to 1; never to 0.
+ */
+int dash_rotary(const dash_rotary_t* x, int* status, void* stream);
+
+typedef enum {
+  DASH_ROTARY_PLAIN = 0,  /* base^(-2i / rotary_dim) */
+  DASH_ROTARY_LINEAR = 1, /* positions squeezed: the same over `factor` */
+  DASH_ROTARY_BASE = 2,   /* base times factor^(n / (n - 2)), n = rotary_dim: the slowest pair as LINEAR, the fastest as PLAIN */
+  DASH_ROTARY_PARTS = 3   /* pairs that turn more than `fast` times over `original` positions as PLAIN, less than
+                             `slow` times as LINEAR, the others between; amplitude 0.1 ln(factor) + 1
+                             (Peng et al., arXiv 2309.00071) */
+} dash_rotary_scaling_t;
+
+/* The frequencies of a context stretched by `factor` >= 1 from `original` positions, into
+   inv_freq[rotary_dim / 2] in HOST memory, and the amplitude that belongs to them.  original, fast
+   and slow are for PARTS (the paper takes 32 and 1).  Host computation in 64 bits. */
+int dash_rotary_frequencies(int rotary_dim, double base, int scaling, double factor, double original, double fast,
+                            double slow, float* inv_freq, float* amplitude);
 
 /* Bytes of workspace for dash_attn_decode (0 if the arguments are invalid). */
 size_t dash_decode_workspace_size(int batch, int heads_q, int heads_kv, int d, int page_size, int table_width);
@@ -444,6 +523,27 @@ size_t dash_decode_workspace_size(int batch, int heads_q, int heads_kv, int d, i
 int dash_attn_decode(const dash_paged_cache_t* cache, const void* q, int64_t q_row_stride, int64_t q_head_stride,
                      void* o, int64_t o_row_stride, int64_t o_head_stride, float* lse, float scale, void* workspace,
                      size_t ws_bytes, int* status, void* stream);
+
+/* Bytes of workspace for dash_attn_prefix_decode (0 if the arguments are invalid). */
+size_t dash_prefix_decode_workspace_size(int batch, int heads_q, int heads_kv, int d, int page_size, int table_width,
+                                         int prefix_width);
+
+/*
+ * dash_attn_decode for a batch whose sequences share their first keys: *prefix_len (a device int, 0 ..
+ * prefix_width * page_size) of them, in the pages prefix_table[0 .. prefix_width-1], which are read and
+ * multiplied once for all sequences.  lens and block_table are those of dash_attn_decode (and
+ * of dash_kv_append), the shared keys among them: sequence s attends to the first
+ * min(*prefix_len, lens[s]) keys of prefix_table and to its keys *prefix_len .. lens[s]-1 of block_table, whose
+ * entries for whole shared pages are not looked at.  A prefix may end inside a page; each sequence's own
+ * page then goes on behind it.  Keys are summed in runs of the prefix, whose number depends on *prefix_len,
+ * batch, heads_q, heads_kv, d and prefix_width * page_size, and in chunks of the rest as by dash_attn_decode.
+ * Workspace of dash_prefix_decode_workspace_size bytes; the other arguments are those of dash_attn_decode.
+ * status: also set to 1 when *prefix_len is out of range (clamped).
+ */
+int dash_attn_prefix_decode(const dash_paged_cache_t* cache, const int32_t* prefix_table, int prefix_width,
+                            const int32_t* prefix_len, const void* q, int64_t q_row_stride, int64_t q_head_stride,
+                            void* o, int64_t o_row_stride, int64_t o_head_stride, float* lse, float scale,
+                            void* workspace, size_t ws_bytes, int* status, void* stream);
 
 /* Packed sequences: the queries of sequence s are rows cu_q[s] .. cu_q[s+1]-1 of q
    (keys: cu_k, k and v); offsets rise from 0 or more.  Rows before cu_q[0] (cu_k[0]) and from

@@ -32,8 +32,10 @@ EXPORTS = ("dash_attn_fwd", "dash_attn_fwd_ex", "dash_attn_bwd", "dash_bwd_works
            "dash_bwd_placement", "dash_mfma_peak", "dash_last_error", "dash_release_workspace",
            "dash_auto_schedule", "dash_model_makespan", "dash_kv_append", "dash_attn_decode",
            "dash_decode_workspace_size", "dash_attn_packed_fwd", "dash_attn_packed_bwd",
-           "dash_packed_workspace_size", "dash_packed_fwd_workspace_size")
-DASH_CACHE_BF16, DASH_CACHE_E4M3 = 0, 1
+           "dash_packed_workspace_size", "dash_packed_fwd_workspace_size", "dash_kv_read", "dash_rotary",
+           "dash_rotary_frequencies", "dash_attn_prefix_decode", "dash_prefix_decode_workspace_size")
+DASH_CACHE_BF16, DASH_CACHE_E4M3, DASH_CACHE_MXFP4, DASH_CACHE_MXFP8 = 0, 1, 4, 8
+ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
 
 
 class DashError(RuntimeError):
@@ -59,7 +61,8 @@ class dash_paged_cache_t(ctypes.Structure):
                 ("table_width", _CI), ("cache_type", _CI), ("k_cache", _VP), ("v_cache", _VP),
                 ("k_page_stride", _I64), ("k_head_stride", _I64), ("k_row_stride", _I64),
                 ("v_page_stride", _I64), ("v_head_stride", _I64), ("v_row_stride", _I64),
-                ("block_table", _VP), ("table_stride", _I64), ("lens", _VP), ("k_scale", _VP), ("v_scale", _VP)]
+                ("block_table", _VP), ("table_stride", _I64), ("lens", _VP), ("k_scale", _VP), ("v_scale", _VP),
+                ("k_mx", _VP), ("v_mx", _VP)]
 
 
 class dash_append_t(ctypes.Structure):
@@ -68,6 +71,19 @@ class dash_append_t(ctypes.Structure):
                 ("q_row_stride", _I64), ("q_head_stride", _I64), ("q_out_row_stride", _I64),
                 ("q_out_head_stride", _I64), ("k_out_row_stride", _I64), ("k_out_head_stride", _I64),
                 ("inv_freq", _VP), ("rotary_dim", _CI), ("interleaved", _CI)]
+
+
+class dash_read_t(ctypes.Structure):
+    _fields_ = [("rows", _CI), ("cu", _VP), ("first", _VP), ("k_out", _VP), ("v_out", _VP), ("k_row_stride", _I64),
+                ("k_head_stride", _I64), ("v_row_stride", _I64), ("v_head_stride", _I64)]
+
+
+class dash_rotary_t(ctypes.Structure):
+    _fields_ = [("rows", _CI), ("heads_q", _CI), ("heads_k", _CI), ("d", _CI), ("positions", _VP), ("cu", _VP), ("start", _VP),
+                ("batch", _CI), ("q", _VP), ("k", _VP), ("q_out", _VP), ("k_out", _VP),
+                ("q_row_stride", _I64), ("q_head_stride", _I64), ("k_row_stride", _I64), ("k_head_stride", _I64),
+                ("q_out_row_stride", _I64), ("q_out_head_stride", _I64), ("k_out_row_stride", _I64), ("k_out_head_stride", _I64),
+                ("inv_freq", _VP), ("rotary_dim", _CI), ("interleaved", _CI), ("amplitude", ctypes.c_float), ("backward", _CI)]
 
 
 class dash_packed_t(ctypes.Structure):
@@ -93,7 +109,8 @@ def _packer(cls):
     return pack
 
 
-_pack_cache, _pack_append, _pack_packed = map(_packer, (dash_paged_cache_t, dash_append_t, dash_packed_t))
+_pack_cache, _pack_append, _pack_packed, _pack_read, _pack_rotary = map(
+    _packer, (dash_paged_cache_t, dash_append_t, dash_packed_t, dash_read_t, dash_rotary_t))
 _lib = None
 
 
@@ -134,12 +151,19 @@ def load():
         lib.dash_packed_fwd_workspace_size.argtypes = [ci] * 6
         lib.dash_packed_fwd_workspace_size.restype = sz
         lib.dash_decode_workspace_size.restype = sz
+        lib.dash_kv_read.argtypes = [vp, vp, vp, vp]
+        lib.dash_rotary.argtypes = [vp, vp, vp]
+        lib.dash_rotary_frequencies.argtypes = [ci, ctypes.c_double, ci] + [ctypes.c_double] * 4 + [vp, ctypes.POINTER(cf)]
+        lib.dash_attn_prefix_decode.argtypes = [vp, vp, ci, vp, vp, _I64, _I64, vp, _I64, _I64, vp, cf, vp, sz, vp, vp]
+        lib.dash_prefix_decode_workspace_size.argtypes = [ci] * 7
+        lib.dash_prefix_decode_workspace_size.restype = sz
         lib.dash_last_error.restype = ctypes.c_char_p
         lib.dash_release_workspace.restype = None
         for f in ("dash_attn_fwd", "dash_attn_fwd_ex", "dash_attn_bwd", "dash_attn_bwd_ex", "dash_attn_bwd_noalloc",
                   "dash_bwd_check", "dash_resolve_schedule", "dash_schedule_table", "dash_bwd_placement",
                   "dash_mfma_peak", "dash_auto_schedule", "dash_model_makespan", "dash_kv_append", "dash_attn_decode",
-                  "dash_attn_packed_fwd", "dash_attn_packed_bwd"):
+                  "dash_attn_packed_fwd", "dash_attn_packed_bwd", "dash_kv_read", "dash_rotary", "dash_rotary_frequencies",
+                  "dash_attn_prefix_decode"):
             getattr(lib, f).restype = ci
         _lib = lib
     return _lib
@@ -368,14 +392,22 @@ def _call(f, dev, stream, *args):
 
 
 def _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q, dev):
-    """dash_paged_cache_t of [pages, heads_kv, page_size, d] caches (any strides, contiguous rows)."""
+    """dash_paged_cache_t of [pages, heads_kv, page_size, d] caches (any strides, contiguous rows), and its
+    d: bfloat16; float8_e4m3fn with a scale per head or none, or with a scale byte per 32 components
+    (uint8 [pages, heads_kv, page_size, d / 32]); or uint8 [..., d / 2], two e2m1 each, with scale bytes."""
     import torch
-    dt = k_cache.dtype
-    if dt is not torch.bfloat16 and dt is not torch.float8_e4m3fn:
-        _bad("caches must be bfloat16 or float8_e4m3fn")
+    dt, u8 = k_cache.dtype, torch.uint8
     if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or v_cache.dtype is not dt or v_cache.get_device() != dev:
         _bad("k_cache and v_cache must be [pages, heads_kv, page_size, d] tensors alike")
     pages, heads_kv, page, d = k_cache.shape
+    if dt is torch.bfloat16:
+        kind = DASH_CACHE_BF16
+    elif dt is torch.float8_e4m3fn:
+        kind = DASH_CACHE_E4M3 if (k_scale is None or k_scale.dtype is not u8) and (v_scale is None or v_scale.dtype is not u8) else DASH_CACHE_MXFP8
+    elif dt is u8:
+        kind, d = DASH_CACHE_MXFP4, 2 * d
+    else:
+        _bad("caches must be bfloat16, float8_e4m3fn or (MXFP4) uint8")
     (kp, kh, kr, k1), (vp, vh, vr, v1) = k_cache.stride(), v_cache.stride()
     if k1 != 1 or v1 != 1:
         _bad("the last dimension of the caches must be contiguous")
@@ -386,11 +418,16 @@ def _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q, dev):
     row, one = block_table.stride()
     if rows != batch or (width > 1 and one != 1):
         _bad("block_table must be [batch, width] with contiguous rows")
+    ks = vs = kx = vx = 0
+    if kind >= DASH_CACHE_MXFP4:
+        if k_scale is None or v_scale is None:
+            _bad("a microscaled cache needs k_scale and v_scale")
+        kx, vx = (_flat(name, x, u8, dev, pages, heads_kv, page, d // 32) for name, x in (("k_scale", k_scale), ("v_scale", v_scale)))
+    else:
+        ks, vs = (_flat(name, x, torch.float32, dev, heads_kv) for name, x in (("k_scale", k_scale), ("v_scale", v_scale)))
     return _pack_cache(
-        batch, heads_q, heads_kv, d, pages, page, width, DASH_CACHE_BF16 if dt is torch.bfloat16 else DASH_CACHE_E4M3,
-        k_cache.data_ptr(), v_cache.data_ptr(), kp, kh, kr, vp, vh, vr, block_table.data_ptr(), row if batch > 1 else width,
-        _flat("lens", lens, torch.int32, dev, batch), _flat("k_scale", k_scale, torch.float32, dev, heads_kv),
-        _flat("v_scale", v_scale, torch.float32, dev, heads_kv))
+        batch, heads_q, heads_kv, d, pages, page, width, kind, k_cache.data_ptr(), v_cache.data_ptr(), kp, kh, kr, vp, vh, vr,
+        block_table.data_ptr(), row if batch > 1 else width, _flat("lens", lens, torch.int32, dev, batch), ks, vs, kx, vx), d
 
 
 def dash_kv_append(k, v, k_cache, v_cache, block_table, lens, cu=None, q=None, q_out=None, k_out=None, inv_freq=None,
@@ -401,6 +438,8 @@ def dash_kv_append(k, v, k_cache, v_cache, block_table, lens, cu=None, q=None, q
     sequence's tokens begin (rows before cu[0] and from cu[-1] on are left alone); without it every
     sequence gets one token.  The rotated
     queries go to ``q_out`` and, if given, the rotated keys to ``k_out``.
+    A microscaled cache (float8_e4m3fn, or uint8 for MXFP4, with uint8 ``k_scale`` and ``v_scale``
+    [pages, heads_kv, page_size, d / 32]) gets its scale bytes too.
     ``status``: optional int32 that a token without a page, or a row between offsets that do
     not rise, sets to 1."""
     import torch
@@ -413,9 +452,9 @@ def dash_kv_append(k, v, k_cache, v_cache, block_table, lens, cu=None, q=None, q
     dev = _gpu(k_cache)
     tokens, heads_kv, d = k.shape
     heads_q = heads_kv if q is None else q.shape[1]
-    c = _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q, dev)
+    c, cd = _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q, dev)
     bf, i32 = torch.bfloat16, torch.int32
-    if k_cache.shape[1] != heads_kv or k_cache.shape[3] != d:
+    if k_cache.shape[1] != heads_kv or cd != d:
         _bad("k and k_cache must have the same heads and head dim")
     none = (0, 0, 0)
     kp, *ks = _rows("k", k, bf, dev, tokens, heads_kv, d)
@@ -445,8 +484,8 @@ def dash_attn_decode(q, k_cache, v_cache, block_table, lens, o, lse=None, scale=
         _bad("q must be [batch, heads_q, d]")
     dev = _gpu(k_cache)
     batch, heads_q, d = q.shape
-    c = _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q, dev)
-    pages, heads_kv, page, cd = k_cache.shape
+    c, cd = _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q, dev)
+    _, heads_kv, page, _ = k_cache.shape
     if lens.numel() != batch or cd != d:
         _bad("q, lens and the caches must have the same batch and head dim")
     lib = load()
@@ -466,6 +505,139 @@ def attn_decode(q, k_cache, v_cache, block_table, lens, scale=None, k_scale=None
     return o
 
 
+def dash_prefix_decode_workspace_size(batch: int, heads_q: int, heads_kv: int, d: int, page_size: int, table_width: int,
+                                      prefix_width: int) -> int:
+    return int(load().dash_prefix_decode_workspace_size(batch, heads_q, heads_kv, d, page_size, table_width, prefix_width))
+
+
+def dash_attn_prefix_decode(q, k_cache, v_cache, block_table, lens, prefix_table, prefix_len, o, lse=None, scale=None,
+                            k_scale=None, v_scale=None, workspace=None, status=None, stream=None):
+    """dash_attn_decode for a batch whose sequences share their first ``prefix_len`` keys (int32, one
+    element, on the device), in the pages ``prefix_table`` (int32 [width]), read once for all of
+    them.  ``lens`` and ``block_table`` count the shared keys as dash_attn_decode does."""
+    import torch
+    if q.dim() != 3:
+        _bad("q must be [batch, heads_q, d]")
+    dev = _gpu(k_cache)
+    batch, heads_q, d = q.shape
+    c, cd = _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q, dev)
+    _, heads_kv, page, _ = k_cache.shape
+    if lens.numel() != batch or cd != d:
+        _bad("q, lens and the caches must have the same batch and head dim")
+    if prefix_table.dim() != 1:
+        _bad("prefix_table must be int32 [width]")
+    width = prefix_table.numel()
+    pt, pl = _flat("prefix_table", prefix_table, torch.int32, dev, width), _flat("prefix_len", prefix_len, torch.int32, dev, prefix_len.numel())
+    if prefix_len.numel() != 1:
+        _bad("prefix_len must be one int32")
+    lib = load()
+    need = 0 if workspace is not None else lib.dash_prefix_decode_workspace_size(batch, heads_q, heads_kv, d, page, block_table.shape[1], width)
+    ws, size, workspace = _space(workspace, need, q, dev, stream)
+    _call(lib.dash_attn_prefix_decode, dev, stream, c, pt, width, pl, *_rows("q", q, torch.bfloat16, dev, batch, heads_q, d),
+          *_rows("o", o, torch.bfloat16, dev, batch, heads_q, d), _flat("lse", lse, torch.float32, dev, batch, heads_q),
+          0.0 if scale is None else scale, ws, size, _flat("status", status, torch.int32, dev, 1))
+
+
+def attn_prefix_decode(q, k_cache, v_cache, block_table, lens, prefix_table, prefix_len, scale=None, k_scale=None, v_scale=None,
+                       workspace=None, status=None):
+    """dash_attn_prefix_decode into a new o."""
+    import torch
+    o = torch.empty_like(q, memory_format=torch.contiguous_format)
+    dash_attn_prefix_decode(q, k_cache, v_cache, block_table, lens, prefix_table, prefix_len, o, None, scale, k_scale, v_scale,
+                            workspace, status)
+    return o
+
+
+def dash_kv_read(k_cache, v_cache, block_table, lens, cu, k_out=None, v_out=None, first=None, k_scale=None, v_scale=None,
+                 status=None, stream=None):
+    """Keys and values of a paged cache of any type as packed bf16 rows into ``k_out`` and ``v_out``
+    ([rows, heads_kv, d], either may be None): rows cu[s] .. cu[s+1]-1 (``cu``: int32 [batch + 1]) receive
+    sequence s's keys ``first``[s] .. (int32 [batch]; None: from its first).  Rows of no sequence are left alone.
+    ``status``: optional int32 that a key behind ``lens`` or in no page sets to 1; its row is left alone."""
+    import torch
+    dev = _gpu(k_cache)
+    heads_kv = k_cache.shape[1] if k_cache.dim() == 4 else 0
+    c, d = _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_kv, dev)
+    out = k_out if k_out is not None else v_out
+    if out is None or out.dim() != 3:
+        _bad("k_out or v_out must be [rows, heads_kv, d]")
+    rows, batch = out.shape[0], lens.numel()
+    bf, i32 = torch.bfloat16, torch.int32
+    none = (0, 0, 0)
+    kp, *ks = none if k_out is None else _rows("k_out", k_out, bf, dev, rows, heads_kv, d)
+    vp, *vs = none if v_out is None else _rows("v_out", v_out, bf, dev, rows, heads_kv, d)
+    x = _pack_read(rows, _flat("cu", cu, i32, dev, batch + 1), _flat("first", first, i32, dev, batch), kp, vp, *ks, *vs)
+    _call(load().dash_kv_read, dev, stream, c, x, _flat("status", status, i32, dev, 1))
+
+
+def kv_read(k_cache, v_cache, block_table, lens, cu, rows: int, first=None, k_scale=None, v_scale=None, status=None):
+    """dash_kv_read into new k and v of ``rows`` rows.  Rows that no key is read into hold whatever the memory held."""
+    import torch
+    if k_cache.dim() != 4:
+        _bad("k_cache and v_cache must be [pages, heads_kv, page_size, d] tensors alike")
+    d = k_cache.shape[3] * (2 if k_cache.dtype is torch.uint8 else 1)
+    k, v = (torch.empty((rows, k_cache.shape[1], d), dtype=torch.bfloat16, device=k_cache.device) for _ in range(2))
+    dash_kv_read(k_cache, v_cache, block_table, lens, cu, k, v, first, k_scale, v_scale, status)
+    return k, v
+
+
+# ----------------------------------------------------------------- rotary positions
+def dash_rotary(q, k, q_out, k_out, inv_freq, positions=None, cu=None, start=None, interleaved: bool = False,
+                amplitude: float = 1.0, backward: bool = False, status=None, stream=None):
+    """Queries and keys (bf16 [rows, heads, d], either may be None) turned by their positions into q_out and
+    k_out (which may be q and k): ``positions`` (int32 [rows]), or ``start``[s] + t - ``cu``[s] for row t of
+    sequence s (int32 [batch], None: 0, and [batch + 1]).  Pair i turns by position * ``inv_freq``[i] (fp32), times
+    ``amplitude``.  ``backward``: q and k are gradients of rotated ones, turned back.  Rows of no sequence are left alone."""
+    import torch
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None):
+        _bad("q and q_out, k and k_out come together")
+    one = q if q is not None else k
+    if one is None or one.dim() != 3 or (k is not None and k.dim() != 3):
+        _bad("q and k must be [rows, heads, d]")
+    if (positions is None) == (cu is None) or (start is not None and cu is None):
+        _bad("either positions, or cu (and start)")
+    if inv_freq is None:
+        _bad("inv_freq must be given")
+    if not float(amplitude):
+        _bad("amplitude must not be 0")
+    dev = _gpu(one)
+    rows, _, d = one.shape
+    bf, i32 = torch.bfloat16, torch.int32
+    none, heads = (0, 0, 0), [0 if x is None else x.shape[1] for x in (q, k)]
+    qp, *qs = none if q is None else _rows("q", q, bf, dev, rows, heads[0], d)
+    kp, *ks = none if k is None else _rows("k", k, bf, dev, rows, heads[1], d)
+    qo, *qos = none if q is None else _rows("q_out", q_out, bf, dev, rows, heads[0], d)
+    ko, *kos = none if k is None else _rows("k_out", k_out, bf, dev, rows, heads[1], d)
+    if cu is not None and (cu.dim() != 1 or cu.numel() < 1):
+        _bad("cu must be int32 [batch + 1]")
+    batch = 0 if cu is None else cu.numel() - 1
+    n = inv_freq.numel()
+    x = _pack_rotary(rows, *heads, d, _flat("positions", positions, i32, dev, rows), _flat("cu", cu, i32, dev, batch + 1),
+                     _flat("start", start, i32, dev, batch), batch, qp, kp, qo, ko, *qs, *ks, *qos, *kos,
+                     _flat("inv_freq", inv_freq, torch.float32, dev, n), 2 * n, interleaved, amplitude, backward)
+    _call(load().dash_rotary, dev, stream, x, _flat("status", status, i32, dev, 1))
+
+
+def rotary(q, k, inv_freq, positions=None, cu=None, start=None, interleaved: bool = False, amplitude: float = 1.0,
+           backward: bool = False):
+    """dash_rotary into new tensors.  Rows that no sequence holds have whatever the memory held."""
+    import torch
+    q_out, k_out = (None if x is None else torch.empty_like(x, memory_format=torch.contiguous_format) for x in (q, k))
+    dash_rotary(q, k, q_out, k_out, inv_freq, positions, cu, start, interleaved, amplitude, backward)
+    return q_out, k_out
+
+
+def dash_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling="plain", factor: float = 1.0, original: float = 0.0,
+                            fast: float = 32.0, slow: float = 1.0):
+    """(inv_freq, amplitude) of a context stretched by ``factor`` from ``original`` positions: a host fp32
+    array [rotary_dim / 2] and a number.  ``scaling``: "plain", "linear", "base" or "parts"."""
+    out, amplitude = np.empty(max(rotary_dim // 2, 1), np.float32), ctypes.c_float()
+    _check(load().dash_rotary_frequencies(rotary_dim, base, ROTARY_SCALINGS.get(scaling, scaling if isinstance(scaling, int) else -1),
+                                          factor, original, fast, slow, out.ctypes.data, ctypes.byref(amplitude)))
+    return out, amplitude.value
+
+
+# ----------------------------------------------------------------- packed attention
 _NO_STRIDES = (0,) * 8
 
 

@@ -68,7 +68,7 @@ __device__ inline Rows rows_of(const PackedArgs& a, int slot, int l) {
 
 template <int D>
 struct PackedView {
-  static constexpr bool kPacked = true;
+  static constexpr bool kPacked = true, kPaged = false;
   const PackedArgs& a;
   int h, hk, q0;
   int nq, nk, off_;  // nk, off_: as the run counts its keys

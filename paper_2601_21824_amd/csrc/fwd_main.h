@@ -42,10 +42,12 @@ namespace dash {
 // workgroup's sequence, the last key that query 0 sees under a causal mask (off; query
 // i sees keys 0 .. i + off), and the buffer resources and byte offsets of its
 // tensors.  Rows at or past nq and nk read 0 and are not written.
+// A paged view (kPaged) copies its tiles itself, and its rows see a number of keys each
+// (limit), of which those that see none are computed on zeros and left out (alive).
 // Dense calls: one N x D matrix per head.
 template <int D>
 struct DenseView {
-  static constexpr bool kPacked = false;
+  static constexpr bool kPacked = false, kPaged = false;
   const FwdArgs& a;
   int bh, nq, nk;
   size_t head;
@@ -146,7 +148,12 @@ __device__ void far_rows(const V& view, int causal, float scale, int row0) {
   const int l = fresh_lane();
   const int g = l >> 5, lc = l & 31, qrow = row0 + lc;
   const float c2 = scale * kLog2e;
-  const auto rq = view.q(), ro = view.o();
+  const auto ro = view.o();
+  const auto rq = [&] { if constexpr (V::kPaged) return 0; else return view.q(); }();
+  const auto q8 = [&](int c) {
+    if constexpr (V::kPaged) return view.q8(qrow, c);
+    else return as_bf16x8(ld16(rq, view.q_at(qrow, c)));
+  };
   const int end = causal ? min(view.nk, row0 + 32 + view.off()) : view.nk;
 #pragma clang loop unroll(disable)
   for (int d0 = 0; d0 < D; d0 += 64) {
@@ -156,16 +163,26 @@ __device__ void far_rows(const V& view, int causal, float scale, int row0) {
     float m = -INFINITY, sum = 0.f;
 #pragma clang loop unroll(disable)
     for (int k0 = 0; k0 < end; k0 += 32) {
-      const auto rk = view.k(k0), rv = view.v(k0);
+      const auto rk = [&] { if constexpr (V::kPaged) return 0; else return view.k(k0); }();
+      const auto rv = [&] { if constexpr (V::kPaged) return 0; else return view.v(k0); }();
+      const auto k8 = [&](int c) {
+        if constexpr (V::kPaged) return view.k8(k0 + lc, c);
+        else return as_bf16x8(ld16(rk, view.k_at(k0, lc, c)));
+      };
+      const auto v1 = [&](int row, int col) -> unsigned {
+        if constexpr (V::kPaged) return view.v1(k0 + row, col);
+        else return ld2(rv, view.v_at(k0, row, col));
+      };
       f32x16 s;
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma clang loop unroll(disable)
       for (int c = 0; c < D; c += 16)
-        s = mfma32(as_bf16x8(ld16(rk, view.k_at(k0, lc, c + 8 * g))),
-                   as_bf16x8(ld16(rq, view.q_at(qrow, c + 8 * g))), s);
+        s = mfma32(k8(c + 8 * g), q8(c + 8 * g), s);
       // element r: key k0 + 8(r/4) + 4g + r%4, query qrow
-      const int lim = (causal ? min(view.nk - 1, qrow + view.off()) : view.nk - 1) - k0 - 4 * g;
+      int lim = causal ? min(view.nk - 1, qrow + view.off()) : view.nk - 1;
+      if constexpr (V::kPaged) lim = view.limit(qrow) - 1;
+      lim -= k0 + 4 * g;
       float mx = -INFINITY;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -191,7 +208,7 @@ __device__ void far_rows(const V& view, int causal, float scale, int row0) {
           unsigned e[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            e[i] = ld2(rv, view.v_at(k0, 16 * h + 8 * (i >> 2) + 4 * g + (i & 3), d0 + 32 * db + lc));
+            e[i] = v1(16 * h + 8 * (i >> 2) + 4 * g + (i & 3), d0 + 32 * db + lc);
           const u32x4 v = {e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
           o[db] = mfma32(as_bf16x8(v), pack8(s, 8 * h), o[db]);
         }
@@ -230,12 +247,14 @@ __device__ __attribute__((always_inline)) inline void attn_fwd_rows(const V& vie
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int Nq = view.nq, Nk = view.nk, off = view.off();
   const int q0w = q0 + 32 * QG * w;
-  const auto rq = view.q();
+  const auto rq = [&] { if constexpr (V::kPaged) return 0; else return view.q(); }();
   const float c2 = scale * kLog2e;
 
   // ---- tiles: K into k[t % 2], V into v[t % VBUF]
   const uint32_t k_lds = lds_base(&sm.k[0][0]), v_lds = lds_base(&sm.v[0][0]);
   auto load_tile = [&](int t) {
+    if constexpr (V::kPaged) return view.request(t * KT, k_lds + (uint32_t)(t & 1) * TILE, v_lds + (uint32_t)(t % VBUF) * TILE);
+    else {
     const auto rk = view.k(t * KT), rv = view.v(t * KT);
     const int r = tid / CPR;
     const uint32_t kb = k_lds + (uint32_t)(t & 1) * TILE + 1024u * w;
@@ -251,6 +270,7 @@ __device__ __attribute__((always_inline)) inline void attn_fwd_rows(const V& vie
         dma16_pair(rk, rv, kb + 4096u * p, vb + 4096u * p, view.k_at(t * KT, row, 8 * c), 0);
       }
     }
+    }
   };
   const int kv_end = causal ? min(Nk, q0 + QROWS + off) : Nk;
   const int nt = (kv_end + KT - 1) / KT;                                // tiles of the workgroup
@@ -258,6 +278,9 @@ __device__ __attribute__((always_inline)) inline void attn_fwd_rows(const V& vie
   int nu = q0w >= Nq ? 1 : ((causal ? min(Nk, q0w + 32 * QG + off) : Nk) + 31) / 32;
   if constexpr (V::kPacked) nu = max(nu, 1);  // (a wave whose rows see nothing: far_rows)
   load_tile(0);
+  // (a paged view's rows: how many keys the lane's row sees, and the least of the wave's)
+  int limit = Nk, least = Nk;
+  if constexpr (V::kPaged) limit = view.limit(q0w + lc), least = view.least(limit);
 
   // Q of this wave's rows: the B operand of S^T
   bf16x8 qreg[QG][KS];
@@ -265,7 +288,8 @@ __device__ __attribute__((always_inline)) inline void attn_fwd_rows(const V& vie
   for (int qg = 0; qg < QG; ++qg)
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
-      qreg[qg][ks] = as_bf16x8(ld16(rq, view.q_at(q0w + 32 * qg + lc, 16 * ks + 8 * g)));
+      if constexpr (V::kPaged) qreg[qg][ks] = view.q8(q0w + 32 * qg + lc, 16 * ks + 8 * g);
+      else qreg[qg][ks] = as_bf16x8(ld16(rq, view.q_at(q0w + 32 * qg + lc, 16 * ks + 8 * g)));
 
   f32x16 oacc[QG][NDB];
 #pragma unroll
@@ -395,11 +419,11 @@ __device__ __attribute__((always_inline)) inline void attn_fwd_rows(const V& vie
   };
   // element (qg, r) of unit u <-> key 32u + 8(r/4) + 4g + r%4, query q0w + 32qg + lc
   auto mask = [&](f32x16(&sc)[QG], int u) {
-    if (!(32 * u + 32 > Nk || (causal && 32 * u + 31 > q0w + off))) return;
+    if (!(32 * u + 32 > (V::kPaged ? least : Nk) || (causal && 32 * u + 31 > q0w + off))) return;
 #pragma unroll
     for (int qg = 0; qg < QG; ++qg) {
       if constexpr (kQAgpr) score_settle(sc[qg]);
-      const int lim = (causal ? min(Nk - 1, q0w + 32 * qg + lc + off) : Nk - 1) - 32 * u - 4 * g;  // last visible key
+      const int lim = (V::kPaged ? limit - 1 : causal ? min(Nk - 1, q0w + 32 * qg + lc + off) : Nk - 1) - 32 * u - 4 * g;  // last visible key
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if (8 * (r >> 2) + (r & 3) > lim) sc[qg][r] = -INFINITY;
@@ -458,6 +482,7 @@ __device__ __attribute__((always_inline)) inline void attn_fwd_rows(const V& vie
   // that nobody reads any more.
   auto publish = [&](int t) {
     if (t >= nt) return;
+    if constexpr (V::kPaged) view.store(k_lds + (uint32_t)(t & 1) * TILE, v_lds + (uint32_t)(t % VBUF) * TILE);
     vm_wait<0>();
     __syncthreads();
     if (t + 1 < nt) load_tile(t + 1);

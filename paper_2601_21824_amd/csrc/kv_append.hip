@@ -18,18 +18,19 @@
 //
 // Measured, heads of 128, 32 over 8: 8192 tokens into an e4m3 cache 40 us, 101 MB in and 84
 // out, 4.6 TB/s; one token of each of 64 sequences, bf16, 4.4 us (1.6 MB).
+#include <type_traits>
+
 #include "common.h"
 #include "ops.h"
 #include "page_index.h"
+#include "mx.h"
 #include "paged.h"
+#include "rotate.h"
 
 namespace dash {
 namespace {
 
 constexpr int kWaves = 4;
-
-__device__ inline float bf_lo(unsigned x) { return __builtin_bit_cast(float, x << 16); }
-__device__ inline float bf_hi(unsigned x) { return __builtin_bit_cast(float, x & 0xffff0000u); }
 
 // 4 values -> e4m3, saturated at 448 (a NaN stays one)
 __device__ inline unsigned pack_e4m3(const float* x) {
@@ -41,12 +42,14 @@ __device__ inline unsigned pack_e4m3(const float* x) {
 }
 
 // ONCE: inputs larger than the last-level cache can hold behind the kernel that made
-// them are read past the caches.
-template <int D, bool ONCE>
+// them are read past the caches.  MX: the cache is microscaled (else bf16 or e4m3).
+template <int D, bool ONCE, int MX>
 __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, int rounds) {
+  using T = std::conditional_t<MX != 0, double, float>;
   constexpr int IPH = D / 16;    // items per head
   constexpr int HPR = 64 / IPH;  // heads per round
-  __shared__ float2 turn[kWaves][D / 2];
+  __shared__ Turn<T> turn[kWaves][D / 2];
+  __shared__ __attribute__((aligned(16))) unsigned most[MX ? kWaves : 1][MX ? 128 : 1];  // of each 8 components of a round's heads
   const CacheArgs& c = a.c;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
   const int hq = a.q ? c.heads_q : 0, heads = hq + 2 * c.heads_kv;
@@ -71,46 +74,15 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, in
   const int old = c.lens[s];
   const int64_t at_place = (int64_t)place + old;
 
-  // sine and cosine of pair i = l, l + 64: whole turns are taken off in 64 bits
   const int pairs = a.inv_freq ? a.rotary >> 1 : 0;
-  for (int i = l; i < pairs; i += 64) {
-    const double turns = (double)at_place * (double)a.inv_freq[i] * 0.15915494309189535;
-    const float part = (float)(2.0 * (turns - rint(turns)));  // half turns, -1 .. 1
-    float sn, cs;
-    sincospif(part, &sn, &cs);
-    turn[w][i] = make_float2(cs, sn);
-  }
-  // (a wave's own LDS writes and reads are in order)
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  fill_turns(turn[w], a.inv_freq, pairs, at_place, l);
 
   // the token's cache row
   const PageRow to = page_row(c.table + s * c.table_stride, c.table_width, c.page_size, c.pages, old < 0 ? -1 : at_place);
   if (!to.ok && l == 0 && c.status) *c.status = 1;
 
-  // The item's two 16-byte chunks (element offsets e0, e1) and their sines: neighbouring
-  // lanes hold neighbouring chunks, so that a load is whole lines
-  const int j = l % IPH, rot = 2 * pairs;
-  const bool split = !a.interleaved && 16 * j < rot;  // chunks of the two halves of 8 pairs
-  int e0 = 8 * j, e1 = 8 * j + D / 2;
-  if (split) {
-    e1 = 8 * j + pairs;
-  } else if (!a.interleaved) {  // components that are not rotated
-    e0 = rot + 8 * (j - rot / 16);
-    e1 = e0 + (D - rot) / 2;
-  }
-  float cs[8], sn[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    // split: pairs 8j .. 8j+7; interleaved: the four of chunk e0 and the four of e1
-    const int at = split ? 8 * j + i : (i < 4 ? e0 : e1) / 2 + (i & 3);
-    const bool on = split || (a.interleaved && (i < 4 ? e0 : e1) < rot);
-    const float2 x = on ? turn[w][at] : make_float2(1.f, 0.f);
-    cs[i] = x.x;
-    sn[i] = x.y;
-  }
-  // whether each chunk is rotated; one that is not keeps its bits (x cos 0 - y sin 0 makes NaN
-  // beside an infinity, and +0 of -0)
-  const bool turned0 = split || (a.interleaved && e0 < rot), turned1 = split || (a.interleaved && e1 < rot);
+  const RotaryItem<D, T> item(turn[w], l % IPH, pairs, a.interleaved);
+  const int e0 = item.e0, e1 = item.e1;
   for (int r = first; r < first + rounds; ++r) {
     const int h = r * HPR + l / IPH;
     if (h >= heads) return;
@@ -122,42 +94,24 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, in
     u32x4 x0 = ONCE ? __builtin_nontemporal_load((const u32x4*)(src + e0)) : *(const u32x4*)(src + e0);
     u32x4 x1 = ONCE ? __builtin_nontemporal_load((const u32x4*)(src + e1)) : *(const u32x4*)(src + e1);
     float y0[8], y1[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      y0[2 * i] = bf_lo(x0[i]);
-      y0[2 * i + 1] = bf_hi(x0[i]);
-      y1[2 * i] = bf_lo(x1[i]);
-      y1[2 * i + 1] = bf_hi(x1[i]);
-    }
-    if (kind != 2 && turned0) {  // (e1 < rot only if e0 is)
-      if (split) {
+    unpack8(x0, y0);
+    unpack8(x1, y1);
+    if (kind != 2 && item.on0) {
+      if constexpr (MX) {  // in 64 bits: what is stored follows from the rotated value, not from an order of roundings
+        double z0[8], z1[8];
+        unpack8(x0, z0);
+        unpack8(x1, z1);
+        item.turn(z0, z1);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float x = y0[i], y = y1[i];
-          y0[i] = x * cs[i] - y * sn[i];
-          y1[i] = x * sn[i] + y * cs[i];
+          y0[i] = (float)z0[i];
+          if (item.on1) y1[i] = (float)z1[i];
         }
       } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x = y0[2 * i], y = y0[2 * i + 1];
-          y0[2 * i] = x * cs[i] - y * sn[i];
-          y0[2 * i + 1] = x * sn[i] + y * cs[i];
-        }
-        if (turned1) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float x = y1[2 * i], y = y1[2 * i + 1];
-            y1[2 * i] = x * cs[4 + i] - y * sn[4 + i];
-            y1[2 * i + 1] = x * sn[4 + i] + y * cs[4 + i];
-          }
-        }
+        item.turn(y0, y1);
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x0[i] = pack_bf16(y0[2 * i], y0[2 * i + 1]);
-        if (turned1) x1[i] = pack_bf16(y1[2 * i], y1[2 * i + 1]);
-      }
+      x0 = pack8_bf16(y0);
+      if (item.on1) x1 = pack8_bf16(y1);
     }
     __bf16* out = kind == 0                ? (__bf16*)a.q_out + t * a.qos.row + h * a.qos.head
                   : kind == 1 && a.k_out   ? (__bf16*)a.k_out + t * a.kos.row + hk * a.kos.head
@@ -168,7 +122,32 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, in
     }
     if (kind == 0 || !to.ok) continue;
     const int64_t at = kind == 1 ? to.page * c.k_page + hk * c.k_head + to.row * c.k_row : to.page * c.v_page + hk * c.v_head + to.row * c.v_row;
-    if (!c.e4m3) {
+    if constexpr (MX) {
+      // a block's largest value: four chunks, which lie with lanes of this head in any order
+      unsigned* of = most[w] + l / IPH * (D / 8);
+      of[e0 / 8] = mx_most(y0);
+      of[e1 / 8] = mx_most(y1);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      const u32x4 m0 = *(const u32x4*)(of + (e0 / 32) * 4), m1 = *(const u32x4*)(of + (e1 / 32) * 4);
+      const auto top = [](u32x4 m) {
+        const unsigned a = m[0] > m[1] ? m[0] : m[1], b = m[2] > m[3] ? m[2] : m[3];
+        return a > b ? a : b;
+      };
+      const int b0 = mx_byte<MX == 2>(top(m0)), b1 = mx_byte<MX == 2>(top(m1));
+      const u32x2 p0 = mx_pack<MX == 2>(y0, b0), p1 = mx_pack<MX == 2>(y1, b1);
+      uint8_t* dst = (uint8_t*)(kind == 1 ? c.k : c.v) + at;
+      if constexpr (MX == 1) {
+        *(u32x2*)(dst + e0) = p0;
+        *(u32x2*)(dst + e1) = p1;
+      } else {
+        *(unsigned*)(dst + e0 / 2) = p0[0];
+        *(unsigned*)(dst + e1 / 2) = p1[0];
+      }
+      uint8_t* bytes = (kind == 1 ? c.k_mx : c.v_mx) + (((int64_t)to.page * c.heads_kv + hk) * c.page_size + to.row) * (D / 32);
+      if (e0 % 32 == 0) bytes[e0 / 32] = (uint8_t)b0;
+      if (e1 % 32 == 0) bytes[e1 / 32] = (uint8_t)b1;
+      asm volatile("" ::: "memory");  // (the next round's maxima behind this one's reads)
+    } else if (c.type == kBf16) {
       __bf16* dst = (__bf16*)(kind == 1 ? c.k : c.v) + at;
       *(u32x4*)(dst + e0) = x0;
       *(u32x4*)(dst + e1) = x1;
@@ -208,10 +187,11 @@ void launch(const AppendArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)((append_waves(a) + kWaves - 1) / kWaves));
   // past the caches from 64 MB of q, k and v on (us, through / past them: 8192 tokens, 32 heads
   // over 8 of 128, 100 MB, 44.2 / 40.3; 16 over 4 of 64, 25 MB, where the cache still holds them, 14.0 / 17.5)
-  if ((long)a.tokens * heads * D * 2 >= 64L << 20)
-    hipLaunchKernelGGL((kv_append_kernel<D, true>), grid, dim3(64 * kWaves), 0, stream, a, rounds);
-  else
-    hipLaunchKernelGGL((kv_append_kernel<D, false>), grid, dim3(64 * kWaves), 0, stream, a, rounds);
+  const bool once = (long)a.tokens * heads * D * 2 >= 64L << 20;
+  const auto kernel = a.c.type == kMx8   ? once ? kv_append_kernel<D, true, 1> : kv_append_kernel<D, false, 1>
+                      : a.c.type == kMx4 ? once ? kv_append_kernel<D, true, 2> : kv_append_kernel<D, false, 2>
+                                         : once ? kv_append_kernel<D, true, 0> : kv_append_kernel<D, false, 0>;
+  hipLaunchKernelGGL(kernel, grid, dim3(64 * kWaves), 0, stream, a, rounds);
 }
 
 }  // namespace

@@ -18,10 +18,11 @@ struct Strides {
 };
 
 // ---------------------------------------------------------------- paged cache
+enum CacheType { kBf16 = 0, kE4m3 = 1, kMx8 = 2, kMx4 = 3 };
 struct CacheArgs {
   int batch, heads_q, heads_kv, d;
   int pages, page_size, table_width;
-  int e4m3;  // element type: 0 bf16, 1 e4m3
+  int type;  // CacheType
   void* k;
   void* v;
   int64_t k_page, k_head, k_row, v_page, v_head, v_row;  // strides in elements
@@ -31,6 +32,8 @@ struct CacheArgs {
   const float* k_scale;  // null: 1
   const float* v_scale;
   int* status;  // null, or set to 1 by a bad page or length
+  uint8_t *k_mx, *v_mx;  // scale bytes [pages][heads_kv][page_size][d / 32]
+  bool e4m3() const { return type == kE4m3; }
 };
 
 struct AppendArgs {
@@ -47,6 +50,34 @@ struct AppendArgs {
 int64_t append_waves(const AppendArgs& a);
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t stream);
 
+struct ReadArgs {
+  CacheArgs c;
+  int rows;
+  const int32_t *cu, *first;  // first null: 0
+  void *k_out, *v_out;        // either may be null
+  Strides ks, vs;
+};
+// waves of the launch
+int64_t read_waves(const ReadArgs& a);
+hipError_t launch_kv_read(const ReadArgs& a, hipStream_t stream);
+
+// ---------------------------------------------------------------- rotary positions
+struct RotaryArgs {
+  int rows, heads_q, heads_k, d, batch;
+  const int32_t *positions, *cu, *start;  // positions, or cu and (null: 0) start
+  const void *q, *k;
+  void *q_out, *k_out;
+  Strides qs, ks, qos, kos;
+  const float* inv_freq;
+  int rotary, interleaved, back;
+  float amplitude;
+  int* status;
+};
+// waves of the launch
+int64_t rotary_waves(const RotaryArgs& a);
+hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);
+
+// ---------------------------------------------------------------- one new token
 struct DecodeArgs {
   CacheArgs c;
   const void* q;
@@ -59,12 +90,25 @@ struct DecodeArgs {
   float* part_o;  // [slots][heads_q][d]
   float* part_m;  // [slots][heads_q][2]: maximum (log2 domain), sum
   int* base;      // [batch][2]: first slot of a sequence, its chunks
+  // behind a shared prefix
+  const int32_t* prefix_table;
+  const int32_t* prefix_len;
+  int prefix_width;
+  int splits;      // runs that the prefix is cut into at most
+  float* prefix_o;  // [splits][batch][heads_q][d], each over its own sum
+  float* prefix_m;  // [splits][batch][heads_q][2]
 };
 int decode_workers(int heads_q, int heads_kv, int d, int table_tokens);
 int decode_slots(int batch, int heads_q, int heads_kv, int d, int table_tokens);
 // waves of the larger launch
 int64_t decode_waves(const DecodeArgs& a);
 hipError_t launch_decode(const DecodeArgs& a, hipStream_t stream);
+// the keys behind the prefix: parts and base alone
+hipError_t launch_decode_tail(const DecodeArgs& a, hipStream_t stream);
+// attention behind a shared prefix (attn_prefix.hip)
+int prefix_splits(int batch, int heads_q, int heads_kv, int d, int prefix_tokens);
+int64_t prefix_waves(const DecodeArgs& a);
+hipError_t launch_prefix(const DecodeArgs& a, hipStream_t stream);
 
 // ---------------------------------------------------------------- packed sequences
 struct PackedArgs {

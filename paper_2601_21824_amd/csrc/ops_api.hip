@@ -1,6 +1,7 @@
 // ops_api.hip -- the C ABI of the variable-length operators (include/dash.h):
 // argument checks, workspace layout and launches.  Host code only; the kernels
-// live in kv_append.hip, attn_decode.hip and attn_packed_*.hip.
+// live in rotary.hip, kv_append.hip, kv_read.hip, attn_decode.hip, attn_prefix.hip and
+// attn_packed_*.hip.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -67,13 +68,16 @@ int check_tensor(const char* name, const void* p, int64_t rows, int heads, int d
   return DASH_OK;
 }
 
+bool is_mx(const dash_paged_cache_t* c) { return c->cache_type == DASH_CACHE_MXFP8 || c->cache_type == DASH_CACHE_MXFP4; }
+
 int check_cache(const dash_paged_cache_t* c, bool written) {
   if (!c) return fail(DASH_ERR_INVALID_ARG, "null cache");
   int rc = check_heads(c->batch, c->heads_q, c->heads_kv, c->d);
   if (rc) return rc;
-  if (c->cache_type != DASH_CACHE_BF16 && c->cache_type != DASH_CACHE_E4M3)
+  const bool mx = is_mx(c);
+  if (c->cache_type != DASH_CACHE_BF16 && c->cache_type != DASH_CACHE_E4M3 && !mx)
     return fail(DASH_ERR_INVALID_ARG, "unknown cache_type");
-  if (c->cache_type == DASH_CACHE_BF16 && (c->k_scale || c->v_scale))
+  if (c->cache_type != DASH_CACHE_E4M3 && (c->k_scale || c->v_scale))
     return fail(DASH_ERR_INVALID_ARG, "k_scale and v_scale are for E4M3 caches");
   if (c->page_size < 16 || c->page_size % 16 || c->page_size > 65536)
     return fail(DASH_ERR_INVALID_ARG, "page_size must be a multiple of 16, at most 65536");
@@ -83,7 +87,10 @@ int check_cache(const dash_paged_cache_t* c, bool written) {
   if (c->pages < 1) return fail(DASH_ERR_INVALID_ARG, "pages must be >= 1");
   if (!c->lens || (!c->block_table && c->table_width > 0)) return fail(DASH_ERR_INVALID_ARG, "null lens or block_table");
   if (c->table_stride < c->table_width && c->batch > 1) return fail(DASH_ERR_INVALID_ARG, "table_stride is below table_width");
-  const int unit = c->cache_type == DASH_CACHE_E4M3 ? 16 : 8;
+  if (mx && (!c->k_mx || !c->v_mx)) return fail(DASH_ERR_INVALID_ARG, "null k_mx or v_mx");
+  if (mx && (((uintptr_t)c->k_mx | (uintptr_t)c->v_mx) & 15) != 0) return fail(DASH_ERR_INVALID_ARG, "k_mx and v_mx must be 16-byte aligned");
+  const int unit = c->cache_type == DASH_CACHE_BF16 ? 8 : 16;
+  const int row = c->cache_type == DASH_CACHE_MXFP4 ? c->d / 2 : c->d;  // elements of a row, as strides count them
   const struct {
     const char* name;
     const void* p;
@@ -91,19 +98,23 @@ int check_cache(const dash_paged_cache_t* c, bool written) {
   } t[2] = {{"k_cache", c->k_cache, c->k_page_stride, c->k_head_stride, c->k_row_stride},
             {"v_cache", c->v_cache, c->v_page_stride, c->v_head_stride, c->v_row_stride}};
   for (const auto& x : t) {
-    if ((rc = check_tensor(x.name, x.p, c->page_size, c->heads_kv, c->d, x.row, x.head, unit, written))) return rc;
+    if ((rc = check_tensor(x.name, x.p, c->page_size, c->heads_kv, row, x.row, x.head, unit, written))) return rc;
     if (x.page < 0 || x.page % unit || x.page > ((int64_t)1 << 40))
       return fail(DASH_ERR_INVALID_ARG, std::string(x.name) + ": page stride must be a multiple of 16 bytes in 0 .. 2^40");
-    if (written && overlap({c->page_size, x.row}, {c->heads_kv, x.head}, {c->pages, x.page}, c->d))
+    if (written && overlap({c->page_size, x.row}, {c->heads_kv, x.head}, {c->pages, x.page}, row))
       return fail(DASH_ERR_INVALID_ARG, std::string(x.name) + ": the strides make pages overlap");
   }
   return DASH_OK;
 }
 
+int cache_type(int t) { return t == DASH_CACHE_BF16 ? dash::kBf16 : t == DASH_CACHE_E4M3 ? dash::kE4m3 : t == DASH_CACHE_MXFP8 ? dash::kMx8 : dash::kMx4; }
+
 dash::CacheArgs cache_args(const dash_paged_cache_t* c, int* status) {
-  return {c->batch, c->heads_q, c->heads_kv, c->d, c->pages, c->page_size, c->table_width, c->cache_type == DASH_CACHE_E4M3,
+  // (the fields of the microscaled types, which a struct of another type may end before)
+  const bool mx = is_mx(c);
+  return {c->batch, c->heads_q, c->heads_kv, c->d, c->pages, c->page_size, c->table_width, cache_type(c->cache_type),
           c->k_cache, c->v_cache, c->k_page_stride, c->k_head_stride, c->k_row_stride, c->v_page_stride, c->v_head_stride,
-          c->v_row_stride, c->block_table, c->table_stride, c->lens, c->k_scale, c->v_scale, status};
+          c->v_row_stride, c->block_table, c->table_stride, c->lens, c->k_scale, c->v_scale, status, mx ? (uint8_t*)c->k_mx : nullptr, mx ? (uint8_t*)c->v_mx : nullptr};
 }
 
 struct DecodeLayout {
@@ -161,6 +172,97 @@ int kv_append(const dash_paged_cache_t* c, const dash_append_t* x, int* status, 
   return e == hipSuccess ? DASH_OK : hip_fail(e, "append launch");
 }
 
+int kv_read(const dash_paged_cache_t* c, const dash_read_t* x, int* status, void* stream) {
+  int rc = check_cache(c, false);
+  if (rc) return rc;
+  if (!x) return fail(DASH_ERR_INVALID_ARG, "null rows");
+  if (x->rows < 0 || x->rows > kMaxRows) return fail(DASH_ERR_INVALID_ARG, "rows must be in 0 .. 2^28");
+  if (x->rows == 0 || c->batch == 0) return DASH_OK;
+  if (!x->cu) return fail(DASH_ERR_INVALID_ARG, "null cu");
+  if (!x->k_out && !x->v_out) return fail(DASH_ERR_INVALID_ARG, "neither k_out nor v_out");
+  if (x->k_out && (rc = check_tensor("k_out", x->k_out, x->rows, c->heads_kv, c->d, x->k_row_stride, x->k_head_stride, 8, true))) return rc;
+  if (x->v_out && (rc = check_tensor("v_out", x->v_out, x->rows, c->heads_kv, c->d, x->v_row_stride, x->v_head_stride, 8, true))) return rc;
+  const dash::ReadArgs a{cache_args(c, status), x->rows, x->cu, x->first, x->k_out, x->v_out,
+                         {x->k_row_stride, x->k_head_stride}, {x->v_row_stride, x->v_head_stride}};
+  if (dash::read_waves(a) > dash::kMaxWaves) return fail(DASH_ERR_UNSUPPORTED, "too many rows for one call");
+  DeviceInfo di;
+  if ((rc = device_info(&di))) return rc;
+  const hipError_t e = dash::launch_kv_read(a, (hipStream_t)stream);
+  return e == hipSuccess ? DASH_OK : hip_fail(e, "read launch");
+}
+
+int rotary(const dash_rotary_t* x, int* status, void* stream) {
+  if (!x) return fail(DASH_ERR_INVALID_ARG, "null rows");
+  int rc = check_heads(x->batch, x->q ? x->heads_q : 1, 1, x->d);
+  if (!rc) rc = check_heads(0, x->k ? x->heads_k : 1, 1, x->d);
+  if (rc) return rc;
+  if (x->rows < 0 || x->rows > kMaxRows) return fail(DASH_ERR_INVALID_ARG, "rows must be in 0 .. 2^28");
+  if (x->rotary_dim < 16 || x->rotary_dim % 16 || x->rotary_dim > x->d)
+    return fail(DASH_ERR_INVALID_ARG, "rotary_dim must be a multiple of 16, at most d");
+  if (!std::isfinite(x->amplitude)) return fail(DASH_ERR_INVALID_ARG, "amplitude must be finite");
+  if (!x->q != !x->q_out) return fail(DASH_ERR_INVALID_ARG, "q and q_out come together");
+  if (!x->k != !x->k_out) return fail(DASH_ERR_INVALID_ARG, "k and k_out come together");
+  if (x->positions && (x->cu || x->start)) return fail(DASH_ERR_INVALID_ARG, "positions, or cu and start");
+  if (x->rows == 0 || (!x->q && !x->k)) return DASH_OK;
+  if (!x->positions && (!x->cu || x->batch < 1)) return x->cu ? DASH_OK : fail(DASH_ERR_INVALID_ARG, "null positions and cu");
+  if (!x->inv_freq) return fail(DASH_ERR_INVALID_ARG, "null inv_freq");
+  const struct {
+    const char *name, *out_name;
+    const void* p;
+    void* out;
+    int heads;
+    int64_t row, head, out_row, out_head;
+  } t[2] = {{"q", "q_out", x->q, x->q_out, x->heads_q, x->q_row_stride, x->q_head_stride, x->q_out_row_stride, x->q_out_head_stride},
+            {"k", "k_out", x->k, x->k_out, x->heads_k, x->k_row_stride, x->k_head_stride, x->k_out_row_stride, x->k_out_head_stride}};
+  for (const auto& y : t) {
+    if (!y.p) continue;
+    if ((rc = check_tensor(y.name, y.p, x->rows, y.heads, x->d, y.row, y.head, 8, false))) return rc;
+    if ((rc = check_tensor(y.out_name, y.out, x->rows, y.heads, x->d, y.out_row, y.out_head, 8, true))) return rc;
+    if (y.p == y.out && ((x->rows > 1 && y.row != y.out_row) || (y.heads > 1 && y.head != y.out_head)))
+      return fail(DASH_ERR_INVALID_ARG, std::string(y.out_name) + ": in place, the strides must be those of " + y.name);
+  }
+  const dash::RotaryArgs a{x->rows, x->heads_q, x->heads_k, x->d, x->batch, x->positions, x->cu, x->start, x->q, x->k, x->q_out, x->k_out,
+                           {x->q_row_stride, x->q_head_stride}, {x->k_row_stride, x->k_head_stride},
+                           {x->q_out_row_stride, x->q_out_head_stride}, {x->k_out_row_stride, x->k_out_head_stride},
+                           x->inv_freq, x->rotary_dim, x->interleaved ? 1 : 0, x->backward ? 1 : 0,
+                           x->amplitude == 0.f ? 1.f : x->amplitude, status};
+  if (dash::rotary_waves(a) > dash::kMaxWaves) return fail(DASH_ERR_UNSUPPORTED, "too many rows for one call");
+  DeviceInfo di;
+  if ((rc = device_info(&di))) return rc;
+  const hipError_t e = dash::launch_rotary(a, (hipStream_t)stream);
+  return e == hipSuccess ? DASH_OK : hip_fail(e, "rotary launch");
+}
+
+int rotary_frequencies(int n, double base, int scaling, double factor, double original, double fast, double slow, float* inv_freq,
+                       float* amplitude) {
+  if (n < 16 || n % 16 || n > 256) return fail(DASH_ERR_INVALID_ARG, "rotary_dim must be a multiple of 16, at most 256");
+  if (!(base > 1.0) || !std::isfinite(base)) return fail(DASH_ERR_INVALID_ARG, "base must be finite and above 1");
+  if (scaling < DASH_ROTARY_PLAIN || scaling > DASH_ROTARY_PARTS) return fail(DASH_ERR_INVALID_ARG, "unknown scaling");
+  if (scaling != DASH_ROTARY_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor))) return fail(DASH_ERR_INVALID_ARG, "factor must be finite and at least 1");
+  if (scaling == DASH_ROTARY_PARTS && (!(original > 0.0) || !std::isfinite(original) || !(slow > 0.0) || !(fast >= slow) || !std::isfinite(fast)))
+    return fail(DASH_ERR_INVALID_ARG, "original and slow must be positive, fast at least slow");
+  if (!inv_freq || !amplitude) return fail(DASH_ERR_INVALID_ARG, "null inv_freq or amplitude");
+  if (scaling == DASH_ROTARY_BASE) base *= std::pow(factor, n / (n - 2.0));
+  // the pair (a real number) that turns so many times over the original positions
+  const auto pair_of = [&](double turns) { return n * std::log(original / (turns * 2.0 * M_PI)) / (2.0 * std::log(base)); };
+  double lo = 0.0, hi = 0.0;
+  if (scaling == DASH_ROTARY_PARTS) {
+    lo = std::max(std::floor(pair_of(fast)), 0.0);
+    hi = std::min(std::ceil(pair_of(slow)), n - 1.0);
+  }
+  for (int i = 0; i < n / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / n);
+    if (scaling == DASH_ROTARY_LINEAR) f /= factor;
+    if (scaling == DASH_ROTARY_PARTS) {
+      const double x = std::min(std::max((i - lo) / std::max(hi - lo, 1e-3), 0.0), 1.0);
+      f = f * (1.0 - x) + f / factor * x;
+    }
+    inv_freq[i] = (float)f;
+  }
+  *amplitude = scaling == DASH_ROTARY_PARTS ? (float)(0.1 * std::log(factor) + 1.0) : 1.f;
+  return DASH_OK;
+}
+
 int attn_decode(const dash_paged_cache_t* c, const void* q, int64_t q_row, int64_t q_head, void* o, int64_t o_row,
                 int64_t o_head, float* lse, float scale, void* workspace, size_t ws_bytes, int* status, void* stream) {
   int rc = check_cache(c, false);
@@ -176,12 +278,57 @@ int attn_decode(const dash_paged_cache_t* c, const void* q, int64_t q_row, int64
   char* ws = (char*)workspace;
   const dash::DecodeArgs a{cache_args(c, status), q, o, lse, {q_row, q_head}, {o_row, o_head}, scale,
                            dash::decode_workers(c->heads_q, c->heads_kv, c->d, c->table_width * c->page_size), L.slots, (float*)(ws + L.part_o),
-                           (float*)(ws + L.part_m), (int*)(ws + L.base)};
+                           (float*)(ws + L.part_m), (int*)(ws + L.base), nullptr, nullptr, 0, 0, nullptr, nullptr};
   if (dash::decode_waves(a) > dash::kMaxWaves) return fail(DASH_ERR_UNSUPPORTED, "batch * heads_q too large for one call");
   DeviceInfo di;
   if ((rc = device_info(&di))) return rc;
   const hipError_t e = dash::launch_decode(a, (hipStream_t)stream);
   return e == hipSuccess ? DASH_OK : hip_fail(e, "decode launch");
+}
+
+struct PrefixLayout {
+  DecodeLayout own;
+  int splits;
+  size_t prefix_o, prefix_m, total;
+};
+PrefixLayout prefix_layout(int batch, int heads_q, int heads_kv, int d, int tokens, int prefix_tokens) {
+  PrefixLayout L;
+  L.own = decode_layout(batch, heads_q, heads_kv, d, tokens);
+  L.splits = dash::prefix_splits(batch, heads_q, heads_kv, d, prefix_tokens);
+  const size_t rows = (size_t)L.splits * batch * heads_q;
+  L.prefix_o = L.own.total;
+  L.prefix_m = L.prefix_o + align256(rows * d * sizeof(float));
+  L.total = L.prefix_m + align256(rows * 2 * sizeof(float));
+  return L;
+}
+
+int attn_prefix_decode(const dash_paged_cache_t* c, const int32_t* prefix_table, int prefix_width, const int32_t* prefix_len,
+                       const void* q, int64_t q_row, int64_t q_head, void* o, int64_t o_row, int64_t o_head, float* lse, float scale,
+                       void* workspace, size_t ws_bytes, int* status, void* stream) {
+  int rc = check_cache(c, false);
+  if (rc) return rc;
+  if ((rc = check_scale(&scale, c->d))) return rc;
+  if (prefix_width < 0 || (int64_t)prefix_width * c->page_size > dash::kMaxKeys)
+    return fail(DASH_ERR_INVALID_ARG, "prefix_width must be >= 0 and prefix_width * page_size below 2^31 - 255");
+  if (c->batch == 0) return DASH_OK;
+  if (!prefix_len || (!prefix_table && prefix_width > 0)) return fail(DASH_ERR_INVALID_ARG, "null prefix_len or prefix_table");
+  if ((rc = check_tensor("q", q, c->batch, c->heads_q, c->d, q_row, q_head, 8, false))) return rc;
+  if ((rc = check_tensor("o", o, c->batch, c->heads_q, c->d, o_row, o_head, 8, true))) return rc;
+  const int tokens = c->table_width * c->page_size;
+  const PrefixLayout L = prefix_layout(c->batch, c->heads_q, c->heads_kv, c->d, tokens, prefix_width * c->page_size);
+  if (!workspace || ws_bytes < L.total)
+    return fail(DASH_ERR_INVALID_ARG, "workspace missing or smaller than dash_prefix_decode_workspace_size()");
+  if (((uintptr_t)workspace & 255) != 0) return fail(DASH_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  char* ws = (char*)workspace;
+  const dash::DecodeArgs a{cache_args(c, status), q, o, lse, {q_row, q_head}, {o_row, o_head}, scale,
+                           dash::decode_workers(c->heads_q, c->heads_kv, c->d, tokens), L.own.slots, (float*)(ws + L.own.part_o),
+                           (float*)(ws + L.own.part_m), (int*)(ws + L.own.base), prefix_table, prefix_len, prefix_width, L.splits,
+                           (float*)(ws + L.prefix_o), (float*)(ws + L.prefix_m)};
+  if (dash::prefix_waves(a) > dash::kMaxWaves) return fail(DASH_ERR_UNSUPPORTED, "batch * heads_q too large for one call");
+  DeviceInfo di;
+  if ((rc = device_info(&di))) return rc;
+  const hipError_t e = dash::launch_prefix(a, (hipStream_t)stream);
+  return e == hipSuccess ? DASH_OK : hip_fail(e, "prefix decode launch");
 }
 
 // what both directions of a packed call need; false in *work: nothing to compute
@@ -364,6 +511,40 @@ extern "C" {
 
 int dash_kv_append(const dash_paged_cache_t* cache, const dash_append_t* x, int* status, void* stream) {
   return guarded([&] { return kv_append(cache, x, status, stream); });
+}
+
+int dash_kv_read(const dash_paged_cache_t* cache, const dash_read_t* x, int* status, void* stream) {
+  return guarded([&] { return kv_read(cache, x, status, stream); });
+}
+
+int dash_rotary(const dash_rotary_t* x, int* status, void* stream) {
+  return guarded([&] { return rotary(x, status, stream); });
+}
+
+int dash_rotary_frequencies(int rotary_dim, double base, int scaling, double factor, double original, double fast, double slow,
+                            float* inv_freq, float* amplitude) {
+  return guarded([&] { return rotary_frequencies(rotary_dim, base, scaling, factor, original, fast, slow, inv_freq, amplitude); });
+}
+
+size_t dash_prefix_decode_workspace_size(int batch, int heads_q, int heads_kv, int d, int page_size, int table_width, int prefix_width) {
+  size_t bytes = 0;
+  guarded([&] {
+    if (check_heads(batch, heads_q, heads_kv, d) == DASH_OK && page_size >= 16 && page_size % 16 == 0 && page_size <= 65536 &&
+        table_width >= 0 && (int64_t)table_width * page_size <= dash::kMaxKeys && prefix_width >= 0 &&
+        (int64_t)prefix_width * page_size <= dash::kMaxKeys)
+      bytes = prefix_layout(batch, heads_q, heads_kv, d, table_width * page_size, prefix_width * page_size).total;
+    return 0;
+  });
+  return bytes;
+}
+
+int dash_attn_prefix_decode(const dash_paged_cache_t* cache, const int32_t* prefix_table, int prefix_width, const int32_t* prefix_len,
+                            const void* q, int64_t q_row_stride, int64_t q_head_stride, void* o, int64_t o_row_stride,
+                            int64_t o_head_stride, float* lse, float scale, void* workspace, size_t ws_bytes, int* status, void* stream) {
+  return guarded([&] {
+    return attn_prefix_decode(cache, prefix_table, prefix_width, prefix_len, q, q_row_stride, q_head_stride, o, o_row_stride, o_head_stride,
+                              lse, scale, workspace, ws_bytes, status, stream);
+  });
 }
 
 size_t dash_decode_workspace_size(int batch, int heads_q, int heads_kv, int d, int page_size, int table_width) {

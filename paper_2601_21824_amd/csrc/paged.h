@@ -31,6 +31,13 @@ __device__ inline int find_sequence(const int32_t* cu, int batch, int t, int l) 
   return find_last(batch, t, l, [&](int s) { return cu[s]; });
 }
 
+// keys of a call's shared prefix, in what its table can hold
+__device__ inline int prefix_of(const DecodeArgs& a) {
+  const int n = *a.prefix_len;
+  const int64_t cap = (int64_t)a.prefix_width * a.c.page_size;
+  return n < 0 ? 0 : n > cap ? (int)cap : n;
+}
+
 // Rows of sequence s among `total`: offsets outside 0 .. total are clamped, and an
 // end before its start makes an empty sequence.
 struct Span {

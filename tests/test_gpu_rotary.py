@@ -1,0 +1,229 @@
+"""Rotary positions on the GPU, forward and backward, against their definition in float64.
+
+Tolerance of a component (u8 = 2^-8, u24 = 2^-24, halves of a bf16 and an fp32 step; a the amplitude):
+its own rounding, u8 |y|, and for sine and cosine (the angle in half turns is rounded to fp32, pi u24, the
+functions 2 u24 more), their product with a (u24) and the two products and their sum 9 u24 a (|x| + |y|).
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2601_21824_amd import binding as dash
+
+pytestmark = pytest.mark.gpu
+
+U8, U24 = 2.0 ** -8, 2.0 ** -24
+BF = torch.bfloat16
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def freqs(n):
+    return (10000.0 ** (-torch.arange(0, n, 2, device="cuda") / n)).float()
+
+
+def halves(x, n, interleaved):
+    return (x[..., 0:2 * n:2], x[..., 1:2 * n:2]) if interleaved else (x[..., :n], x[..., n:2 * n])
+
+
+def rotate64(x, place, inv, interleaved, amplitude=1.0, backward=False):
+    """Differentiable, in float64."""
+    n = inv.numel()
+    ang = (place.double()[:, None] * inv.double())[:, None]
+    c, s = ang.cos() * amplitude, ang.sin() * (-amplitude if backward else amplitude)
+    a, b = halves(x.double(), n, interleaved)
+    y, z = a * c - b * s, a * s + b * c
+    y = torch.stack((y, z), -1).flatten(-2) if interleaved else torch.cat((y, z), -1)
+    return torch.cat((y, x.double()[..., 2 * n:]), -1)
+
+
+def bound(x, ref, inv, interleaved, amplitude):
+    n = inv.numel()
+    a, b = halves(x.double().abs(), n, interleaved)
+    size = a + b
+    size = torch.stack((size, size), -1).flatten(-2) if interleaved else torch.cat((size, size), -1)
+    size = torch.cat((size, torch.zeros_like(x[..., 2 * n:], dtype=torch.float64)), -1)
+    return U8 * ref.abs() * (1 + U8) + 9 * U24 * abs(amplitude) * size
+
+
+def random(*shape, seed=0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed + sum(shape))
+    return torch.randn(shape, generator=g, device="cuda").to(BF)
+
+
+# (d, hq, hk, rows per sequence, first positions, rotary, interleaved, amplitude)
+CASES = [
+    (128, 8, 2, [1], [0], 128, False, 1.0),
+    (128, 32, 8, [1, 1, 1, 1], [131071, 0, 5, 2 ** 31 - 1], 128, False, 1.2),
+    (64, 3, 1, [5, 0, 40, 1], [3, 7, 0, 100], 32, True, 1.0),
+    (64, 5, 5, [17, 33], [0, 47], 64, True, 0.7),
+    (256, 6, 3, [9, 70], [131071, 2], 256, False, 1.0),
+    (256, 7, 1, [9, 70], [-20, 2], 208, True, 1.0),
+    (128, 32, 8, [700, 0, 1, 333], [0, 5, 99, 64], 96, False, 1.0),  # many rounds per wave
+    (128, 1, 1, [300, 601], [0, 0], 16, False, -2.0),
+    (64, 64, 1, [2000], [100000], 64, False, 1.0),
+]
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("d,hq,hk,lens,start,rotary,interleaved,amplitude", CASES)
+def test_rotary(d, hq, hk, lens, start, rotary, interleaved, amplitude, backward):
+    T, head, tail = sum(lens), 2, 3  # rows of nobody before and behind
+    at = [head]
+    for n in lens:
+        at.append(at[-1] + n)
+    q, k, _ = random(T + head + tail, hq + 2 * hk, d).split([hq, hk, hk], dim=1)  # strided views
+    inv, status = freqs(rotary), i32([0])
+    q_out, k_out = torch.full_like(q, 7.0), torch.full_like(k, 7.0)
+    dash.dash_rotary(q, k, q_out, k_out, inv, cu=i32(at), start=i32(start), interleaved=interleaved, amplitude=amplitude,
+                     backward=backward, status=status)
+    assert int(status) == 0
+    place = torch.cat([torch.arange(o, o + n) for o, n in zip(start, lens)]).cuda()
+    own = slice(head, head + T)
+    for x, out in ((q, q_out), (k, k_out)):
+        ref = rotate64(x[own], place, inv, interleaved, amplitude, backward)
+        assert bool(((out[own].double() - ref).abs() <= bound(x[own], ref, inv, interleaved, amplitude)).all())
+        assert torch.equal(out[own, :, rotary:], x[own, :, rotary:])
+        assert bool((out[:head] == 7).all()) and bool((out[head + T:] == 7).all())
+    # the same by positions, in place, and each tensor alone: the same bits
+    if max(start) < 2 ** 31 - 1 - max(lens):
+        pos = torch.full((T + head + tail,), -1, dtype=torch.int32, device="cuda")
+        pos[own] = place.to(torch.int32)
+        q2, k2 = q.clone(), k.clone()
+        dash.dash_rotary(q2, k2, q2, k2, inv, positions=pos, interleaved=interleaved, amplitude=amplitude, backward=backward)
+        assert torch.equal(q2[own], q_out[own]) and torch.equal(k2[own], k_out[own])
+        only = dash.rotary(None, k, inv, positions=pos, interleaved=interleaved, amplitude=amplitude, backward=backward)
+        assert only[0] is None and torch.equal(only[1][own], k_out[own])
+        only = dash.rotary(q, None, inv, positions=pos, interleaved=interleaved, amplitude=amplitude, backward=backward)
+        assert only[1] is None and torch.equal(only[0][own], q_out[own])
+
+
+@pytest.mark.parametrize("d,rotary,interleaved", [(64, 64, False), (64, 32, True), (128, 96, True), (256, 128, False)])
+def test_gradient(d, rotary, interleaved):
+    """The backward against autograd of the definition in float64, and against differences of the forward kernel."""
+    T, h, amplitude = 37, 3, 1.3
+    q, k, dq, dk = (random(T, h, d, seed=s) for s in range(4))
+    inv, pos = freqs(rotary), torch.arange(90, 90 + T, dtype=torch.int32, device="cuda")
+    gq, gk = dash.rotary(dq, dk, inv, positions=pos, interleaved=interleaved, amplitude=amplitude, backward=True)
+    for x, dy, got in ((q, dq, gq), (k, dk, gk)):
+        x = x.double().requires_grad_()
+        rotate64(x, pos, inv, interleaved, amplitude).backward(dy.double())
+        assert bool(((got.double() - x.grad).abs() <= bound(dy, x.grad, inv, interleaved, amplitude)).all())
+    # column i of the Jacobian at a place: (f(x + e_i) - f(x)) for x = 0; row i: the gradient of output i
+    eye = torch.eye(d, device="cuda").to(BF)[:, None].contiguous()
+    pos = torch.full((d,), 1234, dtype=torch.int32, device="cuda")
+    zero = dash.rotary(torch.zeros_like(eye), None, inv, positions=pos, interleaved=interleaved, amplitude=amplitude)[0]
+    cols = (dash.rotary(eye, None, inv, positions=pos, interleaved=interleaved, amplitude=amplitude)[0] - zero)[:, 0].double()
+    rows = dash.rotary(eye, None, inv, positions=pos, interleaved=interleaved, amplitude=amplitude, backward=True)[0][:, 0].double()
+    assert bool(((cols.t() - rows).abs() <= 2 * U8 * rows.abs() * (1 + U8) + 18 * U24 * amplitude).all())
+
+
+def test_components_behind_rotary_dim_keep_their_bits():
+    for d, rotary in ((64, 16), (128, 112), (256, 144)):
+        for interleaved in (False, True):
+            x = random(12, 2, d)
+            for i, odd in enumerate((float("inf"), float("-inf"), float("nan"), -0.0)):
+                x[i::4, :, rotary + i::4] = odd
+            y = dash.rotary(x, None, freqs(rotary), positions=torch.arange(12, dtype=torch.int32, device="cuda"), interleaved=interleaved)[0]
+            assert torch.equal(y[..., rotary:].view(torch.int16), x[..., rotary:].view(torch.int16))
+            assert bool(y[..., :rotary].isfinite().all())
+
+
+@pytest.mark.parametrize("at,reported,kept", [([0, 8, 5, 10], 1, None), ([-2, 4, 8, 12], 1, None), ([0, 2 ** 31 - 1, 3, 12], 1, None),
+                                              ([3, 3, 3, 3], 0, range(12)), ([2, 2, 9, 9], 0, [0, 1, 9, 10, 11]), ([0, 0, 0, 0], 0, range(12))])
+def test_offsets(at, reported, kept):
+    x, out, status = random(12, 2, 64), torch.full((12, 2, 64), 7.0, device="cuda").to(BF), i32([0])
+    dash.dash_rotary(x, None, out, None, freqs(64), cu=i32(at), status=status)
+    assert int(status) == reported
+    if kept is not None:
+        left = torch.zeros(12, dtype=torch.bool, device="cuda")
+        left[list(kept)] = True
+        assert bool((out[left] == 7).all()) and not bool((out[~left] == 7).flatten(1).all(-1).any())
+
+
+def test_empty_and_one_row_and_broadcast_heads():
+    inv = freqs(64)
+    q, k = dash.rotary(random(0, 4, 64), random(0, 1, 64), inv, cu=i32([0, 0]))
+    assert q.shape == (0, 4, 64) and k.shape == (0, 1, 64)
+    one = random(9, 1, 64)
+    pos = i32(list(range(9)))
+    wide = dash.rotary(one.expand(9, 4, 64), None, inv, positions=pos)[0]  # heads at stride 0
+    assert torch.equal(wide, dash.rotary(one, None, inv, positions=pos)[0].expand(9, 4, 64))
+
+
+def test_refusals():
+    x, inv, pos = random(4, 2, 64), freqs(64), i32([0, 1, 2, 3])
+    for word, args, kw in (("positions", (x, None, inv), {}), ("positions", (x, None, inv), dict(positions=pos, cu=i32([0, 4]))),
+                           ("positions", (x, None, inv), dict(positions=pos[:3])), ("start", (x, None, inv), dict(cu=i32([0, 4]), start=i32([0, 1]))),
+                           ("q must", (x.float(), None, inv), dict(positions=pos)), ("rotary_dim", (x, None, freqs(64)[:4]), dict(positions=pos)),
+                           ("inv_freq", (x, None, inv.double()), dict(positions=pos)), ("rotary_dim", (x, None, freqs(128)), dict(positions=pos)),
+                           ("head dim", (random(4, 2, 96), None, inv), dict(positions=pos)), ("amplitude", (x, None, inv), dict(positions=pos, amplitude=0.0)),
+                           ("amplitude", (x, None, inv), dict(positions=pos, amplitude=math.inf)), ("rows", (None, None, inv), dict(positions=pos)),
+                           ("k must", (x, random(5, 2, 64), inv), dict(positions=pos))):
+        with pytest.raises(dash.DashError, match=word):
+            dash.rotary(*args, **kw)
+    both = random(4, 4, 64)
+    with pytest.raises(dash.DashError, match="in place"):  # the same pointer, other strides
+        dash.dash_rotary(both[:, :2], None, both.flatten()[:4 * 2 * 64].view(4, 2, 64), None, inv, positions=pos)
+
+
+def test_captured_with_later_positions_and_on_another_stream():
+    q, k = random(40, 4, 128), random(40, 2, 128)
+    inv = freqs(128)
+    cu, start = i32([0, 11, 40]), i32([5, 9])
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    dash.dash_rotary(q, k, qo, ko, inv, cu=cu, start=start)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dash.dash_rotary(q, k, qo, ko, inv, cu=cu, start=start)
+    for i in range(4):
+        start.copy_(i32([5 + 100 * i, 70000 * i]))
+        cu.copy_(i32([0, 11 + i, 40 - i]))
+        qo.fill_(7.0), ko.fill_(7.0)
+        graph.replay()
+        want = dash.rotary(q, k, inv, cu=cu, start=start)
+        torch.cuda.synchronize()
+        own = slice(0, 40 - i)
+        assert torch.equal(qo[own], want[0][own]) and torch.equal(ko[own], want[1][own])
+        assert bool((qo[40 - i:] == 7).all())
+    side = torch.cuda.Stream()
+    out = torch.empty_like(q)
+    torch.cuda.synchronize()
+    dash.dash_rotary(q, None, out, None, inv, cu=cu, start=start, stream=side)
+    side.synchronize()
+    assert torch.equal(out[:37], qo[:37])
+
+
+def test_training_step_with_rotated_heads():
+    """rotary, packed attention, its backward and the rotation's, as a training step joins them: against autograd of the
+    whole in float64.  Each stage rounds to bf16; errors of q, k of u8 each move scores by up to 2 u8 (|q| |k|) scale =: e, P by
+    a factor e^e, and the gradients are compared in the 2-norm, where independent roundings of 2^-9 rms each add in squares:
+    with about 8 of them 3 u8 is their sum's bound at 3 times its rms."""
+    d, hq, hk, lens = 64, 4, 2, [70, 1, 129]
+    T = sum(lens)
+    at = i32([0, 70, 71, 200])
+    q, k, v, do = (random(T, h, d, seed=s) for s, h in enumerate((hq, hk, hk, hq)))
+    inv, amp = freqs(d), 1.1
+    qr, kr = dash.rotary(q, k, inv, cu=at, amplitude=amp)
+    o, lse = dash.attn_packed_fwd(qr, kr, v, at)
+    dqr, dkr, dv = dash.attn_packed_bwd(qr, kr, v, o, do, lse, at)
+    dq, dk = dash.rotary(dqr, dkr, inv, cu=at, amplitude=amp, backward=True)
+    qq, kk, vv = (x.double().requires_grad_() for x in (q, k, v))
+    place = torch.cat([torch.arange(n) for n in lens]).cuda()
+    a, b = rotate64(qq, place, inv, False, amp), rotate64(kk, place, inv, False, amp)
+    loss, first = 0, 0
+    for n in lens:
+        s = slice(first, first + n)
+        g = hq // hk
+        qs, ks, vs = a[s].transpose(0, 1), b[s].repeat_interleave(g, 1).transpose(0, 1), vv[s].repeat_interleave(g, 1).transpose(0, 1)
+        sc = (qs @ ks.transpose(1, 2).contiguous()) / math.sqrt(d)
+        sc = sc.masked_fill(torch.ones(n, n, dtype=torch.bool, device="cuda").triu(1), -math.inf)
+        loss = loss + ((torch.softmax(sc, -1) @ vs).transpose(0, 1) * do[s].double()).sum()
+        first += n
+    loss.backward()
+    for got, x in ((dq, qq), (dk, kk), (dv, vv)):
+        assert float((got.double() - x.grad).norm() / x.grad.norm()) <= 3 * U8
