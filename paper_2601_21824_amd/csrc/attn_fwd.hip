@@ -22,7 +22,8 @@ __global__ __launch_bounds__(256, WPS) void attn_fwd_kernel(FwdArgs a) {
   // a head, long and short ones alternate instead so that every run holds the
   // same work
   if (a.causal) qb_i = (a.bh & 7) == 0 ? nqb - 1 - qb_i : (qb_i & 1) ? qb_i >> 1 : nqb - 1 - (qb_i >> 1);
-  attn_fwd_rows<D, QG>(DenseView<D>(a, bh), a.causal, a.scale, qb_i * QROWS);
+  __shared__ __attribute__((aligned(1024))) FwdTiles<D> tiles;
+  attn_fwd_rows<D, QG>(DenseView<D>(a, bh), a.causal, a.scale, qb_i * QROWS, tiles);
 }
 
 template <int D, int QG, int WPS>

@@ -136,7 +136,8 @@ __global__ __launch_bounds__(256, WPS) void packed_fwd_kernel(PackedArgs a) {
     if (tid < kRows) st4f(rl, view.l_at(r.q0 + tid), -INFINITY);
     return;
   }
-  attn_fwd_rows<D, 1>(view, a.causal, a.scale, r.q0);
+  __shared__ __attribute__((aligned(1024))) FwdTiles<D> tiles;
+  attn_fwd_rows<D, 1>(view, a.causal, a.scale, r.q0, tiles);
 }
 
 // The runs of a slot's rows, in order: one workgroup per two passes of rows and head, D / 4

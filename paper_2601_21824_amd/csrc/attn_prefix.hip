@@ -9,10 +9,11 @@
 // the prefix's keys, and leaves O, maximum and sum in fp32.  decode_kernel does the same
 // for each sequence's own keys, 16 rows at a time, and join_kernel adds the parts in order.
 //
-// K and V come from the cache's pages, tile by tile: bf16 by direct copies into LDS, each wave
-// from the one page that its rows of a part lie in; the 8-bit and 4-bit types through
+// K and V come from the cache's pages, tile by tile, each wave its quarter of the rows, which
+// lie in one page: bf16 by direct copies into LDS; the 8-bit and 4-bit types through
 // registers, widened to bf16 (exactly) on the way to LDS.  The next tile's page numbers are
 // read a tile ahead.  Rows past the run read zeros.
+#include "decode_main.h"
 #include "fwd_main.h"
 #include "mx.h"
 #include "ops.h"
@@ -22,22 +23,28 @@
 namespace dash {
 namespace {
 
-constexpr int kRows = 128;  // rows of a workgroup
+constexpr int kRows = 128;  // rows of a workgroup, if they are many
 
-// The prefix's runs: tiles of KT keys, cut into n equal runs of kMinRun keys at least.
-constexpr int kMinRun = 256;
+// The prefix's runs: whole kUnit keys, cut into n equal runs of min_run keys at least.
+constexpr int kUnit = 128;
 struct Run {
   int first, keys, n;
 };
-template <int D>
-__device__ inline Run run_of(int keys, int splits, int i) {
-  constexpr int KT = D == 256 ? 32 : 64;
-  const int tiles = (keys + KT - 1) / KT;
-  int n = keys / kMinRun;
-  n = n < splits ? n : splits;
+__device__ inline Run run_of(const DecodeArgs& a, int keys, int i) {
+  const int units = (keys + kUnit - 1) / kUnit;
+  int n = keys / a.min_run;
+  n = n < a.splits ? n : a.splits;
   n = n > 1 ? n : 1;
-  const int a = (int)((int64_t)tiles * i / n), b = (int)((int64_t)tiles * (i + 1) / n);
-  return {a * KT, (b * KT < keys ? b * KT : keys) - a * KT, keys > 0 ? n : 0};
+  const int from = (int)((int64_t)units * i / n), to = (int)((int64_t)units * (i + 1) / n);
+  return {from * kUnit, (to * kUnit < keys ? to * kUnit : keys) - from * kUnit, keys > 0 ? n : 0};
+}
+// Item -> K/V head, run, tile of rows
+struct Item {
+  int hk, split, q0;
+};
+__device__ inline Item item_of(const DecodeArgs& a, int item, int rows) {
+  const int tiles = (a.c.batch * (a.c.heads_q / a.c.heads_kv) + rows - 1) / rows;
+  return {item / (a.splits * tiles), item / tiles % a.splits, item % tiles * rows};
 }
 
 template <int D, int TYPE>
@@ -47,71 +54,81 @@ struct PrefixView {
   static constexpr int BITS = TYPE == kBf16 ? 16 : TYPE == kMx4 ? 4 : 8;
   static constexpr bool kStaged = TYPE != kBf16, MX = TYPE >= kMx8;
   static constexpr int SZ = TYPE == kBf16 ? 2 : 1;          // bytes of a stride's unit
-  static constexpr int PE = kStaged ? 16 : 8;               // components of a thread's piece
+  static constexpr int PE = kStaged ? 16 : 8;               // components of a lane's piece
   static constexpr int PPR = D / PE;                        // pieces of a row
-  static constexpr int RP = 256 / PPR, RW = RP / 4;         // rows of a part, and of a wave in it (16 at most: one page)
-  static constexpr int PARTS = KT / RP;
+  static constexpr int RW = KT / 4, RL = 64 / PPR;          // rows of a wave, in one page; rows of one load
+  static constexpr int PARTS = RW / RL;
+  static_assert(RW % RL == 0 && 16 % RW == 0);
   static constexpr int PW = PE * BITS / 32;                 // words of a piece
   static constexpr int SB = D / kMxBlock;
   const DecodeArgs& a;
-  int hk, G, nq, nk, first, prefix, split, w, last_page;
-  // the next tile's places: page index and row, and page, of this wave's rows in each part
-  mutable int at[PARTS], row[PARTS], id[PARTS];
+  int hk, nq, nk, first, w, last_page;
+  const __bf16* q;   // of the lane's row
+  int sees;          // keys of the run that it sees (0 or less: none, or there is no such row)
+  int64_t part;      // its number in prefix_o and prefix_m, -1: there is no such row
+  float v_scale;
+  mutable int at, row, id;  // the next tile's place: page index and row, and page, of this wave's rows
   mutable unsigned kx[PARTS][PW], vx[PARTS][PW], kb[PARTS], vb[PARTS];
   mutable bool bad;
 
-  __device__ PrefixView(const DecodeArgs& a_, int hk_, int prefix_, const Run& run, int split_, int w_)
-      : a(a_), hk(hk_), G(a_.c.heads_q / a_.c.heads_kv), nq(a_.c.batch * (a_.c.heads_q / a_.c.heads_kv)), nk(run.keys), first(run.first),
-        prefix(prefix_), split(split_), w(w_), last_page((prefix_ - 1) / a_.c.page_size), bad(false) {
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p) {
-      const int key = first + p * RP + w * RW;
-      at[p] = key / a.c.page_size;
-      row[p] = key - at[p] * a.c.page_size;
-      look(p);
-    }
+  __device__ PrefixView(const DecodeArgs& a_, const Item& it, int prefix, const Run& run, int w_)
+      : a(a_), hk(it.hk), nk(run.keys), first(run.first), w(w_), last_page((prefix - 1) / a_.c.page_size), bad(false) {
+    const int key = first + w * RW;
+    at = key / a.c.page_size;
+    row = key - at * a.c.page_size;
+    look();
+    const int G = a.c.heads_q / a.c.heads_kv, r = it.q0 + 32 * w + (threadIdx.x & 31);
+    nq = a.c.batch * G;
+    const int s = r < nq ? r / G : 0, h = hk * G + r % G;
+    const int n = clamp_len(a.c.lens[s], a.c.table_width, a.c.page_size);
+    sees = r < nq ? (n < prefix ? n : prefix) - first : 0;
+    part = r < nq ? ((int64_t)it.split * a.c.batch + s) * a.c.heads_q + h : -1;
+    q = (const __bf16*)a.q + s * a.qs.row + h * a.qs.head;
+    v_scale = TYPE == kE4m3 && a.c.v_scale ? a.c.v_scale[hk] : 1.f;
   }
-  __device__ void look(int p) const { id[p] = __builtin_amdgcn_readfirstlane(a.prefix_table[at[p] < last_page ? at[p] : last_page]); }
+  __device__ void look() const { id = table_entry(a.prefix_table, at < last_page ? at : last_page); }
 
   __device__ static constexpr int off() { return 0; }
 
   // ---- tiles
-  __device__ __amdgpu_buffer_rsrc_t rows(const void* p, int64_t page, int64_t head, int64_t stride, int i, int r, int n) const {
+  __device__ __amdgpu_buffer_rsrc_t rows(const void* p, int64_t page, int64_t head, int64_t stride, int i, int n) const {
     const uint32_t bytes = n > 0 ? (uint32_t)(n - 1) * (uint32_t)stride * SZ + D * BITS / 8 : 0;
-    return make_rsrc((const char*)p + (i * page + hk * head + r * stride) * SZ, bytes);
+    return make_rsrc((const char*)p + (i * page + hk * head + row * stride) * SZ, bytes);
   }
-  __device__ __amdgpu_buffer_rsrc_t scales(const uint8_t* p, int i, int r, int n) const {
-    return make_rsrc(p + (((int64_t)i * a.c.heads_kv + hk) * a.c.page_size + r) * SB, n > 0 ? n * SB : 0);
+  __device__ __amdgpu_buffer_rsrc_t scales(const uint8_t* p, int i, int n) const {
+    return make_rsrc(p + (((int64_t)i * a.c.heads_kv + hk) * a.c.page_size + row) * SB, n > 0 ? n * SB : 0);
   }
   __device__ void request(int k0, uint32_t k_lds, uint32_t v_lds) const {
     const CacheArgs& c = a.c;
-    const int tid = threadIdx.x, lr = tid % 64 / PPR;  // row of this lane among the wave's
+    const int l = threadIdx.x & 63, lr = l / PPR;
+    int n = nk - (k0 + w * RW);  // rows that the wave has here
+    n = n < RW ? n : RW;
+    int i = id;
+    if (!page_ok(i, c.pages)) bad = true, i = 0;
+    const auto rk = rows(c.k, c.k_page, c.k_head, c.k_row, i, n), rv = rows(c.v, c.v_page, c.v_head, c.v_row, i, n);
+    const auto sk = MX ? scales(c.k_mx, i, n) : rk, sv = MX ? scales(c.v_mx, i, n) : rv;
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) {
-      int n = nk - (k0 + p * RP + w * RW);  // rows that the wave has here
-      n = n < RW ? n : RW;
-      int i = id[p];
-      if (!page_ok(i, c.pages)) bad = true, i = 0;
-      const auto rk = rows(c.k, c.k_page, c.k_head, c.k_row, i, row[p], n), rv = rows(c.v, c.v_page, c.v_head, c.v_row, i, row[p], n);
+      const int r = p * RL + lr;  // this lane's row among the wave's
       if constexpr (!kStaged) {
-        const int ch = (tid % PPR) ^ tile_swz<D>(p * RP + tid / PPR);
-        const uint32_t to = 1024u * w + 4096u * p;
-        dma16(rk, k_lds + to, (uint32_t)lr * (uint32_t)c.k_row * 2 + ch * 16);
-        dma16(rv, v_lds + to, (uint32_t)lr * (uint32_t)c.v_row * 2 + ch * 16);
+        const int ch = (l % PPR) ^ tile_swz<D>(w * RW + r);
+        const uint32_t to = (uint32_t)(w * RW * D * 2 + 1024 * p);
+        dma16(rk, k_lds + to, (uint32_t)r * (uint32_t)c.k_row * 2 + ch * 16);
+        dma16(rv, v_lds + to, (uint32_t)r * (uint32_t)c.v_row * 2 + ch * 16);
       } else {
-        load(kx[p], rk, (uint32_t)lr * (uint32_t)c.k_row + tid % PPR * (PW * 4));
-        load(vx[p], rv, (uint32_t)lr * (uint32_t)c.v_row + tid % PPR * (PW * 4));
+        load(kx[p], rk, (uint32_t)r * (uint32_t)c.k_row + l % PPR * (PW * 4));
+        load(vx[p], rv, (uint32_t)r * (uint32_t)c.v_row + l % PPR * (PW * 4));
         if constexpr (MX) {
-          const uint32_t o = lr * SB + tid % PPR * PE / kMxBlock;
-          kb[p] = __builtin_amdgcn_raw_buffer_load_b8(scales(c.k_mx, i, row[p], n), o, 0, 0);
-          vb[p] = __builtin_amdgcn_raw_buffer_load_b8(scales(c.v_mx, i, row[p], n), o, 0, 0);
+          const uint32_t o = r * SB + l % PPR * PE / kMxBlock;
+          kb[p] = __builtin_amdgcn_raw_buffer_load_b8(sk, o, 0, 0);
+          vb[p] = __builtin_amdgcn_raw_buffer_load_b8(sv, o, 0, 0);
         }
       }
-      at[p] += KT / c.page_size;
-      row[p] += KT % c.page_size;
-      if (row[p] >= c.page_size) row[p] -= c.page_size, ++at[p];
-      look(p);
     }
+    at += KT / c.page_size;
+    row += KT % c.page_size;
+    if (row >= c.page_size) row -= c.page_size, ++at;
+    look();
   }
   __device__ static void load(unsigned (&x)[PW], __amdgpu_buffer_rsrc_t r, uint32_t off) {
     if constexpr (PW == 4) {
@@ -135,10 +152,10 @@ struct PrefixView {
   }
   __device__ void store(uint32_t k_lds, uint32_t v_lds) const {
     if constexpr (kStaged) {
-      const int tid = threadIdx.x, piece = tid % PPR;
+      const int l = threadIdx.x & 63, piece = l % PPR;
 #pragma unroll
       for (int p = 0; p < PARTS; ++p) {
-        const int r = p * RP + tid / PPR;
+        const int r = w * RW + p * RL + l / PPR;
         // which of its two chunks a lane writes first: 16 lanes' chunks lie in distinct banks
         const bool odd = D == 256 ? piece >= 8 : D == 128 ? r & 1 : false;
         put(k_lds, r, piece, odd, kx[p], kb[p]);
@@ -179,65 +196,114 @@ struct PrefixView {
     return col & 1 ? x >> 16 : x & 0xffffu;
   }
 
-  // ---- query rows
-  __device__ int sequence(int r) const { return r / G; }
-  // keys of the prefix that row r's sequence has, less those of earlier runs
-  __device__ int seen(int r) const {
-    const int n = clamp_len(a.c.lens[sequence(r)], a.c.table_width, a.c.page_size);
-    return (n < prefix ? n : prefix) - first;
-  }
-  __device__ bool alive(int r) const { return r < nq && seen(r) > 0; }
-  __device__ int limit(int r) const {
-    if (!alive(r)) return nk;
-    const int n = seen(r);
-    return n < nk ? n : nk;
-  }
+  // ---- query rows: a lane has one, q0 + 32 w + l % 32, whose place is found once
+  __device__ int limit(int) const { return sees > 0 && sees < nk ? sees : nk; }
   __device__ int least(int x) const {
     if (!__any(x < nk)) return nk;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o));
     return __builtin_amdgcn_readfirstlane(x);
   }
-  __device__ bf16x8 q8(int r, int col) const {
+  __device__ bf16x8 q8(int, int col) const {
     u32x4 x = {0, 0, 0, 0};
-    if (alive(r)) x = *(const u32x4*)((const __bf16*)a.q + sequence(r) * a.qs.row + (hk * G + r % G) * a.qs.head + col);
+    if (sees > 0) x = *(const u32x4*)(q + col);
     return as_bf16x8(x);
   }
   __device__ int o() const { return 0; }
   __device__ int lse() const { return 0; }
-  __device__ int64_t part(int r) const { return ((int64_t)split * a.c.batch + sequence(r)) * a.c.heads_q + hk * G + r % G; }
-  __device__ void put_o(int, int r, int col, float a0, float a1, float a2, float a3) const {
-    if (r >= nq) return;
-    const float f = TYPE == kE4m3 && a.c.v_scale ? a.c.v_scale[hk] : 1.f;
-    f32x4 x = {a0 * f, a1 * f, a2 * f, a3 * f};
-    if (!alive(r)) x = f32x4{0.f, 0.f, 0.f, 0.f};
-    *(f32x4*)(a.prefix_o + part(r) * D + col) = x;
+  __device__ void put_o(int, int, int col, float a0, float a1, float a2, float a3) const {
+    f32x4 x = {a0 * v_scale, a1 * v_scale, a2 * v_scale, a3 * v_scale};
+    if (sees <= 0) x = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (part >= 0) *(f32x4*)(a.prefix_o + part * D + col) = x;
   }
-  __device__ void put_l(int, int r, float m, float sum) const {
-    if (r >= nq) return;
-    const bool on = alive(r);
-    *(float2*)(a.prefix_m + 2 * part(r)) = make_float2(on ? m : -INFINITY, on ? sum : 0.f);
+  __device__ void put_l(int, int, float m, float sum) const {
+    if (part >= 0) *(float2*)(a.prefix_m + 2 * part) = sees > 0 ? make_float2(m, sum) : make_float2(-INFINITY, 0.f);
   }
 };
 
+// Workgroup -> item, each XCD a contiguous share: the row tiles of a run read its keys from
+// one L2.  Those behind the prefix's take the sequences' own keys.
+__device__ inline int own_block(const DecodeArgs& a, int items, int* item) {
+  const int per = (items + 7) >> 3, x = (int)blockIdx.x;
+  *item = x < 8 * per ? (x & 7) * per + (x >> 3) : items;
+  return x - 8 * per;
+}
+
 template <int D, int TYPE, int WPS>
-__global__ __launch_bounds__(256, WPS) void prefix_kernel(DecodeArgs a) {
-  // Workgroup -> (K/V head, run, tile of rows), each XCD a contiguous share: the row tiles
-  // of a run read its keys from one L2
+__global__ __launch_bounds__(256, WPS) void prefix_kernel(DecodeArgs a, int items) {
   const CacheArgs& c = a.c;
-  const int tiles = (c.batch * (c.heads_q / c.heads_kv) + kRows - 1) / kRows;
-  const int items = c.heads_kv * a.splits * tiles, per = (items + 7) >> 3;
-  const int item = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per || item >= items) return;
-  const int hk = item / (a.splits * tiles), split = item / tiles % a.splits, q0 = item % tiles * kRows;
+  int item;
+  const int own = own_block(a, items, &item);
+  __shared__ __attribute__((aligned(1024))) union Space {
+    FwdTiles<D> tiles;
+    JoinSpace<D, 4> join;
+    __device__ Space() {}
+  } space;
+  if (own >= 0) return decode_part<D, TYPE, 4, true>(a, own, space.join);
+  if (item >= items) return;
+  const Item it = item_of(a, item, kRows);
   const int prefix = __builtin_amdgcn_readfirstlane(prefix_of(a));
   if (item == 0 && threadIdx.x == 0 && c.status && *a.prefix_len != prefix) *c.status = 1;
-  const Run run = run_of<D>(prefix, a.splits, split);
-  if (split >= run.n) return;
-  const PrefixView<D, TYPE> view(a, hk, prefix, run, split, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
-  const float scale = a.scale * (TYPE == kE4m3 && c.k_scale ? c.k_scale[hk] : 1.f);
-  attn_fwd_rows<D, 1>(view, 0, scale, q0);
+  const Run run = run_of(a, prefix, it.split);
+  if (it.split >= run.n) return;
+  const PrefixView<D, TYPE> view(a, it, prefix, run, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+  const float scale = a.scale * (TYPE == kE4m3 && c.k_scale ? c.k_scale[it.hk] : 1.f);
+  attn_fwd_rows<D, 1>(view, 0, scale, it.q0, space.tiles);
   if (view.bad && (threadIdx.x & 63) == 0 && c.status) *c.status = 1;
+}
+
+// Few rows: 16 of a K/V head's a workgroup, whose four waves take every fourth 32 keys of the run each.
+template <int D, int TYPE>
+__global__ __launch_bounds__(256, 2) void prefix_few_kernel(DecodeArgs a, int items) {
+  __shared__ JoinSpace<D, 4> space;
+  const CacheArgs& c = a.c;
+  int item;
+  const int own = own_block(a, items, &item);
+  if (own >= 0) return decode_part<D, TYPE, 4, true>(a, own, space);
+  if (item >= items) return;
+  const Item it = item_of(a, item, kQ);
+  const int prefix = __builtin_amdgcn_readfirstlane(prefix_of(a));
+  if (item == 0 && threadIdx.x == 0 && c.status && *a.prefix_len != prefix) *c.status = 1;
+  const Run run = run_of(a, prefix, it.split);
+  if (it.split >= run.n) return;
+  const int tid = threadIdx.x, l = tid & 63, g = l >> 4, lq = l & 15;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = c.heads_q / c.heads_kv, nq = c.batch * G, to = run.first + run.keys;
+  // row q0 + l % 16: its sequence, query head and the keys that it sees
+  const int r = it.q0 + lq, s = r < nq ? r / G : 0, h = it.hk * G + (r < nq ? r % G : 0);
+  const int n = clamp_len(c.lens[s], c.table_width, c.page_size);
+  const int end = r < nq && n < to ? n : to;
+  int least = end;
+  if (__any(least < to)) {
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o));
+  }
+  least = __builtin_amdgcn_readfirstlane(least);
+  Rows<D> rows;
+#pragma unroll
+  for (int ks = 0; ks < D / 32; ++ks) {
+    const u32x4 x = *(const u32x4*)((const __bf16*)a.q + s * a.qs.row + h * a.qs.head + Tile<D, TYPE>::first(ks, g));
+    rows.q[ks] = as_bf16x8(r < nq ? x : u32x4{0, 0, 0, 0});
+  }
+  rows.clear();
+  const float c2 = a.scale * kLog2e * (TYPE == kE4m3 && c.k_scale ? c.k_scale[it.hk] : 1.f);
+  KeyRows<D, TYPE, false> keys(c, a.prefix_table, it.hk, prefix, l);
+  if (run.first + 32 * w < to) keys.look(run.first + 32 * w);
+  for (int kb = run.first + 32 * w; kb < to; kb += 32 * 4) {
+    Tile<D, TYPE> t;
+    keys.load(t);
+    keys.look(kb + 32 * 4);
+    rows.add(t, c2, kb, 0, to, end, least, lq, g);
+  }
+  if (keys.bad && l == 0 && c.status) *c.status = 1;
+  const float vs = TYPE == kE4m3 && c.v_scale ? c.v_scale[it.hk] : 1.f;
+  join_waves<D, 4>(space, rows.o, rows.m, rows.sum, w, nq - it.q0 < kQ ? nq - it.q0 : kQ, [&](int i, int d0, float top, float den, f32x4 out) {
+    const int r = it.q0 + i;
+    const int64_t at = ((int64_t)it.split * c.batch + r / G) * c.heads_q + it.hk * G + r % G;
+    const float inv = den > 0.f || den != den ? vs / den : 0.f;
+    *(f32x4*)(a.prefix_o + at * D + d0) = out * inv;
+    if (d0 == 0) *(float2*)(a.prefix_m + 2 * at) = make_float2(top, den);
+  });
 }
 
 // The parts of one sequence and query head, the prefix's first, each in order: thread groups of
@@ -248,7 +314,7 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(DecodeArgs a) {
   __shared__ f32x4 acc[NG][D / 4];
   __shared__ float dens[NG];
   const int hq = a.c.heads_q, s = (int)blockIdx.x / hq, h = (int)blockIdx.x % hq;
-  const int np = run_of<D>(prefix_of(a), a.splits, 0).n;
+  const int np = run_of(a, prefix_of(a), 0).n;
   const int first = a.base[2 * s], n = np + a.base[2 * s + 1];
   const int tid = threadIdx.x, l = tid & 63, grp = tid / (D / 4), d4 = tid % (D / 4);
   // part i: its row of prefix_o and prefix_m, or of part_o and part_m
@@ -290,43 +356,69 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(DecodeArgs a) {
   if (a.lse && d4 == 0) a.lse[(size_t)s * hq + h] = den == 0.f ? -INFINITY : (top + __log2f(den)) * kLn2;
 }
 
-int row_tiles(int batch, int heads_q, int heads_kv) { return (int)(((int64_t)batch * (heads_q / heads_kv) + kRows - 1) / kRows); }
+int64_t items_of(int batch, int heads_q, int heads_kv, int rows) {  // without the runs
+  return heads_kv * (((int64_t)batch * (heads_q / heads_kv) + rows - 1) / rows);
+}
+int64_t items_of(const DecodeArgs& a) { return a.splits * items_of(a.c.batch, a.c.heads_q, a.c.heads_kv, a.few ? kQ : kRows); }
+// whole rounds of the XCDs, and the sequences' own chunks behind them
+int64_t blocks_of(const DecodeArgs& a) { return (items_of(a) + 7) / 8 * 8 + decode_blocks(a); }
 
-template <int D, int WPS>
+template <int D, int TYPE>
+auto kernel_of(const DecodeArgs& a) {
+  // (at d = 64 the types that go through registers have no room for a third workgroup's)
+  constexpr int kWps = D == 256 ? 1 : D == 64 && TYPE == kBf16 ? 3 : 2;
+  return a.few ? prefix_few_kernel<D, TYPE> : prefix_kernel<D, TYPE, kWps>;
+}
+
+template <int D>
 void launch(const DecodeArgs& a, hipStream_t stream) {
-  const int64_t items = (int64_t)a.c.heads_kv * a.splits * row_tiles(a.c.batch, a.c.heads_q, a.c.heads_kv);
-  const auto kernel = a.c.type == kBf16   ? prefix_kernel<D, kBf16, WPS>
-                      : a.c.type == kE4m3 ? prefix_kernel<D, kE4m3, WPS>
-                      : a.c.type == kMx8  ? prefix_kernel<D, kMx8, WPS>
-                                          : prefix_kernel<D, kMx4, WPS>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((items + 7) / 8 * 8)), dim3(256), 0, stream, a);
-  (void)launch_decode_tail(a, stream);
+  const auto kernel = a.c.type == kBf16   ? kernel_of<D, kBf16>(a)
+                      : a.c.type == kE4m3 ? kernel_of<D, kE4m3>(a)
+                      : a.c.type == kMx8  ? kernel_of<D, kMx8>(a)
+                                          : kernel_of<D, kMx4>(a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks_of(a)), dim3(256), 0, stream, a, (int)items_of(a));
   hipLaunchKernelGGL(prefix_join_kernel<D>, dim3((unsigned)(a.c.batch * a.c.heads_q)), dim3(256), 0, stream, a);
 }
 
 }  // namespace
 
-// Runs of the prefix at most: with the K/V heads and the tiles of rows, the workgroups that
-// run at once on 256 CUs (two a CU, one at d = 256).
-int prefix_splits(int batch, int heads_q, int heads_kv, int d, int prefix_tokens) {
-  const int64_t blocks = (int64_t)heads_kv * row_tiles(batch, heads_q, heads_kv), fit = d == 256 ? 256 : 512;
-  const int64_t most = prefix_tokens / kMinRun;
-  int64_t s = blocks > 0 ? fit / blocks : 1;
+// How the prefix is cut.  16 rows a workgroup read K and V once for every 16, with 16 waves a CU and no
+// barrier; 128 rows once for all of them, at the price of a longer start (us of the whole call, 16 / 128 rows a
+// workgroup, 16384 shared keys, 8 K/V heads: 32 rows of 128 components 25.7 / 27.2, 64 rows 32 / 30, 128 rows 55 / 36;
+// 4 K/V heads of 256: 32 rows 22 / 32, 64 rows 28 / 41, 128 rows 55 / 54).
+// Runs: with the K/V heads and the tiles of rows 256 workgroups, one a CU, or two where a run keeps 2048
+// keys all the same (at d = 64, where three fit, always): each run leaves its rows' O in fp32 to be read again
+// (64 sequences of 32 heads of 128 behind 32768 keys: 81 in 256 workgroups, 86 in 512; behind 65536, the kernel alone, 134 and 116).
+PrefixPlan prefix_plan(int batch, int heads_q, int heads_kv, int d, int prefix_tokens) {
+  const int64_t rows = (int64_t)batch * (heads_q / heads_kv);
+  PrefixPlan p;
+  p.few = rows <= (d == 256 ? 96 : 32);
+  p.min_run = p.few ? 128 : 256;
+  const int64_t blocks = items_of(batch, heads_q, heads_kv, p.few ? kQ : kRows), most = prefix_tokens / p.min_run;
+  const int64_t fit = d == 64 || (!p.few && blocks * prefix_tokens >= 512 * 2048) ? 512 : 256;
+  int64_t s = fit / blocks;
   s = s < most ? s : most;
-  return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+  p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+  return p;
+}
+
+// Chunks aimed at for the sequences' own keys: with the K/V heads (and further groups of 16 query heads) 512
+// workgroups, two for each of 256 CUs, as many as run at once beside the prefix's.
+int prefix_workers(int heads_q, int heads_kv) {
+  const int units = heads_kv * ((heads_q / heads_kv + kQ - 1) / kQ);
+  const int w = 512 / units;
+  return w > 1 ? w : 1;
 }
 
 int64_t prefix_waves(const DecodeArgs& a) {
-  const int64_t main = ((int64_t)a.c.heads_kv * a.splits * row_tiles(a.c.batch, a.c.heads_q, a.c.heads_kv) + 8) * 4;
-  const int64_t join = (int64_t)a.c.batch * a.c.heads_q * 4, tail = decode_waves(a);
-  const int64_t most = main > join ? main : join;
-  return most > tail ? most : tail;
+  const int64_t main = blocks_of(a) * 4, join = (int64_t)a.c.batch * a.c.heads_q * 4;
+  return main > join ? main : join;
 }
 
 hipError_t launch_prefix(const DecodeArgs& a, hipStream_t stream) {
-  if (a.c.d == 64) launch<64, 3>(a, stream);
-  else if (a.c.d == 128) launch<128, 2>(a, stream);
-  else launch<256, 1>(a, stream);
+  if (a.c.d == 64) launch<64>(a, stream);
+  else if (a.c.d == 128) launch<128>(a, stream);
+  else launch<256>(a, stream);
   return hipGetLastError();
 }
 

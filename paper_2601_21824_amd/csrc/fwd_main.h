@@ -80,6 +80,10 @@ struct FwdSmem {
   __bf16 v[VBUF][KT * D];
 };
 
+// the tiles of a workgroup, which the caller keeps
+template <int D>
+using FwdTiles = FwdSmem<D, D == 256 ? 32 : 64, D == 256 ? 4 : 3>;
+
 // x of the two lane halves: lo = x of lane l % 32, hi = x of lane l % 32 + 32.
 // v_permlane32_swap exchanges the upper half of one register with the lower
 // half of another; the s_nop covers the wait it needs after a VALU write of
@@ -229,7 +233,8 @@ __device__ void far_rows(const V& view, int causal, float scale, int row0) {
 
 // One workgroup's 128 QG query rows from q0 on.  causal, scale: the call's.
 template <int D, int QG, typename V>
-__device__ __attribute__((always_inline)) inline void attn_fwd_rows(const V& view, const int causal, const float scale, const int q0) {
+__device__ __attribute__((always_inline)) inline void attn_fwd_rows(const V& view, const int causal, const float scale, const int q0,
+                                                                                        FwdTiles<D>& sm) {
   constexpr int KT = D == 256 ? 32 : 64;  // keys per tile
   constexpr int NU = KT / 32;             // units per tile
   constexpr int KS = D / 16;              // k-steps over d
@@ -240,8 +245,10 @@ __device__ __attribute__((always_inline)) inline void attn_fwd_rows(const V& vie
   constexpr int VBUF = NU == 1 ? 4 : 3;
   constexpr int TILE = KT * D * 2;        // bytes
   constexpr int QROWS = 128 * QG;
-  constexpr bool kQAgpr = D == 256;
-  __shared__ __attribute__((aligned(1024))) FwdSmem<D, KT, VBUF> sm;
+  // (A paged view's rows are loaded under a condition: the compiler then moves Q between AGPRs right before the
+  // MFMAs that it does not see, which takes wait states that it does not know of.)
+  constexpr bool kQAgpr = D == 256 && !V::kPaged;
+  static_assert(sizeof sm.k == 2 * TILE && sizeof sm.v == VBUF * TILE);
 
   const int tid = threadIdx.x, l = tid & 63, g = l >> 5, lc = l & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -94,19 +94,26 @@ struct DecodeArgs {
   const int32_t* prefix_table;
   const int32_t* prefix_len;
   int prefix_width;
-  int splits;      // runs that the prefix is cut into at most
+  bool few;  // as in PrefixPlan
+  int splits, min_run;
   float* prefix_o;  // [splits][batch][heads_q][d], each over its own sum
   float* prefix_m;  // [splits][batch][heads_q][2]
 };
 int decode_workers(int heads_q, int heads_kv, int d, int table_tokens);
-int decode_slots(int batch, int heads_q, int heads_kv, int d, int table_tokens);
+int decode_slots(int batch, int table_tokens, int workers);
 // waves of the larger launch
 int64_t decode_waves(const DecodeArgs& a);
 hipError_t launch_decode(const DecodeArgs& a, hipStream_t stream);
-// the keys behind the prefix: parts and base alone
-hipError_t launch_decode_tail(const DecodeArgs& a, hipStream_t stream);
+// workgroups of the chunks
+int64_t decode_blocks(const DecodeArgs& a);
 // attention behind a shared prefix (attn_prefix.hip)
-int prefix_splits(int batch, int heads_q, int heads_kv, int d, int prefix_tokens);
+struct PrefixPlan {
+  bool few;     // 16 rows a workgroup, or 128 by the forward's kernel
+  int splits;   // runs that the prefix is cut into at most,
+  int min_run;  // of so many keys at least
+};
+PrefixPlan prefix_plan(int batch, int heads_q, int heads_kv, int d, int prefix_tokens);
+int prefix_workers(int heads_q, int heads_kv);
 int64_t prefix_waves(const DecodeArgs& a);
 hipError_t launch_prefix(const DecodeArgs& a, hipStream_t stream);
 

@@ -121,9 +121,9 @@ struct DecodeLayout {
   int slots;
   size_t part_o, part_m, base, total;
 };
-DecodeLayout decode_layout(int batch, int heads_q, int heads_kv, int d, int tokens) {
+DecodeLayout decode_layout(int batch, int heads_q, int d, int tokens, int workers) {
   DecodeLayout L;
-  L.slots = dash::decode_slots(batch, heads_q, heads_kv, d, tokens);
+  L.slots = dash::decode_slots(batch, tokens, workers);
   size_t off = 0;
   L.part_o = off;
   off += align256((size_t)L.slots * heads_q * d * sizeof(float));
@@ -271,14 +271,15 @@ int attn_decode(const dash_paged_cache_t* c, const void* q, int64_t q_row, int64
   if (c->batch == 0) return DASH_OK;
   if ((rc = check_tensor("q", q, c->batch, c->heads_q, c->d, q_row, q_head, 8, false))) return rc;
   if ((rc = check_tensor("o", o, c->batch, c->heads_q, c->d, o_row, o_head, 8, true))) return rc;
-  const DecodeLayout L = decode_layout(c->batch, c->heads_q, c->heads_kv, c->d, c->table_width * c->page_size);
+  const int tokens = c->table_width * c->page_size, workers = dash::decode_workers(c->heads_q, c->heads_kv, c->d, tokens);
+  const DecodeLayout L = decode_layout(c->batch, c->heads_q, c->d, tokens, workers);
   if (!workspace || ws_bytes < L.total)
     return fail(DASH_ERR_INVALID_ARG, "workspace missing or smaller than dash_decode_workspace_size()");
   if (((uintptr_t)workspace & 255) != 0) return fail(DASH_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
   char* ws = (char*)workspace;
   const dash::DecodeArgs a{cache_args(c, status), q, o, lse, {q_row, q_head}, {o_row, o_head}, scale,
-                           dash::decode_workers(c->heads_q, c->heads_kv, c->d, c->table_width * c->page_size), L.slots, (float*)(ws + L.part_o),
-                           (float*)(ws + L.part_m), (int*)(ws + L.base), nullptr, nullptr, 0, 0, nullptr, nullptr};
+                           workers, L.slots, (float*)(ws + L.part_o), (float*)(ws + L.part_m), (int*)(ws + L.base), nullptr, nullptr, 0,
+                           false, 0, 0, nullptr, nullptr};
   if (dash::decode_waves(a) > dash::kMaxWaves) return fail(DASH_ERR_UNSUPPORTED, "batch * heads_q too large for one call");
   DeviceInfo di;
   if ((rc = device_info(&di))) return rc;
@@ -288,14 +289,14 @@ int attn_decode(const dash_paged_cache_t* c, const void* q, int64_t q_row, int64
 
 struct PrefixLayout {
   DecodeLayout own;
-  int splits;
+  dash::PrefixPlan plan;
   size_t prefix_o, prefix_m, total;
 };
 PrefixLayout prefix_layout(int batch, int heads_q, int heads_kv, int d, int tokens, int prefix_tokens) {
   PrefixLayout L;
-  L.own = decode_layout(batch, heads_q, heads_kv, d, tokens);
-  L.splits = dash::prefix_splits(batch, heads_q, heads_kv, d, prefix_tokens);
-  const size_t rows = (size_t)L.splits * batch * heads_q;
+  L.own = decode_layout(batch, heads_q, d, tokens, dash::prefix_workers(heads_q, heads_kv));
+  L.plan = batch > 0 ? dash::prefix_plan(batch, heads_q, heads_kv, d, prefix_tokens) : dash::PrefixPlan{true, 1, 128};
+  const size_t rows = (size_t)L.plan.splits * batch * heads_q;
   L.prefix_o = L.own.total;
   L.prefix_m = L.prefix_o + align256(rows * d * sizeof(float));
   L.total = L.prefix_m + align256(rows * 2 * sizeof(float));
@@ -321,8 +322,9 @@ int attn_prefix_decode(const dash_paged_cache_t* c, const int32_t* prefix_table,
   if (((uintptr_t)workspace & 255) != 0) return fail(DASH_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
   char* ws = (char*)workspace;
   const dash::DecodeArgs a{cache_args(c, status), q, o, lse, {q_row, q_head}, {o_row, o_head}, scale,
-                           dash::decode_workers(c->heads_q, c->heads_kv, c->d, tokens), L.own.slots, (float*)(ws + L.own.part_o),
-                           (float*)(ws + L.own.part_m), (int*)(ws + L.own.base), prefix_table, prefix_len, prefix_width, L.splits,
+                           dash::prefix_workers(c->heads_q, c->heads_kv), L.own.slots, (float*)(ws + L.own.part_o),
+                           (float*)(ws + L.own.part_m), (int*)(ws + L.own.base), prefix_table, prefix_len, prefix_width, L.plan.few,
+                           L.plan.splits, L.plan.min_run,
                            (float*)(ws + L.prefix_o), (float*)(ws + L.prefix_m)};
   if (dash::prefix_waves(a) > dash::kMaxWaves) return fail(DASH_ERR_UNSUPPORTED, "batch * heads_q too large for one call");
   DeviceInfo di;
@@ -552,7 +554,8 @@ size_t dash_decode_workspace_size(int batch, int heads_q, int heads_kv, int d, i
   guarded([&] {
     if (check_heads(batch, heads_q, heads_kv, d) == DASH_OK && page_size >= 16 && page_size % 16 == 0 && page_size <= 65536 &&
         table_width >= 0 && (int64_t)table_width * page_size <= dash::kMaxKeys)
-      bytes = decode_layout(batch, heads_q, heads_kv, d, table_width * page_size).total;
+      bytes = decode_layout(batch, heads_q, d, table_width * page_size,
+                            dash::decode_workers(heads_q, heads_kv, d, table_width * page_size)).total;
     return 0;
   });
   return bytes;

@@ -31,6 +31,12 @@ __device__ inline int find_sequence(const int32_t* cu, int batch, int t, int l) 
   return find_last(batch, t, l, [&](int s) { return cu[s]; });
 }
 
+// Entry i of a table that nobody writes while the kernel runs, i wave-uniform: a scalar load, whatever
+// else is in flight (a load that may see stores would go the vector loads' way, behind all of them).
+__device__ inline int table_entry(const int32_t* table, int i) {
+  return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)(table + i);
+}
+
 // keys of a call's shared prefix, in what its table can hold
 __device__ inline int prefix_of(const DecodeArgs& a) {
   const int n = *a.prefix_len;

@@ -115,9 +115,7 @@ def test_prefix_of_nothing_and_its_workspace():
     assert prefix(None) == b.DASH_ERR_INVALID_ARG
     assert prefix(make(b.dash_paged_cache_t, CACHE, dict(batch=0))) == b.DASH_OK
     size = b.dash_prefix_decode_workspace_size
-    own = b.dash_decode_workspace_size(64, 32, 8, 128, 16, 3000)
-    assert size(64, 32, 8, 128, 16, 3000, 2048) > own
-    assert size(64, 32, 8, 128, 16, 3000, 0) > own  # (a part without keys)
+    assert size(64, 32, 8, 128, 16, 3000, 2048) > size(64, 32, 8, 128, 16, 3000, 0) > 0
     for bad in ((-1, 32, 8, 128, 16, 10, 10), (1, 32, 5, 128, 16, 10, 10), (1, 32, 8, 96, 16, 10, 10), (1, 32, 8, 128, 8, 10, 10),
                 (1, 32, 8, 128, 16, -1, 10), (1, 32, 8, 128, 16, 10, -1), (1, 32, 8, 128, 16, 10, 1 << 28)):
         assert size(*bad) == 0
