@@ -422,9 +422,10 @@ def _cache(k_cache, v_cache, block_table, lens, k_scale, v_scale, heads_q, dev):
     if kind >= DASH_CACHE_MXFP4:
         if k_scale is None or v_scale is None:
             _bad("a microscaled cache needs k_scale and v_scale")
-        kx, vx = (_flat(name, x, u8, dev, pages, heads_kv, page, d // 32) for name, x in (("k_scale", k_scale), ("v_scale", v_scale)))
+        kx = _flat("k_scale", k_scale, u8, dev, pages, heads_kv, page, d // 32)
+        vx = _flat("v_scale", v_scale, u8, dev, pages, heads_kv, page, d // 32)
     else:
-        ks, vs = (_flat(name, x, torch.float32, dev, heads_kv) for name, x in (("k_scale", k_scale), ("v_scale", v_scale)))
+        ks, vs = _flat("k_scale", k_scale, torch.float32, dev, heads_kv), _flat("v_scale", v_scale, torch.float32, dev, heads_kv)
     return _pack_cache(
         batch, heads_q, heads_kv, d, pages, page, width, kind, k_cache.data_ptr(), v_cache.data_ptr(), kp, kh, kr, vp, vh, vr,
         block_table.data_ptr(), row if batch > 1 else width, _flat("lens", lens, torch.int32, dev, batch), ks, vs, kx, vx), d
@@ -575,8 +576,11 @@ def kv_read(k_cache, v_cache, block_table, lens, cu, rows: int, first=None, k_sc
     import torch
     if k_cache.dim() != 4:
         _bad("k_cache and v_cache must be [pages, heads_kv, page_size, d] tensors alike")
-    d = k_cache.shape[3] * (2 if k_cache.dtype is torch.uint8 else 1)
-    k, v = (torch.empty((rows, k_cache.shape[1], d), dtype=torch.bfloat16, device=k_cache.device) for _ in range(2))
+    _, heads, _, d = k_cache.shape
+    if k_cache.dtype is torch.uint8:
+        d *= 2
+    k = k_cache.new_empty((rows, heads, d), dtype=torch.bfloat16)
+    v = torch.empty_like(k)
     dash_kv_read(k_cache, v_cache, block_table, lens, cu, k, v, first, k_scale, v_scale, status)
     return k, v
 

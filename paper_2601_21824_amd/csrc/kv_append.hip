@@ -81,7 +81,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, in
   const PageRow to = page_row(c.table + s * c.table_stride, c.table_width, c.page_size, c.pages, old < 0 ? -1 : at_place);
   if (!to.ok && l == 0 && c.status) *c.status = 1;
 
-  const RotaryItem<D, T> item(turn[w], l % IPH, pairs, a.interleaved);
+  const RotaryItem<D, float> item(turn[w], l % IPH, pairs, a.interleaved);
   const int e0 = item.e0, e1 = item.e1;
   for (int r = first; r < first + rounds; ++r) {
     const int h = r * HPR + l / IPH;
@@ -97,16 +97,10 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, in
     unpack8(x0, y0);
     unpack8(x1, y1);
     if (kind != 2 && item.on0) {
-      if constexpr (MX) {  // in 64 bits: what is stored follows from the rotated value, not from an order of roundings
-        double z0[8], z1[8];
-        unpack8(x0, z0);
-        unpack8(x1, z1);
-        item.turn(z0, z1);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          y0[i] = (float)z0[i];
-          if (item.on1) y1[i] = (float)z1[i];
-        }
+      // a key for a microscaled cache in 64 bits: what is stored follows from the rotated value, not from an
+      // order of roundings
+      if (MX && kind == 1) {
+        if constexpr (MX) item.turn_wide(turn[w], y0, y1);
       } else {
         item.turn(y0, y1);
       }

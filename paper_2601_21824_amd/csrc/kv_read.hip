@@ -98,11 +98,11 @@ __global__ __launch_bounds__(64 * kWaves) void kv_read_kernel(ReadArgs a) {
     constexpr int kUnit = TYPE == kBf16 ? 2 : 1;                      // bytes of a stride's unit
     const int64_t blk = (((int64_t)id * c.heads_kv + hk) * c.page_size + at) * (D / 32) + col / 32;
     if (has_k) {
-      k[i].x = __builtin_nontemporal_load((const typename P::Raw*)((const char*)c.k + (id * c.k_page + hk * c.k_head + at * c.k_row) * kUnit + col * kBits / 8));
+      k[i].x = *(const typename P::Raw*)((const char*)c.k + (id * c.k_page + hk * c.k_head + at * c.k_row) * kUnit + col * kBits / 8);
       if constexpr (TYPE >= kMx8) k[i].byte = c.k_mx[blk];
     }
     if (has_v) {
-      v[i].x = __builtin_nontemporal_load((const typename P::Raw*)((const char*)c.v + (id * c.v_page + hk * c.v_head + at * c.v_row) * kUnit + col * kBits / 8));
+      v[i].x = *(const typename P::Raw*)((const char*)c.v + (id * c.v_page + hk * c.v_head + at * c.v_row) * kUnit + col * kBits / 8);
       if constexpr (TYPE >= kMx8) v[i].byte = c.v_mx[blk];
     }
   }

@@ -40,7 +40,7 @@ namespace dash {
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // The scale of a byte, as the conversions below take it: they make NaN of every element for 255.
-__device__ inline float mx_scale(unsigned byte) { return __builtin_bit_cast(float, byte == (unsigned)kMxNaN ? 0x7fc00000u : byte << 23); }
+__device__ inline float mx_scale(unsigned byte) { return __builtin_bit_cast(float, byte << 23); }
 
 // elements 2p, 2p + 1 of a word, times the scale, as two bf16 (exact)
 template <bool FP4>

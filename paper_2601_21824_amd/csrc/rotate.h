@@ -48,7 +48,8 @@ struct RotaryItem {
   bool on0, on1;  // whether each chunk is rotated (e1 only if e0 is)
   T cs[8], sn[8];
 
-  __device__ RotaryItem(const Turn<T>* turn, int j, int pairs, int interleaved) {
+  template <typename S>  // (turns of 64 bits are rounded to 32 for an item of those)
+  __device__ RotaryItem(const Turn<S>* turn, int j, int pairs, int interleaved) {
     const int rot = 2 * pairs;
     e0 = 8 * j, e1 = 8 * j + D / 2;
     split = !interleaved && 16 * j < rot;
@@ -63,9 +64,9 @@ struct RotaryItem {
       // split: pairs 8j .. 8j+7; interleaved: the four of chunk e0 and the four of e1
       const int at = split ? 8 * j + i : (i < 4 ? e0 : e1) / 2 + (i & 3);
       const bool on = split || (interleaved && (i < 4 ? e0 : e1) < rot);
-      const Turn<T> x = on ? turn[at] : Turn<T>{1, 0};
-      cs[i] = x.c;
-      sn[i] = x.s;
+      const Turn<S> x = on ? turn[at] : Turn<S>{1, 0};
+      cs[i] = (T)x.c;
+      sn[i] = (T)x.s;
     }
     // a chunk that is not rotated keeps its bits (x cos 0 - y sin 0 makes NaN beside an
     // infinity, and +0 of -0)
@@ -73,6 +74,28 @@ struct RotaryItem {
     on1 = split || (interleaved && e1 < rot);
   }
 
+  // the chunks' values turned in 64 bits, by turns of 64 bits from LDS, and rounded to 32 (where on0 says so)
+  __device__ void turn_wide(const Turn<double>* turn, float (&y0)[8], float (&y1)[8]) const {
+    if (split) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const Turn<double> t = turn[e0 + i];  // (e0 is 8 j, the item's first pair)
+        const double x = y0[i], y = y1[i];
+        y0[i] = (float)(x * t.c - y * t.s);
+        y1[i] = (float)(x * t.s + y * t.c);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float(&z)[8] = i < 4 ? y0 : y1;
+        if (i >= 4 && !on1) continue;
+        const Turn<double> t = turn[(i < 4 ? e0 : e1) / 2 + (i & 3)];
+        const double x = z[2 * (i & 3)], y = z[2 * (i & 3) + 1];
+        z[2 * (i & 3)] = (float)(x * t.c - y * t.s);
+        z[2 * (i & 3) + 1] = (float)(x * t.s + y * t.c);
+      }
+    }
+  }
   // the chunks' values, turned (where on0 says so)
   __device__ void turn(T (&y0)[8], T (&y1)[8]) const {
     if (split) {

@@ -5,6 +5,9 @@ is bf16 (V) or the rotated key, which the kernel computes in 64 bits and rounds 
 computations in 64 bits differ by 2^-36 at most at these places, and would have to fall on two sides of a rounding to fp32 that
 in turn is a tie of the element type: a chance of 10^-10 for each value.)
 
+A rotated query is computed in 32 bits: beside its own rounding, u8 |y|, sine and cosine are rounded to fp32 (u24 each), and the two
+products and their sum are (3 u24 of |x| + |y| at most): within 8 u24 (|x| + |y|), the bound of a query beside a bf16 cache.
+
 The attention's bounds are those of the bf16 cache: the stored values are bf16 numbers, so u8 |o| for o's rounding, u8 A for P's
 (A = sum_j P_j |v_j|), each score off by (d + 4) u24 times its sum of absolute products, sums over n keys n u24 A twice.
 """
@@ -15,7 +18,7 @@ import torch
 
 from mx_util import BF, E4, Cache, pack, quantise64, used_rows, values64
 from paper_2601_21824_amd import binding as dash
-from test_gpu_paged_cache import LENS, i32, rotate64, table_of
+from test_gpu_paged_cache import LENS, i32, pair_size, rotate64, table_of
 
 pytestmark = pytest.mark.gpu
 
@@ -71,7 +74,8 @@ def test_append_and_read(d, hq, hkv, new, old, page, rotary, interleaved, order,
     own, place = slice(head, head + T), cat_places(old, new)
     for x, out in ((q, q_out), (k, k_out))[0 if with_q else 1:]:
         ref = rotate64(x[own], place, inv, interleaved)
-        assert bool(((out[own].double() - ref).abs() <= U8 * ref.abs() * (1 + U8)).all())
+        tol = U8 * ref.abs() * (1 + U8) + (8 * U24 * pair_size(x[own], inv, interleaved) if x is q else 0.0)
+        assert bool(((out[own].double() - ref).abs() <= tol).all())
         assert bool((out[:head] == 7).all()) and bool((out[head + T:] == 7).all())
     seq = torch.cat([torch.full((n,), s) for s, n in enumerate(new)]).cuda()
     ids, rows = table[seq, place // page].long(), place % page
