@@ -42,7 +42,8 @@ __device__ inline unsigned pack_e4m3(const float* x) {
 }
 
 // ONCE: inputs larger than the last-level cache can hold behind the kernel that made
-// them are read past the caches.  MX: the cache is microscaled (else bf16 or e4m3).
+// them are read past the caches (and, MX, its rotated rows written past them).  MX: the cache is
+// microscaled, 1 in 8 bits and 2 in 4 (0: bf16 or e4m3).
 template <int D, bool ONCE, int MX>
 __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, int rounds) {
   using T = std::conditional_t<MX != 0, double, float>;
@@ -110,7 +111,10 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a, in
     __bf16* out = kind == 0                ? (__bf16*)a.q_out + t * a.qos.row + h * a.qos.head
                   : kind == 1 && a.k_out   ? (__bf16*)a.k_out + t * a.kos.row + hk * a.kos.head
                                            : nullptr;
-    if (out) {
+    if (out && ONCE && MX) {
+      __builtin_nontemporal_store(x0, (u32x4*)(out + e0));
+      __builtin_nontemporal_store(x1, (u32x4*)(out + e1));
+    } else if (out) {
       *(u32x4*)(out + e0) = x0;
       *(u32x4*)(out + e1) = x1;
     }
@@ -181,7 +185,8 @@ void launch(const AppendArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)((append_waves(a) + kWaves - 1) / kWaves));
   // past the caches from 64 MB of q, k and v on (us, through / past them: 8192 tokens, 32 heads
   // over 8 of 128, 100 MB, 44.2 / 40.3; 16 over 4 of 64, 25 MB, where the cache still holds them, 14.0 / 17.5)
-  const bool once = (long)a.tokens * heads * D * 2 >= 64L << 20;
+  // (microscaled from 32 MB on: 3001 tokens of 32 heads over 8, 37 MB, and 19385 rows read back behind them 41.2 / 35.8)
+  const bool once = (long)a.tokens * heads * D * 2 >= (a.c.type >= kMx8 ? 32L : 64L) << 20;
   const auto kernel = a.c.type == kMx8   ? once ? kv_append_kernel<D, true, 1> : kv_append_kernel<D, false, 1>
                       : a.c.type == kMx4 ? once ? kv_append_kernel<D, true, 2> : kv_append_kernel<D, false, 2>
                                          : once ? kv_append_kernel<D, true, 0> : kv_append_kernel<D, false, 0>;
