@@ -21,8 +21,9 @@ namespace {
 
 constexpr int kWaves = 4;
 
-// ONCE: rows past what the caches keep are read and written past them.
-template <int D, bool ONCE>
+// PAST: outputs that the caches will not keep are written past them (1), and inputs that they have not
+// kept read past them (2).
+template <int D, int PAST>
 __global__ __launch_bounds__(64 * kWaves) void rotary_kernel(RotaryArgs a, int rounds) {
   constexpr int IPH = D / 16;    // items per head
   constexpr int HPR = 64 / IPH;  // heads per round
@@ -70,8 +71,8 @@ __global__ __launch_bounds__(64 * kWaves) void rotary_kernel(RotaryArgs a, int r
       const bool q = h < hq;
       const __bf16* src = q ? (const __bf16*)a.q + t * a.qs.row + h * a.qs.head : (const __bf16*)a.k + t * a.ks.row + (h - hq) * a.ks.head;
       out[u] = q ? (__bf16*)a.q_out + t * a.qos.row + h * a.qos.head : (__bf16*)a.k_out + t * a.kos.row + (h - hq) * a.kos.head;
-      x[u][0] = ONCE ? __builtin_nontemporal_load((const u32x4*)(src + item.e0)) : *(const u32x4*)(src + item.e0);
-      x[u][1] = ONCE ? __builtin_nontemporal_load((const u32x4*)(src + item.e1)) : *(const u32x4*)(src + item.e1);
+      x[u][0] = PAST == 2 ? __builtin_nontemporal_load((const u32x4*)(src + item.e0)) : *(const u32x4*)(src + item.e0);
+      x[u][1] = PAST == 2 ? __builtin_nontemporal_load((const u32x4*)(src + item.e1)) : *(const u32x4*)(src + item.e1);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -84,7 +85,7 @@ __global__ __launch_bounds__(64 * kWaves) void rotary_kernel(RotaryArgs a, int r
         x[u][0] = pack8_bf16(y0);
         if (item.on1) x[u][1] = pack8_bf16(y1);
       }
-      if (ONCE) {
+      if (PAST) {
         __builtin_nontemporal_store(x[u][0], (u32x4*)(out[u] + item.e0));
         __builtin_nontemporal_store(x[u][1], (u32x4*)(out[u] + item.e1));
       } else {
@@ -111,12 +112,12 @@ template <int D>
 void launch(const RotaryArgs& a, hipStream_t stream) {
   const int heads = (a.q ? a.heads_q : 0) + (a.k ? a.heads_k : 0), rounds = split_of(a).rounds;
   const dim3 grid((unsigned)((rotary_waves(a) + kWaves - 1) / kWaves));
-  // (us, through / past the caches, inputs and outputs that no cache holds: 8192 rows of 32 and 8 heads of
-  // 128, 84 MB each way, 36.1 / 33.6; 5001 of 16 and 4 of 256, 51 MB, 26 / 22.6)
-  if ((long)a.rows * heads * D * 2 >= 32L << 20)
-    hipLaunchKernelGGL((rotary_kernel<D, true>), grid, dim3(64 * kWaves), 0, stream, a, rounds);
-  else
-    hipLaunchKernelGGL((rotary_kernel<D, false>), grid, dim3(64 * kWaves), 0, stream, a, rounds);
+  // (us, through the caches / outputs / both past them, with inputs and outputs that no cache holds: 5001 rows of 16 and 4
+  // heads of 256, 51 MB each way, 25.9 / 22.6 / 21.3, and 21.2 / 18.5 / 21.2 where a cache holds a part; 8192 of 32 and 8 heads
+  // of 128, 84 MB, inputs past the caches alone 36.1, outputs too 33.6)
+  const long bytes = (long)a.rows * heads * D * 2;
+  const auto kernel = bytes >= 64L << 20 ? rotary_kernel<D, 2> : bytes >= 32L << 20 ? rotary_kernel<D, 1> : rotary_kernel<D, 0>;
+  hipLaunchKernelGGL(kernel, grid, dim3(64 * kWaves), 0, stream, a, rounds);
 }
 
 }  // namespace
