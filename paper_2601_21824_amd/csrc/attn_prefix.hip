@@ -9,6 +9,9 @@
 // the prefix's keys, and leaves O, maximum and sum in fp32.  decode_kernel does the same
 // for each sequence's own keys, 16 rows at a time, and join_kernel adds the parts in order.
 //
+// A sequence shorter than the prefix does without it: all of its keys are its own.  (A row either sees
+// a whole run or is left out of it, so that nothing behind a sequence's last key reaches it.)
+//
 // K and V come from the cache's pages, tile by tile, each wave its quarter of the rows, which
 // lie in one page: bf16 by direct copies into LDS; the 8-bit and 4-bit types through
 // registers, widened to bf16 (exactly) on the way to LDS.  The next tile's page numbers are
@@ -64,7 +67,7 @@ struct PrefixView {
   const DecodeArgs& a;
   int hk, nq, nk, first, w, last_page;
   const __bf16* q;   // of the lane's row
-  int sees;          // keys of the run that it sees (0 or less: none, or there is no such row)
+  bool sees;         // whether its sequence has the prefix (else it is computed on zeros and left out)
   int64_t part;      // its number in prefix_o and prefix_m, -1: there is no such row
   float v_scale;
   mutable int at, row, id;  // the next tile's place: page index and row, and page, of this wave's rows
@@ -80,8 +83,7 @@ struct PrefixView {
     const int G = a.c.heads_q / a.c.heads_kv, r = it.q0 + 32 * w + (threadIdx.x & 31);
     nq = a.c.batch * G;
     const int s = r < nq ? r / G : 0, h = hk * G + r % G;
-    const int n = clamp_len(a.c.lens[s], a.c.table_width, a.c.page_size);
-    sees = r < nq ? (n < prefix ? n : prefix) - first : 0;
+    sees = r < nq && has_prefix(a.c, s, prefix);
     part = r < nq ? ((int64_t)it.split * a.c.batch + s) * a.c.heads_q + h : -1;
     q = (const __bf16*)a.q + s * a.qs.row + h * a.qs.head;
     v_scale = TYPE == kE4m3 && a.c.v_scale ? a.c.v_scale[hk] : 1.f;
@@ -197,27 +199,20 @@ struct PrefixView {
   }
 
   // ---- query rows: a lane has one, q0 + 32 w + l % 32, whose place is found once
-  __device__ int limit(int) const { return sees > 0 && sees < nk ? sees : nk; }
-  __device__ int least(int x) const {
-    if (!__any(x < nk)) return nk;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o));
-    return __builtin_amdgcn_readfirstlane(x);
-  }
   __device__ bf16x8 q8(int, int col) const {
     u32x4 x = {0, 0, 0, 0};
-    if (sees > 0) x = *(const u32x4*)(q + col);
+    if (sees) x = *(const u32x4*)(q + col);
     return as_bf16x8(x);
   }
   __device__ int o() const { return 0; }
   __device__ int lse() const { return 0; }
   __device__ void put_o(int, int, int col, float a0, float a1, float a2, float a3) const {
     f32x4 x = {a0 * v_scale, a1 * v_scale, a2 * v_scale, a3 * v_scale};
-    if (sees <= 0) x = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (!sees) x = f32x4{0.f, 0.f, 0.f, 0.f};
     if (part >= 0) *(f32x4*)(a.prefix_o + part * D + col) = x;
   }
   __device__ void put_l(int, int, float m, float sum) const {
-    if (part >= 0) *(float2*)(a.prefix_m + 2 * part) = sees > 0 ? make_float2(m, sum) : make_float2(-INFINITY, 0.f);
+    if (part >= 0) *(float2*)(a.prefix_m + 2 * part) = sees ? make_float2(m, sum) : make_float2(-INFINITY, 0.f);
   }
 };
 
@@ -269,21 +264,14 @@ __global__ __launch_bounds__(256, 2) void prefix_few_kernel(DecodeArgs a, int it
   const int tid = threadIdx.x, l = tid & 63, g = l >> 4, lq = l & 15;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = c.heads_q / c.heads_kv, nq = c.batch * G, to = run.first + run.keys;
-  // row q0 + l % 16: its sequence, query head and the keys that it sees
+  // row q0 + l % 16: its sequence and query head
   const int r = it.q0 + lq, s = r < nq ? r / G : 0, h = it.hk * G + (r < nq ? r % G : 0);
-  const int n = clamp_len(c.lens[s], c.table_width, c.page_size);
-  const int end = r < nq && n < to ? n : to;
-  int least = end;
-  if (__any(least < to)) {
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o));
-  }
-  least = __builtin_amdgcn_readfirstlane(least);
+  const bool sees = r < nq && has_prefix(c, s, prefix);
   Rows<D> rows;
 #pragma unroll
   for (int ks = 0; ks < D / 32; ++ks) {
     const u32x4 x = *(const u32x4*)((const __bf16*)a.q + s * a.qs.row + h * a.qs.head + Tile<D, TYPE>::first(ks, g));
-    rows.q[ks] = as_bf16x8(r < nq ? x : u32x4{0, 0, 0, 0});
+    rows.q[ks] = as_bf16x8(sees ? x : u32x4{0, 0, 0, 0});
   }
   rows.clear();
   const float c2 = a.scale * kLog2e * (TYPE == kE4m3 && c.k_scale ? c.k_scale[it.hk] : 1.f);
@@ -293,16 +281,17 @@ __global__ __launch_bounds__(256, 2) void prefix_few_kernel(DecodeArgs a, int it
     Tile<D, TYPE> t;
     keys.load(t);
     keys.look(kb + 32 * 4);
-    rows.add(t, c2, kb, 0, to, end, least, lq, g);
+    rows.add(t, c2, kb, 0, to, lq, g);
   }
   if (keys.bad && l == 0 && c.status) *c.status = 1;
   const float vs = TYPE == kE4m3 && c.v_scale ? c.v_scale[it.hk] : 1.f;
   join_waves<D, 4>(space, rows.o, rows.m, rows.sum, w, nq - it.q0 < kQ ? nq - it.q0 : kQ, [&](int i, int d0, float top, float den, f32x4 out) {
     const int r = it.q0 + i;
     const int64_t at = ((int64_t)it.split * c.batch + r / G) * c.heads_q + it.hk * G + r % G;
-    const float inv = den > 0.f || den != den ? vs / den : 0.f;
-    *(f32x4*)(a.prefix_o + at * D + d0) = out * inv;
-    if (d0 == 0) *(float2*)(a.prefix_m + 2 * at) = make_float2(top, den);
+    const bool sees = has_prefix(c, r / G, prefix);
+    const float inv = sees && (den > 0.f || den != den) ? vs / den : 0.f;
+    *(f32x4*)(a.prefix_o + at * D + d0) = sees ? out * inv : f32x4{0.f, 0.f, 0.f, 0.f};
+    if (d0 == 0) *(float2*)(a.prefix_m + 2 * at) = sees ? make_float2(top, den) : make_float2(-INFINITY, 0.f);
   });
 }
 

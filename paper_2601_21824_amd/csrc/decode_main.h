@@ -201,10 +201,9 @@ struct Rows {
     m = -INFINITY;
     sum = 0.f;
   }
-  // The 32 keys of t, whose first is kb: those from `from` to `to` - 1, and for the lane's row
-  // those below `end` (`to` or less; least: the least of the wave's).
+  // The 32 keys of t, whose first is kb: those from `from` to `to` - 1.
   template <int TYPE>
-  __device__ void add(Tile<D, TYPE>& t, float c2, int kb, int from, int to, int end, int least, int lq, int g) {
+  __device__ void add(Tile<D, TYPE>& t, float c2, int kb, int from, int to, int lq, int g) {
     f32x4 sc[2];
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
@@ -220,12 +219,14 @@ struct Rows {
       x[e] = sc[e >> 2][e & 3] * c2;
       asm("" : "+v"(x[e]));
     }
-    if (kb + 32 > least || kb < from) {
+    if (kb + 32 > to || kb < from) {  // other keys: no weight, and whatever V holds there is not touched
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int key = kb + 16 * (e >> 2) + 4 * g + (e & 3);
-        if (key >= end || key < from) x[e] = -INFINITY;
-        if (key >= to || key < from) t.hide(e);  // whatever V holds there is not touched
+        if (key >= to || key < from) {
+          x[e] = -INFINITY;
+          t.hide(e);
+        }
       }
     }
     float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
@@ -301,11 +302,12 @@ __device__ inline void decode_part(const DecodeArgs& a, int block, JoinSpace<D, 
   const int nq = G - q0 < kQ ? G - q0 : kQ;  // query heads h0 .. h0 + nq - 1
   const int h0 = hk * G + q0;
 
-  // the first key that this call does itself, and the 16 keys that it lies in
-  const int skip = TAIL ? prefix_of(a) : 0, skip16 = skip & ~15;
+  // TAIL: keys from the prefix's end on, counted from the 16 that it lies in; a sequence that is shorter does
+  // without the prefix
+  const int prefix = TAIL ? prefix_of(a) : 0;
   const auto keys_of = [&](int b) {
     const int n = clamp_len(c.lens[b], c.table_width, c.page_size);
-    return TAIL ? (n > skip16 ? n - skip16 : 0) : n;
+    return TAIL && n >= prefix ? n - (prefix & ~15) : n;
   };
 
   // ---- the slot's sequence s, its chunk number i of n
@@ -337,6 +339,7 @@ __device__ inline void decode_part(const DecodeArgs& a, int block, JoinSpace<D, 
   n = __builtin_amdgcn_readfirstlane(n);
   i = __builtin_amdgcn_readfirstlane(i);
   len = __builtin_amdgcn_readfirstlane(len);
+  const int skip = TAIL && has_prefix(c, s, prefix) ? __builtin_amdgcn_readfirstlane(prefix) : 0, skip16 = skip & ~15;
   const int k0 = skip16 + i * chunk, k1 = skip16 + (len - i * chunk < chunk ? len : i * chunk + chunk);
   if (unit == 0 && i == 0 && tid == 0) {
     a.base[2 * s] = slot;
@@ -361,7 +364,7 @@ __device__ inline void decode_part(const DecodeArgs& a, int block, JoinSpace<D, 
     Tile<D, TYPE> t;
     keys.load(t);
     keys.look(kb + 32 * NW);
-    rows.add(t, c2, kb, TAIL ? skip : 0, k1, k1, k1, lq, g);
+    rows.add(t, c2, kb, skip, k1, lq, g);
   }
   if (keys.bad && l == 0 && c.status) *c.status = 1;
 

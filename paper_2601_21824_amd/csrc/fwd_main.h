@@ -42,8 +42,7 @@ namespace dash {
 // workgroup's sequence, the last key that query 0 sees under a causal mask (off; query
 // i sees keys 0 .. i + off), and the buffer resources and byte offsets of its
 // tensors.  Rows at or past nq and nk read 0 and are not written.
-// A paged view (kPaged) copies its tiles itself, and its rows see a number of keys each
-// (limit), of which those that see none are computed on zeros and left out (alive).
+// A paged view (kPaged) copies its tiles itself and takes its rows from where they are.
 // Dense calls: one N x D matrix per head.
 template <int D>
 struct DenseView {
@@ -184,9 +183,7 @@ __device__ void far_rows(const V& view, int causal, float scale, int row0) {
       for (int c = 0; c < D; c += 16)
         s = mfma32(k8(c + 8 * g), q8(c + 8 * g), s);
       // element r: key k0 + 8(r/4) + 4g + r%4, query qrow
-      int lim = causal ? min(view.nk - 1, qrow + view.off()) : view.nk - 1;
-      if constexpr (V::kPaged) lim = view.limit(qrow) - 1;
-      lim -= k0 + 4 * g;
+      const int lim = (causal ? min(view.nk - 1, qrow + view.off()) : view.nk - 1) - k0 - 4 * g;
       float mx = -INFINITY;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -285,9 +282,6 @@ __device__ __attribute__((always_inline)) inline void attn_fwd_rows(const V& vie
   int nu = q0w >= Nq ? 1 : ((causal ? min(Nk, q0w + 32 * QG + off) : Nk) + 31) / 32;
   if constexpr (V::kPacked) nu = max(nu, 1);  // (a wave whose rows see nothing: far_rows)
   load_tile(0);
-  // (a paged view's rows: how many keys the lane's row sees, and the least of the wave's)
-  int limit = Nk, least = Nk;
-  if constexpr (V::kPaged) limit = view.limit(q0w + lc), least = view.least(limit);
 
   // Q of this wave's rows: the B operand of S^T
   bf16x8 qreg[QG][KS];
@@ -426,11 +420,11 @@ __device__ __attribute__((always_inline)) inline void attn_fwd_rows(const V& vie
   };
   // element (qg, r) of unit u <-> key 32u + 8(r/4) + 4g + r%4, query q0w + 32qg + lc
   auto mask = [&](f32x16(&sc)[QG], int u) {
-    if (!(32 * u + 32 > (V::kPaged ? least : Nk) || (causal && 32 * u + 31 > q0w + off))) return;
+    if (!(32 * u + 32 > Nk || (causal && 32 * u + 31 > q0w + off))) return;
 #pragma unroll
     for (int qg = 0; qg < QG; ++qg) {
       if constexpr (kQAgpr) score_settle(sc[qg]);
-      const int lim = (V::kPaged ? limit - 1 : causal ? min(Nk - 1, q0w + 32 * qg + lc + off) : Nk - 1) - 32 * u - 4 * g;  // last visible key
+      const int lim = (causal ? min(Nk - 1, q0w + 32 * qg + lc + off) : Nk - 1) - 32 * u - 4 * g;  // last visible key
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if (8 * (r >> 2) + (r & 3) > lim) sc[qg][r] = -INFINITY;

@@ -3,6 +3,7 @@
 #pragma once
 #include "common.h"
 #include "ops.h"
+#include "page_index.h"
 
 namespace dash {
 
@@ -43,6 +44,9 @@ __device__ inline int prefix_of(const DecodeArgs& a) {
   const int64_t cap = (int64_t)a.prefix_width * a.c.page_size;
   return n < 0 ? 0 : n > cap ? (int)cap : n;
 }
+
+// whether sequence s is as long as the prefix (a shorter one has all of its keys by its own table)
+__device__ inline bool has_prefix(const CacheArgs& c, int s, int prefix) { return clamp_len(c.lens[s], c.table_width, c.page_size) >= prefix; }
 
 // Rows of sequence s among `total`: offsets outside 0 .. total are clamped, and an
 // end before its start makes an empty sequence.

@@ -155,6 +155,28 @@ def test_infinite_scores():
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("d,hq,hkv,copies", [(64, 4, 2, 1), (128, 8, 1, 9), (256, 16, 1, 4)])  # few rows and many
+def test_shared_keys_behind_a_shorter_sequence_do_not_reach_it(d, hq, hkv, copies, kind):
+    """Sequences that end inside the prefix have their keys alone, whatever the prefix holds behind them."""
+    prefix, page = 700, 16
+    lens = [700, 50, 800, 49, 699, 0, 1] * copies
+    c, q, table, shared = build(kind, d, hq, hkv, prefix, lens, page, spoil=False)
+    want = dash.attn_prefix_decode(q, *c.pools, table, i32(lens), shared, i32([prefix]), **c.scales)
+    for pool, scale in ((c.k, c.k_scale), (c.v, c.v_scale)):
+        page_of, row = int(shared[50 // page]), 50 % page  # key 50
+        if kind.startswith("mx"):
+            scale[page_of, :, row] = 255
+        elif kind == "e4m3":
+            pool.view(torch.uint8)[page_of, :, row] = 0x7F
+        else:
+            pool[page_of, :, row] = float("nan")
+    got = dash.attn_prefix_decode(q, *c.pools, table, i32(lens), shared, i32([prefix]), **c.scales)
+    short = i32(lens) <= 50
+    assert torch.equal(got[short], want[short]) and bool(got[~short].isnan().all())
+    check(*build(kind, d, hq, hkv, prefix, lens, page), prefix, lens)
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_as_without_a_shared_prefix(kind):
     """The same arguments give dash_attn_decode's result, both within their bounds."""
     prefix, lens, page, d = 2000, [2100, 2000, 2345, 2001], 16, 128
