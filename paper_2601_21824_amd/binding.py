@@ -346,6 +346,9 @@ def _rows(name, t, dtype, dev, rows, heads, d):
     return t.data_ptr(), row, head
 
 
+_NONE = (0, 0, 0)  # of a tensor that is not there
+
+
 def _flat(name, t, dtype, dev, *shape):
     """A contiguous tensor of this shape on GPU `dev`, or None: its pointer (0 for None).  A
     vector may have further dimensions of 1."""
@@ -564,10 +567,9 @@ def dash_kv_read(k_cache, v_cache, block_table, lens, cu, k_out=None, v_out=None
         _bad("k_out or v_out must be [rows, heads_kv, d]")
     rows, batch = out.shape[0], lens.numel()
     bf, i32 = torch.bfloat16, torch.int32
-    none = (0, 0, 0)
-    kp, *ks = none if k_out is None else _rows("k_out", k_out, bf, dev, rows, heads_kv, d)
-    vp, *vs = none if v_out is None else _rows("v_out", v_out, bf, dev, rows, heads_kv, d)
-    x = _pack_read(rows, _flat("cu", cu, i32, dev, batch + 1), _flat("first", first, i32, dev, batch), kp, vp, *ks, *vs)
+    kp, k0, k1 = _NONE if k_out is None else _rows("k_out", k_out, bf, dev, rows, heads_kv, d)
+    vp, v0, v1 = _NONE if v_out is None else _rows("v_out", v_out, bf, dev, rows, heads_kv, d)
+    x = _pack_read(rows, _flat("cu", cu, i32, dev, batch + 1), _flat("first", first, i32, dev, batch), kp, vp, k0, k1, v0, v1)
     _call(load().dash_kv_read, dev, stream, c, x, _flat("status", status, i32, dev, 1))
 
 
@@ -595,29 +597,37 @@ def dash_rotary(q, k, q_out, k_out, inv_freq, positions=None, cu=None, start=Non
     import torch
     if (q is None) != (q_out is None) or (k is None) != (k_out is None):
         _bad("q and q_out, k and k_out come together")
-    one = q if q is not None else k
+    one = k if q is None else q
     if one is None or one.dim() != 3 or (k is not None and k.dim() != 3):
         _bad("q and k must be [rows, heads, d]")
     if (positions is None) == (cu is None) or (start is not None and cu is None):
         _bad("either positions, or cu (and start)")
     if inv_freq is None:
         _bad("inv_freq must be given")
-    if not float(amplitude):
+    if amplitude == 0:
         _bad("amplitude must not be 0")
     dev = _gpu(one)
     rows, _, d = one.shape
     bf, i32 = torch.bfloat16, torch.int32
-    none, heads = (0, 0, 0), [0 if x is None else x.shape[1] for x in (q, k)]
-    qp, *qs = none if q is None else _rows("q", q, bf, dev, rows, heads[0], d)
-    kp, *ks = none if k is None else _rows("k", k, bf, dev, rows, heads[1], d)
-    qo, *qos = none if q is None else _rows("q_out", q_out, bf, dev, rows, heads[0], d)
-    ko, *kos = none if k is None else _rows("k_out", k_out, bf, dev, rows, heads[1], d)
-    if cu is not None and (cu.dim() != 1 or cu.numel() < 1):
-        _bad("cu must be int32 [batch + 1]")
-    batch = 0 if cu is None else cu.numel() - 1
+    hq = qp = q0 = q1 = qo = q2 = q3 = hk = kp = k0 = k1 = ko = k2 = k3 = 0
+    if q is not None:
+        hq = q.shape[1]
+        qp, q0, q1 = _rows("q", q, bf, dev, rows, hq, d)
+        qo, q2, q3 = _rows("q_out", q_out, bf, dev, rows, hq, d)
+    if k is not None:
+        hk = k.shape[1]
+        kp, k0, k1 = _rows("k", k, bf, dev, rows, hk, d)
+        ko, k2, k3 = _rows("k_out", k_out, bf, dev, rows, hk, d)
+    batch = at = first = place = 0
+    if cu is None:
+        place = _flat("positions", positions, i32, dev, rows)
+    else:
+        if cu.dim() != 1 or cu.numel() < 1:
+            _bad("cu must be int32 [batch + 1]")
+        batch = cu.numel() - 1
+        at, first = _flat("cu", cu, i32, dev, batch + 1), _flat("start", start, i32, dev, batch)
     n = inv_freq.numel()
-    x = _pack_rotary(rows, *heads, d, _flat("positions", positions, i32, dev, rows), _flat("cu", cu, i32, dev, batch + 1),
-                     _flat("start", start, i32, dev, batch), batch, qp, kp, qo, ko, *qs, *ks, *qos, *kos,
+    x = _pack_rotary(rows, hq, hk, d, place, at, first, batch, qp, kp, qo, ko, q0, q1, k0, k1, q2, q3, k2, k3,
                      _flat("inv_freq", inv_freq, torch.float32, dev, n), 2 * n, interleaved, amplitude, backward)
     _call(load().dash_rotary, dev, stream, x, _flat("status", status, i32, dev, 1))
 
@@ -626,7 +636,8 @@ def rotary(q, k, inv_freq, positions=None, cu=None, start=None, interleaved: boo
            backward: bool = False):
     """dash_rotary into new tensors.  Rows that no sequence holds have whatever the memory held."""
     import torch
-    q_out, k_out = (None if x is None else torch.empty_like(x, memory_format=torch.contiguous_format) for x in (q, k))
+    q_out = None if q is None else torch.empty_like(q, memory_format=torch.contiguous_format)
+    k_out = None if k is None else torch.empty_like(k, memory_format=torch.contiguous_format)
     dash_rotary(q, k, q_out, k_out, inv_freq, positions, cu, start, interleaved, amplitude, backward)
     return q_out, k_out
 
