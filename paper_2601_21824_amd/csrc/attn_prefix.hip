@@ -275,15 +275,16 @@ __global__ __launch_bounds__(256, 2) void prefix_few_kernel(DecodeArgs a, int it
   }
   rows.clear();
   const float c2 = a.scale * kLog2e * (TYPE == kE4m3 && c.k_scale ? c.k_scale[it.hk] : 1.f);
-  KeyRows<D, TYPE, false> keys(c, a.prefix_table, it.hk, prefix, l);
-  if (run.first + 32 * w < to) keys.look(run.first + 32 * w);
-  for (int kb = run.first + 32 * w; kb < to; kb += 32 * 4) {
-    Tile<D, TYPE> t;
-    keys.load(t);
-    keys.look(kb + 32 * 4);
-    rows.add(t, c2, kb, 0, to, lq, g);
+  if (run.first + 32 * w < to) {
+    KeyRows<D, TYPE, false> keys(c, a.prefix_table, it.hk, prefix, run.first + 32 * w, 32 * 4, l);
+    for (int kb = run.first + 32 * w; kb < to; kb += 32 * 4) {
+      Tile<D, TYPE> t;
+      keys.load(t);
+      keys.look();
+      rows.add(t, c2, kb, 0, to, lq, g);
+    }
+    if (keys.bad && l == 0 && c.status) *c.status = 1;
   }
-  if (keys.bad && l == 0 && c.status) *c.status = 1;
   const float vs = TYPE == kE4m3 && c.v_scale ? c.v_scale[it.hk] : 1.f;
   join_waves<D, 4>(space, rows.o, rows.m, rows.sum, w, nq - it.q0 < kQ ? nq - it.q0 : kQ, [&](int i, int d0, float top, float den, f32x4 out) {
     const int r = it.q0 + i;

@@ -137,51 +137,67 @@ struct Tile {
   }
 };
 
-// Where a wave's tiles come from: the rows of one K/V head in the pages of `table`.  PAST: V's rows
-// are not read again soon (a load takes a row whole): past the caches.
+// Where a wave's tiles come from: the rows of one K/V head in the pages of `table`, every `step` keys from
+// `from` on (multiples of 16).  PAST: V's rows are not read again soon (a load takes a row whole): past the caches.
 template <int D, int TYPE, bool PAST>
 struct KeyRows {
   using T = Tile<D, TYPE>;
   static constexpr int SZ = TYPE == kBf16 ? 2 : 1;  // bytes of a stride's unit
   const CacheArgs& c;
   const int32_t* table;
-  int hk, last_page;
-  const char *kbase, *vbase;
-  uint32_t k_lane, v_lane;
-  int lq, g;
-  int id[2], row[2];  // where the next tile's two halves are
+  int last_page;
+  // K/V head hk's first row of page 0; bytes from page to page and row to row; the scales alike
+  const char *k0, *v0, *k_mx, *v_mx;
+  uint64_t k_page, v_page;
+  uint32_t k_row, v_row, mx_page;
+  uint32_t k_lane, v_lane, ks_lane, vs_lane;  // this lane's part of a tile's rows
+  int next, next_row, step_pages, step_rows;  // the place in the table of the tile after the next
+  int id[2], row[2];                          // pages and rows of the next tile's two halves
   bool bad = false;
   // keys: the last one's number and one more, as the table counts
-  __device__ KeyRows(const CacheArgs& c_, const int32_t* table_, int hk_, int keys, int l)
-      : c(c_), table(table_), hk(hk_), last_page(keys > 0 ? (keys - 1) / c_.page_size : 0), kbase((const char*)c_.k + hk_ * c_.k_head * SZ),
-        vbase((const char*)c_.v + hk_ * c_.v_head * SZ), k_lane((uint32_t)((l & 15) * (int)c_.k_row * SZ + 4 * T::KW * (l >> 4))),
-        v_lane((uint32_t)(4 * (l >> 4) * (int)c_.v_row * SZ + (l & 15) * T::VB)), lq(l & 15), g(l >> 4) {}
-  // The next tile: the 32 keys from kb on, kb a multiple of 16.  Its pages are read a tile ahead: their
-  // latency is not the loads'.
-  __device__ void look(int kb) {
+  __device__ KeyRows(const CacheArgs& c_, const int32_t* table_, int hk, int keys, int from, int step, int l)
+      : c(c_), table(table_), last_page(keys > 0 ? (keys - 1) / c_.page_size : 0), k0((const char*)c_.k + hk * c_.k_head * SZ),
+        v0((const char*)c_.v + hk * c_.v_head * SZ), k_page(c_.k_page * SZ), v_page(c_.v_page * SZ), k_row((uint32_t)c_.k_row * SZ),
+        v_row((uint32_t)c_.v_row * SZ), k_lane((l & 15) * k_row + 4 * T::KW * (l >> 4)), v_lane(4 * (l >> 4) * v_row + (l & 15) * T::VB),
+        next(from / c_.page_size), next_row(from % c_.page_size), step_pages(step / c_.page_size), step_rows(step % c_.page_size) {
+    if constexpr (T::MX) {
+      const int64_t head = (int64_t)hk * c.page_size * T::SB;
+      k_mx = (const char*)c.k_mx + head, v_mx = (const char*)c.v_mx + head;
+      mx_page = (uint32_t)c.heads_kv * c.page_size * T::SB;  // (at most 2^12 2^16 2^3)
+      ks_lane = (l & 15) * T::SB, vs_lane = (l >> 4) * (4 * T::SB);
+    }
+    look();
+  }
+  // The next tile's pages, read a tile ahead: their latency is not the loads'.  (Past the last key some page
+  // of the sequence, whose keys are masked.)
+  __device__ void look() {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
-      const int key = kb + 16 * tt, p = key / c.page_size;
-      row[tt] = key - p * c.page_size;
-      id[tt] = table_entry(table, p < last_page ? p : last_page);  // (keys behind the last are masked)
+      int p = next, r = next_row + 16 * tt;
+      if (tt && r >= c.page_size) r -= c.page_size, ++p;
+      row[tt] = r;
+      id[tt] = table_entry(table, p < last_page ? p : last_page);
     }
+    next += step_pages;
+    next_row += step_rows;
+    if (next_row >= c.page_size) next_row -= c.page_size, ++next;
   }
   __device__ void load(T& t) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
-      const int r = row[tt];
-      int id = this->id[tt];
-      if (!page_ok(id, c.pages)) bad = true, id = 0;
-      const char* kp = kbase + (id * c.k_page + r * c.k_row) * SZ;
-      const char* vp = vbase + (id * c.v_page + r * c.v_row) * SZ;
+      const uint32_t r = row[tt];
+      uint32_t i = id[tt];
+      if (!page_ok(i, c.pages)) bad = true, i = 0;
+      const char* kp = k0 + (i * k_page + (uint64_t)r * k_row);
+      const char* vp = v0 + (i * v_page + (uint64_t)r * v_row);
 #pragma unroll
       for (int x = 0; x < T::NK; ++x) load_words<4 * T::KW, false>(t.k[tt][x], kp + k_lane + 16 * T::KW * x);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) load_words<T::VB, PAST>(t.v[4 * tt + x], vp + v_lane + x * (uint32_t)((int)c.v_row * SZ));
+      for (int x = 0; x < 4; ++x) load_words<T::VB, PAST>(t.v[4 * tt + x], vp + v_lane + x * v_row);
       if constexpr (T::MX) {
-        const int64_t row = ((int64_t)id * c.heads_kv + hk) * c.page_size + r;
-        load_words<T::SB, false>(t.ks[tt], (const char*)c.k_mx + (row + lq) * T::SB);
-        load_words<4 * T::SB, false>(t.vs[tt], (const char*)c.v_mx + (row + 4 * g) * T::SB);
+        const uint64_t at = (uint64_t)i * mx_page + r * T::SB;
+        load_words<T::SB, false>(t.ks[tt], k_mx + at + ks_lane);
+        load_words<4 * T::SB, false>(t.vs[tt], v_mx + at + vs_lane);
       }
     }
   }
@@ -358,15 +374,16 @@ __device__ inline void decode_part(const DecodeArgs& a, int block, JoinSpace<D, 
   const float c2 = a.scale * kLog2e * (F8 && c.k_scale ? c.k_scale[hk] : 1.f);
 
   // ---- tiles of 32 keys (those of further 16 query heads read the same keys again, V from memory)
-  KeyRows<D, TYPE, true> keys(c, c.table + (int64_t)s * c.table_stride, hk, len > 0 ? skip16 + len : 0, l);
-  if (k0 + 32 * w < k1) keys.look(k0 + 32 * w);
-  for (int kb = k0 + 32 * w; kb < k1; kb += 32 * NW) {
-    Tile<D, TYPE> t;
-    keys.load(t);
-    keys.look(kb + 32 * NW);
-    rows.add(t, c2, kb, skip, k1, lq, g);
+  if (k0 + 32 * w < k1) {
+    KeyRows<D, TYPE, true> keys(c, c.table + (int64_t)s * c.table_stride, hk, skip16 + len, k0 + 32 * w, 32 * NW, l);
+    for (int kb = k0 + 32 * w; kb < k1; kb += 32 * NW) {
+      Tile<D, TYPE> t;
+      keys.load(t);
+      keys.look();
+      rows.add(t, c2, kb, skip, k1, lq, g);
+    }
+    if (keys.bad && l == 0 && c.status) *c.status = 1;
   }
-  if (keys.bad && l == 0 && c.status) *c.status = 1;
 
   const float vs = F8 && c.v_scale ? c.v_scale[hk] : 1.f;
   join_waves<D, NW>(space, rows.o, rows.m, rows.sum, w, nq, [&](int q, int d0, float top, float den, f32x4 out) {
