@@ -297,35 +297,38 @@ __global__ __launch_bounds__(256, 2) void prefix_few_kernel(DecodeArgs a, int it
 }
 
 // The parts of one sequence and query head, the prefix's first, each in order: thread groups of
-// D / 4 lanes take every NG-th part and are added in order of the group.
+// D / 4 lanes take every NG-th part with a running maximum and are added in order of the group.  Bound by
+// latency, three dependent loads: 4 us for a few rows (finding the maximum first, one load more, 4.7), and for 2048 rows
+// of 18 parts by the parts' 19 MB, 8 us (9.8).
 template <int D>
 __global__ __launch_bounds__(256) void prefix_join_kernel(DecodeArgs a) {
   constexpr int NG = 256 / (D / 4), U = 8;  // U parts' loads in flight together
   __shared__ f32x4 acc[NG][D / 4];
-  __shared__ float dens[NG];
+  __shared__ float dens[NG], tops[NG];
   const int hq = a.c.heads_q, s = (int)blockIdx.x / hq, h = (int)blockIdx.x % hq;
   const int np = run_of(a, prefix_of(a), 0).n;
   const int first = a.base[2 * s], n = np + a.base[2 * s + 1];
-  const int tid = threadIdx.x, l = tid & 63, grp = tid / (D / 4), d4 = tid % (D / 4);
-  // part i: its row of prefix_o and prefix_m, or of part_o and part_m
-  const auto at = [&](int i) { return i < np ? ((int64_t)i * a.c.batch + s) * hq + h : (int64_t)(first + i - np) * hq + h; };
-  const auto stat = [&](int i) { return *(const float2*)((i < np ? a.prefix_m : a.part_m) + 2 * at(i)); };
-  float top = -INFINITY;
-  for (int i = l; i < n; i += 64) top = fmaxf(top, stat(i).x);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  const float mm = top == -INFINITY ? 0.f : top;
-  float den = 0.f;
+  const int tid = threadIdx.x, grp = tid / (D / 4), d4 = tid % (D / 4);
+  float top = -INFINITY, den = 0.f;
   f32x4 out = {0.f, 0.f, 0.f, 0.f};
   for (int i = grp; i < n; i += U * NG) {
     float2 m[U];
     f32x4 o[U];
+    float mx = top;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int iu = i + u * NG < n ? i + u * NG : i;  // (read again, not added)
-      m[u] = stat(iu);
-      o[u] = *(const f32x4*)((iu < np ? a.prefix_o : a.part_o) + at(iu) * D + 4 * d4);
+      // part iu: its row of prefix_o and prefix_m, or of part_o and part_m
+      const int64_t at = iu < np ? ((int64_t)iu * a.c.batch + s) * hq + h : (int64_t)(first + iu - np) * hq + h;
+      m[u] = *(const float2*)((iu < np ? a.prefix_m : a.part_m) + 2 * at);
+      o[u] = *(const f32x4*)((iu < np ? a.prefix_o : a.part_o) + at * D + 4 * d4);
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u) mx = fmaxf(mx, m[u].x);
+    const float mm = mx == -INFINITY ? 0.f : mx, alpha = __builtin_amdgcn_exp2f(top - mm);
+    top = mx;
+    den *= alpha;
+    out *= alpha;
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (i + u * NG < n) {
@@ -335,11 +338,20 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(DecodeArgs a) {
       }
   }
   acc[grp][d4] = out;
-  if (d4 == 0) dens[grp] = den;
+  if (d4 == 0) dens[grp] = den, tops[grp] = top;
   __syncthreads();
   if (grp != 0) return;
 #pragma unroll
-  for (int i = 1; i < NG; ++i) out += acc[i][d4], den += dens[i];
+  for (int i = 1; i < NG; ++i) top = fmaxf(top, tops[i]);
+  const float mm = top == -INFINITY ? 0.f : top;
+  den = 0.f;
+  out = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < NG; ++i) {
+    const float f = __builtin_amdgcn_exp2f(tops[i] - mm);
+    den += f * dens[i];
+    out += f * acc[i][d4];
+  }
   const float inv = den > 0.f || den != den ? 1.f / den : 0.f;
   *(u32x2*)((__bf16*)a.o + s * a.os.row + h * a.os.head + 4 * d4) =
       u32x2{pack_bf16(out[0] * inv, out[1] * inv), pack_bf16(out[2] * inv, out[3] * inv)};
