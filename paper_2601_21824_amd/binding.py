@@ -604,7 +604,7 @@ def dash_rotary(q, k, q_out, k_out, inv_freq, positions=None, cu=None, start=Non
         _bad("either positions, or cu (and start)")
     if inv_freq is None:
         _bad("inv_freq must be given")
-    if amplitude == 0:
+    if -1e-37 < amplitude < 1e-37:  # (0 in the struct is 1)
         _bad("amplitude must not be 0")
     dev = _gpu(one)
     rows, _, d = one.shape

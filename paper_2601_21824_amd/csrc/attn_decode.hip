@@ -3,26 +3,16 @@
 //
 //   o_h = sum_j softmax_j(scale q_h . k_j) v_j over the lens[s] cached keys
 //
-// Bound by memory: K and V are read once for every 16 query heads of a K/V head (with more,
-// each 16 are a workgroup of their own), 4 d bytes a key and head (2 d in e4m3),
-// for 4 d G operations, G query heads to a K/V head.  So the kernel's business is
-// to keep loads in flight.  One workgroup takes a chunk of one sequence's keys for
+// Bound by memory in bf16 and e4m3: K and V are read once for every 16 query heads of a K/V head
+// (with more, each 16 are a workgroup of their own), 4 d bytes a key and head (2 d in e4m3 and MXFP8 and d
+// in MXFP4, d / 16 of scale bytes), for 4 d G operations, G query heads to a K/V head.  So the kernel's
+// business is to keep loads in flight.  One workgroup takes a chunk of one sequence's keys for
 // one K/V head and up to 16 of its query heads; each of its four waves takes every
-// fourth tile of 32 keys by itself, with its own running maximum and sum; the other
-// waves' loads are in flight meanwhile (8 to 16 waves a CU, 16 KB each at d = 128; a
+// fourth tile of 32 keys by itself, with its own running maximum and sum (decode_main.h); the other
+// waves' loads are in flight meanwhile (8 to 16 waves a CU, 16 KB each at d = 128 in bf16; a
 // second tile ahead in registers leaves fewer waves and gains nothing: 538 MB 111 us with it
-// and without).  Nothing goes through LDS until the four waves are joined:
-//   S^T = K Q^T   (MFMA 16x16x32, twice 16 keys) A = K rows, loaded in the operand's own layout
-//   P = exp(S - m), in the C layout: one query a lane, keys 4g .. 4g+3 and 16 + 4g .. +3
-//   O^T += V^T P^T   B = those 8 probabilities as they are; A = V^T: lane l loads rows
-//                 4g .. and 16 + 4g .. of V, D/16 columns each, and picks column by column
-// (g = l / 16).  The columns of V that one lane holds are D/16 neighbours, so that
-// 16 lanes read one whole row; O^T's rows come out in that order.
-// P goes into that product rounded to bf16, the MFMA's operand type: each weight by 2^-8 at most, as
-// much as O itself at the end.  Its sum takes it unrounded; sums, maxima and all that is
-// joined stay in fp32.
-// An e4m3 cache is widened to bf16, which holds every e4m3 value exactly; K's scale goes into
-// the softmax scale and V's into the output.
+// and without).  Only the tiles' page numbers are read a tile ahead.  Nothing goes through LDS until the
+// four waves are joined.  K's scale of an e4m3 cache goes into the softmax scale and V's into the output.
 //
 // The keys of all sequences are cut into chunks of one size, found on the device
 // from lens (so that a captured call follows them): the sum over `workers`.  A sequence of one chunk is written at once; the others' chunks leave
@@ -30,9 +20,10 @@
 // the order of the sums, is fixed by lens and the call's shape, never by timing.
 // (Chunks of at least 128 keys: one tile for each wave.)
 //
-// Measured, 32 heads over 8 of 128: 131072 keys of 64 sequences in bf16 97 us, 5.5 TB/s,
-// and 5 us of joins; of one sequence in e4m3 43 us, 6.2 TB/s, and 6.4; 901 keys, 8 heads over 2 of
-// 64, whole, 8.9 us (four tiles a wave, one after the other).
+// Measured, 32 heads over 8 of 128: 131072 keys of 64 sequences in bf16 96 us, 5.6 TB/s,
+// and 5 us of joins, and in MXFP8 54 us, 5.2 TB/s, where the last round of uneven chunks is what is left; of one sequence
+// in e4m3 42 us, 6.3 TB/s, and 5.4, and in MXFP4 27 us, 5.2 TB/s, bound by the vector instructions that widen
+// it; 901 keys, 8 heads over 2 of 64, whole, 8.9 us (four tiles a wave, one after the other).
 #include "common.h"
 #include "decode_main.h"
 #include "ops.h"

@@ -7,7 +7,8 @@
 // pairs being (i, i + rotary / 2), or (2i, 2i + 1) when interleaved.  The angle is
 // reduced in 64 bits: at p = 10^5 a product in 32 bits is off by 2^-24 10^5 = 0.006
 // radians, more than a bf16 rounding.  The rest is 32 bits with one rounding at the
-// store (bf16, or value / scale[head] in e4m3).
+// store (bf16, or value / scale[head] in e4m3).  Keys for a microscaled cache are rotated in 64 bits and
+// stored with their block's scale byte (mx.h), found from the largest of four chunks through LDS.
 //
 // Bound by memory for prompts (q, k, v in, q and the cache rows out) and by the
 // launch for single tokens.  One wave per token: it takes sine and cosine of every
@@ -17,7 +18,8 @@
 // tokens give each wave one round only, and the waves of a token redo its sines.
 //
 // Measured, heads of 128, 32 over 8: 8192 tokens into an e4m3 cache 40 us, 101 MB in and 84
-// out, 4.6 TB/s; one token of each of 64 sequences, bf16, 4.4 us (1.6 MB).
+// out, 4.6 TB/s, and into an MXFP8 cache 40.7 us, 101 MB and 85; 3001 tokens into an MXFP4 cache 17.6 us, 37 MB and
+// 28; one token of each of 64 sequences, bf16, 4.4 us (1.6 MB).
 #include <type_traits>
 
 #include "common.h"

@@ -8,6 +8,9 @@
 // head, K and V: its lanes find the rows' pages first, one row each, then all loads are
 // in flight together, 8 components a lane.  Rows of one head are neighbours in a page, so the
 // reads are whole lines; a row's 2 d bytes are, in the output.
+//
+// Measured, 8 heads of 128: 8192 rows in MXFP8 11.0 us, 18 MB that the append before has left in the caches and 34 out;
+// 19385 rows in MXFP4 19.4 us, 24 MB in and 79 out, 5.3 TB/s; 64 rows 7.1 us, the searches and dependent loads.
 #include <type_traits>
 
 #include "common.h"
