@@ -326,7 +326,8 @@ __device__ inline void decode_part(const DecodeArgs& a, int block, JoinSpace<D, 
     return TAIL && n >= prefix ? n - (prefix & ~15) : n;
   };
 
-  // ---- the slot's sequence s, its chunk number i of n
+  // ---- the workgroup's sequence s, its chunk number i of n, and where the sequence's parts begin.  Whole chunks of all
+  // sequences first, the rests of sequences behind them: what starts late is short.
   long total = 0;
   int len = 0;
   for (int b = 0; b < c.batch; b += 64) {
@@ -334,31 +335,50 @@ __device__ inline void decode_part(const DecodeArgs& a, int block, JoinSpace<D, 
     total += wave_sum(len >> 12) * 4096l + wave_sum(len & 4095);
   }
   const int chunk = __builtin_amdgcn_readfirstlane(chunk_size(total, a.workers));
-  int s = -1, i = 0, n = 0;
-  for (int b = 0, before = 0; b < c.batch; b += 64) {
+  // lane l's chunks, of sequence b + l, and the whole ones among them, with those of the lanes before it
+  int mine = 0, whole = 0, mines = 0, wholes = 0;
+  const auto look = [&](int b) {
     if (c.batch > 64) len = b + l < c.batch ? keys_of(b + l) : 0;
-    const int mine = b + l < c.batch ? chunks_of(len, chunk) : 0;
-    const int upto = wave_scan(mine);
-    const unsigned long long here = __ballot(before + upto > slot);
+    mine = b + l < c.batch ? chunks_of(len, chunk) : 0;
+    whole = mine - ((int64_t)mine * chunk > len);
+    mines = wave_scan(mine);
+    wholes = wave_scan(whole);
+  };
+  int all = 0;  // whole chunks
+  for (int b = 0; b < c.batch; b += 64) {
+    look(b);
+    all += __builtin_amdgcn_readlane(wholes, 63);
+  }
+  const bool rest = slot >= all;
+  const int want = rest ? slot - all : slot;
+  int s = -1, i = 0, n = 0, base = 0;
+  for (int b = 0, before = 0; b < c.batch; b += 64) {
+    if (c.batch > 64) look(b);
+    const int upto = before + (rest ? mines - wholes : wholes);
+    const unsigned long long here = __ballot(upto > want);
     if (here) {
       const int at = __builtin_ctzll(here);
       s = b + at;
       n = __builtin_amdgcn_readlane(mine, at);
-      i = slot - (before + __builtin_amdgcn_readlane(upto, at) - n);
+      const int w = __builtin_amdgcn_readlane(whole, at);
+      i = rest ? w : want - __builtin_amdgcn_readlane(upto, at) + w;
+      base += __builtin_amdgcn_readlane(mines, at) - n;
       len = __builtin_amdgcn_readlane(len, at);
       break;
     }
-    before += __builtin_amdgcn_readlane(upto, 63);
+    before = __builtin_amdgcn_readlane(upto, 63);
+    base += __builtin_amdgcn_readlane(mines, 63);
   }
   if (s < 0) return;
   s = __builtin_amdgcn_readfirstlane(s);  // wave-uniform: tables are read and addresses made by the scalar unit
   n = __builtin_amdgcn_readfirstlane(n);
   i = __builtin_amdgcn_readfirstlane(i);
   len = __builtin_amdgcn_readfirstlane(len);
+  base = __builtin_amdgcn_readfirstlane(base);
   const int skip = TAIL && has_prefix(c, s, prefix) ? __builtin_amdgcn_readfirstlane(prefix) : 0, skip16 = skip & ~15;
   const int k0 = skip16 + i * chunk, k1 = skip16 + (len - i * chunk < chunk ? len : i * chunk + chunk);
   if (unit == 0 && i == 0 && tid == 0) {
-    a.base[2 * s] = slot;
+    a.base[2 * s] = base;
     a.base[2 * s + 1] = n;
     if (c.status && c.lens[s] != (TAIL ? clamp_len(c.lens[s], c.table_width, c.page_size) : len)) *c.status = 1;
   }
@@ -393,7 +413,7 @@ __device__ inline void decode_part(const DecodeArgs& a, int block, JoinSpace<D, 
           u32x2{pack_bf16(out[0] * inv, out[1] * inv), pack_bf16(out[2] * inv, out[3] * inv)};
       if (a.lse && d0 == 0) a.lse[(size_t)s * c.heads_q + h0 + q] = den == 0.f ? -INFINITY : (top + __log2f(den)) * kLn2;
     } else {
-      const size_t at = (size_t)slot * c.heads_q + h0 + q;
+      const size_t at = (size_t)(base + i) * c.heads_q + h0 + q;
       *(f32x4*)(a.part_o + at * D + d0) = out * vs;
       if (d0 == 0) a.part_m[2 * at] = top, a.part_m[2 * at + 1] = den;
     }
