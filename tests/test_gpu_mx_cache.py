@@ -206,7 +206,9 @@ def attend64(c, q, table, lens, scale):
 DECODES = [(d, hq, hkv, LENS, page, order) for d, page, order in ((64, 16, "phrd"), (128, 48, "prhd"), (256, 64, "hprd"))
            for hq, hkv in ((4, 4), (8, 1), (15, 3), (34, 2))]
 DECODES += [(128, 8, 2, [20000], 16, "phrd"), (64, 64, 1, [9000, 1], 16, "phrd"), (256, 4, 4, [7001, 40, 3000], 32, "phrd"),
-            (128, 4, 1, [1 + 37 * i % 211 for i in range(150)], 16, "phrd")]
+            (128, 4, 1, [1 + 37 * i % 211 for i in range(150)], 16, "phrd"),
+            # more than two rounds of 64 sequences in several chunks each, whole ones only among them, and empty sequences
+            (64, 4, 2, [128 * (i % 11) if i % 3 == 0 else 37 * i * i % 1500 for i in range(150)], 16, "phrd")]
 
 
 @pytest.mark.parametrize("kind", MX)
