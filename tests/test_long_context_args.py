@@ -153,3 +153,10 @@ def test_frequencies():
 def test_frequencies_refuse(args, kw, word):
     with pytest.raises(b.DashError, match=word):
         b.dash_rotary_frequencies(*args, **kw)
+
+
+def test_the_package_has_the_calls():
+    import paper_2601_21824_amd as dash
+    for name in ("dash_rotary", "rotary", "dash_rotary_frequencies", "dash_kv_read", "kv_read", "dash_attn_prefix_decode",
+                 "attn_prefix_decode", "dash_prefix_decode_workspace_size"):
+        assert getattr(dash, name) is getattr(b, name)
