@@ -326,50 +326,51 @@ __device__ inline void decode_part(const DecodeArgs& a, int block, JoinSpace<D, 
     return TAIL && n >= prefix ? n - (prefix & ~15) : n;
   };
 
-  // ---- the workgroup's sequence s, its chunk number i of n, and where the sequence's parts begin.  Whole chunks of all
-  // sequences first, the rests of sequences behind them: what starts late is short.
-  long total = 0;
-  int len = 0;
-  for (int b = 0; b < c.batch; b += 64) {
-    len = b + l < c.batch ? keys_of(b + l) : 0;
-    total += wave_sum(len >> 12) * 4096l + wave_sum(len & 4095);
-  }
+  // ---- the workgroup's sequence s, its chunk number i of n, and where the sequence's parts begin.  First all chunks of at
+  // least half the size, then the shorter rests of sequences: what starts late is short (32 heads over 8 of 128, us,
+  // in the sequences' order / so / whole chunks first: 64 sequences of 131072 keys in bf16 106 / 100 / 106 and in MXFP8
+  // 68 / 61 / 65, of 66000 38 / 37 / 39, 128 of 131072 73 / 70 / 74, 65 of 66000 38.4 / 39.8 / 40.5).
+  int len = l < c.batch ? keys_of(l) : 0;
+  long sum = len;
+#pragma unroll 8
+  for (int b = l + 64; b < c.batch; b += 64) sum += keys_of(b);
+  const long total = wave_sum((int)(sum >> 24)) * (1l << 24) + wave_sum((int)(sum & 0xffffff));  // (a table's keys: below 2^54)
   const int chunk = __builtin_amdgcn_readfirstlane(chunk_size(total, a.workers));
-  // lane l's chunks, of sequence b + l, and the whole ones among them, with those of the lanes before it
-  int mine = 0, whole = 0, mines = 0, wholes = 0;
-  const auto look = [&](int b) {
-    if (c.batch > 64) len = b + l < c.batch ? keys_of(b + l) : 0;
-    mine = b + l < c.batch ? chunks_of(len, chunk) : 0;
-    whole = mine - ((int64_t)mine * chunk > len);
-    mines = wave_scan(mine);
-    wholes = wave_scan(whole);
-  };
-  int all = 0;  // whole chunks
-  for (int b = 0; b < c.batch; b += 64) {
-    look(b);
-    all += __builtin_amdgcn_readlane(wholes, 63);
-  }
-  const bool rest = slot >= all;
-  const int want = rest ? slot - all : slot;
-  int s = -1, i = 0, n = 0, base = 0;
-  for (int b = 0, before = 0; b < c.batch; b += 64) {
-    if (c.batch > 64) look(b);
-    const int upto = before + (rest ? mines - wholes : wholes);
+  // Among `count` sequences from s on, each lane takes a 64th of them, in order; the lane that holds the chunk
+  // leaves its share to the next round (one round up to 64 sequences, two up to 4096).
+  int s = 0, i = 0, n = 0, base = 0, want = slot;
+  bool rest = false;
+  for (int count = c.batch;;) {
+    const int per = (count + 63) >> 6;
+    int mine = 0, first = 0;  // chunks of this lane's share, and those among them that come first
+#pragma unroll 8
+    for (int j = 0; j < per; ++j) {
+      const int at = l * per + j;
+      if (c.batch > 64) len = keys_of(s + (at < count ? at : 0));
+      const unsigned ch = chunk, m = len > 0 ? ((unsigned)len + ch - 1) / ch : 1;  // (below 2^32: chunk_size)
+      if (at < count) mine += m, first += m - (m * ch - (unsigned)len > ch / 2);
+    }
+    const int mines = wave_scan(mine), firsts = wave_scan(first);
+    if (count == c.batch) {
+      const int all = __builtin_amdgcn_readlane(firsts, 63);
+      rest = slot >= all;
+      want = rest ? slot - all : slot;
+    }
+    const int own = rest ? mine - first : first, upto = rest ? mines - firsts : firsts;
     const unsigned long long here = __ballot(upto > want);
-    if (here) {
-      const int at = __builtin_ctzll(here);
-      s = b + at;
+    if (!here) return;  // (in the first round: no such chunk)
+    const int at = __builtin_ctzll(here);
+    want -= __builtin_amdgcn_readlane(upto - own, at);
+    base += __builtin_amdgcn_readlane(mines - mine, at);
+    s += at * per;
+    if (per == 1) {
       n = __builtin_amdgcn_readlane(mine, at);
-      const int w = __builtin_amdgcn_readlane(whole, at);
-      i = rest ? w : want - __builtin_amdgcn_readlane(upto, at) + w;
-      base += __builtin_amdgcn_readlane(mines, at) - n;
+      i = rest ? __builtin_amdgcn_readlane(first, at) : want;
       len = __builtin_amdgcn_readlane(len, at);
       break;
     }
-    before = __builtin_amdgcn_readlane(upto, 63);
-    base += __builtin_amdgcn_readlane(mines, 63);
+    count = count - at * per < per ? count - at * per : per;
   }
-  if (s < 0) return;
   s = __builtin_amdgcn_readfirstlane(s);  // wave-uniform: tables are read and addresses made by the scalar unit
   n = __builtin_amdgcn_readfirstlane(n);
   i = __builtin_amdgcn_readfirstlane(i);

@@ -208,7 +208,9 @@ DECODES = [(d, hq, hkv, LENS, page, order) for d, page, order in ((64, 16, "phrd
 DECODES += [(128, 8, 2, [20000], 16, "phrd"), (64, 64, 1, [9000, 1], 16, "phrd"), (256, 4, 4, [7001, 40, 3000], 32, "phrd"),
             (128, 4, 1, [1 + 37 * i % 211 for i in range(150)], 16, "phrd"),
             # more than two rounds of 64 sequences in several chunks each, whole ones only among them, and empty sequences
-            (64, 4, 2, [128 * (i % 11) if i % 3 == 0 else 37 * i * i % 1500 for i in range(150)], 16, "phrd")]
+            (64, 4, 2, [128 * (i % 11) if i % 3 == 0 else 37 * i * i % 1500 for i in range(150)], 16, "phrd"),
+            # more than 64 * 64 sequences
+            (64, 4, 1, [1 + i % 3 if i % 400 else 1200 + i // 10 for i in range(4101)], 16, "phrd")]
 
 
 @pytest.mark.parametrize("kind", MX)
