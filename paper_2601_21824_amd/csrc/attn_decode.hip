@@ -20,9 +20,8 @@
 // the order of the sums, is fixed by lens and the call's shape, never by timing.
 // (Chunks of at least 128 keys: one tile for each wave.)
 //
-// Measured, 32 heads over 8 of 128: 131072 keys of 64 sequences in bf16 96 us, 5.6 TB/s,
-// and 5 us of joins, and in MXFP8 51 us, 5.7 TB/s (54 with chunks in the sequences' order), 8 of which are the uneven
-// chunks'; of one sequence in e4m3 42 us, 6.3 TB/s, and 5.4, and in MXFP4 27 us, 5.3 TB/s, bound by the vector instructions that widen
+// Measured, 32 heads over 8 of 128: 131072 keys of 64 sequences in bf16 90 us, 6.0 TB/s,
+// and 5 us of joins, and in MXFP8 47 us, 6.2 TB/s; of one sequence in e4m3 42 us, 6.3 TB/s, and 5.4, and in MXFP4 27 us, 5.3 TB/s, bound by the vector instructions that widen
 // it; 901 keys, 8 heads over 2 of 64, whole, 8.9 us (four tiles a wave, one after the other).
 #include "common.h"
 #include "decode_main.h"
