@@ -347,8 +347,8 @@ __device__ inline void decode_part(const DecodeArgs& a, int block, JoinSpace<D, 
     for (int j = 0; j < per; ++j) {
       const int at = l * per + j;
       if (c.batch > 64) len = keys_of(s + (at < count ? at : 0));
-      const unsigned ch = chunk, m = len > 0 ? ((unsigned)len + ch - 1) / ch : 1;  // (below 2^32: chunk_size)
-      if (at < count) mine += m, first += m - (m * ch - (unsigned)len > ch / 2);
+      const int m = chunks_of(len, chunk);
+      if (at < count) mine += m, first += m - ((unsigned)m * (unsigned)chunk - (unsigned)len > (unsigned)chunk / 2);  // (32 bits, as chunks_of)
     }
     const int mines = wave_scan(mine), firsts = wave_scan(first);
     if (count == c.batch) {

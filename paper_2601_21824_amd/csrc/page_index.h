@@ -49,6 +49,7 @@ DASH_PAGE_HD int chunk_size(int64_t total, int workers) {
   const int64_t c = workers > 0 ? chunk_keys(total, workers) : kMaxKeys;
   return c < kMaxKeys ? (int)c : kMaxKeys;
 }
-DASH_PAGE_HD int chunks_of(int len, int64_t chunk) { return len > 0 ? (int)((len + chunk - 1) / chunk) : 1; }
+// (a length above chunk: both, and their sum, in 32 bits)
+DASH_PAGE_HD int chunks_of(int len, int64_t chunk) { return len > chunk ? (int)(((uint32_t)len + (uint32_t)chunk - 1) / (uint32_t)chunk) : 1; }
 
 }  // namespace dash
