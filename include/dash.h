@@ -388,7 +388,7 @@ typedef struct {
   int64_t table_stride;
   const int32_t* lens; /* [batch] */
   /* [heads_kv] or NULL (1): a cached value stands for itself times its head's
-     scale.  E4M3 only. */
+     scale, which may have either sign or, where a cache is read, be 0.  E4M3 only. */
   const float* k_scale;
   const float* v_scale;
   /* MXFP8 and MXFP4 only (not looked at for the other types): the scale bytes, contiguous

@@ -35,6 +35,16 @@ namespace {
 
 constexpr int kRows = 128;  // rows of a workgroup, if they are many
 
+// The forward masks and takes maxima before it multiplies by the softmax scale, which so has to be above 0: K's scale
+// of an e4m3 head may be anything, and its sign, or 0, goes into Q.
+struct ScoreScale {
+  float scale, q;  // q: 1, -1 or 0 (times which an infinity is NaN, as it is for the other kernels)
+};
+__device__ inline ScoreScale score_scale(float scale, float k_scale) {
+  const float s = scale * k_scale;
+  return {s == 0.f ? scale : __builtin_fabsf(s), s == 0.f ? 0.f : s < 0.f ? -1.f : 1.f};
+}
+
 // The prefix's runs: whole kUnit keys, cut into n equal runs of min_run keys at least.
 constexpr int kUnit = 128;
 struct Run {
@@ -76,13 +86,13 @@ struct PrefixView {
   const __bf16* q;   // of the lane's row
   bool sees;         // whether its sequence has the prefix (else it is computed on zeros and left out)
   int64_t part;      // its number in prefix_o and prefix_m, -1: there is no such row
-  float v_scale;
+  float v_scale, q_scale;
   mutable int at, row, id;  // the next tile's place: page index and row, and page, of this wave's rows
   mutable unsigned kx[PARTS][PW], vx[PARTS][PW], kb[PARTS], vb[PARTS];
   mutable bool bad;
 
-  __device__ PrefixView(const DecodeArgs& a_, const Item& it, int prefix, const Run& run, int w_)
-      : a(a_), hk(it.hk), nk(run.keys), first(run.first), w(w_), last_page((prefix - 1) / a_.c.page_size), bad(false) {
+  __device__ PrefixView(const DecodeArgs& a_, const Item& it, int prefix, const Run& run, int w_, float q_scale_)
+      : a(a_), hk(it.hk), nk(run.keys), first(run.first), w(w_), last_page((prefix - 1) / a_.c.page_size), q_scale(q_scale_), bad(false) {
     const int key = first + w * RW;
     at = key / a.c.page_size;
     row = key - at * a.c.page_size;
@@ -209,6 +219,11 @@ struct PrefixView {
   __device__ bf16x8 q8(int, int col) const {
     u32x4 x = {0, 0, 0, 0};
     if (sees) x = *(const u32x4*)(q + col);
+    if constexpr (TYPE == kE4m3) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        x[i] = pack_bf16(__builtin_bit_cast(float, x[i] << 16) * q_scale, __builtin_bit_cast(float, x[i] & 0xffff0000u) * q_scale);
+    }
     return as_bf16x8(x);
   }
   __device__ int o() const { return 0; }
@@ -248,9 +263,9 @@ __global__ __launch_bounds__(256, WPS) void prefix_kernel(DecodeArgs a, int item
   if (item == 0 && threadIdx.x == 0 && c.status && *a.prefix_len != prefix) *c.status = 1;
   const Run run = run_of(a, prefix, it.split);
   if (it.split >= run.n) return;
-  const PrefixView<D, TYPE> view(a, it, prefix, run, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
-  const float scale = a.scale * (TYPE == kE4m3 && c.k_scale ? c.k_scale[it.hk] : 1.f);
-  attn_fwd_rows<D, 1>(view, 0, scale, it.q0, space.tiles);
+  const ScoreScale score = score_scale(a.scale, TYPE == kE4m3 && c.k_scale ? c.k_scale[it.hk] : 1.f);
+  const PrefixView<D, TYPE> view(a, it, prefix, run, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), score.q);
+  attn_fwd_rows<D, 1>(view, 0, score.scale, it.q0, space.tiles);
   if (view.bad && (threadIdx.x & 63) == 0 && c.status) *c.status = 1;
 }
 

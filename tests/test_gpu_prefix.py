@@ -349,3 +349,22 @@ def test_prefix_at_the_far_end_of_a_large_cache():
         off = (d + 4) * U24 * (q[s].double().abs() @ k.abs().t().contiguous()).amax() / 16
         tol = 2.0 ** -8 * (p @ v).abs() + (2.0 ** -8 * (1 + 2.0 ** -8) + 2 * off + 2 * n * U24 + 24 * U24) * a
         assert bool(((o[s].double() - p @ v).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("prefix,wide", [(704, 16.0), (701, 1.0)])
+@pytest.mark.parametrize("d,copies", [(64, 1), (64, 3), (128, 1), (128, 3), (256, 1), (256, 6)])  # few rows and many
+def test_scales_of_any_sign(d, copies, prefix, wide):
+    """An e4m3 head whose keys' scale is negative, or 0 (every key of it scores 0), by either kernel, to the bounds of `check`, which
+    take the scale by its absolute value; and the same call without the shared prefix."""
+    hq, hkv, page = 16, 4, 16
+    lens = [prefix, 50, 800, prefix + 2, 699, 0] * copies
+    c, q, table, shared = build("e4m3", d, hq, hkv, prefix, lens, page)
+    q = q * wide
+    c.k_scale = torch.tensor([0.5, 0.0, -0.7, -0.0], device="cuda")
+    c.v_scale = torch.tensor([-0.5, 0.6, 0.0, 0.8], device="cuda")
+    o, lse = check(c, q, table, shared, prefix, lens)
+    if prefix % page == 0:  # (the sequences' own copies of the last page are whole)
+        o2, lse2 = torch.empty_like(o), torch.empty_like(lse)
+        dash.dash_attn_decode(q, *c.pools, table, i32(lens), o2, lse2, **c.scales)
+        _, _, tol = attend64(c, q, table, lens, 1 / math.sqrt(d))
+        assert bool(((o.double() - o2.double()).abs() <= 2.1 * tol).all())
