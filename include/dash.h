@@ -534,7 +534,8 @@ size_t dash_prefix_decode_workspace_size(int batch, int heads_q, int heads_kv, i
  * multiplied once for all sequences.  lens and block_table are those of dash_attn_decode (and
  * of dash_kv_append), the shared keys among them: sequence s attends to the *prefix_len
  * keys of prefix_table and to its keys *prefix_len .. lens[s]-1 of block_table, whose
- * entries for whole shared pages are not looked at; one with lens[s] < *prefix_len to its lens[s] keys of block_table
+ * entries for whole shared pages are not looked at (with lens[s] = *prefix_len none is); one with
+ * lens[s] < *prefix_len to its lens[s] keys of block_table
  * alone, as in dash_attn_decode.  A prefix may end inside a page; each sequence's own
  * page then goes on behind it.  Keys are summed in runs of the prefix, whose number depends on *prefix_len,
  * batch, heads_q, heads_kv, d and prefix_width * page_size, and in chunks of the rest as by dash_attn_decode.

@@ -318,12 +318,12 @@ __device__ inline void decode_part(const DecodeArgs& a, int block, JoinSpace<D, 
   const int nq = G - q0 < kQ ? G - q0 : kQ;  // query heads h0 .. h0 + nq - 1
   const int h0 = hk * G + q0;
 
-  // TAIL: keys from the prefix's end on, counted from the 16 that it lies in; a sequence that is shorter does
-  // without the prefix
+  // TAIL: keys from the prefix's end on, counted from the 16 that it lies in (none: none, not the prefix's last few, for which
+  // a sequence need not have a page); a sequence that is shorter does without the prefix
   const int prefix = TAIL ? prefix_of(a) : 0;
   const auto keys_of = [&](int b) {
     const int n = clamp_len(c.lens[b], c.table_width, c.page_size);
-    return TAIL && n >= prefix ? n - (prefix & ~15) : n;
+    return !TAIL || n < prefix ? n : n > prefix ? n - (prefix & ~15) : 0;
   };
 
   // ---- the workgroup's sequence s, its chunk number i of n, and where the sequence's parts begin.  First all chunks of at

@@ -368,3 +368,24 @@ def test_scales_of_any_sign(d, copies, prefix, wide):
         dash.dash_attn_decode(q, *c.pools, table, i32(lens), o2, lse2, **c.scales)
         _, _, tol = attend64(c, q, table, lens, 1 / math.sqrt(d))
         assert bool(((o.double() - o2.double()).abs() <= 2.1 * tol).all())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("d,copies", [(64, 1), (128, 5), (256, 13)])  # few rows and many
+def test_a_sequence_that_ends_with_the_prefix_needs_no_page(d, copies, kind):
+    """Without keys of its own, a sequence has no page of its own either: its entries are not looked at, and nothing is reported."""
+    prefix, page = 701, 16
+    lens = [prefix, prefix + 1, prefix] * copies
+    c, q, table, shared = build(kind, d, 16, 2, prefix, lens, page)
+    want, lse = check(c, q, table, shared, prefix, lens)
+    t = table.clone()
+    t[i32(lens) == prefix] = -1
+    status, o = i32([0]), torch.empty_like(want)
+    dash.dash_attn_prefix_decode(q, *c.pools, t, i32(lens), shared, i32([prefix]), o, status=status, **c.scales)
+    assert int(status) == 0 and torch.equal(o, want)
+    alone = i32([prefix] * len(lens))  # nobody has a key of their own
+    dash.dash_attn_prefix_decode(q, *c.pools, torch.full_like(t, -1), alone, shared, i32([prefix]), o, status=status, **c.scales)
+    assert int(status) == 0
+    ends = i32(lens) == prefix
+    _, _, tol = attend64(c, q, table, lens, 1 / math.sqrt(d))
+    assert bool(((o[ends].double() - want[ends].double()).abs() <= 2.1 * tol[ends]).all())
