@@ -36,13 +36,14 @@ namespace {
 constexpr int kRows = 128;  // rows of a workgroup, if they are many
 
 // The forward masks and takes maxima before it multiplies by the softmax scale, which so has to be above 0: K's scale
-// of an e4m3 head may be anything, and its sign, or 0, goes into Q.
+// of an e4m3 head may be anything, and its sign, or 0, goes into Q.  (The product in decode_main.h's order: equal scores
+// 2^24 and more from 0 would otherwise differ by a rounding that moves weights.)
 struct ScoreScale {
-  float scale, q;  // q: 1, -1 or 0 (times which an infinity is NaN, as it is for the other kernels)
+  float c2, q;  // q: 1, -1 or 0 (times which an infinity is NaN, as it is for the other kernels)
 };
 __device__ inline ScoreScale score_scale(float scale, float k_scale) {
-  const float s = scale * k_scale;
-  return {s == 0.f ? scale : __builtin_fabsf(s), s == 0.f ? 0.f : s < 0.f ? -1.f : 1.f};
+  const float c2 = scale * kLog2e, s = c2 * k_scale;
+  return {s == 0.f ? c2 : __builtin_fabsf(s), s == 0.f ? 0.f : s < 0.f ? -1.f : 1.f};
 }
 
 // The prefix's runs: whole kUnit keys, cut into n equal runs of min_run keys at least.
@@ -265,7 +266,7 @@ __global__ __launch_bounds__(256, WPS) void prefix_kernel(DecodeArgs a, int item
   if (it.split >= run.n) return;
   const ScoreScale score = score_scale(a.scale, TYPE == kE4m3 && c.k_scale ? c.k_scale[it.hk] : 1.f);
   const PrefixView<D, TYPE> view(a, it, prefix, run, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), score.q);
-  attn_fwd_rows<D, 1>(view, 0, score.scale, it.q0, space.tiles);
+  attn_fwd_rows<D, 1>(view, 0, score.c2, it.q0, space.tiles);
   if (view.bad && (threadIdx.x & 63) == 0 && c.status) *c.status = 1;
 }
 

@@ -150,7 +150,7 @@ template <int D, typename V>
 __device__ void far_rows(const V& view, int causal, float scale, int row0) {
   const int l = fresh_lane();
   const int g = l >> 5, lc = l & 31, qrow = row0 + lc;
-  const float c2 = scale * kLog2e;
+  const float c2 = V::kPaged ? scale : scale * kLog2e;
   const auto ro = view.o();
   const auto rq = [&] { if constexpr (V::kPaged) return 0; else return view.q(); }();
   const auto q8 = [&](int c) {
@@ -228,7 +228,8 @@ __device__ void far_rows(const V& view, int causal, float scale, int row0) {
   }
 }
 
-// One workgroup's 128 QG query rows from q0 on.  causal, scale: the call's.
+// One workgroup's 128 QG query rows from q0 on.  causal, scale: the call's (a paged view's has log2 e in it already: it is
+// joined with parts of decode_main.h, and has to be rounded as there).
 template <int D, int QG, typename V>
 __device__ __attribute__((always_inline)) inline void attn_fwd_rows(const V& view, const int causal, const float scale, const int q0,
                                                                                         FwdTiles<D>& sm) {
@@ -252,7 +253,7 @@ __device__ __attribute__((always_inline)) inline void attn_fwd_rows(const V& vie
   const int Nq = view.nq, Nk = view.nk, off = view.off();
   const int q0w = q0 + 32 * QG * w;
   const auto rq = [&] { if constexpr (V::kPaged) return 0; else return view.q(); }();
-  const float c2 = scale * kLog2e;
+  const float c2 = V::kPaged ? scale : scale * kLog2e;
 
   // ---- tiles: K into k[t % 2], V into v[t % VBUF]
   const uint32_t k_lds = lds_base(&sm.k[0][0]), v_lds = lds_base(&sm.v[0][0]);

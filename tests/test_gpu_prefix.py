@@ -389,3 +389,131 @@ def test_a_sequence_that_ends_with_the_prefix_needs_no_page(d, copies, kind):
     ends = i32(lens) == prefix
     _, _, tol = attend64(c, q, table, lens, 1 / math.sqrt(d))
     assert bool(((o[ends].double() - want[ends].double()).abs() <= 2.1 * tol[ends]).all())
+
+
+def first_block(c, rows, code, exponent=0):
+    """Keys `rows` (truth values [pages, page]) get `code` in component 0 and, in a microscaled cache, 0 in the others of its
+    block and the scale 2^exponent.  A code is a value (bf16) or an element's bits, of a tensor [heads, 1] or one for all."""
+    k = (c.k if c.kind == "bf16" else c.k.view(torch.uint8)).transpose(1, 2)
+    x = k[rows]
+    x[..., 0] = code
+    if c.kind.startswith("mx"):
+        x[..., 1:32 if c.kind == "mxfp8" else 16] = 0
+        s = c.k_scale.transpose(1, 2)
+        y = s[rows]
+        y[..., 0] = 127 + exponent
+        s[rows] = y
+    k[rows] = x
+
+
+def rows_of_keys(table, shared, lens, prefix, keys, pages, page):
+    """The cached rows of these keys of the prefix: the shared ones, and those of sequences' own copies."""
+    r = torch.zeros((pages, page), dtype=torch.bool, device="cuda")
+    for j in keys:
+        r[int(shared[j // page]), j % page] = True
+        for s, n in enumerate(lens):
+            if n > j:
+                r[int(table[s, j // page]), j % page] = True
+    return r
+
+
+# many rows: what the forward's pipelined loop leaves to its careful one, on rows that lie in pages
+FAR = [(64, 6, 16, "phrd"), (128, 6, 48, "prhd"), (256, 14, 64, "hprd")]
+
+
+@pytest.mark.parametrize("kind", KINDS + ["e4m3-"])
+@pytest.mark.parametrize("prefix", [701, 640])
+@pytest.mark.parametrize("d,copies,page,order", FAR)
+def test_runs_that_begin_with_infinite_scores(d, copies, page, order, prefix, kind):
+    """Of every 128 shared keys the first 32 score -infinity (overflowing, or an infinity in K), so that every run's rows are done
+    again by the careful loop, on ordinary scores and all components.  Bounds of `check`; "-": scales of both signs."""
+    lens = [prefix, 50, 800, 20, 1500] * copies
+    c, q, table, shared = build(kind[:-1] if kind == "e4m3-" else kind, d, 8, 2, prefix, lens, page, order)
+    if kind == "e4m3-":
+        c.k_scale = torch.tensor([-0.7, 0.4], device="cuda")
+    pages = c.k.shape[0]
+    quiet = [j for j in range(prefix) if j % 128 < 32]
+    live = ~(c.k.double().isnan() if kind == "bf16" else c.k.view(torch.uint8) == 0x7F).all(-1).all(1)
+    if kind.startswith("mx"):
+        live = (c.k_scale != 255).all(-1).all(1)
+    k = (c.k if kind == "bf16" else c.k.view(torch.uint8)).transpose(1, 2)
+    x = k[live]
+    x[..., 0] = 0
+    k[live] = x
+    least = {"bf16": -math.inf, "mxfp8": 0xFE, "mxfp4": 0x0F}.get(kind)
+    if least is None:  # e4m3: -448 times the scale's sign
+        least = torch.where(c.k_scale > 0, 0xFE, 0x7E).to(torch.uint8)
+    first_block(c, rows_of_keys(table, shared, lens, prefix, quiet, pages, page), least, 100)
+    q = q.clone()
+    q[..., 0] = {"bf16": 1.0, "mxfp8": 2.0 ** 100, "mxfp4": 2.0 ** 100}.get(kind, 2.0 ** 127)
+    B, hq, _ = q.shape
+    o, lse, status = torch.full((B, hq, d), 9.0, device="cuda").to(BF), torch.full((B, hq), 9.0, device="cuda"), i32([0])
+    dash.dash_attn_prefix_decode(q, *c.pools, table, i32(lens), shared, i32([prefix]), o, lse, status=status, **c.scales)
+    assert int(status) == 0
+    k_all, v_all = c.all64()
+    for s, n in enumerate(lens):
+        j = torch.tensor([i for i in range(n) if i >= prefix or i % 128 >= 32], device="cuda", dtype=torch.long)
+        if len(j) == 0:
+            assert bool((o[s] == 0).all()) and bool((lse[s] == -math.inf).all())
+            continue
+        k, v = (x[table[s, j // page].long(), :, j % page].transpose(0, 1) for x in (k_all, v_all))
+        qq = q[s].double().reshape(2, hq // 2, d)
+        qq[..., 0] = 0
+        sc = qq @ k.transpose(1, 2).contiguous() / math.sqrt(d)
+        p = torch.softmax(sc, -1)
+        a, oo = p @ v.abs(), p @ v
+        off = (d + 4) * U24 / math.sqrt(d) * (qq.abs() @ k.abs().transpose(1, 2).contiguous()).amax(-1, keepdim=True)
+        tol = 2.0 ** -8 * oo.abs() + (2.0 ** -8 * (1 + 2.0 ** -8) + 2 * off + 2 * n * U24 + 16 * U24) * a
+        tol = tol + 8 * U24 * tol.clamp(min=oo.abs().amax())
+        assert bool(((o[s].double().reshape(2, hq // 2, d) - oo).abs() <= tol).all()), (s, n)
+        ref = torch.logsumexp(sc, -1).reshape(hq)
+        assert bool(((lse[s].double() - ref).abs() <= 2e-5 * ref.abs().clamp(min=1)).all()), (s, n)
+    assert torch.equal(o, dash.attn_prefix_decode(q, *c.pools, table, i32(lens), shared, i32([prefix]), **c.scales))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("d,copies,page,order", FAR)
+def test_many_rows_with_scores_far_from_zero(d, copies, page, order, kind):
+    """One key far above all others, in a run's first unit, its last, partial one or behind the prefix: it weighs exactly 1, so that O
+    is its V, rounded.  And all keys alike and far below 0: O is the mean of V, by P of exactly 1 and sums in fp32."""
+    prefix, lens = 701, [701, 50, 800, 1500] * copies
+    one = {"bf16": 1.0, "e4m3": 0x38, "mxfp8": 0x38, "mxfp4": 0x02}[kind]
+
+    def run(key, q0):
+        c, q, table, shared = build(kind, d, 8, 2, prefix, lens, page, order, spoil=False)
+        everywhere = torch.ones(c.k.shape[0], page, dtype=torch.bool, device="cuda")
+        first_block(c, everywhere, one if key is None else 0)
+        if key is not None:
+            first_block(c, rows_of_keys(table, shared, lens, prefix, [key], c.k.shape[0], page) if key < prefix else
+                        used_key(table, lens, key, c.k.shape[0], page), one)
+        q = torch.zeros_like(q) if key is None else q.clone()
+        q[..., 0] = q0
+        o, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+        dash.dash_attn_prefix_decode(q, *c.pools, table, i32(lens), shared, i32([prefix]), o, lse, **c.scales)
+        return c, table, o, lse
+
+    for key in (0, 31, 385, 700, 750):
+        c, table, o, lse = run(key, 2.0 ** 30)
+        v = c.all64()[1]
+        for s, n in enumerate(lens):
+            if n > key:
+                want = v[int(table[s, key // page]), :, key % page].repeat_interleave(4, 0)
+                assert bool(((o[s].double() - want).abs() <= 2.0 ** -8 * want.abs()).all()), (key, s)
+            assert bool(o[s].isfinite().all()) and bool(lse[s].isfinite().all())
+    c, table, o, lse = run(None, -2.0 ** 26)
+    ks = c.k_scale.double() if kind == "e4m3" else torch.ones(2, dtype=torch.float64, device="cuda")
+    for s, n in enumerate(lens):
+        _, v = c.rows64(table, s, n)
+        want, a = (x.repeat_interleave(4, 0) for x in (v.mean(1), v.abs().mean(1)))
+        assert bool(((o[s].double() - want).abs() <= 2.0 ** -8 * want.abs() + (2 * n + 24) * U24 * a).all()), s
+        ref = (-2.0 ** 26 / math.sqrt(d) * ks).repeat_interleave(4) + math.log(n)
+        assert bool(((lse[s].double() - ref).abs() <= 8 * U24 * ref.abs()).all()), s
+
+
+def used_key(table, lens, key, pages, page):
+    """The cached row of one key behind the prefix, in every sequence that has it."""
+    r = torch.zeros((pages, page), dtype=torch.bool, device="cuda")
+    for s, n in enumerate(lens):
+        if n > key:
+            r[int(table[s, key // page]), key % page] = True
+    return r
