@@ -394,3 +394,53 @@ def test_refusals():
         args = dict(dict(cu=i32([0, 2, 4]), k_out=kr, v_out=None), **kw)
         with pytest.raises(dash.DashError, match=word):
             dash.dash_kv_read(*x8.pools, table, lens, **args, **x8.scales)
+
+
+@pytest.mark.parametrize("d,hq,hkv,rotary,interleaved", [(64, 16, 8, 64, False), (128, 32, 8, 96, True), (256, 16, 4, 256, False)])
+@pytest.mark.parametrize("kind", KINDS)
+def test_appends_and_reads_too_large_for_the_caches(d, hq, hkv, rotary, interleaved, kind):
+    """Appends from 32 MB of q, k and v on (64 beside a bf16 or e4m3 cache), and reads of as much, go past the caches: the bits of
+    calls of fewer rows, q and k also in place."""
+    page, old = 32, [5, 0, 1000]
+    tokens = (33 if kind in MX else 66) * 2 ** 20 // ((hq + 2 * hkv) * d * 2) + 1
+    lens = [tokens // 4, tokens // 2, tokens - tokens // 4 - tokens // 2]
+    assert max(lens) * (hq + 2 * hkv) * d * 2 < (32 if kind in MX else 64) * 2 ** 20
+    table, pages = table_of([o + n for o, n in zip(old, lens)], page)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(d + hq)
+    q, k, v = (torch.randn((tokens, h, d), generator=g, device="cuda").to(BF) for h in (hq, hkv, hkv))
+    inv = (10000.0 ** (-torch.arange(0, rotary, 2, device="cuda") / rotary)).float()
+    at = offsets(lens)
+    big, small, inside = (Cache(kind, pages, hkv, page, d) for _ in range(3))
+    kw = dict(inv_freq=inv, interleaved=interleaved)
+    q1, k1, status = torch.empty_like(q), torch.empty_like(k), i32([0])
+    dash.dash_kv_append(k, v, *big.pools, table, i32(old), cu=i32(at), q=q, q_out=q1, k_out=k1, status=status, **kw, **big.scales)
+    q2, k2 = torch.empty_like(q), torch.empty_like(k)
+    for s, n in enumerate(lens):
+        part = slice(at[s], at[s] + n)
+        dash.dash_kv_append(k[part], v[part], *small.pools, table[s:s + 1], i32(old[s:s + 1]), cu=i32([0, n]), q=q[part], q_out=q2[part],
+                            k_out=k2[part], status=status, **kw, **small.scales)
+    dash.dash_kv_append(k, v, *inside.pools, table, i32(old), cu=i32(at), q=q, q_out=q, k_out=k, status=status, **kw, **inside.scales)
+    assert int(status) == 0
+    bits = lambda c: [x if x.dtype is BF else x.view(torch.uint8) for x in c.pools] + ([c.k_scale, c.v_scale] if kind in MX else [])  # noqa: E731
+    for c in (big, inside):
+        assert all(torch.equal(x, y) for x, y in zip(bits(c), bits(small)))
+    assert all(torch.equal(x, q2) for x in (q1, q)) and all(torch.equal(x, k2) for x in (k1, k))
+    # read back: all keys, and again, by few
+    all_keys = i32([o + n for o, n in zip(old, lens)])
+    rows = int(all_keys.sum())
+    repeat = 33 * 2 ** 20 // (rows * hkv * d * 4) + 1  # sequences of the same keys
+    t, n = table.repeat(repeat, 1), all_keys.repeat(repeat)
+    cu = torch.cat((i32([0]), n.cumsum(0).to(torch.int32)))
+    assert rows * repeat * hkv * d * 4 >= 32 * 2 ** 20
+    ko, vo = dash.kv_read(*big.pools, t, n, cu, rows * repeat, status=status, **big.scales)
+    first = 0
+    for s, m in enumerate(all_keys.tolist()):
+        for part in range(0, m, 900):
+            few = min(900, m - part)
+            kf, vf = dash.kv_read(*big.pools, table[s:s + 1], all_keys[s:s + 1], i32([0, few]), few, first=i32([part]), status=status, **big.scales)
+            for r in range(repeat):
+                own = slice(r * rows + first + part, r * rows + first + part + few)
+                assert torch.equal(ko[own], kf) and torch.equal(vo[own], vf)
+        first += m
+    assert int(status) == 0

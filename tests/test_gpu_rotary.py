@@ -227,3 +227,26 @@ def test_training_step_with_rotated_heads():
     loss.backward()
     for got, x in ((dq, qq), (dk, kk), (dv, vv)):
         assert float((got.double() - x.grad).norm() / x.grad.norm()) <= 3 * U8
+
+
+@pytest.mark.parametrize("d,hq,hk,interleaved,backward", [(64, 16, 16, True, False), (128, 32, 8, False, True), (256, 16, 4, False, False)])
+@pytest.mark.parametrize("mb", [33, 66])
+def test_calls_too_large_for_the_caches(d, hq, hk, interleaved, backward, mb):
+    """From 32 MB of q and k on outputs, from 64 MB inputs too go past the caches: the bits of calls of fewer rows, also in place."""
+    rows, inv = mb * 2 ** 20 // ((hq + hk) * d * 2) + 3, freqs(d - 16)
+    q, k = random(rows, hq, d, seed=1), random(rows, hk, d, seed=2)
+    at = i32([2, rows // 3, rows - 1])  # (rows before and behind the sequences are left alone)
+    start = [7, 100000]
+    place = torch.cat((torch.arange(rows // 3 - 2) + start[0], torch.arange(rows - 1 - rows // 3) + start[1])).to(torch.int32).cuda()
+    kw = dict(interleaved=interleaved, amplitude=1.2, backward=backward)
+    q_out, k_out = torch.full_like(q, 7.0), torch.full_like(k, 7.0)
+    dash.dash_rotary(q, k, q_out, k_out, inv, cu=at, start=i32(start), **kw)
+    want_q, want_k = q.clone(), k.clone()
+    for r in range(2, rows - 1, 700):
+        part = slice(r, min(r + 700, rows - 1))
+        want_q[part], want_k[part] = dash.rotary(q[part], k[part], inv, positions=place[r - 2:part.stop - 2].contiguous(), **kw)
+    own = slice(2, rows - 1)
+    for x, y in ((q_out, want_q), (k_out, want_k)):
+        assert torch.equal(x[own], y[own]) and bool((x[:2] == 7).all()) and bool((x[rows - 1:] == 7).all())
+    dash.dash_rotary(q, k, q, k, inv, cu=at, start=i32(start), **kw)
+    assert torch.equal(q, want_q) and torch.equal(k, want_k)
