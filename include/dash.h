@@ -415,7 +415,9 @@ typedef struct {
   int64_t q_row_stride, q_head_stride, q_out_row_stride, q_out_head_stride;
   int64_t k_out_row_stride, k_out_head_stride;
   /* [rotary_dim / 2] or NULL (no rotation): pair i of a token at place p turns by
-     the angle p * inv_freq[i] */
+     the angle p * inv_freq[i].  There is no amplitude: where the frequencies come with one (DASH_ROTARY_PARTS), the
+     tokens go through dash_rotary first, with start = lens, and NULL is given here.  (A softmax scale times its
+     square would stand for it only where rotary_dim is d.) */
   const float* inv_freq;
   int rotary_dim;  /* a multiple of 16, at most d; the components behind it stay */
   int interleaved; /* 0: pairs (i, i + rotary_dim/2); else (2i, 2i + 1) */

@@ -444,6 +444,8 @@ def dash_kv_append(k, v, k_cache, v_cache, block_table, lens, cu=None, q=None, q
     queries go to ``q_out`` and, if given, the rotated keys to ``k_out``.
     A microscaled cache (float8_e4m3fn, or uint8 for MXFP4, with uint8 ``k_scale`` and ``v_scale``
     [pages, heads_kv, page_size, d / 32]) gets its scale bytes too.
+    The rotation by ``inv_freq`` has no amplitude: with frequencies that come with one, dash_rotary (``start`` = lens)
+    goes before this call, which then gets none.
     ``status``: optional int32 that a token without a page, or a row between offsets that do
     not rise, sets to 1."""
     import torch
