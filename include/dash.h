@@ -496,9 +496,13 @@ typedef enum {
   DASH_ROTARY_PLAIN = 0,  /* base^(-2i / rotary_dim) */
   DASH_ROTARY_LINEAR = 1, /* positions squeezed: the same over `factor` */
   DASH_ROTARY_BASE = 2,   /* base times factor^(n / (n - 2)), n = rotary_dim: the slowest pair as LINEAR, the fastest as PLAIN */
-  DASH_ROTARY_PARTS = 3   /* pairs that turn more than `fast` times over `original` positions as PLAIN, less than
-                             `slow` times as LINEAR, the others between; amplitude 0.1 ln(factor) + 1
-                             (Peng et al., arXiv 2309.00071) */
+  /* Pairs that turn more than `fast` times over `original` positions as PLAIN, less than `slow` times as LINEAR, the
+     others between, and the amplitude 0.1 ln(factor) + 1 (after Peng et al., arXiv 2309.00071).  In steps, as trained
+     models compute it: with c(t) = n ln(original / (2 pi t)) / (2 ln base), the place of the pair that turns t times,
+     lo = max(floor(c(fast)), 0) and hi = min(ceil(c(slow)), n - 1), pair i takes (1 - x) base^(-2i / n) + x base^(-2i / n) / factor,
+     x = (i - lo) / max(hi - lo, 0.001) in 0 .. 1: linear in the pair's number between whole pairs, where the
+     paper's own ramp is linear in the turns. */
+  DASH_ROTARY_PARTS = 3
 } dash_rotary_scaling_t;
 
 /* The frequencies of a context stretched by `factor` >= 1 from `original` positions, into

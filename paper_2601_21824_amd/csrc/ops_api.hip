@@ -243,7 +243,8 @@ int rotary_frequencies(int n, double base, int scaling, double factor, double or
     return fail(DASH_ERR_INVALID_ARG, "original and slow must be positive, fast at least slow");
   if (!inv_freq || !amplitude) return fail(DASH_ERR_INVALID_ARG, "null inv_freq or amplitude");
   if (scaling == DASH_ROTARY_BASE) base *= std::pow(factor, n / (n - 2.0));
-  // the pair (a real number) that turns so many times over the original positions
+  // the pair (a real number) that turns so many times over the original positions; from there on the steps, the rounding to
+  // whole pairs, n - 1 and 1e-3 among them, are those that models with such frequencies are trained with
   const auto pair_of = [&](double turns) { return n * std::log(original / (turns * 2.0 * M_PI)) / (2.0 * std::log(base)); };
   double lo = 0.0, hi = 0.0;
   if (scaling == DASH_ROTARY_PARTS) {

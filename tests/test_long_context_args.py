@@ -160,3 +160,34 @@ def test_the_package_has_the_calls():
     for name in ("dash_rotary", "rotary", "dash_rotary_frequencies", "dash_kv_read", "kv_read", "dash_attn_prefix_decode",
                  "attn_prefix_decode", "dash_prefix_decode_workspace_size"):
         assert getattr(dash, name) is getattr(b, name)
+
+
+def test_frequencies_by_parts_between_the_borders():
+    """dash.h's steps by hand.  n = 128, base 10^4, from 4096 positions: ln(4096 / (64 pi)) = 3.0142 and ln(4096 / (2 pi)) = 6.4799
+    over 2 ln 10^4 / 128 = 0.143911 are 20.94 and 45.03, so pairs 20 and 46 are the borders."""
+    f, _ = b.dash_rotary_frequencies(128, scaling="parts", factor=8.0, original=4096.0)
+    ratio = f / 10000.0 ** (-np.arange(0, 128, 2) / 128)
+    for i, want in ((0, 1), (20, 1), (21, 1 - 7 / 8 / 26), (33, 1 - 7 / 16), (40, 1 - 7 / 8 * 20 / 26), (45, 1 - 7 / 8 * 25 / 26), (46, 1 / 8), (63, 1 / 8)):
+        assert np.isclose(ratio[i], want, rtol=2 ** -22, atol=0), i
+    # n = 16, base 100, from 64 positions, 4 turns and 1: ln(64 / (8 pi)) = 0.9346 and ln(64 / (2 pi)) = 2.3210 over 0.575646
+    # are 1.62 and 4.03: pairs 1 and 5
+    f, _ = b.dash_rotary_frequencies(16, base=100.0, scaling="parts", factor=2.0, original=64.0, fast=4.0)
+    ratio = f / 100.0 ** (-np.arange(0, 16, 2) / 16)
+    assert np.allclose(ratio, [1, 1, 0.875, 0.75, 0.625, 0.5, 0.5, 0.5], rtol=2 ** -22, atol=0)
+    # one pair where both borders fall together: those before it keep theirs, those behind it take the other
+    f, _ = b.dash_rotary_frequencies(16, base=100.0, scaling="parts", factor=2.0, original=2 * math.pi * 100.0 ** (6 / 16), fast=1.0)
+    assert set(np.round(f / 100.0 ** (-np.arange(0, 16, 2) / 16), 5)) <= {1.0, 0.75, 0.5}
+
+
+@pytest.mark.parametrize("n,base,factor,original,fast,slow", [(64, 10000.0, 8.0, 4096.0, 32.0, 1.0), (128, 500000.0, 16.0, 8192.0, 32.0, 1.0),
+                                                              (256, 1000.0, 3.0, 100.0, 8.0, 0.5), (96, 10000.0, 2.0, 50.0, 5.0, 1e-4)])
+def test_frequencies_by_parts_in_steps(n, base, factor, original, fast, slow):
+    """dash.h's steps, one pair at a time."""
+    f, a = b.dash_rotary_frequencies(n, base, "parts", factor, original, fast, slow)
+    c = [n * math.log(original / (2 * math.pi * t)) / (2 * math.log(base)) for t in (fast, slow)]
+    lo, hi = max(math.floor(c[0]), 0), min(math.ceil(c[1]), n - 1)
+    for i in range(n // 2):
+        x = min(max((i - lo) / max(hi - lo, 0.001), 0.0), 1.0)
+        g = base ** (-2 * i / n)
+        assert abs(f[i] - ((1 - x) * g + x * g / factor)) <= 2.0 ** -23 * g
+    assert abs(a - (0.1 * math.log(factor) + 1)) <= 2.0 ** -23 * a
