@@ -455,9 +455,9 @@ typedef struct {
 /*
  * Keys and values of a paged cache of any type as packed bf16 rows (what
  * dash_attn_packed_fwd takes): the cached value (BF16), times its head's scale and
- * rounded (E4M3), or times 2^e, which is exact (MXFP8, MXFP4).  A row whose key is negative, at or behind lens[s], or in a page outside 0 .. pages-1
- * is left alone and sets status, NULL or a device int, to 1, and so do offsets that do not
- * rise; the call never sets it to 0.
+ * rounded (E4M3), or times 2^e, which is exact (MXFP8, MXFP4).  A row whose key is negative, at or
+ * behind lens[s], or in a page outside 0 .. pages-1 is left alone and sets status, NULL or a device int, to 1, and
+ * so does a row of cu[0] .. cu[batch]-1 that offsets that do not rise leave without a sequence; the call never sets it to 0.
  */
 int dash_kv_read(const dash_paged_cache_t* cache, const dash_read_t* x, int* status, void* stream);
 
@@ -487,8 +487,8 @@ typedef struct {
 /*
  * Rotary positions: (x, y) of each pair becomes amplitude (x cos - y sin, x sin + y cos), or,
  * backward, amplitude (x cos + y sin, y cos - x sin).  The angle is reduced in 64 bits, the rest is
- * in 32 with one rounding at the store.  status: NULL or a device int that offsets that do not
- * rise set to 1; never to 0.
+ * in 32 with one rounding at the store.  status: NULL or a device int that the call sets to 1 when offsets that do
+ * not rise leave a row of cu[0] .. cu[batch]-1 without a sequence; never to 0.
  */
 int dash_rotary(const dash_rotary_t* x, int* status, void* stream);
 

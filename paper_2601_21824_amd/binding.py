@@ -559,7 +559,8 @@ def dash_kv_read(k_cache, v_cache, block_table, lens, cu, k_out=None, v_out=None
     """Keys and values of a paged cache of any type as packed bf16 rows into ``k_out`` and ``v_out``
     ([rows, heads_kv, d], either may be None): rows cu[s] .. cu[s+1]-1 (``cu``: int32 [batch + 1]) receive
     sequence s's keys ``first``[s] .. (int32 [batch]; None: from its first).  Rows of no sequence are left alone.
-    ``status``: optional int32 that a key behind ``lens`` or in no page sets to 1; its row is left alone."""
+    ``status``: optional int32 that a key behind ``lens`` or in no page, or a row between offsets that do not rise, sets
+    to 1; its row is left alone."""
     import torch
     dev = _gpu(k_cache)
     heads_kv = k_cache.shape[1] if k_cache.dim() == 4 else 0
@@ -595,7 +596,8 @@ def dash_rotary(q, k, q_out, k_out, inv_freq, positions=None, cu=None, start=Non
     """Queries and keys (bf16 [rows, heads, d], either may be None) turned by their positions into q_out and
     k_out (which may be q and k): ``positions`` (int32 [rows]), or ``start``[s] + t - ``cu``[s] for row t of
     sequence s (int32 [batch], None: 0, and [batch + 1]).  Pair i turns by position * ``inv_freq``[i] (fp32), times
-    ``amplitude``.  ``backward``: q and k are gradients of rotated ones, turned back.  Rows of no sequence are left alone."""
+    ``amplitude``.  ``backward``: q and k are gradients of rotated ones, turned back.  Rows of no sequence are left alone.
+    ``status``: optional int32 that a row between offsets that do not rise sets to 1."""
     import torch
     if (q is None) != (q_out is None) or (k is None) != (k_out is None):
         _bad("q and q_out, k and k_out come together")

@@ -96,3 +96,25 @@ def test_a_context_by_parts_served_as_it_is_trained(rotary, kind):
         move = 2 * U8 * (qs.abs() @ ks.abs().transpose(1, 2).contiguous()).amax(-1, keepdim=True) / math.sqrt(d)
         a = (p @ vs.abs()) * (torch.expm1(2 * move * (1 + U8)) + 0.0)
         assert bool(((one[s].double().reshape(hk, hq // hk, d) - p @ vs).abs() <= tol[s].reshape(hk, hq // hk, d) + a).all())
+
+
+@pytest.mark.parametrize("at", [[0, 10, 4], [0, 10, 4, 12], [5, 3], [0, 6, 6, 12]])
+def test_offsets_that_fall(at):
+    """The rotation and the read each report exactly when they leave a row of cu[0] .. cu[-1] - 1 alone (where offsets fall, two sequences
+    may claim a row, and which of them it goes to, if any, is the call's own); rows outside those are nobody's, whatever an earlier
+    sequence's end says, and are left alone."""
+    d, rows, batch = 64, 12, len(at) - 1
+    x = torch.ones((rows, 2, d), device="cuda").to(BF)
+    out, s1, s2 = torch.full_like(x, 7.0), i32([0]), i32([0])
+    inv = (10000.0 ** (-torch.arange(0, d, 2, device="cuda") / d)).float()
+    dash.dash_rotary(x, None, out, None, inv, cu=i32(at), status=s1)
+    table, pages = table_of([16] * batch, 16)
+    c = Cache("bf16", pages, 2, 16, d)
+    k, v = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    dash.dash_kv_read(*c.pools, table, i32([16] * batch), i32(at), k, v, status=s2)
+    for status, ys in ((s1, [out]), (s2, [k, v])):
+        for y in ys:
+            left = (y == 7).flatten(1).all(-1)
+            assert int(status) == int(left[at[0]:at[-1]].any()) and bool(left[:at[0]].all()) and bool(left[max(at[0], at[-1]):].all())
+    for r in range(min(at[-1], 4) if at[0] == 0 else 0):  # (of sequence 0 alone)
+        assert torch.equal(k[r], c.k[int(table[0, 0]), :, r]) and not bool((out[r] == 7).all())
