@@ -321,10 +321,11 @@ __device__ inline void decode_part(const DecodeArgs& a, int block, JoinSpace<D, 
   // TAIL: keys from the prefix's end on, counted from the 16 that it lies in (none: none, not the prefix's last few, for which
   // a sequence need not have a page); a sequence that is shorter does without the prefix
   const int prefix = TAIL ? prefix_of(a) : 0;
-  const auto keys_of = [&](int b) {
-    const int n = clamp_len(c.lens[b], c.table_width, c.page_size);
+  const auto keys_in = [&](int length) {
+    const int n = clamp_len(length, c.table_width, c.page_size);
     return !TAIL || n < prefix ? n : n > prefix ? n - (prefix & ~15) : 0;
   };
+  const auto keys_of = [&](int b) { return keys_in(c.lens[b]); };
 
   // ---- the workgroup's sequence s, its chunk number i of n, and where the sequence's parts begin.  First all chunks of at
   // least half the size, then the shorter rests of sequences: what starts late is short (32 heads over 8 of 128, us,
@@ -343,12 +344,26 @@ __device__ inline void decode_part(const DecodeArgs& a, int block, JoinSpace<D, 
   for (int count = c.batch;;) {
     const int per = (count + 63) >> 6;
     int mine = 0, first = 0;  // chunks of this lane's share, and those among them that come first
-#pragma unroll 8
-    for (int j = 0; j < per; ++j) {
-      const int at = l * per + j;
-      if (c.batch > 64) len = keys_of(s + (at < count ? at : 0));
-      const int m = chunks_of(len, chunk);
-      if (at < count) mine += m, first += m - ((unsigned)m * (unsigned)chunk - (unsigned)len > (unsigned)chunk / 2);  // (32 bits, as chunks_of)
+    const auto add = [&](int keys) {
+      const int m = chunks_of(keys, chunk);
+      mine += m, first += m - ((unsigned)m * (unsigned)chunk - (unsigned)keys > (unsigned)chunk / 2);  // (32 bits, as chunks_of)
+    };
+    if (per == 1) {
+      if (c.batch > 64) len = keys_of(s + (l < count ? l : 0));
+      if (l < count) add(len);
+    } else {
+      // four neighbours a load (the batch's last four where fewer follow): the lanes' shares lie a line or more apart
+      // (4096 sequences of 100 keys, 8 heads over 2 of 64, us: one a load 523, four 233)
+      typedef int lens4 __attribute__((ext_vector_type(4), aligned(4)));
+      const int from = s + l * per, to = s + (l * per + per < count ? l * per + per : count);
+#pragma unroll 2
+      for (int j = from; j < from + per; j += 4) {
+        const int p = j < c.batch - 4 ? j : c.batch - 4;
+        const lens4 x = *(const lens4*)(c.lens + p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (p + e >= j && p + e < to) add(keys_in(x[e]));
+      }
     }
     const int mines = wave_scan(mine), firsts = wave_scan(first);
     if (count == c.batch) {

@@ -444,3 +444,29 @@ def test_appends_and_reads_too_large_for_the_caches(d, hq, hkv, rotary, interlea
                 assert torch.equal(ko[own], kf) and torch.equal(vo[own], vf)
         first += m
     assert int(status) == 0
+
+
+@pytest.mark.parametrize("kind", ["bf16", "mxfp8"])
+@pytest.mark.parametrize("batch", [65, 66, 67, 69, 128, 130, 257, 259, 4097])
+def test_lengths_at_any_address(batch, kind):
+    """Batches that no share of 64 lanes divides, their lengths at the end of a tensor and at an address that only 4 divides."""
+    d, hq, hkv, page = 64, 4, 2, 16
+    lens = [1 + 7 * i % 53 if i % 97 else 600 + i % 400 for i in range(batch)]
+    table, pages = table_of(lens, page)
+    c = Cache(kind, pages, hkv, page, d)
+    c.spoil(used_rows(table, lens, page, pages))
+    g = torch.Generator(device="cuda")
+    g.manual_seed(batch)
+    q = torch.randn((batch, hq, d), generator=g, device="cuda").to(BF)
+    ro, rl, tol = attend64(c, q, table, lens, 1 / math.sqrt(d))
+    want = None
+    for front in (0, 1, 2, 3):
+        n = i32([10 ** 6] * front + lens)[front:]  # (what is before it does not matter)
+        o, lse, status = torch.empty_like(q), torch.empty((batch, hq), device="cuda"), i32([0])
+        dash.dash_attn_decode(q, *c.pools, table, n, o, lse, status=status, **c.scales)
+        assert int(status) == 0 and bool(((o.double() - ro).abs() <= tol).all())
+        assert bool(((lse.double() - rl).abs() <= 2e-5 * rl.abs().clamp(min=1)).all())
+        assert want is None or torch.equal(o, want)
+        want = o
+        p = dash.attn_prefix_decode(q, *c.pools, table, n, table[0, :1].contiguous(), i32([0]), **c.scales)  # (nothing shared)
+        assert bool(((p.double() - ro).abs() <= tol + 8 * U24 * tol.clamp(min=ro.abs().amax())).all())
