@@ -59,7 +59,7 @@ __device__ inline void put(void* p, int64_t at, u32x4 x) {
   else *(u32x4*)((__bf16*)p + at) = x;
 }
 
-// PAST: outputs larger than what reads them next will find in a cache are written past the caches.
+// PAST: large outputs are written past the caches.
 template <int D, int TYPE, bool PAST>
 __global__ __launch_bounds__(64 * kWaves) void kv_read_kernel(ReadArgs a) {
   constexpr int LPR = D / 8;       // lanes a row
@@ -130,7 +130,10 @@ __global__ __launch_bounds__(64 * kWaves) void kv_read_kernel(ReadArgs a) {
 template <int D, int TYPE>
 void launch(const ReadArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)((read_waves(a) + kWaves - 1) / kWaves));
-  // (us, through / past the caches: 19385 rows of 8 heads of 128 in MXFP4, 79 MB out, 31 / 19.4; 8192 in MXFP8, 34 MB, 12.2 / 11.1)
+  // The call itself, among calls whose data no cache holds together, us, through / past the caches: 19385 rows of 8 heads of 128 in
+  // MXFP4, 79 MB out, 31 / 19.4; 8192 in MXFP8, 34 MB, 12.2 / 11.1.  With the packed attention that reads them, and 640 MB of other
+  // data through the caches before each pass, it is even up to about 80 MB: those 19385 rows and 3001 queries 489.0 / 488.7, 16684
+  // rows and 300 queries 336 / 338 (in a loop of the two calls alone 63 / 69); larger reads lose up to 1% (51001 bf16 rows 968 / 980).
   const bool past = (int64_t)a.rows * a.c.heads_kv * D * 2 * ((a.k_out != nullptr) + (a.v_out != nullptr)) >= 32L << 20;
   hipLaunchKernelGGL((past ? kv_read_kernel<D, TYPE, true> : kv_read_kernel<D, TYPE, false>), grid, dim3(64 * kWaves), 0, stream, a);
 }

@@ -24,8 +24,7 @@ namespace {
 
 constexpr int kWaves = 4;
 
-// PAST: outputs that the caches will not keep are written past them (1), and inputs that they have not
-// kept read past them (2).
+// PAST: large outputs are written past the caches (1), and larger inputs read past them too (2).
 template <int D, int PAST>
 __global__ __launch_bounds__(64 * kWaves) void rotary_kernel(RotaryArgs a, int rounds) {
   constexpr int IPH = D / 16;    // items per head
@@ -115,9 +114,11 @@ template <int D>
 void launch(const RotaryArgs& a, hipStream_t stream) {
   const int heads = (a.q ? a.heads_q : 0) + (a.k ? a.heads_k : 0), rounds = split_of(a).rounds;
   const dim3 grid((unsigned)((rotary_waves(a) + kWaves - 1) / kWaves));
-  // (us, through the caches / outputs / both past them, with inputs and outputs that no cache holds: 5001 rows of 16 and 4
-  // heads of 256, 51 MB each way, 25.9 / 22.6 / 21.3, and 21.2 / 18.5 / 21.2 where a cache holds a part; 8192 of 32 and 8 heads
-  // of 128, 84 MB, inputs past the caches alone 36.1, outputs too 33.6)
+  // The call itself, us, through the caches / outputs / both past them, with inputs and outputs that no cache holds: 5001 rows of 16
+  // and 4 heads of 256, 51 MB each way, 25.9 / 22.6 / 21.3, and 21.2 / 18.5 / 21.2 where a cache holds a part; 8192 of 32 and 8 heads
+  // of 128, 84 MB, 39 / - / 33.5, inputs alone past them 36.1.  With the packed attention behind it, and 640 MB of other data through the
+  // caches before each pass, it is even within 1%: 32 and 8 heads of 128, 4096 rows 342 / 344 / 342, 6000 383 / 386 / 386, 8192
+  // 436 / 435 / 436, 12000 559 / 553 / 552 (in a loop of the two calls alone 72 / 76 / 76, 117 / 121 / 121, 174 / 174 / 175, 300 / 294 / 294).
   const long bytes = (long)a.rows * heads * D * 2;
   const auto kernel = bytes >= 64L << 20 ? rotary_kernel<D, 2> : bytes >= 32L << 20 ? rotary_kernel<D, 1> : rotary_kernel<D, 0>;
   hipLaunchKernelGGL(kernel, grid, dim3(64 * kWaves), 0, stream, a, rounds);
