@@ -20,9 +20,11 @@
 //
 // Bound by the issue of four waves a CU where the batch is large, 4 d operations a row and key: 64 sequences of 32
 // heads over 8 of 128 behind 32768 shared bf16 keys and with 256 of their own on average, 35 GFLOP, 70 us, 500 TFLOP/s (a prompt's
-// forward, with eight waves, 980).  Smaller ones by latency, the start and a dozen dependent tiles: 24 sequences behind 16384
-// keys in MXFP8 24 us; by 16 rows, 3 of 8 heads over 2 of 64 behind 700 keys 5.8 us, 8 of 16 over 4 of 256 behind
-// 9001 in MXFP4 14.
+// forward, with eight waves, 980).  Smaller ones by the launch and the search of 800 to 960 workgroups, most of which
+// find no own keys (6.2 us with nothing to attend to), and by dependent tiles: 24 sequences behind 16384 keys in MXFP8, eight tiles
+// of 64 keys a workgroup at 1.7 us each (they go through registers, of which one instantiation, d = 128 in MXFP8, has three
+// too few), 24 us; by 16 rows, 8 of 16 heads over 4 of 256 behind 9001 keys in MXFP4, two or three tiles a wave, 13.7, of which a first tile
+// is 1.9, the others 4.8 and own keys 0.9; 3 of 8 over 2 of 64 behind 700 keys 5.8.
 #include "decode_main.h"
 #include "fwd_main.h"
 #include "mx.h"
@@ -423,6 +425,7 @@ PrefixPlan prefix_plan(int batch, int heads_q, int heads_kv, int d, int prefix_t
   const int64_t fit = d == 64 || (!p.few && blocks * prefix_tokens >= 512 * 2048) ? 512 : 256;
   int64_t s = fit / blocks;
   s = s < most ? s : most;
+  // (64 runs at most: a bound on the parts that the join reads.  One K/V head and few rows leave CUs idle with it: more was not measured.)
   p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
   return p;
 }

@@ -33,7 +33,6 @@ struct CacheArgs {
   const float* v_scale;
   int* status;  // null, or set to 1 by a bad page or length
   uint8_t *k_mx, *v_mx;  // scale bytes [pages][heads_kv][page_size][d / 32]
-  bool e4m3() const { return type == kE4m3; }
 };
 
 struct AppendArgs {
