@@ -356,7 +356,7 @@ __device__ inline void decode_part(const DecodeArgs& a, int block, JoinSpace<D, 
       // (4096 sequences of 100 keys, 8 heads over 2 of 64, us: one a load 523, four 233)
       typedef int lens4 __attribute__((ext_vector_type(4), aligned(4)));
       const int from = s + l * per, to = s + (l * per + per < count ? l * per + per : count);
-#pragma unroll 2
+#pragma unroll 1
       for (int j = from; j < from + per; j += 4) {
         const int p = j < c.batch - 4 ? j : c.batch - 4;
         const lens4 x = *(const lens4*)(c.lens + p);
