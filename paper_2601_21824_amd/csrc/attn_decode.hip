@@ -22,7 +22,7 @@
 //
 // Measured, 32 heads over 8 of 128: 131072 keys of 64 sequences in bf16 90 us, 6.0 TB/s,
 // and 5 us of joins, and in MXFP8 47 us, 6.2 TB/s; of one sequence in e4m3 42 us, 6.3 TB/s, and 5.4, and in MXFP4 27 us, 5.3 TB/s, bound by the vector instructions that widen
-// it; 901 keys, 8 heads over 2 of 64, whole, 8.9 us (four tiles a wave, one after the other).
+// it; 901 keys, 8 heads over 2 of 64, whole, 8.1 us (four tiles a wave, one after the other).
 #include "common.h"
 #include "decode_main.h"
 #include "ops.h"
@@ -99,7 +99,7 @@ void launch_main(const DecodeArgs& a, hipStream_t stream) {
 
 template <int D>
 void launch(const DecodeArgs& a, hipStream_t stream) {
-  if (a.workers == 0) return launch_main<D, 8>(a, stream);
+  if (a.workers == 0) return launch_main<D, kWholeWaves>(a, stream);
   launch_main<D, 4>(a, stream);
   if (a.slots > a.c.batch)  // (else no sequence can have two chunks)
     hipLaunchKernelGGL(join_kernel<D>, dim3((unsigned)(a.c.batch * a.c.heads_q)), dim3(256), 0, stream, a);
@@ -130,7 +130,7 @@ int64_t decode_blocks(const DecodeArgs& a) {
   return (int64_t)a.slots * a.c.heads_kv * ((G + kQ - 1) / kQ);
 }
 int64_t decode_waves(const DecodeArgs& a) {
-  const int64_t main = decode_blocks(a) * (a.workers == 0 ? 8 : 4);
+  const int64_t main = decode_blocks(a) * (a.workers == 0 ? kWholeWaves : 4);
   const int64_t join = a.slots > a.c.batch ? (int64_t)a.c.batch * a.c.heads_q * 4 : 0;
   return main > join ? main : join;
 }

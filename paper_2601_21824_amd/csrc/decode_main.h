@@ -21,6 +21,7 @@
 namespace dash {
 
 constexpr int kQ = 16;  // query rows of an MFMA
+constexpr int kWholeWaves = 8;  // waves of a workgroup where every sequence is one chunk (workers 0); else four
 
 // two e4m3 values of a word (its low or high half) as the upper halves of two floats
 template <bool HI>
@@ -331,60 +332,68 @@ __device__ inline void decode_part(const DecodeArgs& a, int block, JoinSpace<D, 
   // least half the size, then the shorter rests of sequences: what starts late is short (32 heads over 8 of 128, us,
   // in the sequences' order / so / whole chunks first: 64 sequences of 131072 keys in bf16 106 / 100 / 106 and in MXFP8
   // 68 / 61 / 65, of 66000 38 / 37 / 39, 128 of 131072 73 / 70 / 74, 65 of 66000 38.4 / 39.8 / 40.5).
-  int len = l < c.batch ? keys_of(l) : 0;
-  long sum = len;
+  // (Sequences that are one chunk each: the workgroup's number, without a search: one of 28 keys, 8 heads over 2 of 64, 3.7 us and
+  // 400 of 100 keys 9.0; with a search over all lengths 4.3 and 17.)
+  int s = slot, i = 0, n = 1, base = slot, chunk = kMaxKeys, len = 0;
+  if constexpr (NW == kWholeWaves) {
+    len = keys_of(slot);
+  } else {
+    s = base = 0;
+    len = l < c.batch ? keys_of(l) : 0;
+    long sum = len;
 #pragma unroll 8
-  for (int b = l + 64; b < c.batch; b += 64) sum += keys_of(b);
-  const long total = wave_sum((int)(sum >> 24)) * (1l << 24) + wave_sum((int)(sum & 0xffffff));  // (a table's keys: below 2^54)
-  const int chunk = __builtin_amdgcn_readfirstlane(chunk_size(total, a.workers));
-  // Among `count` sequences from s on, each lane takes a 64th of them, in order; the lane that holds the chunk
-  // leaves its share to the next round (one round up to 64 sequences, two up to 4096).
-  int s = 0, i = 0, n = 0, base = 0, want = slot;
-  bool rest = false;
-  for (int count = c.batch;;) {
-    const int per = (count + 63) >> 6;
-    int mine = 0, first = 0;  // chunks of this lane's share, and those among them that come first
-    const auto add = [&](int keys) {
-      const int m = chunks_of(keys, chunk);
-      mine += m, first += m - ((unsigned)m * (unsigned)chunk - (unsigned)keys > (unsigned)chunk / 2);  // (32 bits, as chunks_of)
-    };
-    if (per == 1) {
-      if (c.batch > 64) len = keys_of(s + (l < count ? l : 0));
-      if (l < count) add(len);
-    } else {
-      // four neighbours a load (the batch's last four where fewer follow): the lanes' shares lie a line or more apart
-      // (4096 sequences of 100 keys, 8 heads over 2 of 64, us: one a load 523, four 233)
-      typedef int lens4 __attribute__((ext_vector_type(4), aligned(4)));
-      const int from = s + l * per, to = s + (l * per + per < count ? l * per + per : count);
+    for (int b = l + 64; b < c.batch; b += 64) sum += keys_of(b);
+    const long total = wave_sum((int)(sum >> 24)) * (1l << 24) + wave_sum((int)(sum & 0xffffff));  // (a table's keys: below 2^54)
+    chunk = __builtin_amdgcn_readfirstlane(chunk_size(total, a.workers));
+    // Among `count` sequences from s on, each lane takes a 64th of them, in order; the lane that holds the chunk
+    // leaves its share to the next round (one round up to 64 sequences, two up to 4096).
+    int want = slot;
+    bool rest = false;
+    for (int count = c.batch;;) {
+      const int per = (count + 63) >> 6;
+      int mine = 0, first = 0;  // chunks of this lane's share, and those among them that come first
+      const auto add = [&](int keys) {
+        const int m = chunks_of(keys, chunk);
+        mine += m, first += m - ((unsigned)m * (unsigned)chunk - (unsigned)keys > (unsigned)chunk / 2);  // (32 bits, as chunks_of)
+      };
+      if (per == 1) {
+        if (c.batch > 64) len = keys_of(s + (l < count ? l : 0));
+        if (l < count) add(len);
+      } else {
+        // four neighbours a load (the batch's last four where fewer follow): the lanes' shares lie a line or more apart
+        // (4096 sequences of 100 keys, 8 heads over 2 of 64, us: one a load 523, four 233)
+        typedef int lens4 __attribute__((ext_vector_type(4), aligned(4)));
+        const int from = s + l * per, to = s + (l * per + per < count ? l * per + per : count);
 #pragma unroll 1
-      for (int j = from; j < from + per; j += 4) {
-        const int p = j < c.batch - 4 ? j : c.batch - 4;
-        const lens4 x = *(const lens4*)(c.lens + p);
+        for (int j = from; j < from + per; j += 4) {
+          const int p = j < c.batch - 4 ? j : c.batch - 4;
+          const lens4 x = *(const lens4*)(c.lens + p);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (p + e >= j && p + e < to) add(keys_in(x[e]));
+          for (int e = 0; e < 4; ++e)
+            if (p + e >= j && p + e < to) add(keys_in(x[e]));
+        }
       }
+      const int mines = wave_scan(mine), firsts = wave_scan(first);
+      if (count == c.batch) {
+        const int all = __builtin_amdgcn_readlane(firsts, 63);
+        rest = slot >= all;
+        want = rest ? slot - all : slot;
+      }
+      const int own = rest ? mine - first : first, upto = rest ? mines - firsts : firsts;
+      const unsigned long long here = __ballot(upto > want);
+      if (!here) return;  // (in the first round: no such chunk)
+      const int at = __builtin_ctzll(here);
+      want -= __builtin_amdgcn_readlane(upto - own, at);
+      base += __builtin_amdgcn_readlane(mines - mine, at);
+      s += at * per;
+      if (per == 1) {
+        n = __builtin_amdgcn_readlane(mine, at);
+        i = rest ? __builtin_amdgcn_readlane(first, at) : want;
+        len = __builtin_amdgcn_readlane(len, at);
+        break;
+      }
+      count = count - at * per < per ? count - at * per : per;
     }
-    const int mines = wave_scan(mine), firsts = wave_scan(first);
-    if (count == c.batch) {
-      const int all = __builtin_amdgcn_readlane(firsts, 63);
-      rest = slot >= all;
-      want = rest ? slot - all : slot;
-    }
-    const int own = rest ? mine - first : first, upto = rest ? mines - firsts : firsts;
-    const unsigned long long here = __ballot(upto > want);
-    if (!here) return;  // (in the first round: no such chunk)
-    const int at = __builtin_ctzll(here);
-    want -= __builtin_amdgcn_readlane(upto - own, at);
-    base += __builtin_amdgcn_readlane(mines - mine, at);
-    s += at * per;
-    if (per == 1) {
-      n = __builtin_amdgcn_readlane(mine, at);
-      i = rest ? __builtin_amdgcn_readlane(first, at) : want;
-      len = __builtin_amdgcn_readlane(len, at);
-      break;
-    }
-    count = count - at * per < per ? count - at * per : per;
   }
   s = __builtin_amdgcn_readfirstlane(s);  // wave-uniform: tables are read and addresses made by the scalar unit
   n = __builtin_amdgcn_readfirstlane(n);
